@@ -57,7 +57,10 @@
 extern "C" {
 #endif
 
-typedef enum { IVF_F32 = 0, IVF_U8 = 1, IVF_I8 = 2 } ivf_dtype;  /* IVF_I8: signed bytes (SPACEV-shaped data, Table 2) */
+typedef enum {
+    IVF_F32 = 0, IVF_U8 = 1, IVF_I8 = 2,  /* points and queries of the index; IVF_I8: signed bytes (SPACEV-shaped data, Table 2) */
+    IVF_F16 = 3, IVF_BF16 = 4             /* queries and caches of the ivf_kv_* operators only */
+} ivf_dtype;
 
 typedef enum {
     IVF_OK = 0,
@@ -66,8 +69,9 @@ typedef enum {
     IVF_ERR_ALLOC = -3,          /* workspace allocation failed                                   */
     IVF_ERR_CUDA = -4,           /* a CUDA runtime/driver call failed (see ivf_last_error)        */
     IVF_ERR_DEVICE_TIMEOUT = -5, /* a bounded device-side wait expired; results are invalid       */
-    IVF_ERR_BAD_ID = -6,         /* ivf_centroid_update met an id outside [0, nlist); row skipped */
-    IVF_ERR_BOUNDS = -7          /* checked build only: an index check inside a kernel failed     */
+    IVF_ERR_BAD_ID = -6,         /* an id, page, position or length was out of range and skipped  */
+    IVF_ERR_BOUNDS = -7,         /* checked build only: an index check inside a kernel failed     */
+    IVF_ERR_NO_PAGES = -8        /* ivf_kv_tables: too few free pages, columns, tokens or blocks  */
 } ivf_status;
 
 /*
@@ -383,6 +387,114 @@ int ivf_pq_search(const void* queries, int64_t nq, int d, ivf_dtype qtype, const
                   const int32_t* probe_ids, int nprobe, const int64_t* list_offsets, const uint8_t* codes,
                   int64_t n_codes, const float* codebooks, int pq_m, int n_rerank, const int64_t* vec_ids,
                   int64_t* out_ids, float* out_est, int64_t* out_counts, void* stream);
+
+/*
+ * Block cache: attention over a key/value cache whose blocks are routed to like inverted lists.
+ * (These operators have no counterpart in the paper: they serve a language model that keeps its cache in
+ * this library's shape -- lists, one summary per list, a cheap score that picks the lists of each query.)
+ *
+ * A cache holds pages of `page_size` tokens (16, 32, 64 or 128); block j of a request is the page that its
+ * row of the block table names.  Element types are IVF_F16 and IVF_BF16, head_dim a multiple of 16 up to 256,
+ * n_heads a multiple of n_kv_heads with at most 64 query heads to a kv head.  Strides are in elements,
+ * non-negative multiples of 8; the head_dim axis is contiguous; base addresses are 16-byte aligned.  All
+ * arrays are device memory.  A step of a server is
+ *
+ *   ivf_kv_tables -> ivf_kv_append -> ivf_kv_summarize -> ivf_kv_select -> ivf_kv_attend
+ *
+ * on one stream.  The calls return without waiting and may be captured in a CUDA graph.  Sums, norms, scores
+ * and softmax statistics are held in 32 bits.
+ */
+typedef struct ivf_kv_cache {
+    void* k;                /* element (page, kv head, token, i) at k + page*k_stride[0] + head*k_stride[1] + token*k_stride[2] + i */
+    void* v;
+    int64_t k_stride[3];
+    int64_t v_stride[3];
+    int64_t num_pages;
+    int page_size;
+    int n_kv_heads;
+    int head_dim;
+    ivf_dtype dtype;
+} ivf_kv_cache;
+
+/*
+ * Block tables, token positions and cache slots from request lengths.
+ *   cached, fresh   [n_req] tokens in the cache before the step, and new ones (zero of either is fine); n_req <= 16384
+ *   free_pages      [n_free] page ids, taken from the front in request order
+ *   table           [n_req][max_blocks], rows table_stride apart: on entry row b holds the ceil(cached/page_size)
+ *                   pages of request b; the pages of its new blocks are entered behind them, and -1 in every
+ *                   later column
+ *   kv_lens         [n_req] cached + fresh;  token_start [n_req + 1] prefix sums of fresh
+ *   token_req, token_pos, token_slot  [max_tokens] of each new token, request by request: its request, its
+ *                   position, and page * page_size + offset of its place; -1 past the last token
+ *   touched_page, touched_fill  [max_touched] the pages that hold new tokens, in the same order, and how many
+ *                   tokens each then holds; -1 and 0 past the last.  max_tokens / page_size + 2 * n_req is
+ *                   always enough.
+ *   used            [1] pages taken from free_pages
+ * Where pages, columns, tokens or touched blocks do not suffice the surplus gets -1 (`used` still says what was
+ * asked for) and the status word IVF_ERR_NO_PAGES.  A negative length counts as 0 for the whole request and sets
+ * IVF_ERR_BAD_ID.  The call may be repeated on the same arrays.
+ */
+int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int page_size, const int32_t* free_pages, int n_free,
+                  int32_t* table, int64_t table_stride, int max_blocks, int32_t* kv_lens, int32_t* token_start,
+                  int32_t* token_req, int32_t* token_pos, int64_t* token_slot, int64_t max_tokens, int32_t* touched_page,
+                  int32_t* touched_fill, int64_t max_touched, int32_t* used, void* stream);
+
+/*
+ * Norm of queries and keys for each head, position rotation, and the write into the cache, in one pass.
+ *   q, k, v         [n_tokens][n_heads or cache->n_kv_heads][head_dim], strides (token, head): slices of one
+ *                   projection's output are fine
+ *   q_weight, k_weight  [head_dim] float32 weights of y = x * rsqrt(mean(x^2) + eps) * weight; NULL: no norm
+ *   rotary          [n_pos][rot_dim] float32: rot_dim/2 cosines, then rot_dim/2 sines of a position; the first
+ *                   rot_dim entries (a multiple of 16; 0: no rotation) of a head are rotated in pairs
+ *                   (i, i + rot_dim/2), or (2i, 2i + 1) with interleaved != 0
+ *   q_out           rotated queries (may be q itself with q's strides); keys and values go to token_slot
+ * A token whose position is negative is padding: zeros in q_out and nothing written; a negative slot writes
+ * nothing to the cache.  A position or slot past its range counts as padding and sets IVF_ERR_BAD_ID.  Two
+ * tokens must not have the same slot.
+ */
+int ivf_kv_append(const void* q, const int64_t q_stride[2], const void* k, const int64_t k_stride[2], const void* v,
+                  const int64_t v_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, const int32_t* token_pos,
+                  const int64_t* token_slot, const float* rotary, int n_pos, int rot_dim, int interleaved, const float* q_weight,
+                  const float* k_weight, float eps, void* q_out, const int64_t q_out_stride[2], void* stream);
+
+/*
+ * Summaries of cache pages: for pages[i] and every kv head the mean of its first fills[i] keys, coded as
+ * scale = max|mean| / 127, code = round(mean / scale).
+ *   codes           [num_pages][n_kv_heads][head_dim] int8, scales [num_pages][n_kv_heads] float32; only the
+ *                   listed pages are written.  Page -1 or fill 0 is padding.
+ * The mean is summed in a fixed order: the codes are the same on every call.  cache->v is not used.
+ */
+int ivf_kv_summarize(const ivf_kv_cache* cache, const int32_t* pages, const int32_t* fills, int64_t n, int8_t* codes,
+                     float* scales, void* stream);
+
+/*
+ * The blocks that each new token attends to, for every kv head.
+ *   q               [n_tokens][n_heads][head_dim], as ivf_kv_append returns it; strides (token, head)
+ *   out             [n_tokens][n_kv_heads][n_select] int32 block numbers, ascending, -1 after the last
+ * Visible are blocks 0 .. token_pos / page_size with a page in the table.  The first n_first and the last n_last (>= 1) blocks are
+ * always taken; the others by the score of the kv head's group: the sum of its query heads, coded like a summary,
+ * times the block's codes (an exact whole number) times its scale, rounded once to 32 bits.  Equal scores go to the
+ * lower block, so the result is the same on every call.  n_select <= 1024, max_blocks <= 49152.  A negative
+ * request or position is padding: all -1.
+ */
+int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int64_t n_tokens, int n_heads, int n_kv_heads,
+                  int head_dim, const int8_t* codes, const float* scales, int64_t num_pages, const int32_t* table,
+                  int64_t table_stride, int n_req, int max_blocks, int page_size, const int32_t* token_req,
+                  const int32_t* token_pos, int n_select, int n_first, int n_last, int32_t* out, void* stream);
+
+/*
+ * Attention of each new token over its selected blocks, tokens at positions <= token_pos only:
+ * out = softmax(scale * q K^T) V for every query head, out_lse (may be NULL) [n_tokens][n_heads] float32 the
+ * natural logarithm of the softmax's sum.
+ *   selected        [n_tokens][n_kv_heads][n_select] as ivf_kv_select gives them: ascending without repeats, -1 after the
+ *                   last; a user's own choice is fine.  A block past the token's own is ignored.
+ * A token that sees nothing (padding, or no block selected) gets zeros and an out_lse of -infinity.  What pages hold past
+ * a request's last token is never used, whatever it is.
+ */
+int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache,
+                  const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_req,
+                  const int32_t* token_pos, const int32_t* selected, int n_select, float scale, void* out,
+                  const int64_t out_stride[2], float* out_lse, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,11 @@
 #include "fused_topk.cuh"
 #include "merge.cuh"
 #include "candidates.cuh"
+#include "kv_append.cuh"
+#include "kv_attend.cuh"
+#include "kv_select.cuh"
+#include "kv_summary.cuh"
+#include "kv_tables.cuh"
 #include "pq.cuh"
 #include "prep.cuh"
 #include "update.cuh"
@@ -1441,6 +1446,11 @@ int ivf_check(void* stream) {
         CUDA_TRY(cudaMemset(ctx->status, 0, sizeof h));
         if (h[0] == IVF_ERR_DEVICE_TIMEOUT)
             return fail(IVF_ERR_DEVICE_TIMEOUT, "a device-side wait expired (wait site %d, block %d)", h[1], h[2]);
+        if (h[1] >= KV_SITE_TABLES && h[1] <= KV_SITE_ATTEND && (h[0] == IVF_ERR_BAD_ID || h[0] == IVF_ERR_NO_PAGES)) {
+            static const char* const names[] = {"ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend"};
+            return fail(h[0], h[0] == IVF_ERR_NO_PAGES ? "%s had too few free pages, table columns, tokens or touched blocks"
+                                                       : "%s skipped a length, position, slot, page or block out of range", names[h[1] - KV_SITE_TABLES]);
+        }
         if (h[0] == IVF_ERR_BAD_ID) return fail(IVF_ERR_BAD_ID, "ivf_centroid_update skipped ids outside [0, nlist)");
         if (h[0] == IVF_ERR_BOUNDS)
             return fail(IVF_ERR_BOUNDS, "an index check of the checked build failed (site %d, block %d, index %d)", h[1], h[2], h[3]);
@@ -1743,3 +1753,4 @@ extern "C" int ivf_centroid_update_noalloc(const void* points, ivf_dtype ptype, 
     LAUNCH_CHECK();
     return IVF_OK;
 }
+#include "kv_api.cuh"

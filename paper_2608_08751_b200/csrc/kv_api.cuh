@@ -1,0 +1,278 @@
+// Host side of the block-cache operators: argument checks (before any CUDA call) and launches.
+// Included by ivf_api.cu, whose error text, device context and launch counter it uses.
+#pragma once
+
+namespace {
+
+inline bool kv_page_ok(int page_size) { return page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128; }
+inline int kv_shift(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
+inline bool kv_misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+int kv_check_page(int page_size) {
+    if (!kv_page_ok(page_size)) return fail(IVF_ERR_UNSUPPORTED, "page_size = %d: must be 16, 32, 64 or 128", page_size);
+    return IVF_OK;
+}
+int kv_check_dim(int dim) {
+    if (dim < 16 || dim > kKvMaxDim || dim % 16 != 0)
+        return fail(IVF_ERR_UNSUPPORTED, "head_dim = %d: must be a multiple of 16 in [16, %d]", dim, kKvMaxDim);
+    return IVF_OK;
+}
+int kv_check_heads(int n_heads, int n_kv_heads) {
+    if (n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads != 0)
+        return fail(IVF_ERR_INVALID_ARG, "%d query heads, %d kv heads: the second must divide the first", n_heads, n_kv_heads);
+    if (n_heads / n_kv_heads > kKvMaxGroup || n_kv_heads > 1024)
+        return fail(IVF_ERR_UNSUPPORTED, "%d query heads, %d kv heads: at most %d to a group and 1024 groups", n_heads, n_kv_heads, kKvMaxGroup);
+    return IVF_OK;
+}
+int kv_check_rows(const char* what, const void* p, const int64_t* stride, int n) {
+    if (!p || !stride) return fail(IVF_ERR_INVALID_ARG, "%s: null pointer argument", what);
+    if (kv_misaligned(p, 16)) return fail(IVF_ERR_INVALID_ARG, "%s must be 16-byte aligned", what);
+    for (int i = 0; i < n; ++i)
+        if (stride[i] < 0 || stride[i] % 8 != 0)
+            return fail(IVF_ERR_INVALID_ARG, "%s: stride %lld must be a non-negative multiple of 8 elements", what, (long long)stride[i]);
+    return IVF_OK;
+}
+int kv_check_cache(const ivf_kv_cache* c, bool keys, bool values) {
+    if (!c) return fail(IVF_ERR_INVALID_ARG, "null cache descriptor");
+    if (c->dtype != IVF_F16 && c->dtype != IVF_BF16)
+        return fail(IVF_ERR_INVALID_ARG, "element type %d: caches are IVF_F16 or IVF_BF16", static_cast<int>(c->dtype));
+    int rc = kv_check_page(c->page_size);
+    if (rc == IVF_OK) rc = kv_check_dim(c->head_dim);
+    if (rc != IVF_OK) return rc;
+    if (c->num_pages < 0 || c->num_pages > 0x7FFFFFFF)
+        return fail(IVF_ERR_INVALID_ARG, "num_pages = %lld", (long long)c->num_pages);
+    if (keys && (rc = kv_check_rows("key cache", c->k, c->k_stride, 3)) != IVF_OK) return rc;
+    if (values && (rc = kv_check_rows("value cache", c->v, c->v_stride, 3)) != IVF_OK) return rc;
+    return IVF_OK;
+}
+KvPlane kv_plane(void* base, const int64_t* s) { return KvPlane{base, s[0], s[1], s[2]}; }
+
+// The table and the tokens' request and position, as select and attend take them.
+int kv_check_tokens(const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_req,
+                    const int32_t* token_pos) {
+    if (n_req < 1 || max_blocks < 1 || table_stride < max_blocks)
+        return fail(IVF_ERR_INVALID_ARG, "block table: n_req = %d, max_blocks = %d, stride %lld", n_req, max_blocks, (long long)table_stride);
+    if (!table || !token_req || !token_pos) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    return IVF_OK;
+}
+
+template <typename T>
+int kv_launch_append(const KvAppendParams& p, int num_sms, cudaStream_t stream) {
+    int lg = 2;
+    while (lg * 8 < p.dim) lg *= 2;
+    const int groups = kAppThreads / lg;
+    const int rows = p.n_heads + 2 * p.n_kv_heads;
+    const int most = (rows + groups - 1) / groups;
+    // few tokens: the rows of one token are shared out over several CTAs
+    const int y = p.n_tokens * 2 < num_sms ? most : 1;
+    const dim3 grid(static_cast<unsigned>(p.n_tokens), y);
+    switch (lg) {
+        case 2: kv_append_kernel<T, 2><<<grid, kAppThreads, 0, stream>>>(p); break;
+        case 4: kv_append_kernel<T, 4><<<grid, kAppThreads, 0, stream>>>(p); break;
+        case 8: kv_append_kernel<T, 8><<<grid, kAppThreads, 0, stream>>>(p); break;
+        case 16: kv_append_kernel<T, 16><<<grid, kAppThreads, 0, stream>>>(p); break;
+        default: kv_append_kernel<T, 32><<<grid, kAppThreads, 0, stream>>>(p); break;
+    }
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+
+template <typename T>
+int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) {
+    int lg = 2;
+    while (lg * 8 < p.dim) lg *= 2;
+    const dim3 grid(static_cast<unsigned>(n), p.n_kv_heads);
+    switch (lg) {
+        case 2: kv_summary_kernel<T, 2><<<grid, kSumThreads, 0, stream>>>(p); break;
+        case 4: kv_summary_kernel<T, 4><<<grid, kSumThreads, 0, stream>>>(p); break;
+        case 8: kv_summary_kernel<T, 8><<<grid, kSumThreads, 0, stream>>>(p); break;
+        case 16: kv_summary_kernel<T, 16><<<grid, kSumThreads, 0, stream>>>(p); break;
+        default: kv_summary_kernel<T, 32><<<grid, kSumThreads, 0, stream>>>(p); break;
+    }
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+
+template <typename T, int DP>
+int kv_launch_rows(const KvAttendParams& p, cudaStream_t stream) {
+    CUDA_TRY(cudaFuncSetAttribute(kv_attend_rows_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP>::kSmem));
+    const dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_kv_heads, (p.group + 15) / 16);
+    kv_attend_rows_kernel<T, DP><<<grid, kRowsThreads, RowsShape<DP>::kSmem, stream>>>(p);
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+template <typename T>
+int kv_launch_attend(const KvAttendParams& p, cudaStream_t stream) {
+    if (p.dim <= 64) return kv_launch_rows<T, 64>(p, stream);
+    if (p.dim <= 128) return kv_launch_rows<T, 128>(p, stream);
+    return kv_launch_rows<T, 256>(p, stream);
+}
+
+constexpr int64_t kKvMaxTokens = 0x7FFFFFFF;
+
+}  // namespace
+
+extern "C" {
+
+int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int page_size, const int32_t* free_pages, int n_free,
+                  int32_t* table, int64_t table_stride, int max_blocks, int32_t* kv_lens, int32_t* token_start,
+                  int32_t* token_req, int32_t* token_pos, int64_t* token_slot, int64_t max_tokens, int32_t* touched_page,
+                  int32_t* touched_fill, int64_t max_touched, int32_t* used, void* stream_) {
+    if (n_req < 0 || n_free < 0 || max_tokens < 0 || max_touched < 0)
+        return fail(IVF_ERR_INVALID_ARG, "negative size: n_req = %d, n_free = %d, max_tokens = %lld, max_touched = %lld", n_req, n_free,
+                    (long long)max_tokens, (long long)max_touched);
+    if (int rc = kv_check_page(page_size)) return rc;
+    if (n_req > kTabMaxReq) return fail(IVF_ERR_UNSUPPORTED, "n_req = %d: at most %d requests", n_req, kTabMaxReq);
+    if (max_tokens > kKvMaxTokens || max_touched > kKvMaxTokens) return fail(IVF_ERR_UNSUPPORTED, "at most 2^31 - 1 tokens and touched blocks");
+    if (n_req == 0) return IVF_OK;
+    if (max_blocks < 1 || table_stride < max_blocks)
+        return fail(IVF_ERR_INVALID_ARG, "block table: max_blocks = %d, stride %lld", max_blocks, (long long)table_stride);
+    if (!cached || !fresh || !table || !kv_lens || !token_start || !used || (n_free > 0 && !free_pages) ||
+        (max_tokens > 0 && (!token_req || !token_pos || !token_slot)) || (max_touched > 0 && (!touched_page || !touched_fill)))
+        return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    DeviceCtx* pctx = nullptr;
+    if (int rc = get_ctx(&pctx)) return rc;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    KvTablesParams p;
+    p.cached = cached, p.fresh = fresh, p.free_pages = free_pages;
+    p.n_req = n_req, p.page_shift = kv_shift(page_size), p.n_free = n_free, p.max_blocks = max_blocks;
+    p.table = table, p.table_stride = table_stride;
+    p.kv_lens = kv_lens, p.token_start = token_start, p.token_req = token_req, p.token_pos = token_pos, p.token_slot = token_slot;
+    p.max_tokens = max_tokens, p.touched_page = touched_page, p.touched_fill = touched_fill, p.max_touched = max_touched;
+    p.used = used, p.status = pctx->status;
+    const size_t smem = 3 * (static_cast<size_t>(n_req) + 1) * sizeof(int);
+    if (smem > 48 * 1024)
+        CUDA_TRY(cudaFuncSetAttribute(kv_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    const int64_t items = (static_cast<int64_t>(n_req) * max_blocks) / 8 + max_tokens + max_touched;
+    int64_t grid = (items + kTabThreads - 1) / kTabThreads;
+    if (grid > pctx->num_sms) grid = pctx->num_sms;
+    kv_tables_kernel<<<static_cast<unsigned>(grid), kTabThreads, smem, stream>>>(p);
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+
+int ivf_kv_append(const void* q, const int64_t q_stride[2], const void* k, const int64_t k_stride[2], const void* v,
+                  const int64_t v_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, const int32_t* token_pos,
+                  const int64_t* token_slot, const float* rotary, int n_pos, int rot_dim, int interleaved, const float* q_weight,
+                  const float* k_weight, float eps, void* q_out, const int64_t q_out_stride[2], void* stream_) {
+    if (n_tokens < 0) return fail(IVF_ERR_INVALID_ARG, "negative token count %lld", (long long)n_tokens);
+    if (n_tokens > kKvMaxTokens) return fail(IVF_ERR_UNSUPPORTED, "at most 2^31 - 1 tokens");
+    int rc = kv_check_cache(cache, n_tokens > 0, n_tokens > 0);
+    if (rc == IVF_OK) rc = kv_check_heads(n_heads, cache->n_kv_heads);
+    if (rc != IVF_OK) return rc;
+    if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16 != 0)
+        return fail(IVF_ERR_UNSUPPORTED, "rot_dim = %d: must be a multiple of 16 in [0, head_dim = %d]", rot_dim, cache->head_dim);
+    if (rot_dim > 0 && n_pos < 1) return fail(IVF_ERR_INVALID_ARG, "n_pos = %d rows of angles", n_pos);
+    if (!(eps >= 0.0f)) return fail(IVF_ERR_INVALID_ARG, "eps must not be negative");
+    if (n_tokens == 0) return IVF_OK;
+    if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("k", k, k_stride, 2)) != IVF_OK ||
+        (rc = kv_check_rows("v", v, v_stride, 2)) != IVF_OK || (rc = kv_check_rows("q_out", q_out, q_out_stride, 2)) != IVF_OK)
+        return rc;
+    if (!token_pos || !token_slot || (rot_dim > 0 && !rotary)) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    if (kv_misaligned(rotary, 16) || kv_misaligned(q_weight, 16) || kv_misaligned(k_weight, 16))
+        return fail(IVF_ERR_INVALID_ARG, "rotary, q_weight and k_weight must be 16-byte aligned");
+    DeviceCtx* pctx = nullptr;
+    if ((rc = get_ctx(&pctx)) != IVF_OK) return rc;
+    KvAppendParams p;
+    p.q = q, p.k = k, p.v = v, p.q_out = q_out;
+    for (int i = 0; i < 2; ++i)
+        p.q_stride[i] = q_stride[i], p.k_stride[i] = k_stride[i], p.v_stride[i] = v_stride[i], p.qo_stride[i] = q_out_stride[i];
+    p.n_tokens = n_tokens, p.n_heads = n_heads, p.n_kv_heads = cache->n_kv_heads, p.dim = cache->head_dim;
+    p.page_shift = kv_shift(cache->page_size), p.num_pages = cache->num_pages;
+    p.kc = kv_plane(cache->k, cache->k_stride), p.vc = kv_plane(cache->v, cache->v_stride);
+    p.token_pos = token_pos, p.token_slot = token_slot, p.rotary = rotary, p.n_pos = n_pos, p.rot_dim = rot_dim;
+    p.interleaved = interleaved, p.q_weight = q_weight, p.k_weight = k_weight, p.eps = eps, p.status = pctx->status;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return cache->dtype == IVF_F16 ? kv_launch_append<__half>(p, pctx->num_sms, stream)
+                                   : kv_launch_append<__nv_bfloat16>(p, pctx->num_sms, stream);
+}
+
+int ivf_kv_summarize(const ivf_kv_cache* cache, const int32_t* pages, const int32_t* fills, int64_t n, int8_t* codes,
+                     float* scales, void* stream_) {
+    if (n < 0) return fail(IVF_ERR_INVALID_ARG, "negative page count %lld", (long long)n);
+    if (n > kKvMaxTokens) return fail(IVF_ERR_UNSUPPORTED, "at most 2^31 - 1 pages");
+    int rc = kv_check_cache(cache, n > 0, false);
+    if (rc == IVF_OK) rc = kv_check_heads(cache->n_kv_heads, cache->n_kv_heads);
+    if (rc != IVF_OK || n == 0) return rc;
+    if (!pages || !fills || !codes || !scales) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    if (kv_misaligned(codes, 16)) return fail(IVF_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+    DeviceCtx* pctx = nullptr;
+    if ((rc = get_ctx(&pctx)) != IVF_OK) return rc;
+    KvSummaryParams p;
+    p.kc = kv_plane(cache->k, cache->k_stride), p.num_pages = cache->num_pages;
+    p.n_kv_heads = cache->n_kv_heads, p.dim = cache->head_dim, p.page_size = cache->page_size;
+    p.pages = pages, p.fills = fills, p.codes = codes, p.scales = scales, p.status = pctx->status;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return cache->dtype == IVF_F16 ? kv_launch_summary<__half>(p, n, stream) : kv_launch_summary<__nv_bfloat16>(p, n, stream);
+}
+
+int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int64_t n_tokens, int n_heads, int n_kv_heads,
+                  int head_dim, const int8_t* codes, const float* scales, int64_t num_pages, const int32_t* table,
+                  int64_t table_stride, int n_req, int max_blocks, int page_size, const int32_t* token_req,
+                  const int32_t* token_pos, int n_select, int n_first, int n_last, int32_t* out, void* stream_) {
+    if (n_tokens < 0) return fail(IVF_ERR_INVALID_ARG, "negative token count %lld", (long long)n_tokens);
+    if (n_tokens > kKvMaxTokens) return fail(IVF_ERR_UNSUPPORTED, "at most 2^31 - 1 tokens");
+    if (dtype != IVF_F16 && dtype != IVF_BF16) return fail(IVF_ERR_INVALID_ARG, "element type %d: queries are IVF_F16 or IVF_BF16", static_cast<int>(dtype));
+    int rc = kv_check_page(page_size);
+    if (rc == IVF_OK) rc = kv_check_dim(head_dim);
+    if (rc == IVF_OK) rc = kv_check_heads(n_heads, n_kv_heads);
+    if (rc != IVF_OK) return rc;
+    if (n_select < 1 || n_select > kKvMaxSelect) return fail(IVF_ERR_UNSUPPORTED, "n_select = %d: must be in [1, %d]", n_select, kKvMaxSelect);
+    if (n_first < 0 || n_last < 1 || n_first > n_select || n_last > n_select - n_first)
+        return fail(IVF_ERR_INVALID_ARG, "n_first = %d, n_last = %d: n_last must be at least 1 and both fit n_select = %d", n_first, n_last, n_select);
+    if (num_pages < 0 || num_pages > 0x7FFFFFFF) return fail(IVF_ERR_INVALID_ARG, "num_pages = %lld", (long long)num_pages);
+    if (n_tokens == 0) return IVF_OK;
+    if ((rc = kv_check_tokens(table, table_stride, n_req, max_blocks, token_req, token_pos)) != IVF_OK) return rc;
+    if (max_blocks > kSelMaxBlocks) return fail(IVF_ERR_UNSUPPORTED, "max_blocks = %d: at most %d blocks of one request", max_blocks, kSelMaxBlocks);
+    if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK) return rc;
+    if (!codes || !scales || !out) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    if (kv_misaligned(codes, 16)) return fail(IVF_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+    DeviceCtx* pctx = nullptr;
+    if ((rc = get_ctx(&pctx)) != IVF_OK) return rc;
+    KvSelectParams p;
+    p.q = q, p.q_stride[0] = q_stride[0], p.q_stride[1] = q_stride[1], p.n_tokens = n_tokens;
+    p.group = n_heads / n_kv_heads, p.n_kv_heads = n_kv_heads, p.dim = head_dim;
+    p.codes = codes, p.scales = scales, p.num_pages = num_pages;
+    p.table = table, p.table_stride = table_stride, p.n_req = n_req, p.max_blocks = max_blocks, p.page_shift = kv_shift(page_size);
+    p.token_req = token_req, p.token_pos = token_pos, p.n_select = n_select, p.n_first = n_first, p.n_last = n_last;
+    p.out = out, p.status = pctx->status;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int smem = max_blocks * 4;
+    const dim3 grid(static_cast<unsigned>(n_tokens), n_kv_heads);
+    auto kernel = dtype == IVF_F16 ? kv_select_kernel<__half> : kv_select_kernel<__nv_bfloat16>;
+    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    kernel<<<grid, kSelThreads, smem, stream>>>(p);
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+
+int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache,
+                  const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_req,
+                  const int32_t* token_pos, const int32_t* selected, int n_select, float scale, void* out,
+                  const int64_t out_stride[2], float* out_lse, void* stream_) {
+    if (n_tokens < 0) return fail(IVF_ERR_INVALID_ARG, "negative token count %lld", (long long)n_tokens);
+    if (n_tokens > kKvMaxTokens) return fail(IVF_ERR_UNSUPPORTED, "at most 2^31 - 1 tokens");
+    int rc = kv_check_cache(cache, n_tokens > 0, n_tokens > 0);
+    if (rc == IVF_OK) rc = kv_check_heads(n_heads, cache->n_kv_heads);
+    if (rc != IVF_OK) return rc;
+    if (n_select < 1 || n_select > kKvMaxSelect) return fail(IVF_ERR_UNSUPPORTED, "n_select = %d: must be in [1, %d]", n_select, kKvMaxSelect);
+    if (!(scale - scale == 0.0f)) return fail(IVF_ERR_INVALID_ARG, "scale must be finite");
+    if (n_tokens == 0) return IVF_OK;
+    if ((rc = kv_check_tokens(table, table_stride, n_req, max_blocks, token_req, token_pos)) != IVF_OK) return rc;
+    if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("out", out, out_stride, 2)) != IVF_OK) return rc;
+    if (!selected) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    DeviceCtx* pctx = nullptr;
+    if ((rc = get_ctx(&pctx)) != IVF_OK) return rc;
+    KvAttendParams p;
+    p.q = q, p.q_stride[0] = q_stride[0], p.q_stride[1] = q_stride[1], p.n_tokens = n_tokens;
+    p.group = n_heads / cache->n_kv_heads, p.n_kv_heads = cache->n_kv_heads, p.dim = cache->head_dim;
+    p.kc = kv_plane(cache->k, cache->k_stride), p.vc = kv_plane(cache->v, cache->v_stride), p.num_pages = cache->num_pages;
+    p.table = table, p.table_stride = table_stride, p.n_req = n_req, p.max_blocks = max_blocks, p.page_shift = kv_shift(cache->page_size);
+    p.token_req = token_req, p.token_pos = token_pos, p.selected = selected, p.n_select = n_select;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = pctx->status;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return cache->dtype == IVF_F16 ? kv_launch_attend<__half>(p, stream) : kv_launch_attend<__nv_bfloat16>(p, stream);
+}
+
+}  // extern "C"
