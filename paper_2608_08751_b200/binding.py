@@ -8,6 +8,8 @@ There is no fallback: if the library cannot be loaded the import of a symbol rai
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 from typing import NamedTuple
 
@@ -487,53 +489,27 @@ def ivf_assign_update(points: torch.Tensor, centroids: torch.Tensor, sums: torch
 
 
 # ------------------------------------------------------------------ block cache
-def _dtype16(t: torch.Tensor, name: str) -> int:
-    if t.dtype == torch.float16:
-        return IVF_F16
-    if t.dtype == torch.bfloat16:
-        return IVF_BF16
-    raise TypeError(f"{name} must be float16 or bfloat16, got {t.dtype}")
+_kv = None
 
 
-def _strided(t: torch.Tensor, name: str, dim: int, dtype: torch.dtype, dev: torch.device) -> torch.Tensor:
-    if t.dim() != dim or not t.is_cuda or t.device != dev or t.dtype != dtype or (t.numel() and t.stride(-1) != 1):
-        raise ValueError(f"{name} must be a {dim}-D CUDA tensor of {dtype} on {dev} with a contiguous last axis")
-    return t
-
-
-def _on(t: torch.Tensor, name: str, dtype: torch.dtype, dev: torch.device, *shape) -> torch.Tensor:
-    _dev(t, name, dtype)
-    if t.device != dev:
-        raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t
-
-
-def _strides(t: torch.Tensor, n: int):
-    # an axis of one element may carry any stride: 0 says as much
-    return (ctypes.c_int64 * n)(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(n)))
-
-
-def _kv_cache(k_cache: torch.Tensor, v_cache: torch.Tensor | None) -> _KvCache:
-    code = _dtype16(k_cache, "k_cache")
-    dev = k_cache.device
-    _strided(k_cache, "k_cache", 4, k_cache.dtype, dev)
-    if v_cache is not None:
-        _strided(v_cache, "v_cache", 4, k_cache.dtype, dev)
-        if v_cache.shape != k_cache.shape:
-            raise ValueError("k_cache and v_cache must have the same shape [num_pages, kv_heads, page_size, head_dim]")
-    n, h, page, d = k_cache.shape
-    v = k_cache if v_cache is None else v_cache
-    return _KvCache(_ptr(k_cache), _ptr(v), _strides(k_cache, 3), _strides(v, 3), n, page, h, d, code)
-
-
-def _kv_table(table: torch.Tensor, dev: torch.device) -> torch.Tensor:
-    return _strided(table, "table", 2, torch.int32, dev)
-
-
-def _table_stride(table: torch.Tensor) -> int:
-    return table.stride(0) if table.shape[0] > 1 else max(table.stride(0), table.shape[1])
+def _bind():
+    """The compiled marshalling module of the operators below, bound to the loaded library; built if missing or stale."""
+    global _kv
+    if _kv is None:
+        L = lib()
+        path = _build.BIND_PATH
+        try:
+            path = _build.build_bind()
+        except Exception as exc:  # no compiler on this machine: use what travelled with the tree
+            if not os.path.exists(path):
+                raise RuntimeError(f"_kv_bind.so is missing and could not be built: {exc}") from exc
+        loader = importlib.machinery.ExtensionFileLoader("_kv_bind", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kv_bind", loader))
+        loader.exec_module(module)
+        names = ("ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend", "ivf_last_error")
+        module.init(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in names), IvfError)
+        _kv = module
+    return _kv
 
 
 class KvPlan(NamedTuple):
@@ -553,37 +529,8 @@ def ivf_kv_tables(cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.T
     """Block tables, positions and cache slots of a step from the request lengths (int32 [n_req] each): `table`
     [n_req, max_blocks] int32 is extended in place by pages from the front of free_pages; the plan of the
     new tokens comes back (or is written into `plan`, an earlier call's)."""
-    dev = table.device
-    _kv_table(table, dev)
-    n, blocks = table.shape
-    _on(cached, "cached", torch.int32, dev, n)
-    _on(fresh, "fresh", torch.int32, dev, n)
-    _on(free_pages, "free_pages", torch.int32, dev, free_pages.numel())
-    if max_touched is None:
-        max_touched = max_tokens // max(1, page_size) + 2 * n if plan is None else plan.touched_page.shape[0]
-    if plan is None:
-        # one allocation: the 8-byte slots first, then the 4-byte arrays
-        sizes = (n, n + 1, max_tokens, max_tokens, max_touched, max_touched, 1)
-        buf = torch.empty(2 * max_tokens + sum(sizes), dtype=torch.int32, device=dev)
-        a = buf[2 * max_tokens:].split(sizes)
-        plan = KvPlan(a[0], a[1], a[2], a[3], buf[:2 * max_tokens].view(torch.int64), a[4], a[5], a[6])
-    else:
-        _on(plan.kv_lens, "plan.kv_lens", torch.int32, dev, n)
-        _on(plan.token_start, "plan.token_start", torch.int32, dev, n + 1)
-        _on(plan.token_req, "plan.token_req", torch.int32, dev, max_tokens)
-        _on(plan.token_pos, "plan.token_pos", torch.int32, dev, max_tokens)
-        _on(plan.token_slot, "plan.token_slot", torch.int64, dev, max_tokens)
-        _on(plan.touched_page, "plan.touched_page", torch.int32, dev, max_touched)
-        _on(plan.touched_fill, "plan.touched_fill", torch.int32, dev, max_touched)
-        _on(plan.used, "plan.used", torch.int32, dev, 1)
-    with torch.cuda.device(dev):
-        rc = lib().ivf_kv_tables(_ptr(cached), _ptr(fresh), n, page_size, _ptr(free_pages), free_pages.numel(), _ptr(table),
-                                 _table_stride(table), blocks, _ptr(plan.kv_lens), _ptr(plan.token_start), _ptr(plan.token_req),
-                                 _ptr(plan.token_pos), _ptr(plan.token_slot), max_tokens, _ptr(plan.touched_page),
-                                 _ptr(plan.touched_fill), max_touched, _ptr(plan.used), _stream(dev))
-    if rc != IVF_OK:
-        _raise(rc)
-    return plan
+    got = (_kv or _bind()).kv_tables(cached, fresh, free_pages, table, page_size, max_tokens, max_touched, plan)
+    return KvPlan._make(got) if plan is None else plan
 
 
 def ivf_kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -593,51 +540,13 @@ def ivf_kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: to
     """Norms q [n, heads, d] and k [n, kv_heads, d] for each head, rotates them by their positions (rotary: float32
     [n_pos, rot_dim], cosines then sines) and writes k and v into the caches [pages, kv_heads, page_size, d] at
     token_slot; the queries come back."""
-    cache = _kv_cache(k_cache, v_cache)
-    dev = k_cache.device
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _strided(t, name, 3, k_cache.dtype, dev)
-    n, heads, d = q.shape
-    if k.shape != (n, cache.n_kv_heads, cache.head_dim) or v.shape != k.shape or d != cache.head_dim:
-        raise ValueError("shape mismatch between q, k, v and the caches")
-    _on(token_pos, "token_pos", torch.int32, dev, n)
-    _on(token_slot, "token_slot", torch.int64, dev, n)
-    n_pos = rot = 0
-    if rotary is not None:
-        if rotary.dim() != 2:
-            raise ValueError("rotary must be [n_pos, rot_dim]")
-        n_pos, rot = rotary.shape
-        _on(rotary, "rotary", torch.float32, dev, n_pos, rot)
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _on(w, name, torch.float32, dev, d)
-    if q_out is None:
-        q_out = torch.empty((n, heads, d), dtype=q.dtype, device=dev)
-    elif _strided(q_out, "q_out", 3, q.dtype, dev).shape != q.shape:
-        raise ValueError("q_out must have q's shape")
-    with torch.cuda.device(dev):
-        rc = lib().ivf_kv_append(_ptr(q), _strides(q, 2), _ptr(k), _strides(k, 2), _ptr(v), _strides(v, 2), n, heads, ctypes.byref(cache),
-                                 _ptr(token_pos), _ptr(token_slot), _ptr(rotary), n_pos, rot, int(interleaved), _ptr(q_weight),
-                                 _ptr(k_weight), eps, _ptr(q_out), _strides(q_out, 2), _stream(dev))
-    if rc != IVF_OK:
-        _raise(rc)
-    return q_out
+    return (_kv or _bind()).kv_append(q, k, v, k_cache, v_cache, token_pos, token_slot, rotary, interleaved, q_weight, k_weight, eps, q_out)
 
 
 def ivf_kv_summarize(k_cache: torch.Tensor, pages: torch.Tensor, fills: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
     """Mean key of the first fills[i] tokens of pages[i] for each kv head, as int8 codes [num_pages, kv_heads, d] and
     float32 scales [num_pages, kv_heads], written in place."""
-    cache = _kv_cache(k_cache, None)
-    dev = k_cache.device
-    n = pages.numel()
-    _on(pages, "pages", torch.int32, dev, n)
-    _on(fills, "fills", torch.int32, dev, n)
-    _on(codes, "codes", torch.int8, dev, cache.num_pages, cache.n_kv_heads, cache.head_dim)
-    _on(scales, "scales", torch.float32, dev, cache.num_pages, cache.n_kv_heads)
-    with torch.cuda.device(dev):
-        rc = lib().ivf_kv_summarize(ctypes.byref(cache), _ptr(pages), _ptr(fills), n, _ptr(codes), _ptr(scales), _stream(dev))
-    if rc != IVF_OK:
-        _raise(rc)
+    (_kv or _bind()).kv_summarize(k_cache, pages, fills, codes, scales)
 
 
 def ivf_kv_select(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, table: torch.Tensor, token_req: torch.Tensor,
@@ -645,28 +554,7 @@ def ivf_kv_select(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, ta
                   out: torch.Tensor | None = None) -> torch.Tensor:
     """int32 [n, kv_heads, n_select]: the blocks each token attends to, ascending, -1 after the last; the first n_first
     and last n_last visible blocks always, the others by the summaries' scores."""
-    code = _dtype16(q, "q")
-    dev = q.device
-    _strided(q, "q", 3, q.dtype, dev)
-    n, heads, d = q.shape
-    if codes.dim() != 3 or codes.shape[2] != d:
-        raise ValueError("codes must be [num_pages, kv_heads, head_dim]")
-    pages, kv_heads = codes.shape[:2]
-    _on(codes, "codes", torch.int8, dev, pages, kv_heads, d)
-    _on(scales, "scales", torch.float32, dev, pages, kv_heads)
-    _kv_table(table, dev)
-    _on(token_req, "token_req", torch.int32, dev, n)
-    _on(token_pos, "token_pos", torch.int32, dev, n)
-    if out is None:
-        out = torch.empty((n, kv_heads, n_select), dtype=torch.int32, device=dev)
-    _on(out, "out", torch.int32, dev, n, kv_heads, n_select)
-    with torch.cuda.device(dev):
-        rc = lib().ivf_kv_select(_ptr(q), _strides(q, 2), code, n, heads, kv_heads, d, _ptr(codes), _ptr(scales), pages, _ptr(table),
-                                 _table_stride(table), table.shape[0], table.shape[1], page_size, _ptr(token_req), _ptr(token_pos),
-                                 n_select, n_first, n_last, _ptr(out), _stream(dev))
-    if rc != IVF_OK:
-        _raise(rc)
-    return out
+    return (_kv or _bind()).kv_select(q, codes, scales, table, token_req, token_pos, page_size, n_select, n_first, n_last, out)
 
 
 def ivf_kv_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, token_req: torch.Tensor,
@@ -674,31 +562,7 @@ def ivf_kv_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
                   want_lse: bool = False):
     """(out [n, heads, d] in q's type, lse float32 [n, heads] or None): attention of each token over its selected blocks
     (int32 [n, kv_heads, n_select]), positions up to its own."""
-    cache = _kv_cache(k_cache, v_cache)
-    dev = k_cache.device
-    _strided(q, "q", 3, k_cache.dtype, dev)
-    n, heads, d = q.shape
-    if d != cache.head_dim:
-        raise ValueError("head_dim mismatch between q and the caches")
-    if selected.dim() != 3:
-        raise ValueError("selected must be [n, kv_heads, n_select]")
-    n_select = selected.shape[2]
-    _on(selected, "selected", torch.int32, dev, n, cache.n_kv_heads, n_select)
-    _kv_table(table, dev)
-    _on(token_req, "token_req", torch.int32, dev, n)
-    _on(token_pos, "token_pos", torch.int32, dev, n)
-    if out is None:
-        out = torch.empty((n, heads, d), dtype=q.dtype, device=dev)
-    elif _strided(out, "out", 3, q.dtype, dev).shape != q.shape:
-        raise ValueError("out must have q's shape")
-    lse = torch.empty((n, heads), dtype=torch.float32, device=dev) if want_lse else None
-    with torch.cuda.device(dev):
-        rc = lib().ivf_kv_attend(_ptr(q), _strides(q, 2), n, heads, ctypes.byref(cache), _ptr(table), _table_stride(table), table.shape[0],
-                                 table.shape[1], _ptr(token_req), _ptr(token_pos), _ptr(selected), n_select, scale, _ptr(out),
-                                 _strides(out, 2), _ptr(lse), _stream(dev))
-    if rc != IVF_OK:
-        _raise(rc)
-    return out, lse
+    return (_kv or _bind()).kv_attend(q, k_cache, v_cache, table, token_req, token_pos, selected, scale, out, want_lse)
 
 
 def ivf_check(device=None) -> None:

@@ -636,5 +636,9 @@ def test_binding_refuses_mismatched_tensors():
         B.ivf_kv_attend(wide, kc, vc, state[3], pos, pos, torch.zeros(27, 2, 4, dtype=torch.int32, device="cuda"), 1.0)
     with pytest.raises(B.IvfError):
         B.ivf_kv_attend(q, kc, vc, state[3], pos, pos, torch.zeros(27, 2, 4, dtype=torch.int32, device="cuda"), math.nan)
+    with pytest.raises(ValueError):  # no gradients are computed: said, not dropped
+        B.ivf_kv_attend(q.clone().requires_grad_(), kc, vc, state[3], pos, pos, torch.zeros(27, 2, 4, dtype=torch.int32, device="cuda"), 1.0)
+    with pytest.raises(TypeError):
+        B.ivf_kv_summarize(kc, [1], pos, state[6], state[7])
     empty = B.ivf_kv_attend(q[:0], kc, vc, state[3], pos[:0], pos[:0], torch.zeros(0, 2, 4, dtype=torch.int32, device="cuda"), 1.0)
     assert empty[0].shape == (0, 6, 64)
