@@ -401,7 +401,8 @@ int ivf_pq_search(const void* queries, int64_t nq, int d, ivf_dtype qtype, const
  *
  *   ivf_kv_tables -> ivf_kv_append -> ivf_kv_summarize -> ivf_kv_select -> ivf_kv_attend
  *
- * on one stream.  The calls return without waiting and may be captured in a CUDA graph.  Sums, norms, scores
+ * on one stream.  The calls return without waiting and may be captured in a CUDA graph (after a first call of the
+ * same sizes, which sizes the workspace).  Sums, norms, scores
  * and softmax statistics are held in 32 bits.
  */
 typedef struct ivf_kv_cache {
@@ -495,6 +496,9 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
                   const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_req,
                   const int32_t* token_pos, const int32_t* selected, int n_select, float scale, void* out,
                   const int64_t out_stride[2], float* out_lse, void* stream);
+/* Test hook: 0 = the kernel of ivf_kv_attend is chosen by the sizes, 1 = always the one that takes tokens singly,
+ * 2 = the one that takes windows of tokens wherever it can run. */
+int ivf_debug_set_kv_attend(int kernel);
 
 #ifdef __cplusplus
 }

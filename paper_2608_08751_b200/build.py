@@ -20,7 +20,7 @@ BIND_PATH = os.path.join(_PKG, "_kv_bind.so")
 _SOURCES = ["ivf_api.cu"]
 _HEADERS = ["ptx.cuh", "check.cuh", "scales.cuh", "fused_topk.cuh", "merge.cuh", "prep.cuh", "update.cuh", "pq.cuh",
             "candidates.cuh", "kv_common.cuh", "kv_tables.cuh", "kv_append.cuh", "kv_summary.cuh", "kv_select.cuh",
-            "kv_attend.cuh", "kv_api.cuh"]
+            "kv_attend.cuh", "kv_attend_tile.cuh", "kv_api.cuh"]
 
 
 def _nvcc() -> str:

@@ -93,19 +93,74 @@ int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) 
     return IVF_OK;
 }
 
+int g_kv_attend = 0;  // test hook (ivf_debug_set_kv_attend): 0 = by the sizes, 1 = rows kernel only, 2 = tile kernel wherever it can run
+
 template <typename T, int DP>
-int kv_launch_rows(const KvAttendParams& p, cudaStream_t stream) {
+int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     CUDA_TRY(cudaFuncSetAttribute(kv_attend_rows_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP>::kSmem));
-    const dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_kv_heads, (p.group + 15) / 16);
+    dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_kv_heads, (p.group + 15) / 16);
+    if (p.done) {
+        const int64_t most = std::max(1, 2 * ctx.num_sms / p.n_kv_heads);
+        if (p.n_tokens > most) grid.x = static_cast<unsigned>(most);
+    }
     kv_attend_rows_kernel<T, DP><<<grid, kRowsThreads, RowsShape<DP>::kSmem, stream>>>(p);
     LAUNCH_CHECK();
     return IVF_OK;
 }
 template <typename T>
-int kv_launch_attend(const KvAttendParams& p, cudaStream_t stream) {
-    if (p.dim <= 64) return kv_launch_rows<T, 64>(p, stream);
-    if (p.dim <= 128) return kv_launch_rows<T, 128>(p, stream);
-    return kv_launch_rows<T, 256>(p, stream);
+int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    if (p.dim <= 64) return kv_launch_rows<T, 64>(p, ctx, stream);
+    if (p.dim <= 128) return kv_launch_rows<T, 128>(p, ctx, stream);
+    return kv_launch_rows<T, 256>(p, ctx, stream);
+}
+
+// A page of one head, 64 columns wide, with the 128-byte swizzle.
+bool kv_make_map(CUtensorMap* map, const KvPlane& c, const KvAttendParams& p, bool bf16) {
+    const int64_t page = 1 << p.page_shift;
+    const int64_t size[4] = {p.dim, page, p.n_kv_heads, p.num_pages};
+    const int64_t stride[3] = {c.token_stride, c.head_stride, c.page_stride};
+    cuuint64_t dims[4], strides[3];
+    for (int i = 0; i < 4; ++i) dims[i] = static_cast<cuuint64_t>(size[i]);
+    for (int i = 0; i < 3; ++i) {
+        if (stride[i] == 0 && size[i + 1] > 1) return false;  // an expanded axis: the map has no zero strides
+        strides[i] = static_cast<cuuint64_t>(stride[i] == 0 ? p.dim : stride[i]) * 2;
+        if (strides[i] >= (cuuint64_t(1) << 40)) return false;
+    }
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(page), 1, 1}, step[4] = {1, 1, 1, 1};
+    return g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, c.base, dims, strides, box, step,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DB>
+int kv_launch_tile(const KvAttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
+    CUDA_TRY(cudaFuncSetAttribute(kv_attend_tile_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_smem<DB>()));
+    const dim3 grid(static_cast<unsigned>((p.n_tokens + p.window - 1) / p.window), p.n_kv_heads);
+    kv_attend_tile_kernel<T, DB><<<grid, TileShape<DB>::kThreads, tile_smem<DB>(), stream>>>(mk, mv, p);
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+
+template <typename T>
+int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
+    p.done = nullptr;
+    p.window = (p.dim > 128 ? 1 : 2) * (128 / p.group);
+    p.limit_ns = g_wait_limit_ns.load();
+    CUtensorMap mk, mv;
+    const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+    bool tile = g_kv_attend != 1 && p.dim >= 64 && p.max_blocks < kTileMaxBlocks && p.num_pages > 0 &&
+                (p.dim <= 128 || p.page_shift <= 6);  // a tile of wide heads has 64 keys
+    if (g_kv_attend == 0) tile = tile && p.n_tokens >= 2 * p.n_req && p.n_tokens * p.group >= 128;
+    if (tile) {
+        if (int rc = get_encode()) return rc;
+        tile = kv_make_map(&mk, p.kc, p, bf16) && kv_make_map(&mv, p.vc, p, bf16);
+    }
+    if (!tile) return kv_launch_rows<T>(p, ctx, stream);
+    const int64_t windows = (p.n_tokens + p.window - 1) / p.window;
+    WS(WS_KV_DONE, static_cast<size_t>(windows) * p.n_kv_heads, p.done);
+    const int rc = p.dim <= 64 ? kv_launch_tile<T, 1>(p, mk, mv, stream) : p.dim <= 128 ? kv_launch_tile<T, 2>(p, mk, mv, stream)
+                                                                                       : kv_launch_tile<T, 4>(p, mk, mv, stream);
+    return rc != IVF_OK ? rc : kv_launch_rows<T>(p, ctx, stream);
 }
 
 constexpr int64_t kKvMaxTokens = 0x7FFFFFFF;
@@ -272,7 +327,13 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
     p.scale_log2 = scale * 1.4426950408889634f;
     p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = pctx->status;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    return cache->dtype == IVF_F16 ? kv_launch_attend<__half>(p, stream) : kv_launch_attend<__nv_bfloat16>(p, stream);
+    return cache->dtype == IVF_F16 ? kv_launch_attend<__half>(p, *pctx, stream) : kv_launch_attend<__nv_bfloat16>(p, *pctx, stream);
+}
+
+int ivf_debug_set_kv_attend(int kernel) {
+    if (kernel < 0 || kernel > 2) return fail(IVF_ERR_INVALID_ARG, "kernel = %d", kernel);
+    g_kv_attend = kernel;
+    return IVF_OK;
 }
 
 }  // extern "C"

@@ -25,6 +25,11 @@ struct KvAttendParams {
     int64_t out_stride[2];
     float* lse;  // [n_tokens][n_heads] or null
     int* status;
+    // windows of `window` tokens that the tile kernel has finished (flag 1) or left to the rows kernel (flag 0);
+    // null where the rows kernel runs alone
+    uint8_t* done;  // [windows][n_kv_heads]
+    int window;
+    uint64_t limit_ns;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -89,13 +94,9 @@ __device__ __forceinline__ uint32_t rows_addr(uint32_t base, int r, int c) {
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendParams p) {
+__device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64_t t, uint8_t* rows_smem, int* s_page, int* s_first, int& s_n) {
     using S = RowsShape<DP>;
-    extern __shared__ __align__(128) uint8_t rows_smem[];
-    __shared__ int s_page[kKvMaxSelect], s_first[kKvMaxSelect];
-    __shared__ int s_n;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t t = blockIdx.x;
     const int h = blockIdx.y, g0 = blockIdx.z * 16;
     const int rows = min(16, p.group - g0);
     const int n_heads = p.group * p.n_kv_heads;
@@ -300,6 +301,25 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
         for (int j = 0; j < 8; ++j) acc[j] *= inv;
         *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + (head0 + r) * p.out_stride[1] + c * 8) = pack8<T>(acc);
         if (c == 0 && p.lse) p.lse[t * n_heads + head0 + r] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+    }
+    __syncthreads();  // the next token's lists and ring lie over this one's
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendParams p) {
+    extern __shared__ __align__(128) uint8_t rows_smem[];
+    __shared__ int s_page[kKvMaxSelect], s_first[kKvMaxSelect];
+    __shared__ int s_n;
+    if (p.done == nullptr) {
+        attend_rows<T, DP>(p, blockIdx.x, rows_smem, s_page, s_first, s_n);
+        return;
+    }
+    // what the tile kernel left: 32 tokens are looked at at a time
+    for (int64_t t0 = blockIdx.x; t0 < p.n_tokens; t0 += static_cast<int64_t>(gridDim.x) * 32) {
+        const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
+        unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && p.done[mine / p.window * p.n_kv_heads + blockIdx.y] == 0);
+        for (; left; left &= left - 1)
+            attend_rows<T, DP>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, rows_smem, s_page, s_first, s_n);
     }
 }
 

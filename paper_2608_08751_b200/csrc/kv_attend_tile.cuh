@@ -1,0 +1,533 @@
+// Attention over selected blocks for prompt chunks: 5th-generation tensor cores, keys and values by TMA.
+//
+// Neighbouring tokens of a prompt select much the same blocks.  A CTA takes a window of consecutive tokens and one kv
+// head; its rows are (token, query head of the group), 128 to an engine, and it walks the union of the blocks
+// that any token of the window selected, each block fetched once for all rows.  A row that did not select a
+// block sees it masked.
+//
+//   producer warp   merges the tokens' ascending lists (the smallest head of all lists is the next block, the
+//                   lanes whose list shows it are its members), looks the pages up and issues the copies
+//   MMA warp        of each engine: S = Q K^T into TMEM, then O += P V with P read from TMEM
+//   softmax warps   of each engine, one thread per row: S out of TMEM, running maximum and sum in registers, P back
+//                   into TMEM over S.  O is rescaled only when the maximum has grown by more than 2^8 since
+//                   the reference was set; the reference cancels in the final division.
+//
+// S(j + 1) is issued when P(j) V has retired, so P and S share their TMEM columns and the softmax warps may touch O.
+// The other engine's products run meanwhile.
+//
+// What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
+// value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
+// such a window, and one whose tokens belong to many requests, is left to the rows kernel by its flag.
+#pragma once
+#include "kv_attend.cuh"
+
+namespace ivf {
+
+// DB: 64-element blocks of a head (1, 2, 4).
+template <int DB>
+struct TileShape {
+    static constexpr int kEngines = DB == 4 ? 1 : 2;
+    static constexpr int kKeys = DB == 4 ? 64 : 128;  // keys of a tile
+    static constexpr int kStages = DB == 1 ? 4 : 2;
+    static constexpr int kPages = kKeys / 16;  // pages of a tile at most
+    static constexpr int kBlockBytes = kKeys * 128;     // 64 columns of all keys
+    static constexpr int kPlaneBytes = DB * kBlockBytes;
+    static constexpr int kStageBytes = 2 * kPlaneBytes;
+    static constexpr int kQBytes = DB * 128 * 128;      // of one engine
+    static constexpr int kListInts = 7168;
+    static constexpr int kRows = 128 * kEngines;
+    static constexpr int kWarps = 5 * kEngines + 1;     // softmax, MMA, producer
+    static constexpr int kThreads = kWarps * 32;
+    static constexpr int kOCol = kKeys;                 // TMEM columns of an engine: S (and P), then O
+    static constexpr int kEngineCols = DB == 4 ? 512 : 256;
+};
+
+template <int DB>
+struct TileInfo {  // what the producer says about a stage
+    int n_pages;
+    int first[TileShape<DB>::kPages];      // position of the page's first token
+    int dead[TileShape<DB>::kPages];       // tokens from here on lie past the window's last: value rows to be zeroed
+    uint32_t members[TileShape<DB>::kPages][8];  // tokens of the window that selected the page
+};
+
+template <int DB>
+struct TileControl {
+    uint64_t k_full[4], v_full[4], empty[4];
+    uint64_t s_full[2], p_ready[2], pv_done[2], drain[2];
+    TileInfo<DB> info[4];
+    int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows];
+    uint32_t tmem;
+    int abort_flag, bad;
+};
+
+template <int DB>
+constexpr int tile_smem() {
+    using S = TileShape<DB>;
+    return 1024 + S::kEngines * S::kQBytes + S::kStages * S::kStageBytes + S::kListInts * 4 + static_cast<int>(sizeof(TileControl<DB>));
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A holds two 16-bit numbers to a column.
+__device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A wait of a whole warp: its lanes give up together, since they meet in warp-wide instructions later.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl, int where) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, ctl, where));
+}
+
+template <typename T>
+struct UmmaType;
+template <>
+struct UmmaType<__half> { static constexpr uint32_t kFormat = 0; };
+template <>
+struct UmmaType<__nv_bfloat16> { static constexpr uint32_t kFormat = 1; };
+
+// Instruction descriptor: 16-bit A and B of one type, fp32 accumulator, M = 128.  b_mn: B lies with its N axis contiguous.
+template <typename T>
+__device__ __forceinline__ uint32_t tile_idesc(int n, bool b_mn) {
+    return (1u << 4) | (UmmaType<T>::kFormat << 7) | (UmmaType<T>::kFormat << 10) | (b_mn ? 1u << 16 : 0u) |
+           (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
+}
+
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+constexpr int kTileMaxBlocks = 1 << 24;  // block number and segment share a key
+
+template <typename T, int DB>
+__global__ void __launch_bounds__(TileShape<DB>::kThreads, 1)
+kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const KvAttendParams p) {
+    using S = TileShape<DB>;
+    extern __shared__ uint8_t tile_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* ring = smem + S::kEngines * S::kQBytes;
+    int* s_list = reinterpret_cast<int*>(ring + S::kStages * S::kStageBytes);
+    TileControl<DB>& c = *reinterpret_cast<TileControl<DB>*>(s_list + S::kListInts);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int h = blockIdx.y;
+    const int64_t w0 = static_cast<int64_t>(blockIdx.x) * p.window;
+    const int tokens = static_cast<int>(min(static_cast<int64_t>(p.window), p.n_tokens - w0));
+    const int per_engine = 128 / p.group;  // tokens of an engine
+    uint8_t* done = p.done + static_cast<int64_t>(blockIdx.x) * p.n_kv_heads + h;
+
+    // ---- the window's tokens; one of many requests is left to the rows kernel: below 8 tokens to a request the
+    // union is hardly shared
+    int change = 0;
+    if (tid < S::kRows) {
+        int req = -1, pos = -1;
+        if (tid < tokens) {
+            req = p.token_req[w0 + tid];
+            pos = p.token_pos[w0 + tid];
+            change = tid > 0 && req != p.token_req[w0 + tid - 1];
+            if (req >= p.n_req) {
+                kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
+                req = -1;
+            }
+            if (pos < 0) req = -1;
+        }
+        c.req[tid] = req;
+        c.pos[tid] = pos;
+    }
+    const int segments = __syncthreads_count(change) + 1;
+    if (segments > 1 && segments * 8 > tokens) {
+        if (tid == 0) *done = 0;
+        return;
+    }
+
+    if (tid == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(&c.k_full[i], 1);
+            mbar_init(&c.v_full[i], 1);
+            mbar_init(&c.empty[i], S::kEngines);
+        }
+        for (int e = 0; e < S::kEngines; ++e) {
+            mbar_init(&c.s_full[e], 1);
+            mbar_init(&c.p_ready[e], 128);
+            mbar_init(&c.pv_done[e], 1);
+            mbar_init(&c.drain[e], 1);
+        }
+        c.abort_flag = 0;
+        c.bad = 0;
+        fence_mbar_init();
+    }
+    if (warp == S::kWarps - 1) {
+        if (lane == 0) {
+            tma_prefetch_desc(&map_k);
+            tma_prefetch_desc(&map_v);
+        }
+        tmem_alloc(&c.tmem, 512);
+        tmem_relinquish();
+    }
+    // selections to shared memory where they fit
+    const bool lists_here = tokens * p.n_select <= S::kListInts;
+    if (lists_here) {
+        for (int i = tid; i < tokens * p.n_select; i += S::kThreads) {
+            const int tok = i / p.n_select, at = i - tok * p.n_select;
+            s_list[i] = p.selected[((w0 + tok) * p.n_kv_heads + h) * p.n_select + at];
+        }
+    }
+    // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits
+    {
+        const float sign = p.scale_log2 < 0.0f ? -1.0f : 1.0f;
+        const uint32_t flip = sign < 0.0f ? 0x80008000u : 0u;  // a negative scale is a positive one of negated queries
+        constexpr int kPieces = DB * 8;
+        for (int i = tid; i < S::kRows * kPieces; i += S::kThreads) {
+            const int row = i / kPieces, piece = i % kPieces;
+            const int e = row >> 7, r = row & 127;
+            const int tok = e * per_engine + r / p.group;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < per_engine * p.group && tok < tokens && piece * 8 < p.dim) {
+                v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (w0 + tok) * p.q_stride[0] +
+                                                    (static_cast<int64_t>(h) * p.group + r % p.group) * p.q_stride[1] + piece * 8);
+                v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+            }
+            *reinterpret_cast<uint4*>(smem + e * S::kQBytes + (piece >> 3) * (128 * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v;
+        }
+        fence_proxy_async_smem();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = c.tmem;
+    WaitCtl ctl;
+    ctl.abort_flag = &c.abort_flag;
+    ctl.status = p.status;
+    ctl.limit_ns = p.limit_ns;
+    const int page_size = 1 << p.page_shift;
+    const int per_tile = S::kKeys >> p.page_shift;
+
+    if (warp == S::kWarps - 1) {
+        // ------------------------------------------------------------ producer
+        const int slots = (tokens + 31) >> 5;
+        uint32_t cur[8];
+        int at[8] = {}, seg[8] = {};
+        auto entry = [&](int k) -> uint32_t {
+            const int tok = k * 32 + lane;
+            if (tok >= tokens || c.req[tok] < 0 || at[k] >= p.n_select) return kNoKey;
+            const int b = lists_here ? s_list[tok * p.n_select + at[k]] : p.selected[((w0 + tok) * p.n_kv_heads + h) * p.n_select + at[k]];
+            if (b < 0 || b > (c.pos[tok] >> p.page_shift)) return kNoKey;
+            return (static_cast<uint32_t>(seg[k]) << 24) | static_cast<uint32_t>(b);
+        };
+        int n_seg = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            cur[k] = kNoKey;
+            seg[k] = -1;
+            if (k < slots) {
+                const int tok = k * 32 + lane;
+                const bool step = tok > 0 && tok < tokens && c.req[tok] != c.req[tok - 1];
+                const unsigned m = __ballot_sync(0xFFFFFFFFu, step);
+                seg[k] = n_seg + __popc(m & (0xFFFFFFFFu >> (31 - lane)));
+                n_seg += __popc(m);
+                cur[k] = entry(k);
+            }
+        }
+        int last_seg = -1, last_pos = -1;
+        bool ok = true;
+        int j = 0;
+        for (;; ++j) {
+            const int stage = j % S::kStages;
+            if (j >= S::kStages && !(ok = warp_wait(&c.empty[stage], (j / S::kStages - 1) & 1, ctl, 201))) break;
+            TileInfo<DB>& info = c.info[stage];
+            int n = 0, my_page = -1;
+            while (n < per_tile) {
+                uint32_t least = kNoKey;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < slots) least = min(least, cur[k]);
+                const uint32_t key = __reduce_min_sync(0xFFFFFFFFu, least);
+                if (key == kNoKey) break;
+                int owner = -1;
+                uint32_t mine = 0;  // lane k keeps word k of the members
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (k < slots) {
+                        const bool member = cur[k] == key;
+                        const unsigned m = __ballot_sync(0xFFFFFFFFu, member);
+                        if (m && owner < 0) owner = k * 32 + __ffs(m) - 1;
+                        if (lane == k) mine = m;
+                        if (member) {
+                            ++at[k];
+                            cur[k] = entry(k);
+                        }
+                    }
+                }
+                const int block = static_cast<int>(key & 0xFFFFFFu), s = static_cast<int>(key >> 24);
+                if (s != last_seg) {  // the last position that any token of the segment sees
+                    int far = -1;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < slots && seg[k] == s && k * 32 + lane < tokens) far = max(far, c.pos[k * 32 + lane]);
+                    last_pos = __reduce_max_sync(0xFFFFFFFFu, far);
+                    last_seg = s;
+                }
+                int page = -1;
+                if (block < p.max_blocks) page = p.table[c.req[owner] * p.table_stride + block];
+                if (page < 0 || page >= p.num_pages) {
+                    if (lane == 0 && (block >= p.max_blocks || page >= p.num_pages)) kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
+                    continue;
+                }
+                if (lane == n) my_page = page;
+                if (lane < 8) info.members[n][lane] = mine;
+                if (lane == 0) {
+                    info.first[n] = block << p.page_shift;
+                    info.dead[n] = min(page_size, last_pos + 1 - (block << p.page_shift));
+                }
+                ++n;
+            }
+            if (lane == 0) info.n_pages = n;
+            __syncwarp();
+            if (lane == 0) {
+                if (n == 0) {
+                    mbar_arrive(&c.k_full[stage]);
+                } else {
+                    mbar_arrive_expect_tx(&c.k_full[stage], n * DB * page_size * 128);
+                    mbar_arrive_expect_tx(&c.v_full[stage], n * DB * page_size * 128);
+                }
+            }
+            __syncwarp();
+            if (n == 0) break;
+            if (lane < n) {
+                const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * page_size * 128;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, 0, h, my_page);
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, 0, h, my_page);
+            }
+            __syncwarp();
+        }
+        if (!ok && lane == 0) {
+            // gave up: let the copies already issued land before the CTA goes away (bounded)
+            const uint64_t t0 = global_timer_ns();
+            for (int i = max(0, j - S::kStages); i < j; ++i) {
+                const uint32_t ph = (i / S::kStages) & 1;
+                while ((!mbar_try_wait(&c.k_full[i % S::kStages], ph) || !mbar_try_wait(&c.v_full[i % S::kStages], ph)) &&
+                       global_timer_ns() - t0 < 2000000000ull) {
+                }
+            }
+        }
+    } else if (warp >= 4 * S::kEngines) {
+        // ------------------------------------------------------------ MMA of engine e
+        const int e = warp - 4 * S::kEngines;
+        if (lane == 0) {
+            const uint32_t t_s = tmem + e * S::kEngineCols, t_o = t_s + S::kOCol;
+            const uint32_t q_lo = umma_desc_lo(smem_u32(smem) + e * S::kQBytes);
+            const uint32_t ring0 = smem_u32(ring);
+            const uint32_t idesc_o = tile_idesc<T>(p.dim, true);
+            const int ksteps = p.dim >> 4;
+            bool ok = true, issued = false;
+            for (int j = 0;; ++j) {
+                const int stage = j % S::kStages;
+                const uint32_t ph = (j / S::kStages) & 1;
+                if (!(ok = mbar_wait(&c.k_full[stage], ph, ctl, 202))) break;
+                const int keys = c.info[stage].n_pages << p.page_shift;
+                if (keys == 0) break;
+                if (j > 0 && !(ok = mbar_wait(&c.pv_done[e], (j - 1) & 1, ctl, 203))) break;
+                tc_fence_after_sync();
+                const uint32_t k_lo = umma_desc_lo(ring0 + stage * S::kStageBytes);
+                const uint32_t idesc_s = tile_idesc<T>(keys, false);
+                for (int k = 0; k < ksteps; ++k) {
+                    const uint32_t in = (k & 3) * 2, blk = k >> 2;
+                    umma_f16(t_s, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
+                             umma_desc_join(k_lo + blk * (S::kBlockBytes >> 4) + in, kDescHiSw128), idesc_s, k > 0);
+                }
+                umma_commit(&c.s_full[e]);
+                issued = true;
+                if (!(ok = mbar_wait(&c.v_full[stage], ph, ctl, 204))) break;
+                if (!(ok = mbar_wait(&c.p_ready[e], j & 1, ctl, 205))) break;
+                tc_fence_after_sync();
+                // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
+                const uint32_t v_addr = ring0 + stage * S::kStageBytes + S::kPlaneBytes;
+                const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
+                for (int k = 0; k < keys >> 4; ++k)
+                    umma_f16_ts(t_o, t_s + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (j > 0 || k > 0) ? 1u : 0u);
+                umma_commit(&c.pv_done[e]);
+                umma_commit(&c.empty[stage]);
+            }
+            if (!ok && issued) {
+                umma_commit(&c.drain[e]);
+                const uint64_t t0 = global_timer_ns();
+                while (!mbar_try_wait(&c.drain[e], 0) && global_timer_ns() - t0 < 2000000000ull) {
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ softmax of engine e: thread = row = TMEM lane
+        const int e = warp >> 2, r = (warp & 3) * 32 + lane;
+        const int in_engine = r / p.group;
+        const int tok = e * per_engine + in_engine;
+        const bool row_live = r < per_engine * p.group && tok < tokens;
+        const int pos = row_live && c.req[tok] >= 0 ? c.pos[tok] : -1;
+        const int word = row_live ? tok >> 5 : 0;
+        const uint32_t bit = row_live && pos >= 0 ? 1u << (tok & 31) : 0u;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + e * S::kEngineCols + lanes, t_o = t_s + S::kOCol;
+        const float scale = fmaxf(fabsf(p.scale_log2), 1.2e-38f);  // zero would turn masked logits into NaN
+        const float slack = 8.0f / scale;
+        float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum
+        bool ok = true;
+        int j = 0;
+        for (;; ++j) {
+            const int stage = j % S::kStages;
+            const uint32_t ph = (j / S::kStages) & 1;
+            if (!(ok = warp_wait(&c.k_full[stage], ph, ctl, 206))) break;
+            const TileInfo<DB>& info = c.info[stage];
+            const int n_pages = info.n_pages;
+            if (n_pages == 0) break;
+            // value rows that no token of the window sees
+            bool zeroed = false;
+            for (int i = 0; i < n_pages; ++i) {
+                if (info.dead[i] < page_size) {
+                    if (!zeroed && !(ok = warp_wait(&c.v_full[stage], ph, ctl, 207))) break;
+                    zeroed = true;
+                    const int rows = page_size - info.dead[i];
+                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * page_size + info.dead[i]) * 128;
+                    for (int x = r; x < rows * 8 * DB; x += 128) {
+                        const int piece = x & 7, rest = x >> 3;
+                        *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            }
+            if (!ok) break;
+            if (zeroed) fence_proxy_async_smem();
+            if (!(ok = warp_wait(&c.s_full[e], j & 1, ctl, 208))) break;
+            tc_fence_after_sync();
+            uint32_t s[S::kKeys / 32][32];
+#pragma unroll
+            for (int q = 0; q < S::kKeys / 32; ++q) tmem_ld_32x32b_x32(t_s + q * 32, s[q]);
+#pragma unroll
+            for (int q = 0; q < S::kKeys / 32; ++q) tmem_wait_ld_regs(s[q]);
+            // keys seen in each group of 16: all, none or the first few
+            float top = -INFINITY;
+            uint32_t some = 0;  // groups that some row of the warp sees
+#pragma unroll
+            for (int g = 0; g < S::kKeys / 16; ++g) {
+                const int i = (g * 16) >> p.page_shift;
+                int seen = 0;
+                if (i < n_pages && (info.members[i][word] & bit)) seen = pos + 1 - info.first[i] - ((g * 16) & (page_size - 1));
+                if (__any_sync(0xFFFFFFFFu, seen > 0)) {
+                    some |= 1u << g;
+                    if (!__all_sync(0xFFFFFFFFu, seen >= 16)) {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            if (x >= seen) s[g >> 1][(g & 1) * 16 + x] = 0xFF800000u;
+                    }
+                    float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 16; x += 2) {
+                        t0 = fmaxf(t0, __uint_as_float(s[g >> 1][(g & 1) * 16 + x]));
+                        t1 = fmaxf(t1, __uint_as_float(s[g >> 1][(g & 1) * 16 + x + 1]));
+                    }
+                    top = fmaxf(top, fmaxf(t0, t1));
+                }
+            }
+            const bool grow = top > m + slack || (m == -INFINITY && top > m);
+            if (__any_sync(0xFFFFFFFFu, grow)) {
+                const float fix = grow ? (l > 0.0f ? exp2_fast((m - top) * scale) : 1.0f) : 1.0f;
+                if (grow) m = top;
+                if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {
+                    l *= fix;
+                    for (int q = 0; q < (p.dim + 31) / 32; ++q) {
+                        uint32_t o[32];
+                        tmem_ld_32x32b_x32(t_o + q * 32, o);
+                        tmem_wait_ld_regs(o);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fix);
+                        tmem_st_32x32b_x32(t_o + q * 32, o);
+                    }
+                }
+            }
+            const float base = m == -INFINITY ? 0.0f : m * scale;
+            float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+            for (int q = 0; q < S::kKeys / 64; ++q) {
+                uint32_t out[32];
+#pragma unroll
+                for (int g = 4 * q; g < 4 * q + 4; ++g) {
+                    if (some >> g & 1) {
+#pragma unroll
+                        for (int x = 0; x < 16; x += 2) {
+                            const float a = exp2_fast(fmaf(__uint_as_float(s[g >> 1][(g & 1) * 16 + x]), scale, -base));
+                            const float b = exp2_fast(fmaf(__uint_as_float(s[g >> 1][(g & 1) * 16 + x + 1]), scale, -base));
+                            sum0 += a;
+                            sum1 += b;
+                            out[(g & 3) * 8 + x / 2] = Pair16<T>::pack(a, b);
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) out[(g & 3) * 8 + x] = 0u;
+                    }
+                }
+                tmem_st_32x32b_x32(t_s + q * 32, out);
+            }
+            l += sum0 + sum1;
+            tmem_wait_st();
+            tc_fence_before_sync();
+            mbar_arrive(&c.p_ready[e]);
+        }
+        if (ok && j > 0 && (ok = warp_wait(&c.pv_done[e], (j - 1) & 1, ctl, 209))) tc_fence_after_sync();
+        if (ok) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int64_t head = static_cast<int64_t>(h) * p.group + r % p.group;
+            T* dst = static_cast<T*>(p.out) + (w0 + tok) * p.out_stride[0] + head * p.out_stride[1];
+            bool bad = false;
+            for (int q = 0; q < (p.dim + 31) / 32; ++q) {
+                uint32_t o[32];
+                if (j > 0) {
+                    tmem_ld_32x32b_x32(t_o + q * 32, o);
+                    tmem_wait_ld_regs(o);
+                }
+                if (row_live) {
+#pragma unroll
+                    for (int x = 0; x < 32; x += 8) {
+                        if (q * 32 + x < p.dim) {
+                            float f[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                f[i] = l == 0.0f ? 0.0f : __uint_as_float(o[x + i]) * inv;
+                                bad |= !(fabsf(f[i]) <= 3.4e38f);
+                            }
+                            *reinterpret_cast<uint4*>(dst + q * 32 + x) = pack8<T>(f);
+                        }
+                    }
+                }
+            }
+            if (row_live && p.lse)
+                p.lse[(w0 + tok) * p.group * p.n_kv_heads + head] = l == 0.0f ? -INFINITY : (m * scale + log2f(l)) * 0.69314718055994531f;
+            if (bad) c.bad = 1;
+        }
+    }
+    // ------------------------------------------------------------ teardown (also the abort path)
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == S::kWarps - 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 512);
+    }
+    if (tid == 0) *done = c.bad ? 0 : 1;
+}
+
+}  // namespace ivf

@@ -339,6 +339,14 @@ def test_selection_skips_what_is_out_of_range():
 
 # ---------------------------------------------------------------------------------------------- attend
 
+@pytest.fixture(params=["by size", "single tokens", "windows"])
+def kernel(request):
+    """Every attention test runs with the kernel chosen by the sizes and with either forced."""
+    B.ivf_debug_set_kv_attend(["by size", "single tokens", "windows"].index(request.param))
+    yield request.param
+    B.ivf_debug_set_kv_attend(0)
+
+
 def _attend_case(contexts, fresh, kv, group, dim, page, take, kind, layout, seed, forced_last=True, shared=False):
     """Caches whose places past a request's end hold NaN, and a random ascending selection for each token."""
     g = _gen(seed)
@@ -393,7 +401,7 @@ ATTEND = [
 
 
 @pytest.mark.parametrize("contexts,fresh,kv,group,dim,page,take,kind,layout", ATTEND)
-def test_attention_of_single_and_drafted_tokens(contexts, fresh, kv, group, dim, page, take, kind, layout):
+def test_attention_of_single_and_drafted_tokens(kernel, contexts, fresh, kv, group, dim, page, take, kind, layout):
     kc, vc, table, req, pos, q, sel = _attend_case(contexts, fresh, kv, group, dim, page, take, kind, layout, seed=dim + take)
     scale = 1 / math.sqrt(dim)
     got, lse = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), scale, want_lse=True)
@@ -416,7 +424,7 @@ PROMPT = [
 
 
 @pytest.mark.parametrize("contexts,fresh,kv,group,dim,page,take,kind,layout,shared", PROMPT)
-def test_attention_of_prompt_chunks(contexts, fresh, kv, group, dim, page, take, kind, layout, shared):
+def test_attention_of_prompt_chunks(kernel, contexts, fresh, kv, group, dim, page, take, kind, layout, shared):
     kc, vc, table, req, pos, q, sel = _attend_case(contexts, fresh, kv, group, dim, page, take, kind, layout, seed=dim + take + 1, shared=shared)
     scale = 1 / math.sqrt(dim)
     got, lse = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), scale, want_lse=True)
@@ -429,7 +437,7 @@ def test_attention_of_prompt_chunks(contexts, fresh, kv, group, dim, page, take,
 
 @pytest.mark.parametrize("fresh", [1, 70])
 @pytest.mark.parametrize("dim,kind", [(64, "fp16"), (128, "bf16"), (256, "bf16")])
-def test_attention_rows_that_see_nothing_and_odd_selections(fresh, dim, kind):
+def test_attention_rows_that_see_nothing_and_odd_selections(kernel, fresh, dim, kind):
     kc, vc, table, req, pos, q, sel = _attend_case([600, 333, 90], fresh, 2, 4, dim, 32, 5, kind, "head", seed=fresh)
     n = len(req)
     sel[0] = -1                     # nothing selected
@@ -449,7 +457,7 @@ def test_attention_rows_that_see_nothing_and_odd_selections(fresh, dim, kind):
 
 
 @pytest.mark.parametrize("fresh", [1, 48])
-def test_attention_with_large_and_equal_logits(fresh):
+def test_attention_with_large_and_equal_logits(kernel, fresh):
     # logits of several hundred (one key takes all), then all equal (the mean of the values): no overflow, no drift
     kc, vc, table, req, pos, q, sel = _attend_case([900], fresh, 1, 8, 128, 64, 6, "bf16", "head", seed=9)
     for scale in (30.0, -30.0, 0.0):
@@ -460,7 +468,7 @@ def test_attention_with_large_and_equal_logits(fresh):
 
 
 @pytest.mark.parametrize("fresh", [1, 64])
-def test_values_of_tokens_that_are_not_seen_may_be_anything(fresh):
+def test_values_of_tokens_that_are_not_seen_may_be_anything(kernel, fresh):
     # infinities and NaN in blocks that a token did not select, and at positions after its own: other tokens of
     # the same tile read those blocks, this one must not notice
     kc, vc, table, req, pos, q, sel = _attend_case([640], fresh, 1, 4, 128, 64, 4, "bf16", "head", seed=31)
@@ -484,7 +492,7 @@ def test_values_of_tokens_that_are_not_seen_may_be_anything(fresh):
         _check_attend(clean[untouched], None, part, "bf16", 128)
 
 
-def test_attention_refuses_what_is_out_of_range():
+def test_attention_refuses_what_is_out_of_range(kernel):
     kc, vc, table, req, pos, q, sel = _attend_case([100, 100], 1, 1, 2, 64, 16, 3, "bf16", "head", seed=2)
     bad = table.copy()
     bad[0, sel[0, 0, 0]] = 10000  # a page past the cache: its block is left out
@@ -502,7 +510,7 @@ def test_attention_refuses_what_is_out_of_range():
     assert (got[1] == 0).all()
 
 
-def test_offsets_past_32_bits():
+def test_offsets_past_32_bits(kernel):
     # pages that start 2^31 elements into the cache and further
     page, dim, kv = 128, 128, 1
     pages = (1 << 31) // (page * dim) + 8
@@ -566,7 +574,7 @@ def _whole_state(seed, lengths, tokens, dim=64, kv=2, heads=6):
 LENGTHS = [(100, 1), (31, 1), (32, 1), (0, 20), (333, 1), (64, 0)]
 
 
-def test_the_five_calls_as_one_step():
+def test_the_five_calls_as_one_step(kernel):
     qkv, state = _whole_state(1, LENGTHS, 27)  # 24 tokens and padding
     plan, qr, sel, out, lse = _whole_step(None, *qkv, state)
     B.ivf_check()
@@ -581,7 +589,7 @@ def test_the_five_calls_as_one_step():
             assert (c == _np(state[6])[p]).all() and (s == state[7].cpu().numpy()[p]).all()
 
 
-def test_another_stream_and_a_captured_graph_give_the_same():
+def test_another_stream_and_a_captured_graph_give_the_same(kernel):
     qkv, state = _whole_state(2, LENGTHS, 27)
     first = [t.clone() for t in _whole_step(None, *qkv, state)[1:]]
     side = torch.cuda.Stream()
