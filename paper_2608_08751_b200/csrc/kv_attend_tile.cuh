@@ -52,9 +52,9 @@ struct TileInfo {  // what the producer says about a stage
 
 template <int DB>
 struct TileControl {
-    uint64_t k_full[4], v_full[4], empty[4];
+    uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4];
     uint64_t s_full[2], p_ready[2], pv_done[2], drain[2];
-    TileInfo<DB> info[4];
+    TileInfo<DB> info[TileShape<DB>::kStages + 1];
     int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows];
     uint32_t tmem;
     int abort_flag, bad;
@@ -92,7 +92,55 @@ __device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_
           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
 }
+// 16 columns, the wait included.
+__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// Two 32-bit numbers in one 64-bit register pair: sm_100 multiplies and adds them in one instruction.
+__device__ __forceinline__ uint64_t pair32(float a, float b) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float lo32(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float hi32(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max3f(uint32_t a, uint32_t b, uint32_t c) {
+    return max3f(__uint_as_float(a), __uint_as_float(b), __uint_as_float(c));
+}
 
 // A wait of a whole warp: its lanes give up together, since they meet in warp-wide instructions later.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl, int where) {
@@ -160,7 +208,8 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&c.k_full[i], 1);
             mbar_init(&c.v_full[i], 1);
-            mbar_init(&c.empty[i], S::kEngines);
+            mbar_init(&c.k_empty[i], S::kEngines);
+            mbar_init(&c.v_empty[i], S::kEngines);
         }
         for (int e = 0; e < S::kEngines; ++e) {
             mbar_init(&c.s_full[e], 1);
@@ -180,33 +229,31 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         tmem_alloc(&c.tmem, 512);
         tmem_relinquish();
     }
-    // selections to shared memory where they fit
+    // selections to shared memory where they fit, a warp to a token; all copies are in flight at once
     const bool lists_here = tokens * p.n_select <= S::kListInts;
     if (lists_here) {
-        for (int i = tid; i < tokens * p.n_select; i += S::kThreads) {
-            const int tok = i / p.n_select, at = i - tok * p.n_select;
-            s_list[i] = p.selected[((w0 + tok) * p.n_kv_heads + h) * p.n_select + at];
+        for (int tok = warp; tok < tokens; tok += S::kWarps) {
+            const int32_t* src = p.selected + ((w0 + tok) * p.n_kv_heads + h) * p.n_select;
+            for (int i = lane; i < p.n_select; i += 32) cp_async4(smem_u32(s_list + tok * p.n_select + i), src + i);
         }
     }
     // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits
     {
-        const float sign = p.scale_log2 < 0.0f ? -1.0f : 1.0f;
-        const uint32_t flip = sign < 0.0f ? 0x80008000u : 0u;  // a negative scale is a positive one of negated queries
-        constexpr int kPieces = DB * 8;
-        for (int i = tid; i < S::kRows * kPieces; i += S::kThreads) {
-            const int row = i / kPieces, piece = i % kPieces;
+        constexpr int kPieces = DB * 8, kStep = S::kThreads / kPieces;  // rows at a time
+        const int piece = tid % kPieces;
+        for (int row = tid / kPieces; row < S::kRows && tid < kStep * kPieces; row += kStep) {
             const int e = row >> 7, r = row & 127;
-            const int tok = e * per_engine + r / p.group;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < per_engine * p.group && tok < tokens && piece * 8 < p.dim) {
-                v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (w0 + tok) * p.q_stride[0] +
-                                                    (static_cast<int64_t>(h) * p.group + r % p.group) * p.q_stride[1] + piece * 8);
-                v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
-            }
-            *reinterpret_cast<uint4*>(smem + e * S::kQBytes + (piece >> 3) * (128 * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v;
+            const int in_engine = r / p.group;
+            const int tok = e * per_engine + in_engine;
+            const bool ok = in_engine < per_engine && tok < tokens && piece * 8 < p.dim;
+            const T* src = static_cast<const T*>(p.q);
+            if (ok) src += (w0 + tok) * p.q_stride[0] + (static_cast<int64_t>(h) * p.group + r - in_engine * p.group) * p.q_stride[1] + piece * 8;
+            cp_async16(smem_u32(smem + e * S::kQBytes + (piece >> 3) * (128 * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)), src, ok);
         }
-        fence_proxy_async_smem();
     }
+    cp_async_commit();
+    cp_async_wait<0>();
+    fence_proxy_async_smem();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -244,14 +291,13 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 cur[k] = entry(k);
             }
         }
-        int last_seg = -1, last_pos = -1;
+        int last_seg = -1, last_pos = -1, k_issued = 0, v_issued = 0;
         bool ok = true;
         int j = 0;
         for (;; ++j) {
-            const int stage = j % S::kStages;
-            if (j >= S::kStages && !(ok = warp_wait(&c.empty[stage], (j / S::kStages - 1) & 1, ctl, 201))) break;
-            TileInfo<DB>& info = c.info[stage];
-            int n = 0, my_page = -1;
+            // the next tile's pages are gathered while its stage is still in use; the info ring is one longer
+            TileInfo<DB>& info = c.info[j % (S::kStages + 1)];
+            int n = 0, my_block = 0, my_owner = 0;
             while (n < per_tile) {
                 uint32_t least = kNoKey;
 #pragma unroll
@@ -283,13 +329,10 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     last_pos = __reduce_max_sync(0xFFFFFFFFu, far);
                     last_seg = s;
                 }
-                int page = -1;
-                if (block < p.max_blocks) page = p.table[c.req[owner] * p.table_stride + block];
-                if (page < 0 || page >= p.num_pages) {
-                    if (lane == 0 && (block >= p.max_blocks || page >= p.num_pages)) kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
-                    continue;
+                if (lane == n) {
+                    my_block = block;
+                    my_owner = owner;
                 }
-                if (lane == n) my_page = page;
                 if (lane < 8) info.members[n][lane] = mine;
                 if (lane == 0) {
                     info.first[n] = block << p.page_shift;
@@ -297,37 +340,57 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
                 ++n;
             }
-            if (lane == 0) info.n_pages = n;
+            // all pages of the tile are looked up at once; a page that is not there sees no members
+            int page = -1;
             __syncwarp();
-            if (lane == 0) {
-                if (n == 0) {
-                    mbar_arrive(&c.k_full[stage]);
-                } else {
-                    mbar_arrive_expect_tx(&c.k_full[stage], n * DB * page_size * 128);
-                    mbar_arrive_expect_tx(&c.v_full[stage], n * DB * page_size * 128);
+            if (lane < n) {
+                if (my_block < p.max_blocks) page = p.table[c.req[my_owner] * p.table_stride + my_block];
+                if (my_block >= p.max_blocks || page >= p.num_pages) {
+                    kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
+                    page = -1;
+                }
+                if (page < 0) {
+                    page = 0;  // a stand-in, all of it zeroed or unseen
+                    info.dead[lane] = 0;
+                    for (int k = 0; k < 8; ++k) info.members[lane][k] = 0;
                 }
             }
+            if (lane == 0) info.n_pages = n;
+            const int stage = j % S::kStages;
+            const uint32_t used = (j / S::kStages - 1) & 1;
+            const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * page_size * 128;
+            if (j >= S::kStages && !(ok = warp_wait(&c.k_empty[stage], used, ctl, 201))) break;
             __syncwarp();
+            if (lane == 0) {
+                if (n == 0) mbar_arrive(&c.k_full[stage]);
+                else mbar_arrive_expect_tx(&c.k_full[stage], n * DB * page_size * 128);
+            }
             if (n == 0) break;
+            __syncwarp();
             if (lane < n) {
-                const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * page_size * 128;
 #pragma unroll
-                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, 0, h, my_page);
+                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, 0, h, page);
+            }
+            k_issued = j + 1;
+            if (j >= S::kStages && !(ok = warp_wait(&c.v_empty[stage], used, ctl, 210))) break;
+            if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], n * DB * page_size * 128);
+            __syncwarp();
+            if (lane < n) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
-                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, 0, h, my_page);
+                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, 0, h, page);
             }
-            __syncwarp();
+            v_issued = j + 1;
         }
         if (!ok && lane == 0) {
             // gave up: let the copies already issued land before the CTA goes away (bounded)
             const uint64_t t0 = global_timer_ns();
-            for (int i = max(0, j - S::kStages); i < j; ++i) {
-                const uint32_t ph = (i / S::kStages) & 1;
-                while ((!mbar_try_wait(&c.k_full[i % S::kStages], ph) || !mbar_try_wait(&c.v_full[i % S::kStages], ph)) &&
-                       global_timer_ns() - t0 < 2000000000ull) {
+            for (int i = max(0, k_issued - S::kStages); i < k_issued; ++i)
+                while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                 }
-            }
+            for (int i = max(0, v_issued - S::kStages); i < v_issued; ++i)
+                while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
+                }
         }
     } else if (warp >= 4 * S::kEngines) {
         // ------------------------------------------------------------ MMA of engine e
@@ -337,24 +400,26 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             const uint32_t q_lo = umma_desc_lo(smem_u32(smem) + e * S::kQBytes);
             const uint32_t ring0 = smem_u32(ring);
             const uint32_t idesc_o = tile_idesc<T>(p.dim, true);
+            const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const int ksteps = p.dim >> 4;
             bool ok = true, issued = false;
             for (int j = 0;; ++j) {
                 const int stage = j % S::kStages;
                 const uint32_t ph = (j / S::kStages) & 1;
                 if (!(ok = mbar_wait(&c.k_full[stage], ph, ctl, 202))) break;
-                const int keys = c.info[stage].n_pages << p.page_shift;
+                const int keys = c.info[j % (S::kStages + 1)].n_pages << p.page_shift;
                 if (keys == 0) break;
                 if (j > 0 && !(ok = mbar_wait(&c.pv_done[e], (j - 1) & 1, ctl, 203))) break;
                 tc_fence_after_sync();
                 const uint32_t k_lo = umma_desc_lo(ring0 + stage * S::kStageBytes);
-                const uint32_t idesc_s = tile_idesc<T>(keys, false);
+                const uint32_t idesc_s = tile_idesc<T>(keys, false) | negate;
                 for (int k = 0; k < ksteps; ++k) {
                     const uint32_t in = (k & 3) * 2, blk = k >> 2;
                     umma_f16(t_s, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
                              umma_desc_join(k_lo + blk * (S::kBlockBytes >> 4) + in, kDescHiSw128), idesc_s, k > 0);
                 }
                 umma_commit(&c.s_full[e]);
+                umma_commit(&c.k_empty[stage]);
                 issued = true;
                 if (!(ok = mbar_wait(&c.v_full[stage], ph, ctl, 204))) break;
                 if (!(ok = mbar_wait(&c.p_ready[e], j & 1, ctl, 205))) break;
@@ -365,7 +430,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 for (int k = 0; k < keys >> 4; ++k)
                     umma_f16_ts(t_o, t_s + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (j > 0 || k > 0) ? 1u : 0u);
                 umma_commit(&c.pv_done[e]);
-                umma_commit(&c.empty[stage]);
+                umma_commit(&c.v_empty[stage]);
             }
             if (!ok && issued) {
                 umma_commit(&c.drain[e]);
@@ -394,15 +459,28 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             const int stage = j % S::kStages;
             const uint32_t ph = (j / S::kStages) & 1;
             if (!(ok = warp_wait(&c.k_full[stage], ph, ctl, 206))) break;
-            const TileInfo<DB>& info = c.info[stage];
+            const TileInfo<DB>& info = c.info[j % (S::kStages + 1)];
             const int n_pages = info.n_pages;
             if (n_pages == 0) break;
-            // value rows that no token of the window sees
-            bool zeroed = false;
+            // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees
+            uint32_t full = 0, part = 0;
+            int rem = 0;
+            bool tail = false;
             for (int i = 0; i < n_pages; ++i) {
-                if (info.dead[i] < page_size) {
-                    if (!zeroed && !(ok = warp_wait(&c.v_full[stage], ph, ctl, 207))) break;
-                    zeroed = true;
+                const int seen = (info.members[i][word] & bit) ? min(max(pos + 1 - info.first[i], 0), page_size) : 0;
+                const int g0 = (i << p.page_shift) >> 4;
+                full |= ((1u << (seen >> 4)) - 1) << g0;
+                if (seen & 15) {
+                    part |= 1u << (g0 + (seen >> 4));
+                    rem = seen & 15;
+                }
+                tail |= info.dead[i] < page_size;
+            }
+            const uint32_t mine = full | part;
+            const uint32_t some = __reduce_or_sync(0xFFFFFFFFu, mine), cut = __reduce_or_sync(0xFFFFFFFFu, part);
+            if (tail) {  // value rows that no token of the window sees
+                if (!(ok = warp_wait(&c.v_full[stage], ph, ctl, 207))) break;
+                for (int i = 0; i < n_pages; ++i) {
                     const int rows = page_size - info.dead[i];
                     uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * page_size + info.dead[i]) * 128;
                     for (int x = r; x < rows * 8 * DB; x += 128) {
@@ -410,9 +488,8 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                         *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                     }
                 }
+                fence_proxy_async_smem();
             }
-            if (!ok) break;
-            if (zeroed) fence_proxy_async_smem();
             if (!(ok = warp_wait(&c.s_full[e], j & 1, ctl, 208))) break;
             tc_fence_after_sync();
             uint32_t s[S::kKeys / 32][32];
@@ -420,28 +497,25 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             for (int q = 0; q < S::kKeys / 32; ++q) tmem_ld_32x32b_x32(t_s + q * 32, s[q]);
 #pragma unroll
             for (int q = 0; q < S::kKeys / 32; ++q) tmem_wait_ld_regs(s[q]);
-            // keys seen in each group of 16: all, none or the first few
-            float top = -INFINITY;
-            uint32_t some = 0;  // groups that some row of the warp sees
+            if (cut) {
 #pragma unroll
-            for (int g = 0; g < S::kKeys / 16; ++g) {
-                const int i = (g * 16) >> p.page_shift;
-                int seen = 0;
-                if (i < n_pages && (info.members[i][word] & bit)) seen = pos + 1 - info.first[i] - ((g * 16) & (page_size - 1));
-                if (__any_sync(0xFFFFFFFFu, seen > 0)) {
-                    some |= 1u << g;
-                    if (!__all_sync(0xFFFFFFFFu, seen >= 16)) {
+                for (int g = 0; g < S::kKeys / 16; ++g) {
+                    if (cut >> g & 1) {
+                        const int seen = part >> g & 1 ? rem : 16;
 #pragma unroll
                         for (int x = 0; x < 16; ++x)
                             if (x >= seen) s[g >> 1][(g & 1) * 16 + x] = 0xFF800000u;
                     }
-                    float t0 = -INFINITY, t1 = -INFINITY;
+                }
+            }
+            float top = -INFINITY;
 #pragma unroll
-                    for (int x = 0; x < 16; x += 2) {
-                        t0 = fmaxf(t0, __uint_as_float(s[g >> 1][(g & 1) * 16 + x]));
-                        t1 = fmaxf(t1, __uint_as_float(s[g >> 1][(g & 1) * 16 + x + 1]));
-                    }
-                    top = fmaxf(top, fmaxf(t0, t1));
+            for (int g = 0; g < S::kKeys / 16; ++g) {
+                if (some >> g & 1) {
+                    const uint32_t* v = &s[g >> 1][(g & 1) * 16];
+                    const float a = max3f(v[0], v[1], v[2]), b = max3f(v[3], v[4], v[5]), d = max3f(v[6], v[7], v[8]), f = max3f(v[9], v[10], v[11]);
+                    const float t = fmaxf(max3f(max3f(a, b, d), f, max3f(v[12], v[13], v[14])), __uint_as_float(v[15]));
+                    if (mine >> g & 1) top = fmaxf(top, t);
                 }
             }
             const bool grow = top > m + slack || (m == -INFINITY && top > m);
@@ -450,49 +524,51 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 if (grow) m = top;
                 if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {
                     l *= fix;
-                    for (int q = 0; q < (p.dim + 31) / 32; ++q) {
-                        uint32_t o[32];
-                        tmem_ld_32x32b_x32(t_o + q * 32, o);
-                        tmem_wait_ld_regs(o);
+                    for (int q = 0; q < p.dim >> 4; ++q) {  // 16 columns at a time: the logits stay in registers
+                        uint32_t o[16];
+                        tmem_ld_32x32b_x16(t_o + q * 16, o);
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fix);
-                        tmem_st_32x32b_x32(t_o + q * 32, o);
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * fix);
+                        tmem_st_32x32b_x16(t_o + q * 16, o);
                     }
                 }
             }
             const float base = m == -INFINITY ? 0.0f : m * scale;
-            float sum0 = 0.0f, sum1 = 0.0f;
+            uint64_t sum = 0;  // two 32-bit sums side by side
+            const uint64_t scale2 = pair32(scale, scale);
 #pragma unroll
-            for (int q = 0; q < S::kKeys / 64; ++q) {
-                uint32_t out[32];
+            for (int g2 = 0; g2 < S::kKeys / 32; ++g2) {
+                uint32_t out[16];
 #pragma unroll
-                for (int g = 4 * q; g < 4 * q + 4; ++g) {
+                for (int g = 2 * g2; g < 2 * g2 + 2; ++g) {
                     if (some >> g & 1) {
+                        const float off = mine >> g & 1 ? -base : -INFINITY;  // a group that the row does not see: all weights 0
+                        const uint64_t off2 = pair32(off, off);
 #pragma unroll
                         for (int x = 0; x < 16; x += 2) {
-                            const float a = exp2_fast(fmaf(__uint_as_float(s[g >> 1][(g & 1) * 16 + x]), scale, -base));
-                            const float b = exp2_fast(fmaf(__uint_as_float(s[g >> 1][(g & 1) * 16 + x + 1]), scale, -base));
-                            sum0 += a;
-                            sum1 += b;
-                            out[(g & 3) * 8 + x / 2] = Pair16<T>::pack(a, b);
+                            const uint64_t z = fma2(pair32(__uint_as_float(s[g2][(g & 1) * 16 + x]), __uint_as_float(s[g2][(g & 1) * 16 + x + 1])), scale2, off2);
+                            const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
+                            sum = add2(sum, pair32(a, b));
+                            out[(g & 1) * 8 + x / 2] = Pair16<T>::pack(a, b);
                         }
                     } else {
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) out[(g & 3) * 8 + x] = 0u;
+                        for (int x = 0; x < 8; ++x) out[(g & 1) * 8 + x] = 0u;
                     }
                 }
-                tmem_st_32x32b_x32(t_s + q * 32, out);
+                tmem_st_32x32b_x16(t_s + g2 * 16, out);
             }
-            l += sum0 + sum1;
+            l += lo32(sum) + hi32(sum);
             tmem_wait_st();
             tc_fence_before_sync();
             mbar_arrive(&c.p_ready[e]);
         }
         if (ok && j > 0 && (ok = warp_wait(&c.pv_done[e], (j - 1) & 1, ctl, 209))) tc_fence_after_sync();
         if (ok) {
+            // through the engine's query tile, which its products have left: a warp's 32 rows go out with whole
+            // rows side by side
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int64_t head = static_cast<int64_t>(h) * p.group + r % p.group;
-            T* dst = static_cast<T*>(p.out) + (w0 + tok) * p.out_stride[0] + head * p.out_stride[1];
+            uint8_t* stash = smem + e * S::kQBytes + (warp & 3) * (32 * DB * 128);
             bool bad = false;
             for (int q = 0; q < (p.dim + 31) / 32; ++q) {
                 uint32_t o[32];
@@ -500,23 +576,35 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     tmem_ld_32x32b_x32(t_o + q * 32, o);
                     tmem_wait_ld_regs(o);
                 }
-                if (row_live) {
 #pragma unroll
-                    for (int x = 0; x < 32; x += 8) {
-                        if (q * 32 + x < p.dim) {
-                            float f[8];
+                for (int x = 0; x < 32; x += 8) {
+                    if (q * 32 + x < p.dim) {
+                        float f[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                f[i] = l == 0.0f ? 0.0f : __uint_as_float(o[x + i]) * inv;
-                                bad |= !(fabsf(f[i]) <= 3.4e38f);
-                            }
-                            *reinterpret_cast<uint4*>(dst + q * 32 + x) = pack8<T>(f);
+                        for (int i = 0; i < 8; ++i) {
+                            f[i] = l == 0.0f ? 0.0f : __uint_as_float(o[x + i]) * inv;
+                            bad |= row_live && !(fabsf(f[i]) <= 3.4e38f);
                         }
+                        *reinterpret_cast<uint4*>(stash + lane * (DB * 128) + (((q * 4 + x / 8) ^ (lane & 7)) << 4)) = pack8<T>(f);
                     }
                 }
             }
+            __syncwarp();
+            const int pieces = p.dim >> 3;
+            constexpr int kAtOnce = 32 / (DB * 8) > 0 ? 32 / (DB * 8) : 1;  // rows of a store
+            for (int row0 = 0; row0 < 32; row0 += kAtOnce) {
+                const int row = row0 + lane / (DB * 8 < 32 ? DB * 8 : 32), piece = lane % (DB * 8 < 32 ? DB * 8 : 32);
+                const int er = (warp & 3) * 32 + row, et = er / p.group;
+                const int tk = e * per_engine + et;
+                if (et < per_engine && tk < tokens && piece < pieces) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(stash + row * (DB * 128) + ((piece ^ (row & 7)) << 4));
+                    *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + (w0 + tk) * p.out_stride[0] +
+                                              (static_cast<int64_t>(h) * p.group + er - et * p.group) * p.out_stride[1] + piece * 8) = v;
+                }
+            }
             if (row_live && p.lse)
-                p.lse[(w0 + tok) * p.group * p.n_kv_heads + head] = l == 0.0f ? -INFINITY : (m * scale + log2f(l)) * 0.69314718055994531f;
+                p.lse[(w0 + tok) * p.group * p.n_kv_heads + static_cast<int64_t>(h) * p.group + r - in_engine * p.group] =
+                    l == 0.0f ? -INFINITY : (m * scale + log2f(l)) * 0.69314718055994531f;
             if (bad) c.bad = 1;
         }
     }
