@@ -114,7 +114,7 @@ int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t s
     return kv_launch_rows<T, 256>(p, ctx, stream);
 }
 
-// A page of one head, 64 columns wide, with the 128-byte swizzle.
+// A page of one head (64 tokens of it at most), 64 columns wide, with the 128-byte swizzle.
 bool kv_make_map(CUtensorMap* map, const KvPlane& c, const KvAttendParams& p, bool bf16) {
     const int64_t page = 1 << p.page_shift;
     const int64_t size[4] = {p.dim, page, p.n_kv_heads, p.num_pages};
@@ -126,7 +126,7 @@ bool kv_make_map(CUtensorMap* map, const KvPlane& c, const KvAttendParams& p, bo
         strides[i] = static_cast<cuuint64_t>(stride[i] == 0 ? p.dim : stride[i]) * 2;
         if (strides[i] >= (cuuint64_t(1) << 40)) return false;
     }
-    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(page), 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(std::min<int64_t>(page, 64)), 1, 1}, step[4] = {1, 1, 1, 1};
     return g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, c.base, dims, strides, box, step,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -144,12 +144,11 @@ int kv_launch_tile(const KvAttendParams& p, const CUtensorMap& mk, const CUtenso
 template <typename T>
 int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     p.done = nullptr;
-    p.window = (p.dim > 128 ? 1 : 2) * (128 / p.group);
+    p.window = 128 / p.group;
     p.limit_ns = g_wait_limit_ns.load();
     CUtensorMap mk, mv;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    bool tile = g_kv_attend != 1 && p.dim >= 64 && p.max_blocks < kTileMaxBlocks && p.num_pages > 0 &&
-                (p.dim <= 128 || p.page_shift <= 6);  // a tile of wide heads has 64 keys
+    bool tile = g_kv_attend != 1 && p.dim >= 64 && p.max_blocks < kTileMaxBlocks && p.num_pages > 0;
     if (g_kv_attend == 0) tile = tile && p.n_tokens >= 2 * p.n_req && p.n_tokens * p.group >= 128;
     if (tile) {
         if (int rc = get_encode()) return rc;

@@ -1,19 +1,20 @@
 // Attention over selected blocks for prompt chunks: 5th-generation tensor cores, keys and values by TMA.
 //
 // Neighbouring tokens of a prompt select much the same blocks.  A CTA takes a window of consecutive tokens and one kv
-// head; its rows are (token, query head of the group), 128 to an engine, and it walks the union of the blocks
-// that any token of the window selected, each block fetched once for all rows.  A row that did not select a
-// block sees it masked.
+// head; its 128 rows are (token, query head of the group), and it walks the union of the blocks that any token of the
+// window selected, each block fetched once for all rows.  A row that did not select a block sees it masked.
 //
 //   producer warp   merges the tokens' ascending lists (the smallest head of all lists is the next block, the
 //                   lanes whose list shows it are its members), looks the pages up and issues the copies
-//   MMA warp        of each engine: S = Q K^T into TMEM, then O += P V with P read from TMEM
-//   softmax warps   of each engine, one thread per row: S out of TMEM, running maximum and sum in registers, P back
-//                   into TMEM over S.  O is rescaled only when the maximum has grown by more than 2^8 since
-//                   the reference was set; the reference cancels in the final division.
+//   MMA warp        S = Q K^T into TMEM, then O += P V with P read from TMEM
+//   softmax warps   one thread per row: S out of TMEM, running maximum and sum in registers, P back into TMEM over
+//                   S.  O is rescaled only when the maximum has grown by more than 2^8 since the reference was
+//                   set; the reference cancels in the final division.
 //
-// S(j + 1) is issued when P(j) V has retired, so P and S share their TMEM columns and the softmax warps may touch O.
-// The other engine's products run meanwhile.
+// A tile is 64 keys.  S and P of a tile share 64 TMEM columns and there are two such buffers: S(j + 2) is issued when
+// P(j) V has retired, while the softmax warps are at work on tile j + 1, so they never wait for a product.  With one
+// buffer of 128 keys the products and the softmax of a CTA took turns: 5,600 cycles for 128 keys against the
+// figures below.  Two CTAs live on an SM (one for heads wider than 128) and fill each other's waits.
 //
 // What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
 // value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
@@ -26,35 +27,36 @@ namespace ivf {
 // DB: 64-element blocks of a head (1, 2, 4).
 template <int DB>
 struct TileShape {
-    static constexpr int kEngines = DB == 4 ? 1 : 2;
-    static constexpr int kKeys = DB == 4 ? 64 : 128;  // keys of a tile
-    static constexpr int kStages = DB == 1 ? 4 : 2;
-    static constexpr int kPages = kKeys / 16;  // pages of a tile at most
+    static constexpr int kCtas = DB == 4 ? 1 : 2;       // on an SM
+    static constexpr int kKeys = 64;                    // keys of a tile
+    static constexpr int kStages = 2;
+    static constexpr int kInfos = kStages + 2;          // the producer gathers a tile's pages ahead of its stage
+    static constexpr int kPages = kKeys / 16;           // boxes of a tile at most
     static constexpr int kBlockBytes = kKeys * 128;     // 64 columns of all keys
     static constexpr int kPlaneBytes = DB * kBlockBytes;
     static constexpr int kStageBytes = 2 * kPlaneBytes;
-    static constexpr int kQBytes = DB * 128 * 128;      // of one engine
-    static constexpr int kListInts = 7168;
-    static constexpr int kRows = 128 * kEngines;
-    static constexpr int kWarps = 5 * kEngines + 1;     // softmax, MMA, producer
+    static constexpr int kQBytes = DB * 128 * 128;
+    static constexpr int kListInts = 2560;
+    static constexpr int kRows = 128;
+    static constexpr int kWarps = 6;                    // softmax 0-3, MMA 4, producer 5
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kOCol = kKeys;                 // TMEM columns of an engine: S (and P), then O
-    static constexpr int kEngineCols = DB == 4 ? 512 : 256;
+    static constexpr int kOCol = 2 * kKeys;             // TMEM columns: S (and P) twice, then O
+    static constexpr int kCols = DB == 4 ? 512 : 256;
 };
 
 template <int DB>
 struct TileInfo {  // what the producer says about a stage
-    int n_pages;
-    int first[TileShape<DB>::kPages];      // position of the page's first token
+    int n_boxes;  // pages, or halves of a page of 128; 0 ends the list
+    int first[TileShape<DB>::kPages];      // position of the box's first token
     int dead[TileShape<DB>::kPages];       // tokens from here on lie past the window's last: value rows to be zeroed
-    uint32_t members[TileShape<DB>::kPages][8];  // tokens of the window that selected the page
+    uint32_t members[TileShape<DB>::kPages][4];  // tokens of the window that selected it
 };
 
 template <int DB>
 struct TileControl {
-    uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4];
-    uint64_t s_full[2], p_ready[2], pv_done[2], drain[2];
-    TileInfo<DB> info[TileShape<DB>::kStages + 1];
+    uint64_t info_full[4], k_full[2], v_full[2], k_empty[2], v_empty[2];
+    uint64_t s_full[2], p_ready[2], pv_done[2], drain;  // by the tile's parity: a waiter may be one tile late, not two
+    TileInfo<DB> info[TileShape<DB>::kInfos];
     int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows];
     uint32_t tmem;
     int abort_flag, bad;
@@ -63,7 +65,7 @@ struct TileControl {
 template <int DB>
 constexpr int tile_smem() {
     using S = TileShape<DB>;
-    return 1024 + S::kEngines * S::kQBytes + S::kStages * S::kStageBytes + S::kListInts * 4 + static_cast<int>(sizeof(TileControl<DB>));
+    return 1024 + S::kQBytes + S::kStages * S::kStageBytes + S::kListInts * 4 + static_cast<int>(sizeof(TileControl<DB>));
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
@@ -165,19 +167,18 @@ constexpr uint32_t kNoKey = 0xFFFFFFFFu;
 constexpr int kTileMaxBlocks = 1 << 24;  // block number and segment share a key
 
 template <typename T, int DB>
-__global__ void __launch_bounds__(TileShape<DB>::kThreads, 1)
+__global__ void __launch_bounds__(TileShape<DB>::kThreads, TileShape<DB>::kCtas)
 kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const KvAttendParams p) {
     using S = TileShape<DB>;
     extern __shared__ uint8_t tile_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* ring = smem + S::kEngines * S::kQBytes;
+    uint8_t* ring = smem + S::kQBytes;
     int* s_list = reinterpret_cast<int*>(ring + S::kStages * S::kStageBytes);
     TileControl<DB>& c = *reinterpret_cast<TileControl<DB>*>(s_list + S::kListInts);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y;
     const int64_t w0 = static_cast<int64_t>(blockIdx.x) * p.window;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(p.window), p.n_tokens - w0));
-    const int per_engine = 128 / p.group;  // tokens of an engine
     uint8_t* done = p.done + static_cast<int64_t>(blockIdx.x) * p.n_kv_heads + h;
 
     // ---- the window's tokens; one of many requests is left to the rows kernel: below 8 tokens to a request the
@@ -208,15 +209,17 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&c.k_full[i], 1);
             mbar_init(&c.v_full[i], 1);
-            mbar_init(&c.k_empty[i], S::kEngines);
-            mbar_init(&c.v_empty[i], S::kEngines);
+            mbar_init(&c.k_empty[i], 1);
+            mbar_init(&c.v_empty[i], 1);
         }
-        for (int e = 0; e < S::kEngines; ++e) {
-            mbar_init(&c.s_full[e], 1);
-            mbar_init(&c.p_ready[e], 128);
-            mbar_init(&c.pv_done[e], 1);
-            mbar_init(&c.drain[e], 1);
-        }
+        for (int i = 0; i < S::kInfos; ++i) mbar_init(&c.info_full[i], 1);
+        mbar_init(&c.s_full[0], 1);
+        mbar_init(&c.s_full[1], 1);
+        mbar_init(&c.p_ready[0], 128);
+        mbar_init(&c.p_ready[1], 128);
+        mbar_init(&c.pv_done[0], 1);
+        mbar_init(&c.pv_done[1], 1);
+        mbar_init(&c.drain, 1);
         c.abort_flag = 0;
         c.bad = 0;
         fence_mbar_init();
@@ -226,7 +229,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             tma_prefetch_desc(&map_k);
             tma_prefetch_desc(&map_v);
         }
-        tmem_alloc(&c.tmem, 512);
+        tmem_alloc(&c.tmem, S::kCols);
         tmem_relinquish();
     }
     // selections to shared memory where they fit, a warp to a token; all copies are in flight at once
@@ -242,13 +245,11 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         constexpr int kPieces = DB * 8, kStep = S::kThreads / kPieces;  // rows at a time
         const int piece = tid % kPieces;
         for (int row = tid / kPieces; row < S::kRows && tid < kStep * kPieces; row += kStep) {
-            const int e = row >> 7, r = row & 127;
-            const int in_engine = r / p.group;
-            const int tok = e * per_engine + in_engine;
-            const bool ok = in_engine < per_engine && tok < tokens && piece * 8 < p.dim;
+            const int tok = row / p.group;
+            const bool ok = tok < tokens && piece * 8 < p.dim;
             const T* src = static_cast<const T*>(p.q);
-            if (ok) src += (w0 + tok) * p.q_stride[0] + (static_cast<int64_t>(h) * p.group + r - in_engine * p.group) * p.q_stride[1] + piece * 8;
-            cp_async16(smem_u32(smem + e * S::kQBytes + (piece >> 3) * (128 * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)), src, ok);
+            if (ok) src += (w0 + tok) * p.q_stride[0] + (static_cast<int64_t>(h) * p.group + row - tok * p.group) * p.q_stride[1] + piece * 8;
+            cp_async16(smem_u32(smem + (piece >> 3) * (128 * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4)), src, ok);
         }
     }
     cp_async_commit();
@@ -262,14 +263,15 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     ctl.abort_flag = &c.abort_flag;
     ctl.status = p.status;
     ctl.limit_ns = p.limit_ns;
-    const int page_size = 1 << p.page_shift;
-    const int per_tile = S::kKeys >> p.page_shift;
+    // a page of 128 tokens is fetched as two boxes of 64
+    const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;
+    const int per_tile = S::kKeys >> box_shift;
 
     if (warp == S::kWarps - 1) {
         // ------------------------------------------------------------ producer
         const int slots = (tokens + 31) >> 5;
-        uint32_t cur[8];
-        int at[8] = {}, seg[8] = {};
+        uint32_t cur[4];
+        int at[4] = {}, seg[4] = {};
         auto entry = [&](int k) -> uint32_t {
             const int tok = k * 32 + lane;
             if (tok >= tokens || c.req[tok] < 0 || at[k] >= p.n_select) return kNoKey;
@@ -279,7 +281,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         };
         int n_seg = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
             cur[k] = kNoKey;
             seg[k] = -1;
             if (k < slots) {
@@ -292,56 +294,73 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             }
         }
         int last_seg = -1, last_pos = -1, k_issued = 0, v_issued = 0;
-        bool ok = true;
-        int j = 0;
-        for (;; ++j) {
-            // the next tile's pages are gathered while its stage is still in use; the info ring is one longer
-            TileInfo<DB>& info = c.info[j % (S::kStages + 1)];
+        int half_block = -1, half_owner = 0;  // a page of 128 whose second box is due
+        uint32_t half_mine = 0;
+        int page = -1, row = 0;  // of this lane's box
+        // the pages of tile j: their members into the info ring, the number of boxes back
+        auto gather = [&](int j) -> int {
+            TileInfo<DB>& info = c.info[j % S::kInfos];
             int n = 0, my_block = 0, my_owner = 0;
             while (n < per_tile) {
-                uint32_t least = kNoKey;
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < slots) least = min(least, cur[k]);
-                const uint32_t key = __reduce_min_sync(0xFFFFFFFFu, least);
-                if (key == kNoKey) break;
-                int owner = -1;
+                int block, owner = -1, sub = 0;
                 uint32_t mine = 0;  // lane k keeps word k of the members
+                if (half_block >= 0) {
+                    block = half_block;
+                    owner = half_owner;
+                    mine = half_mine;
+                    sub = 64;
+                    half_block = -1;
+                } else {
+                    uint32_t least = kNoKey;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (k < slots) {
-                        const bool member = cur[k] == key;
-                        const unsigned m = __ballot_sync(0xFFFFFFFFu, member);
-                        if (m && owner < 0) owner = k * 32 + __ffs(m) - 1;
-                        if (lane == k) mine = m;
-                        if (member) {
-                            ++at[k];
-                            cur[k] = entry(k);
+                    for (int k = 0; k < 4; ++k)
+                        if (k < slots) least = min(least, cur[k]);
+                    const uint32_t key = __reduce_min_sync(0xFFFFFFFFu, least);
+                    if (key == kNoKey) break;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k < slots) {
+                            const bool member = cur[k] == key;
+                            const unsigned m = __ballot_sync(0xFFFFFFFFu, member);
+                            if (m && owner < 0) owner = k * 32 + __ffs(m) - 1;
+                            if (lane == k) mine = m;
+                            if (member) {
+                                ++at[k];
+                                cur[k] = entry(k);
+                            }
                         }
                     }
-                }
-                const int block = static_cast<int>(key & 0xFFFFFFu), s = static_cast<int>(key >> 24);
-                if (s != last_seg) {  // the last position that any token of the segment sees
-                    int far = -1;
+                    block = static_cast<int>(key & 0xFFFFFFu);
+                    const int s = static_cast<int>(key >> 24);
+                    if (s != last_seg) {  // the last position that any token of the segment sees
+                        int far = -1;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < slots && seg[k] == s && k * 32 + lane < tokens) far = max(far, c.pos[k * 32 + lane]);
-                    last_pos = __reduce_max_sync(0xFFFFFFFFu, far);
-                    last_seg = s;
+                        for (int k = 0; k < 4; ++k)
+                            if (k < slots && seg[k] == s && k * 32 + lane < tokens) far = max(far, c.pos[k * 32 + lane]);
+                        last_pos = __reduce_max_sync(0xFFFFFFFFu, far);
+                        last_seg = s;
+                    }
+                    if (p.page_shift == 7 && (block << 7) + 64 <= last_pos) {
+                        half_block = block;
+                        half_owner = owner;
+                        half_mine = mine;
+                    }
                 }
+                const int first = (block << p.page_shift) + sub;
                 if (lane == n) {
                     my_block = block;
                     my_owner = owner;
+                    row = sub;
                 }
-                if (lane < 8) info.members[n][lane] = mine;
+                if (lane < 4) info.members[n][lane] = mine;
                 if (lane == 0) {
-                    info.first[n] = block << p.page_shift;
-                    info.dead[n] = min(page_size, last_pos + 1 - (block << p.page_shift));
+                    info.first[n] = first;
+                    info.dead[n] = min(box, last_pos + 1 - first);
                 }
                 ++n;
             }
             // all pages of the tile are looked up at once; a page that is not there sees no members
-            int page = -1;
+            page = -1;
             __syncwarp();
             if (lane < n) {
                 if (my_block < p.max_blocks) page = p.table[c.req[my_owner] * p.table_stride + my_block];
@@ -350,35 +369,41 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     page = -1;
                 }
                 if (page < 0) {
-                    page = 0;  // a stand-in, all of it zeroed or unseen
+                    page = 0;  // a stand-in, all of it zeroed and unseen
                     info.dead[lane] = 0;
-                    for (int k = 0; k < 8; ++k) info.members[lane][k] = 0;
+                    for (int k = 0; k < 4; ++k) info.members[lane][k] = 0;
                 }
             }
-            if (lane == 0) info.n_pages = n;
+            if (lane == 0) info.n_boxes = n;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.info_full[j % S::kInfos]);
+            return n;
+        };
+        bool ok = true;
+        int n = gather(0);
+        for (int j = 0;; ++j) {
             const int stage = j % S::kStages;
             const uint32_t used = (j / S::kStages - 1) & 1;
-            const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * page_size * 128;
-            if (j >= S::kStages && !(ok = warp_wait(&c.k_empty[stage], used, ctl, 201))) break;
-            __syncwarp();
-            if (lane == 0) {
-                if (n == 0) mbar_arrive(&c.k_full[stage]);
-                else mbar_arrive_expect_tx(&c.k_full[stage], n * DB * page_size * 128);
-            }
+            const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * box * 128;
+            const int bytes = n * DB * box * 128;
             if (n == 0) break;
+            if (j >= S::kStages && !(ok = warp_wait(&c.k_empty[stage], used, ctl, 201))) break;
+            if (lane == 0) mbar_arrive_expect_tx(&c.k_full[stage], bytes);
             __syncwarp();
             if (lane < n) {
 #pragma unroll
-                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, 0, h, page);
+                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, row, h, page);
             }
             k_issued = j + 1;
+            const int v_page = page, v_row = row, v_n = n;
+            n = gather(j + 1);  // while the values' stage is still in use
             if (j >= S::kStages && !(ok = warp_wait(&c.v_empty[stage], used, ctl, 210))) break;
-            if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], n * DB * page_size * 128);
+            if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], bytes);
             __syncwarp();
-            if (lane < n) {
+            if (lane < v_n) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
-                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, 0, h, page);
+                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, v_row, h, v_page);
             }
             v_issued = j + 1;
         }
@@ -392,64 +417,75 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                 }
         }
-    } else if (warp >= 4 * S::kEngines) {
-        // ------------------------------------------------------------ MMA of engine e
-        const int e = warp - 4 * S::kEngines;
+    } else if (warp == 4) {
+        // ------------------------------------------------------------ MMA
         if (lane == 0) {
-            const uint32_t t_s = tmem + e * S::kEngineCols, t_o = t_s + S::kOCol;
-            const uint32_t q_lo = umma_desc_lo(smem_u32(smem) + e * S::kQBytes);
+            const uint32_t t_s = tmem, t_o = t_s + S::kOCol;
+            const uint32_t q_lo = umma_desc_lo(smem_u32(smem));
             const uint32_t ring0 = smem_u32(ring);
             const uint32_t idesc_o = tile_idesc<T>(p.dim, true);
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const int ksteps = p.dim >> 4;
             bool ok = true, issued = false;
-            for (int j = 0;; ++j) {
+            // S of tile j into its buffer; false when the tiles are over or a wait gave up
+            auto score = [&](int j) -> bool {
                 const int stage = j % S::kStages;
-                const uint32_t ph = (j / S::kStages) & 1;
-                if (!(ok = mbar_wait(&c.k_full[stage], ph, ctl, 202))) break;
-                const int keys = c.info[j % (S::kStages + 1)].n_pages << p.page_shift;
-                if (keys == 0) break;
-                if (j > 0 && !(ok = mbar_wait(&c.pv_done[e], (j - 1) & 1, ctl, 203))) break;
+                if (!(ok = mbar_wait(&c.info_full[j % S::kInfos], (j / S::kInfos) & 1, ctl, 212))) return false;
+                const int keys = c.info[j % S::kInfos].n_boxes << box_shift;
+                if (keys == 0) return false;
+                if (!(ok = mbar_wait(&c.k_full[stage], (j / S::kStages) & 1, ctl, 202))) return false;
                 tc_fence_after_sync();
                 const uint32_t k_lo = umma_desc_lo(ring0 + stage * S::kStageBytes);
                 const uint32_t idesc_s = tile_idesc<T>(keys, false) | negate;
                 for (int k = 0; k < ksteps; ++k) {
                     const uint32_t in = (k & 3) * 2, blk = k >> 2;
-                    umma_f16(t_s, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
+                    umma_f16(t_s + (j & 1) * S::kKeys, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
                              umma_desc_join(k_lo + blk * (S::kBlockBytes >> 4) + in, kDescHiSw128), idesc_s, k > 0);
                 }
-                umma_commit(&c.s_full[e]);
+                umma_commit(&c.s_full[j & 1]);
                 umma_commit(&c.k_empty[stage]);
                 issued = true;
-                if (!(ok = mbar_wait(&c.v_full[stage], ph, ctl, 204))) break;
-                if (!(ok = mbar_wait(&c.p_ready[e], j & 1, ctl, 205))) break;
+                return true;
+            };
+            bool more = score(0);
+            int tiles = more ? 1 : 0;
+            if (more && (more = score(1))) tiles = 2;
+            for (int j = 0; ok && j < tiles; ++j) {
+                const int stage = j % S::kStages;
+                const int keys = c.info[j % S::kInfos].n_boxes << box_shift;
+                if (!(ok = mbar_wait(&c.v_full[stage], (j / S::kStages) & 1, ctl, 204))) break;
+                if (!(ok = mbar_wait(&c.p_ready[j & 1], (j >> 1) & 1, ctl, 205))) break;
                 tc_fence_after_sync();
                 // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
                 const uint32_t v_addr = ring0 + stage * S::kStageBytes + S::kPlaneBytes;
                 const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
                 for (int k = 0; k < keys >> 4; ++k)
-                    umma_f16_ts(t_o, t_s + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (j > 0 || k > 0) ? 1u : 0u);
-                umma_commit(&c.pv_done[e]);
+                    umma_f16_ts(t_o, t_s + (j & 1) * S::kKeys + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o,
+                                (j > 0 || k > 0) ? 1u : 0u);
+                umma_commit(&c.pv_done[j & 1]);
                 umma_commit(&c.v_empty[stage]);
+                if (more) {
+                    if (!(ok = mbar_wait(&c.pv_done[j & 1], (j >> 1) & 1, ctl, 203))) break;  // P(j) lies where S(j + 2) goes
+                    if ((more = score(j + 2))) tiles = j + 3;
+                }
             }
             if (!ok && issued) {
-                umma_commit(&c.drain[e]);
+                umma_commit(&c.drain);
                 const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain[e], 0) && global_timer_ns() - t0 < 2000000000ull) {
+                while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
                 }
             }
         }
     } else {
-        // ------------------------------------------------------------ softmax of engine e: thread = row = TMEM lane
-        const int e = warp >> 2, r = (warp & 3) * 32 + lane;
-        const int in_engine = r / p.group;
-        const int tok = e * per_engine + in_engine;
-        const bool row_live = r < per_engine * p.group && tok < tokens;
+        // ------------------------------------------------------------ softmax: thread = row = TMEM lane
+        const int r = tid;
+        const int tok = r / p.group;
+        const bool row_live = tok < tokens;
         const int pos = row_live && c.req[tok] >= 0 ? c.pos[tok] : -1;
         const int word = row_live ? tok >> 5 : 0;
         const uint32_t bit = row_live && pos >= 0 ? 1u << (tok & 31) : 0u;
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + e * S::kEngineCols + lanes, t_o = t_s + S::kOCol;
+        const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+        const uint32_t t_s0 = tmem + lanes, t_o = t_s0 + S::kOCol;
         const float scale = fmaxf(fabsf(p.scale_log2), 1.2e-38f);  // zero would turn masked logits into NaN
         const float slack = 8.0f / scale;
         float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum
@@ -458,31 +494,32 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         for (;; ++j) {
             const int stage = j % S::kStages;
             const uint32_t ph = (j / S::kStages) & 1;
-            if (!(ok = warp_wait(&c.k_full[stage], ph, ctl, 206))) break;
-            const TileInfo<DB>& info = c.info[j % (S::kStages + 1)];
-            const int n_pages = info.n_pages;
-            if (n_pages == 0) break;
+            if (!(ok = warp_wait(&c.info_full[j % S::kInfos], (j / S::kInfos) & 1, ctl, 206))) break;
+            const TileInfo<DB>& info = c.info[j % S::kInfos];
+            const int n_boxes = info.n_boxes;
+            if (n_boxes == 0) break;
+            const uint32_t t_s = t_s0 + (j & 1) * S::kKeys;
             // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees
             uint32_t full = 0, part = 0;
             int rem = 0;
             bool tail = false;
-            for (int i = 0; i < n_pages; ++i) {
-                const int seen = (info.members[i][word] & bit) ? min(max(pos + 1 - info.first[i], 0), page_size) : 0;
-                const int g0 = (i << p.page_shift) >> 4;
+            for (int i = 0; i < n_boxes; ++i) {
+                const int seen = (info.members[i][word] & bit) ? min(max(pos + 1 - info.first[i], 0), box) : 0;
+                const int g0 = (i << box_shift) >> 4;
                 full |= ((1u << (seen >> 4)) - 1) << g0;
                 if (seen & 15) {
                     part |= 1u << (g0 + (seen >> 4));
                     rem = seen & 15;
                 }
-                tail |= info.dead[i] < page_size;
+                tail |= info.dead[i] < box;
             }
             const uint32_t mine = full | part;
             const uint32_t some = __reduce_or_sync(0xFFFFFFFFu, mine), cut = __reduce_or_sync(0xFFFFFFFFu, part);
             if (tail) {  // value rows that no token of the window sees
                 if (!(ok = warp_wait(&c.v_full[stage], ph, ctl, 207))) break;
-                for (int i = 0; i < n_pages; ++i) {
-                    const int rows = page_size - info.dead[i];
-                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * page_size + info.dead[i]) * 128;
+                for (int i = 0; i < n_boxes; ++i) {
+                    const int rows = box - info.dead[i];
+                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * box + info.dead[i]) * 128;
                     for (int x = r; x < rows * 8 * DB; x += 128) {
                         const int piece = x & 7, rest = x >> 3;
                         *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
@@ -490,7 +527,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
                 fence_proxy_async_smem();
             }
-            if (!(ok = warp_wait(&c.s_full[e], j & 1, ctl, 208))) break;
+            if (!(ok = warp_wait(&c.s_full[j & 1], (j >> 1) & 1, ctl, 208))) break;
             tc_fence_after_sync();
             uint32_t s[S::kKeys / 32][32];
 #pragma unroll
@@ -501,7 +538,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 #pragma unroll
                 for (int g = 0; g < S::kKeys / 16; ++g) {
                     if (cut >> g & 1) {
-                        const int seen = part >> g & 1 ? rem : 16;
+                        const int seen = full >> g & 1 ? 16 : part >> g & 1 ? rem : 0;  // what lies past a request's end may be NaN
 #pragma unroll
                         for (int x = 0; x < 16; ++x)
                             if (x >= seen) s[g >> 1][(g & 1) * 16 + x] = 0xFF800000u;
@@ -523,6 +560,8 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 const float fix = grow ? (l > 0.0f ? exp2_fast((m - top) * scale) : 1.0f) : 1.0f;
                 if (grow) m = top;
                 if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {
+                    if (!(ok = warp_wait(&c.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, ctl, 211))) break;  // (a sum that is not zero: j > 0)
+                    tc_fence_after_sync();
                     l *= fix;
                     for (int q = 0; q < p.dim >> 4; ++q) {  // 16 columns at a time: the logits stay in registers
                         uint32_t o[16];
@@ -561,14 +600,14 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             l += lo32(sum) + hi32(sum);
             tmem_wait_st();
             tc_fence_before_sync();
-            mbar_arrive(&c.p_ready[e]);
+            mbar_arrive(&c.p_ready[j & 1]);
         }
-        if (ok && j > 0 && (ok = warp_wait(&c.pv_done[e], (j - 1) & 1, ctl, 209))) tc_fence_after_sync();
+        if (ok && j > 0 && (ok = warp_wait(&c.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, ctl, 209))) tc_fence_after_sync();
         if (ok) {
-            // through the engine's query tile, which its products have left: a warp's 32 rows go out with whole
+            // through the query tile, which the products have left: a warp's 32 rows go out with whole
             // rows side by side
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            uint8_t* stash = smem + e * S::kQBytes + (warp & 3) * (32 * DB * 128);
+            uint8_t* stash = smem + warp * (32 * DB * 128);
             bool bad = false;
             for (int q = 0; q < (p.dim + 31) / 32; ++q) {
                 uint32_t o[32];
@@ -594,16 +633,15 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             constexpr int kAtOnce = 32 / (DB * 8) > 0 ? 32 / (DB * 8) : 1;  // rows of a store
             for (int row0 = 0; row0 < 32; row0 += kAtOnce) {
                 const int row = row0 + lane / (DB * 8 < 32 ? DB * 8 : 32), piece = lane % (DB * 8 < 32 ? DB * 8 : 32);
-                const int er = (warp & 3) * 32 + row, et = er / p.group;
-                const int tk = e * per_engine + et;
-                if (et < per_engine && tk < tokens && piece < pieces) {
+                const int out_row = warp * 32 + row, tk = out_row / p.group;
+                if (tk < tokens && piece < pieces) {
                     const uint4 v = *reinterpret_cast<const uint4*>(stash + row * (DB * 128) + ((piece ^ (row & 7)) << 4));
                     *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + (w0 + tk) * p.out_stride[0] +
-                                              (static_cast<int64_t>(h) * p.group + er - et * p.group) * p.out_stride[1] + piece * 8) = v;
+                                              (static_cast<int64_t>(h) * p.group + out_row - tk * p.group) * p.out_stride[1] + piece * 8) = v;
                 }
             }
             if (row_live && p.lse)
-                p.lse[(w0 + tok) * p.group * p.n_kv_heads + static_cast<int64_t>(h) * p.group + r - in_engine * p.group] =
+                p.lse[(w0 + tok) * p.group * p.n_kv_heads + static_cast<int64_t>(h) * p.group + r - tok * p.group] =
                     l == 0.0f ? -INFINITY : (m * scale + log2f(l)) * 0.69314718055994531f;
             if (bad) c.bad = 1;
         }
@@ -613,7 +651,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     __syncthreads();
     if (warp == S::kWarps - 1) {
         tc_fence_after_sync();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, S::kCols);
     }
     if (tid == 0) *done = c.bad ? 0 : 1;
 }
