@@ -4,8 +4,11 @@
 // head; its 128 rows are (token, query head of the group), and it walks the union of the blocks that any token of the
 // window selected, each block fetched once for all rows.  A row that did not select a block sees it masked.
 //
-//   producer warp   merges the tokens' ascending lists (the smallest head of all lists is the next block, the
-//                   lanes whose list shows it are its members), looks the pages up and issues the copies
+//   before the loop all warps build the plan: a bitmap of the blocks that the window's tokens selected, its prefix
+//                   sums give every block its place, and every (token, block) sets the token's bit there.  (A
+//                   warp that merged the tokens' lists tile by tile needed 2,600 cycles for a tile and held all
+//                   the others up.)
+//   producer        one thread: keys and values of the next tiles by TMA as their stages come free
 //   MMA warp        S = Q K^T into TMEM, then O += P V with P read from TMEM
 //   softmax warps   one thread per row: S out of TMEM, running maximum and sum in registers, P back into TMEM over
 //                   S.  O is rescaled only when the maximum has grown by more than 2^8 since the reference was
@@ -18,7 +21,8 @@
 //
 // What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
 // value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
-// such a window, and one whose tokens belong to many requests, is left to the rows kernel by its flag.
+// such a window, one whose tokens belong to many requests and one whose plan is too long is left to the rows
+// kernel by its flag.
 #pragma once
 #include "kv_attend.cuh"
 
@@ -30,13 +34,12 @@ struct TileShape {
     static constexpr int kCtas = DB == 4 ? 1 : 2;       // on an SM
     static constexpr int kKeys = 64;                    // keys of a tile
     static constexpr int kStages = 2;
-    static constexpr int kInfos = kStages + 2;          // the producer gathers a tile's pages ahead of its stage
-    static constexpr int kPages = kKeys / 16;           // boxes of a tile at most
     static constexpr int kBlockBytes = kKeys * 128;     // 64 columns of all keys
     static constexpr int kPlaneBytes = DB * kBlockBytes;
     static constexpr int kStageBytes = 2 * kPlaneBytes;
     static constexpr int kQBytes = DB * 128 * 128;
-    static constexpr int kListInts = 2560;
+    static constexpr int kBoxes = 448;                  // of a plan
+    static constexpr int kMapWords = 1024;              // bitmap of 32,768 blocks at a time, in the ring before the loop
     static constexpr int kRows = 128;
     static constexpr int kWarps = 6;                    // softmax 0-3, MMA 4, producer 5
     static constexpr int kThreads = kWarps * 32;
@@ -45,19 +48,18 @@ struct TileShape {
 };
 
 template <int DB>
-struct TileInfo {  // what the producer says about a stage
-    int n_boxes;  // pages, or halves of a page of 128; 0 ends the list
-    int first[TileShape<DB>::kPages];      // position of the box's first token
-    int dead[TileShape<DB>::kPages];       // tokens from here on lie past the window's last: value rows to be zeroed
-    uint32_t members[TileShape<DB>::kPages][4];  // tokens of the window that selected it
-};
-
-template <int DB>
 struct TileControl {
-    uint64_t info_full[4], k_full[2], v_full[2], k_empty[2], v_empty[2];
-    uint64_t s_full[2], p_ready[2], pv_done[2], drain;  // by the tile's parity: a waiter may be one tile late, not two
-    TileInfo<DB> info[TileShape<DB>::kInfos];
-    int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows];
+    uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2];
+    // by the tile's parity: a waiter may be one tile late, not two
+    uint64_t s_full[2], p_ready[2], pv_done[2], drain;
+    // the plan, a box being a page or a half of a page of 128
+    uint32_t members[TileShape<DB>::kBoxes][4];  // tokens of the window that selected it
+    int first[TileShape<DB>::kBoxes];            // position of its first token
+    int page[TileShape<DB>::kBoxes];
+    uint8_t dead[TileShape<DB>::kBoxes];         // tokens from here on lie past the window's last: value rows to be zeroed
+    int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows], seg[TileShape<DB>::kRows];
+    int seg_last[TileShape<DB>::kRows];          // last position that a token of the segment sees
+    int warp_sum[TileShape<DB>::kWarps];
     uint32_t tmem;
     int abort_flag, bad;
 };
@@ -65,7 +67,7 @@ struct TileControl {
 template <int DB>
 constexpr int tile_smem() {
     using S = TileShape<DB>;
-    return 1024 + S::kQBytes + S::kStages * S::kStageBytes + S::kListInts * 4 + static_cast<int>(sizeof(TileControl<DB>));
+    return 1024 + S::kQBytes + S::kStages * S::kStageBytes + static_cast<int>(sizeof(TileControl<DB>));
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
@@ -173,8 +175,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     extern __shared__ uint8_t tile_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = smem + S::kQBytes;
-    int* s_list = reinterpret_cast<int*>(ring + S::kStages * S::kStageBytes);
-    TileControl<DB>& c = *reinterpret_cast<TileControl<DB>*>(s_list + S::kListInts);
+    TileControl<DB>& c = *reinterpret_cast<TileControl<DB>*>(ring + S::kStages * S::kStageBytes);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y;
     const int64_t w0 = static_cast<int64_t>(blockIdx.x) * p.window;
@@ -198,6 +199,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
         c.req[tid] = req;
         c.pos[tid] = pos;
+        c.seg_last[tid] = -1;
     }
     const int segments = __syncthreads_count(change) + 1;
     if (segments > 1 && segments * 8 > tokens) {
@@ -212,35 +214,20 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             mbar_init(&c.k_empty[i], 1);
             mbar_init(&c.v_empty[i], 1);
         }
-        for (int i = 0; i < S::kInfos; ++i) mbar_init(&c.info_full[i], 1);
-        mbar_init(&c.s_full[0], 1);
-        mbar_init(&c.s_full[1], 1);
-        mbar_init(&c.p_ready[0], 128);
-        mbar_init(&c.p_ready[1], 128);
-        mbar_init(&c.pv_done[0], 1);
-        mbar_init(&c.pv_done[1], 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&c.s_full[i], 1);
+            mbar_init(&c.p_ready[i], 128);
+            mbar_init(&c.pv_done[i], 1);
+        }
         mbar_init(&c.drain, 1);
         c.abort_flag = 0;
         c.bad = 0;
         fence_mbar_init();
+        tma_prefetch_desc(&map_k);
+        tma_prefetch_desc(&map_v);
     }
-    if (warp == S::kWarps - 1) {
-        if (lane == 0) {
-            tma_prefetch_desc(&map_k);
-            tma_prefetch_desc(&map_v);
-        }
-        tmem_alloc(&c.tmem, S::kCols);
-        tmem_relinquish();
-    }
-    // selections to shared memory where they fit, a warp to a token; all copies are in flight at once
-    const bool lists_here = tokens * p.n_select <= S::kListInts;
-    if (lists_here) {
-        for (int tok = warp; tok < tokens; tok += S::kWarps) {
-            const int32_t* src = p.selected + ((w0 + tok) * p.n_kv_heads + h) * p.n_select;
-            for (int i = lane; i < p.n_select; i += 32) cp_async4(smem_u32(s_list + tok * p.n_select + i), src + i);
-        }
-    }
-    // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits
+    // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits; they come while
+    // the plan is built
     {
         constexpr int kPieces = DB * 8, kStep = S::kThreads / kPieces;  // rows at a time
         const int piece = tid % kPieces;
@@ -253,8 +240,126 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
     }
     cp_async_commit();
+
+    // ---- the plan
+    const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
+    const int halves = 1 << (p.page_shift - box_shift);
+    const int per_tile = S::kKeys >> box_shift;
+    uint32_t* map = reinterpret_cast<uint32_t*>(ring);
+    int* rank = reinterpret_cast<int*>(map + S::kMapWords);  // selected blocks before a word of the map
+    for (int i = tid; i < S::kBoxes * 4; i += S::kThreads) (&c.members[0][0])[i] = 0;
+    if (segments == 1) {
+        if (tid < S::kRows) c.seg[tid] = 0;
+    } else if (tid < 32) {
+        int before = 0;
+        for (int t0 = 0; t0 < tokens; t0 += 32) {
+            const int t = t0 + lane;
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, t > 0 && t < tokens && c.req[t] != c.req[t - 1]);
+            c.seg[t] = before + __popc(m & (0xFFFFFFFFu >> (31 - lane)));
+            before += __popc(m);
+        }
+    }
+    __syncthreads();
+    if (tid < tokens && c.req[tid] >= 0) atomicMax(&c.seg_last[c.seg[tid]], c.pos[tid]);
+    __syncthreads();
+    int boxes = 0;
+    for (int s = 0; s < segments && boxes >= 0; ++s) {
+        const int last_pos = c.seg_last[s], last_block = last_pos >> p.page_shift;  // -1: nobody sees anything
+        for (int base = 0; base <= last_block; base += S::kMapWords * 32) {
+            const int words = min((last_block - base) / 32 + 1, S::kMapWords);
+            for (int i = tid; i < words; i += S::kThreads) map[i] = 0;
+            __syncthreads();
+            // entries (token, block) of this segment and range: once to fill the map, once to set the members
+            auto each = [&](auto&& f) {
+                for (int tok = warp; tok < tokens; tok += S::kWarps) {
+                    if (c.seg[tok] != s || c.req[tok] < 0) continue;
+                    const int own = c.pos[tok] >> p.page_shift;
+                    const int32_t* src = p.selected + ((w0 + tok) * p.n_kv_heads + h) * p.n_select;
+                    for (int i = lane; i < p.n_select; i += 32) {
+                        const int b = src[i];
+                        if (b >= base && b <= own && b - base < words * 32) f(tok, b - base);
+                    }
+                }
+            };
+            each([&](int, int b) { atomicOr(&map[b >> 5], 1u << (b & 31)); });
+            __syncthreads();
+            constexpr int kPer = (S::kMapWords + S::kThreads - 1) / S::kThreads;
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (tid * kPer + i < words) mine += __popc(map[tid * kPer + i]);
+            int upto = mine;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int v = __shfl_up_sync(0xFFFFFFFFu, upto, off);
+                if (lane >= off) upto += v;
+            }
+            if (lane == 31) c.warp_sum[warp] = upto;
+            __syncthreads();
+            int before = upto - mine, found = 0;
+#pragma unroll
+            for (int w = 0; w < S::kWarps; ++w) {
+                if (w < warp) before += c.warp_sum[w];
+                found += c.warp_sum[w];
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (tid * kPer + i < words) {
+                    rank[tid * kPer + i] = before;
+                    before += __popc(map[tid * kPer + i]);
+                }
+            }
+            __syncthreads();
+            if (boxes + found * halves > S::kBoxes) {
+                boxes = -1;
+                break;
+            }
+            each([&](int tok, int b) {
+                const uint32_t word = map[b >> 5];
+                const int at = boxes + (rank[b >> 5] + __popc(word & ((1u << (b & 31)) - 1))) * halves;
+                const int first = (base + b) << p.page_shift;
+                for (int half = 0; half < halves; ++half) {
+                    atomicOr(&c.members[at + half][tok >> 5], 1u << (tok & 31));
+                    c.first[at + half] = first + half * 64;
+                    c.dead[at + half] = static_cast<uint8_t>(max(0, min(box, last_pos + 1 - first - half * 64)));
+                    c.page[at + half] = c.req[tok];  // whose page: looked up below
+                }
+            });
+            boxes += found * halves;
+            if (halves == 2 && boxes > 0 && base + S::kMapWords * 32 > last_block) {
+                __syncthreads();
+                if (c.first[boxes - 1] > last_pos) --boxes;  // the last block's second half is empty
+            }
+            __syncthreads();
+        }
+    }
+    if (boxes < 0) {  // more than the plan holds: a tile would serve a few of its rows only
+        cp_async_wait<0>();
+        if (tid == 0) *done = 0;
+        return;
+    }
+    for (int b = tid; b < boxes; b += S::kThreads) {
+        const int block = c.first[b] >> p.page_shift;
+        int page = -1;
+        if (block < p.max_blocks) page = p.table[c.page[b] * p.table_stride + block];
+        if (block >= p.max_blocks || page >= p.num_pages) {
+            kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
+            page = -1;
+        }
+        if (page < 0) {
+            page = 0;  // a stand-in, all of it zeroed and unseen
+            c.dead[b] = 0;
+            for (int k = 0; k < 4; ++k) c.members[b][k] = 0;
+        }
+        c.page[b] = page;
+    }
+    const int tiles = (boxes + per_tile - 1) / per_tile;
+    if (warp == S::kWarps - 1) {
+        tmem_alloc(&c.tmem, S::kCols);
+        tmem_relinquish();
+    }
     cp_async_wait<0>();
-    fence_proxy_async_smem();
+    fence_proxy_async_smem();  // the queries; and the map's words, before copies land on them
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -263,159 +368,63 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     ctl.abort_flag = &c.abort_flag;
     ctl.status = p.status;
     ctl.limit_ns = p.limit_ns;
-    // a page of 128 tokens is fetched as two boxes of 64
-    const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;
-    const int per_tile = S::kKeys >> box_shift;
-
     if (warp == S::kWarps - 1) {
-        // ------------------------------------------------------------ producer
-        const int slots = (tokens + 31) >> 5;
-        uint32_t cur[4];
-        int at[4] = {}, seg[4] = {};
-        auto entry = [&](int k) -> uint32_t {
-            const int tok = k * 32 + lane;
-            if (tok >= tokens || c.req[tok] < 0 || at[k] >= p.n_select) return kNoKey;
-            const int b = lists_here ? s_list[tok * p.n_select + at[k]] : p.selected[((w0 + tok) * p.n_kv_heads + h) * p.n_select + at[k]];
-            if (b < 0 || b > (c.pos[tok] >> p.page_shift)) return kNoKey;
-            return (static_cast<uint32_t>(seg[k]) << 24) | static_cast<uint32_t>(b);
-        };
-        int n_seg = 0;
+        // ------------------------------------------------------------ producer: keys and values in whatever order stages come free
+        if (lane == 0) {
+            const uint32_t ring0 = smem_u32(ring);
+            auto copy = [&](int j, const CUtensorMap* from, uint64_t* full, uint32_t to) {
+                const int b0 = j * per_tile, n = min(per_tile, boxes - b0);
+                mbar_arrive_expect_tx(full, n * DB * box * 128);
+                for (int i = 0; i < n; ++i) {
+                    const int row = halves == 2 ? c.first[b0 + i] & 64 : 0, page = c.page[b0 + i];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            cur[k] = kNoKey;
-            seg[k] = -1;
-            if (k < slots) {
-                const int tok = k * 32 + lane;
-                const bool step = tok > 0 && tok < tokens && c.req[tok] != c.req[tok - 1];
-                const unsigned m = __ballot_sync(0xFFFFFFFFu, step);
-                seg[k] = n_seg + __popc(m & (0xFFFFFFFFu >> (31 - lane)));
-                n_seg += __popc(m);
-                cur[k] = entry(k);
-            }
-        }
-        int last_seg = -1, last_pos = -1, k_issued = 0, v_issued = 0;
-        int half_block = -1, half_owner = 0;  // a page of 128 whose second box is due
-        uint32_t half_mine = 0;
-        int page = -1, row = 0;  // of this lane's box
-        // the pages of tile j: their members into the info ring, the number of boxes back
-        auto gather = [&](int j) -> int {
-            TileInfo<DB>& info = c.info[j % S::kInfos];
-            int n = 0, my_block = 0, my_owner = 0;
-            while (n < per_tile) {
-                int block, owner = -1, sub = 0;
-                uint32_t mine = 0;  // lane k keeps word k of the members
-                if (half_block >= 0) {
-                    block = half_block;
-                    owner = half_owner;
-                    mine = half_mine;
-                    sub = 64;
-                    half_block = -1;
+                    for (int d = 0; d < DB; ++d) tma_load_4d(to + i * box * 128 + d * S::kBlockBytes, from, full, d * 64, row, h, page);
+                }
+            };
+            auto is_free = [&](uint64_t* empty, int j) {
+                return j < S::kStages || mbar_test_wait(&empty[j % S::kStages], (j / S::kStages - 1) & 1);
+            };
+            int k = 0, v = 0;
+            uint64_t since = 0;
+            uint32_t idle = 0;
+            bool ok = true;
+            while (v < tiles) {
+                bool moved = false;
+                if (k < tiles && is_free(c.k_empty, k)) {
+                    copy(k, &map_k, &c.k_full[k % S::kStages], ring0 + (k % S::kStages) * S::kStageBytes);
+                    ++k;
+                    moved = true;
+                }
+                if (v < k && is_free(c.v_empty, v)) {
+                    copy(v, &map_v, &c.v_full[v % S::kStages], ring0 + (v % S::kStages) * S::kStageBytes + S::kPlaneBytes);
+                    ++v;
+                    moved = true;
+                }
+                if (moved) {
+                    idle = 0;
                 } else {
-                    uint32_t least = kNoKey;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < slots) least = min(least, cur[k]);
-                    const uint32_t key = __reduce_min_sync(0xFFFFFFFFu, least);
-                    if (key == kNoKey) break;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (k < slots) {
-                            const bool member = cur[k] == key;
-                            const unsigned m = __ballot_sync(0xFFFFFFFFu, member);
-                            if (m && owner < 0) owner = k * 32 + __ffs(m) - 1;
-                            if (lane == k) mine = m;
-                            if (member) {
-                                ++at[k];
-                                cur[k] = entry(k);
-                            }
+                    __nanosleep(40);
+                    if ((++idle & 63u) == 0u) {
+                        const uint64_t t = global_timer_ns();
+                        if (idle == 64u) since = t;
+                        if (t - since > ctl.limit_ns) report_timeout(ctl, 201);
+                        if (*ctl.abort_flag) {
+                            ok = false;
+                            break;
                         }
                     }
-                    block = static_cast<int>(key & 0xFFFFFFu);
-                    const int s = static_cast<int>(key >> 24);
-                    if (s != last_seg) {  // the last position that any token of the segment sees
-                        int far = -1;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k < slots && seg[k] == s && k * 32 + lane < tokens) far = max(far, c.pos[k * 32 + lane]);
-                        last_pos = __reduce_max_sync(0xFFFFFFFFu, far);
-                        last_seg = s;
+                }
+            }
+            if (!ok) {
+                // gave up: let the copies already issued land before the CTA goes away (bounded)
+                const uint64_t t0 = global_timer_ns();
+                for (int i = max(0, k - S::kStages); i < k; ++i)
+                    while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                     }
-                    if (p.page_shift == 7 && (block << 7) + 64 <= last_pos) {
-                        half_block = block;
-                        half_owner = owner;
-                        half_mine = mine;
+                for (int i = max(0, v - S::kStages); i < v; ++i)
+                    while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                     }
-                }
-                const int first = (block << p.page_shift) + sub;
-                if (lane == n) {
-                    my_block = block;
-                    my_owner = owner;
-                    row = sub;
-                }
-                if (lane < 4) info.members[n][lane] = mine;
-                if (lane == 0) {
-                    info.first[n] = first;
-                    info.dead[n] = min(box, last_pos + 1 - first);
-                }
-                ++n;
             }
-            // all pages of the tile are looked up at once; a page that is not there sees no members
-            page = -1;
-            __syncwarp();
-            if (lane < n) {
-                if (my_block < p.max_blocks) page = p.table[c.req[my_owner] * p.table_stride + my_block];
-                if (my_block >= p.max_blocks || page >= p.num_pages) {
-                    kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
-                    page = -1;
-                }
-                if (page < 0) {
-                    page = 0;  // a stand-in, all of it zeroed and unseen
-                    info.dead[lane] = 0;
-                    for (int k = 0; k < 4; ++k) info.members[lane][k] = 0;
-                }
-            }
-            if (lane == 0) info.n_boxes = n;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.info_full[j % S::kInfos]);
-            return n;
-        };
-        bool ok = true;
-        int n = gather(0);
-        for (int j = 0;; ++j) {
-            const int stage = j % S::kStages;
-            const uint32_t used = (j / S::kStages - 1) & 1;
-            const uint32_t kb = smem_u32(ring) + stage * S::kStageBytes + lane * box * 128;
-            const int bytes = n * DB * box * 128;
-            if (n == 0) break;
-            if (j >= S::kStages && !(ok = warp_wait(&c.k_empty[stage], used, ctl, 201))) break;
-            if (lane == 0) mbar_arrive_expect_tx(&c.k_full[stage], bytes);
-            __syncwarp();
-            if (lane < n) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d) tma_load_4d(kb + d * S::kBlockBytes, &map_k, &c.k_full[stage], d * 64, row, h, page);
-            }
-            k_issued = j + 1;
-            const int v_page = page, v_row = row, v_n = n;
-            n = gather(j + 1);  // while the values' stage is still in use
-            if (j >= S::kStages && !(ok = warp_wait(&c.v_empty[stage], used, ctl, 210))) break;
-            if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], bytes);
-            __syncwarp();
-            if (lane < v_n) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    tma_load_4d(kb + S::kPlaneBytes + d * S::kBlockBytes, &map_v, &c.v_full[stage], d * 64, v_row, h, v_page);
-            }
-            v_issued = j + 1;
-        }
-        if (!ok && lane == 0) {
-            // gave up: let the copies already issued land before the CTA goes away (bounded)
-            const uint64_t t0 = global_timer_ns();
-            for (int i = max(0, k_issued - S::kStages); i < k_issued; ++i)
-                while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
-                }
-            for (int i = max(0, v_issued - S::kStages); i < v_issued; ++i)
-                while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
-                }
         }
     } else if (warp == 4) {
         // ------------------------------------------------------------ MMA
@@ -427,16 +436,14 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const int ksteps = p.dim >> 4;
             bool ok = true, issued = false;
-            // S of tile j into its buffer; false when the tiles are over or a wait gave up
-            auto score = [&](int j) -> bool {
+            auto keys_of = [&](int j) { return min(per_tile, boxes - j * per_tile) << box_shift; };
+            // S of tile j into its buffer
+            auto score = [&](int j) {
                 const int stage = j % S::kStages;
-                if (!(ok = mbar_wait(&c.info_full[j % S::kInfos], (j / S::kInfos) & 1, ctl, 212))) return false;
-                const int keys = c.info[j % S::kInfos].n_boxes << box_shift;
-                if (keys == 0) return false;
-                if (!(ok = mbar_wait(&c.k_full[stage], (j / S::kStages) & 1, ctl, 202))) return false;
+                if (!(ok = mbar_wait(&c.k_full[stage], (j / S::kStages) & 1, ctl, 202))) return;
                 tc_fence_after_sync();
                 const uint32_t k_lo = umma_desc_lo(ring0 + stage * S::kStageBytes);
-                const uint32_t idesc_s = tile_idesc<T>(keys, false) | negate;
+                const uint32_t idesc_s = tile_idesc<T>(keys_of(j), false) | negate;
                 for (int k = 0; k < ksteps; ++k) {
                     const uint32_t in = (k & 3) * 2, blk = k >> 2;
                     umma_f16(t_s + (j & 1) * S::kKeys, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
@@ -445,28 +452,25 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 umma_commit(&c.s_full[j & 1]);
                 umma_commit(&c.k_empty[stage]);
                 issued = true;
-                return true;
             };
-            bool more = score(0);
-            int tiles = more ? 1 : 0;
-            if (more && (more = score(1))) tiles = 2;
+            if (tiles > 0) score(0);
+            if (ok && tiles > 1) score(1);
             for (int j = 0; ok && j < tiles; ++j) {
                 const int stage = j % S::kStages;
-                const int keys = c.info[j % S::kInfos].n_boxes << box_shift;
                 if (!(ok = mbar_wait(&c.v_full[stage], (j / S::kStages) & 1, ctl, 204))) break;
                 if (!(ok = mbar_wait(&c.p_ready[j & 1], (j >> 1) & 1, ctl, 205))) break;
                 tc_fence_after_sync();
                 // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
                 const uint32_t v_addr = ring0 + stage * S::kStageBytes + S::kPlaneBytes;
                 const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-                for (int k = 0; k < keys >> 4; ++k)
+                for (int k = 0; k < keys_of(j) >> 4; ++k)
                     umma_f16_ts(t_o, t_s + (j & 1) * S::kKeys + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o,
                                 (j > 0 || k > 0) ? 1u : 0u);
                 umma_commit(&c.pv_done[j & 1]);
                 umma_commit(&c.v_empty[stage]);
-                if (more) {
+                if (j + 2 < tiles) {
                     if (!(ok = mbar_wait(&c.pv_done[j & 1], (j >> 1) & 1, ctl, 203))) break;  // P(j) lies where S(j + 2) goes
-                    if ((more = score(j + 2))) tiles = j + 3;
+                    score(j + 2);
                 }
             }
             if (!ok && issued) {
@@ -490,36 +494,33 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         const float slack = 8.0f / scale;
         float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum
         bool ok = true;
-        int j = 0;
-        for (;; ++j) {
+        for (int j = 0; j < tiles; ++j) {
             const int stage = j % S::kStages;
-            const uint32_t ph = (j / S::kStages) & 1;
-            if (!(ok = warp_wait(&c.info_full[j % S::kInfos], (j / S::kInfos) & 1, ctl, 206))) break;
-            const TileInfo<DB>& info = c.info[j % S::kInfos];
-            const int n_boxes = info.n_boxes;
-            if (n_boxes == 0) break;
+            const int b0 = j * per_tile, n_boxes = min(per_tile, boxes - b0);
             const uint32_t t_s = t_s0 + (j & 1) * S::kKeys;
             // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees
             uint32_t full = 0, part = 0;
             int rem = 0;
             bool tail = false;
             for (int i = 0; i < n_boxes; ++i) {
-                const int seen = (info.members[i][word] & bit) ? min(max(pos + 1 - info.first[i], 0), box) : 0;
+                const int seen = (c.members[b0 + i][word] & bit) ? min(max(pos + 1 - c.first[b0 + i], 0), box) : 0;
                 const int g0 = (i << box_shift) >> 4;
                 full |= ((1u << (seen >> 4)) - 1) << g0;
                 if (seen & 15) {
                     part |= 1u << (g0 + (seen >> 4));
                     rem = seen & 15;
                 }
-                tail |= info.dead[i] < box;
+                tail |= c.dead[b0 + i] < box;
             }
             const uint32_t mine = full | part;
-            const uint32_t some = __reduce_or_sync(0xFFFFFFFFu, mine), cut = __reduce_or_sync(0xFFFFFFFFu, part);
+            const bool some = __any_sync(0xFFFFFFFFu, mine != 0);
+            // keys that only part of a group's rows see, and columns that hold no key of the request
+            const bool cut = __any_sync(0xFFFFFFFFu, part != 0) || tail || n_boxes < per_tile;
             if (tail) {  // value rows that no token of the window sees
-                if (!(ok = warp_wait(&c.v_full[stage], ph, ctl, 207))) break;
+                if (!(ok = warp_wait(&c.v_full[stage], (j / S::kStages) & 1, ctl, 207))) break;
                 for (int i = 0; i < n_boxes; ++i) {
-                    const int rows = box - info.dead[i];
-                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * box + info.dead[i]) * 128;
+                    const int rows = box - c.dead[b0 + i];
+                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * box + c.dead[b0 + i]) * 128;
                     for (int x = r; x < rows * 8 * DB; x += 128) {
                         const int piece = x & 7, rest = x >> 3;
                         *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
@@ -529,31 +530,35 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             }
             if (!(ok = warp_wait(&c.s_full[j & 1], (j >> 1) & 1, ctl, 208))) break;
             tc_fence_after_sync();
-            uint32_t s[S::kKeys / 32][32];
+            constexpr int kGroups = S::kKeys / 16;
+            if (!some) {  // no row of the warp selected any of it
+                const uint32_t none[16] = {};
 #pragma unroll
-            for (int q = 0; q < S::kKeys / 32; ++q) tmem_ld_32x32b_x32(t_s + q * 32, s[q]);
-#pragma unroll
-            for (int q = 0; q < S::kKeys / 32; ++q) tmem_wait_ld_regs(s[q]);
+                for (int q = 0; q < S::kKeys / 32; ++q) tmem_st_32x32b_x16(t_s + q * 16, none);
+                tmem_wait_st();
+                tc_fence_before_sync();
+                mbar_arrive(&c.p_ready[j & 1]);
+                continue;
+            }
+            uint32_t s[S::kKeys];
+            tmem_ld_32x32b_x64(t_s, s);
+            tmem_wait_ld_regs(s);
             if (cut) {
 #pragma unroll
-                for (int g = 0; g < S::kKeys / 16; ++g) {
-                    if (cut >> g & 1) {
-                        const int seen = full >> g & 1 ? 16 : part >> g & 1 ? rem : 0;  // what lies past a request's end may be NaN
+                for (int g = 0; g < kGroups; ++g) {
+                    const int seen = full >> g & 1 ? 16 : part >> g & 1 ? rem : 0;
 #pragma unroll
-                        for (int x = 0; x < 16; ++x)
-                            if (x >= seen) s[g >> 1][(g & 1) * 16 + x] = 0xFF800000u;
-                    }
+                    for (int x = 0; x < 16; ++x)
+                        if (x >= seen) s[g * 16 + x] = 0xFF800000u;
                 }
             }
             float top = -INFINITY;
 #pragma unroll
-            for (int g = 0; g < S::kKeys / 16; ++g) {
-                if (some >> g & 1) {
-                    const uint32_t* v = &s[g >> 1][(g & 1) * 16];
-                    const float a = max3f(v[0], v[1], v[2]), b = max3f(v[3], v[4], v[5]), d = max3f(v[6], v[7], v[8]), f = max3f(v[9], v[10], v[11]);
-                    const float t = fmaxf(max3f(max3f(a, b, d), f, max3f(v[12], v[13], v[14])), __uint_as_float(v[15]));
-                    if (mine >> g & 1) top = fmaxf(top, t);
-                }
+            for (int g = 0; g < kGroups; ++g) {
+                const uint32_t* v = &s[g * 16];
+                const float a = max3f(v[0], v[1], v[2]), b = max3f(v[3], v[4], v[5]), d = max3f(v[6], v[7], v[8]), f = max3f(v[9], v[10], v[11]);
+                const float t = fmaxf(max3f(max3f(a, b, d), f, max3f(v[12], v[13], v[14])), __uint_as_float(v[15]));
+                top = fmaxf(top, mine >> g & 1 ? t : -INFINITY);
             }
             const bool grow = top > m + slack || (m == -INFINITY && top > m);
             if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -573,36 +578,29 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
             }
             const float base = m == -INFINITY ? 0.0f : m * scale;
-            uint64_t sum = 0;  // two 32-bit sums side by side
+            uint64_t sum[2] = {0, 0};  // of two 32-bit sums each
             const uint64_t scale2 = pair32(scale, scale);
 #pragma unroll
-            for (int g2 = 0; g2 < S::kKeys / 32; ++g2) {
+            for (int q = 0; q < S::kKeys / 32; ++q) {
                 uint32_t out[16];
 #pragma unroll
-                for (int g = 2 * g2; g < 2 * g2 + 2; ++g) {
-                    if (some >> g & 1) {
-                        const float off = mine >> g & 1 ? -base : -INFINITY;  // a group that the row does not see: all weights 0
-                        const uint64_t off2 = pair32(off, off);
-#pragma unroll
-                        for (int x = 0; x < 16; x += 2) {
-                            const uint64_t z = fma2(pair32(__uint_as_float(s[g2][(g & 1) * 16 + x]), __uint_as_float(s[g2][(g & 1) * 16 + x + 1])), scale2, off2);
-                            const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
-                            sum = add2(sum, pair32(a, b));
-                            out[(g & 1) * 8 + x / 2] = Pair16<T>::pack(a, b);
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) out[(g & 1) * 8 + x] = 0u;
-                    }
+                for (int x = 0; x < 32; x += 2) {
+                    const int i = q * 32 + x;
+                    const float off = mine >> (i / 16) & 1 ? -base : -INFINITY;  // a group that the row does not see: all weights 0
+                    const uint64_t z = fma2(pair32(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, pair32(off, off));
+                    const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
+                    sum[x / 2 & 1] = add2(sum[x / 2 & 1], pair32(a, b));
+                    out[x / 2] = Pair16<T>::pack(a, b);
                 }
-                tmem_st_32x32b_x16(t_s + g2 * 16, out);
+                tmem_st_32x32b_x16(t_s + q * 16, out);
             }
-            l += lo32(sum) + hi32(sum);
+            const uint64_t both = add2(sum[0], sum[1]);
+            l += lo32(both) + hi32(both);
             tmem_wait_st();
             tc_fence_before_sync();
             mbar_arrive(&c.p_ready[j & 1]);
         }
-        if (ok && j > 0 && (ok = warp_wait(&c.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, ctl, 209))) tc_fence_after_sync();
+        if (ok && tiles > 0 && (ok = warp_wait(&c.pv_done[(tiles - 1) & 1], ((tiles - 1) >> 1) & 1, ctl, 209))) tc_fence_after_sync();
         if (ok) {
             // through the query tile, which the products have left: a warp's 32 rows go out with whole
             // rows side by side
@@ -611,7 +609,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             bool bad = false;
             for (int q = 0; q < (p.dim + 31) / 32; ++q) {
                 uint32_t o[32];
-                if (j > 0) {
+                if (tiles > 0) {
                     tmem_ld_32x32b_x32(t_o + q * 32, o);
                     tmem_wait_ld_regs(o);
                 }
