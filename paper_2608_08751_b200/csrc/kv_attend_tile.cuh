@@ -8,16 +8,16 @@
 //                   sums give every block its place, and every (token, block) sets the token's bit there.  (A
 //                   warp that merged the tokens' lists tile by tile needed 2,600 cycles for a tile and held all
 //                   the others up.)
-//   producer        one thread: keys and values of the next tiles by TMA as their stages come free
-//   MMA warp        S = Q K^T into TMEM, then O += P V with P read from TMEM
-//   softmax warps   one thread per row: S out of TMEM, running maximum and sum in registers, P back into TMEM over
-//                   S.  O is rescaled only when the maximum has grown by more than 2^8 since the reference was
-//                   set; the reference cancels in the final division.
+//   three threads   of a warp each issue the copies (TMA), S = Q K^T into TMEM, and O += P V with P read from TMEM.
+//                   One thread for both products spent 2,300 cycles of issue and waits on a tile, and everybody
+//                   else's time with it.
+//   softmax warps   one thread per row: S out of TMEM, maximum and sum in registers, P into TMEM.  O is rescaled
+//                   only when the maximum has grown by more than 2^8 past the reference of the exponentials; the
+//                   reference cancels in the final division.
 //
-// A tile is 64 keys.  S and P of a tile share 64 TMEM columns and there are two such buffers: S(j + 2) is issued when
-// P(j) V has retired, while the softmax warps are at work on tile j + 1, so they never wait for a product.  With one
-// buffer of 128 keys the products and the softmax of a CTA took turns: 5,600 cycles for 128 keys against the
-// figures below.  Two CTAs live on an SM (one for heads wider than 128) and fill each other's waits.
+// A tile is 64 keys.  There is one S and there are two P: S(j + 1) is computed as soon as the rows of S(j) are in
+// registers, so the softmax warps never wait for a product.  (With P over S, S(j + 2) had to wait for P(j) V.)  Two
+// CTAs live on an SM (one for heads wider than 128).
 //
 // What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
 // value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
@@ -41,9 +41,9 @@ struct TileShape {
     static constexpr int kBoxes = 448;                  // of a plan
     static constexpr int kMapWords = 1024;              // bitmap of 32,768 blocks at a time, in the ring before the loop
     static constexpr int kRows = 128;
-    static constexpr int kWarps = 6;                    // softmax 0-3, MMA 4, producer 5
+    static constexpr int kWarps = 7;                    // softmax 0-3, S 4, P V 5, copies 6
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kOCol = 2 * kKeys;             // TMEM columns: S (and P) twice, then O
+    static constexpr int kPCol = kKeys, kOCol = 2 * kKeys;  // TMEM columns: S, P twice (16-bit: half as wide), O
     static constexpr int kCols = DB == 4 ? 512 : 256;
 };
 
@@ -51,12 +51,15 @@ template <int DB>
 struct TileControl {
     uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2];
     // by the tile's parity: a waiter may be one tile late, not two
-    uint64_t s_full[2], p_ready[2], pv_done[2], drain;
+    uint64_t s_free, s_full[2], p_ready[2], pv_done[2], drain[2];
     // the plan, a box being a page or a half of a page of 128
-    uint32_t members[TileShape<DB>::kBoxes][4];  // tokens of the window that selected it
-    int first[TileShape<DB>::kBoxes];            // position of its first token
-    int page[TileShape<DB>::kBoxes];
-    uint8_t dead[TileShape<DB>::kBoxes];         // tokens from here on lie past the window's last: value rows to be zeroed
+    struct alignas(16) Box {
+        int first;         // position of its first token
+        int dead;          // tokens from here on lie past the window's last: value rows to be zeroed
+        int page;
+        uint32_t members;  // tokens 0-31 of the window that selected it
+    } box[TileShape<DB>::kBoxes];
+    uint32_t more[TileShape<DB>::kBoxes][3];  // tokens 32-127
     int req[TileShape<DB>::kRows], pos[TileShape<DB>::kRows], seg[TileShape<DB>::kRows];
     int seg_last[TileShape<DB>::kRows];          // last position that a token of the segment sees
     int warp_sum[TileShape<DB>::kWarps];
@@ -146,6 +149,9 @@ __device__ __forceinline__ float max3f(uint32_t a, uint32_t b, uint32_t c) {
     return max3f(__uint_as_float(a), __uint_as_float(b), __uint_as_float(c));
 }
 
+// row / group for row < 128: `inv` = 65536 / group + 1
+__device__ __forceinline__ int token_of(int row, uint32_t inv) { return static_cast<int>((static_cast<uint32_t>(row) * inv) >> 16); }
+
 // A wait of a whole warp: its lanes give up together, since they meet in warp-wide instructions later.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl, int where) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, ctl, where));
@@ -182,6 +188,25 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     const int tokens = static_cast<int>(min(static_cast<int64_t>(p.window), p.n_tokens - w0));
     uint8_t* done = p.done + static_cast<int64_t>(blockIdx.x) * p.n_kv_heads + h;
 
+    // ---- queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits; they come
+    // while the plan is built
+    const uint32_t inv_group = 65536u / p.group + 1;
+    {
+        constexpr int kPieces = DB * 8, kStep = S::kThreads / kPieces;  // rows at a time
+        const int piece = tid % kPieces, row0 = tid / kPieces;
+        const bool in = tid < kStep * kPieces && piece * 8 < p.dim;
+        const T* q0 = static_cast<const T*>(p.q) + w0 * p.q_stride[0] + static_cast<int64_t>(h) * p.group * p.q_stride[1] + piece * 8;
+        const uint32_t to = smem_u32(smem) + (piece >> 3) * (128 * 128);
+#pragma unroll
+        for (int row = row0; row < S::kRows; row += kStep) {
+            const int tok = token_of(row, inv_group);
+            const bool ok = in && tok < tokens;
+            const T* src = ok ? q0 + tok * p.q_stride[0] + (row - tok * p.group) * p.q_stride[1] : static_cast<const T*>(p.q);
+            if (tid < kStep * kPieces) cp_async16(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4), src, ok);
+        }
+    }
+    cp_async_commit();
+
     // ---- the window's tokens; one of many requests is left to the rows kernel: below 8 tokens to a request the
     // union is hardly shared
     int change = 0;
@@ -203,6 +228,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     }
     const int segments = __syncthreads_count(change) + 1;
     if (segments > 1 && segments * 8 > tokens) {
+        cp_async_wait<0>();
         if (tid == 0) *done = 0;
         return;
     }
@@ -219,35 +245,25 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             mbar_init(&c.p_ready[i], 128);
             mbar_init(&c.pv_done[i], 1);
         }
-        mbar_init(&c.drain, 1);
+        mbar_init(&c.s_free, 128);
+        mbar_init(&c.drain[0], 1);
+        mbar_init(&c.drain[1], 1);
         c.abort_flag = 0;
         c.bad = 0;
         fence_mbar_init();
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
     }
-    // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits; they come while
-    // the plan is built
-    {
-        constexpr int kPieces = DB * 8, kStep = S::kThreads / kPieces;  // rows at a time
-        const int piece = tid % kPieces;
-        for (int row = tid / kPieces; row < S::kRows && tid < kStep * kPieces; row += kStep) {
-            const int tok = row / p.group;
-            const bool ok = tok < tokens && piece * 8 < p.dim;
-            const T* src = static_cast<const T*>(p.q);
-            if (ok) src += (w0 + tok) * p.q_stride[0] + (static_cast<int64_t>(h) * p.group + row - tok * p.group) * p.q_stride[1] + piece * 8;
-            cp_async16(smem_u32(smem + (piece >> 3) * (128 * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4)), src, ok);
-        }
-    }
-    cp_async_commit();
-
     // ---- the plan
     const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
     const int halves = 1 << (p.page_shift - box_shift);
     const int per_tile = S::kKeys >> box_shift;
     uint32_t* map = reinterpret_cast<uint32_t*>(ring);
     int* rank = reinterpret_cast<int*>(map + S::kMapWords);  // selected blocks before a word of the map
-    for (int i = tid; i < S::kBoxes * 4; i += S::kThreads) (&c.members[0][0])[i] = 0;
+    for (int i = tid; i < S::kBoxes; i += S::kThreads) {
+        c.box[i].members = 0;
+        if (tokens > 32) c.more[i][0] = c.more[i][1] = c.more[i][2] = 0;
+    }
     if (segments == 1) {
         if (tid < S::kRows) c.seg[tid] = 0;
     } else if (tid < 32) {
@@ -260,7 +276,16 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
     }
     __syncthreads();
-    if (tid < tokens && c.req[tid] >= 0) atomicMax(&c.seg_last[c.seg[tid]], c.pos[tid]);
+    if (segments == 1) {
+        if (tid < 32) {  // one request: its token of the largest position
+            int far = -1;
+            for (int t = lane; t < tokens; t += 32) far = max(far, c.req[t] >= 0 ? c.pos[t] : -1);
+            far = __reduce_max_sync(0xFFFFFFFFu, far);
+            if (lane == 0) c.seg_last[0] = far;
+        }
+    } else if (tid < tokens && c.req[tid] >= 0) {
+        atomicMax(&c.seg_last[c.seg[tid]], c.pos[tid]);
+    }
     __syncthreads();
     int boxes = 0;
     for (int s = 0; s < segments && boxes >= 0; ++s) {
@@ -271,14 +296,20 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             __syncthreads();
             // entries (token, block) of this segment and range: once to fill the map, once to set the members
             auto each = [&](auto&& f) {
-                for (int tok = warp; tok < tokens; tok += S::kWarps) {
-                    if (c.seg[tok] != s || c.req[tok] < 0) continue;
-                    const int own = c.pos[tok] >> p.page_shift;
-                    const int32_t* src = p.selected + ((w0 + tok) * p.n_kv_heads + h) * p.n_select;
-                    for (int i = lane; i < p.n_select; i += 32) {
-                        const int b = src[i];
-                        if (b >= base && b <= own && b - base < words * 32) f(tok, b - base);
+                constexpr int kAtOnce = 4;
+                for (int e0 = tid; e0 < tokens * p.n_select; e0 += S::kThreads * kAtOnce) {
+                    int tok[kAtOnce], b[kAtOnce];
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) {
+                        const int e = e0 + k * S::kThreads;
+                        tok[k] = e / p.n_select;
+                        b[k] = tok[k] < tokens ? p.selected[((w0 + tok[k]) * p.n_kv_heads + h) * p.n_select + e - tok[k] * p.n_select] : -1;
                     }
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k)
+                        if (tok[k] < tokens && c.seg[tok[k]] == s && c.req[tok[k]] >= 0 && b[k] >= base && b[k] <= (c.pos[tok[k]] >> p.page_shift) &&
+                            b[k] - base < words * 32)
+                            f(tok[k], b[k] - base);
                 }
             };
             each([&](int, int b) { atomicOr(&map[b >> 5], 1u << (b & 31)); });
@@ -319,16 +350,16 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 const int at = boxes + (rank[b >> 5] + __popc(word & ((1u << (b & 31)) - 1))) * halves;
                 const int first = (base + b) << p.page_shift;
                 for (int half = 0; half < halves; ++half) {
-                    atomicOr(&c.members[at + half][tok >> 5], 1u << (tok & 31));
-                    c.first[at + half] = first + half * 64;
-                    c.dead[at + half] = static_cast<uint8_t>(max(0, min(box, last_pos + 1 - first - half * 64)));
-                    c.page[at + half] = c.req[tok];  // whose page: looked up below
+                    atomicOr(tok < 32 ? &c.box[at + half].members : &c.more[at + half][(tok >> 5) - 1], 1u << (tok & 31));
+                    c.box[at + half].first = first + half * 64;
+                    c.box[at + half].dead = max(0, min(box, last_pos + 1 - first - half * 64));
+                    c.box[at + half].page = c.req[tok];  // whose page: looked up below
                 }
             });
             boxes += found * halves;
             if (halves == 2 && boxes > 0 && base + S::kMapWords * 32 > last_block) {
                 __syncthreads();
-                if (c.first[boxes - 1] > last_pos) --boxes;  // the last block's second half is empty
+                if (c.box[boxes - 1].first > last_pos) --boxes;  // the last block's second half is empty
             }
             __syncthreads();
         }
@@ -339,19 +370,19 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         return;
     }
     for (int b = tid; b < boxes; b += S::kThreads) {
-        const int block = c.first[b] >> p.page_shift;
+        const int block = c.box[b].first >> p.page_shift;
         int page = -1;
-        if (block < p.max_blocks) page = p.table[c.page[b] * p.table_stride + block];
+        if (block < p.max_blocks) page = p.table[c.box[b].page * p.table_stride + block];
         if (block >= p.max_blocks || page >= p.num_pages) {
             kv_report(p.status, kKvStatusBadId, KV_SITE_ATTEND);
             page = -1;
         }
         if (page < 0) {
             page = 0;  // a stand-in, all of it zeroed and unseen
-            c.dead[b] = 0;
-            for (int k = 0; k < 4; ++k) c.members[b][k] = 0;
+            c.box[b].dead = 0;
+            c.box[b].members = c.more[b][0] = c.more[b][1] = c.more[b][2] = 0;
         }
-        c.page[b] = page;
+        c.box[b].page = page;
     }
     const int tiles = (boxes + per_tile - 1) / per_tile;
     if (warp == S::kWarps - 1) {
@@ -368,15 +399,16 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     ctl.abort_flag = &c.abort_flag;
     ctl.status = p.status;
     ctl.limit_ns = p.limit_ns;
-    if (warp == S::kWarps - 1) {
-        // ------------------------------------------------------------ producer: keys and values in whatever order stages come free
+    const uint32_t ring0 = smem_u32(ring);
+    auto keys_of = [&](int j) { return min(per_tile, boxes - j * per_tile) << box_shift; };
+    if (warp == 6) {
+        // ------------------------------------------------------------ copies: keys and values in whatever order stages come free
         if (lane == 0) {
-            const uint32_t ring0 = smem_u32(ring);
             auto copy = [&](int j, const CUtensorMap* from, uint64_t* full, uint32_t to) {
                 const int b0 = j * per_tile, n = min(per_tile, boxes - b0);
                 mbar_arrive_expect_tx(full, n * DB * box * 128);
                 for (int i = 0; i < n; ++i) {
-                    const int row = halves == 2 ? c.first[b0 + i] & 64 : 0, page = c.page[b0 + i];
+                    const int row = halves == 2 ? c.box[b0 + i].first & 64 : 0, page = c.box[b0 + i].page;
 #pragma unroll
                     for (int d = 0; d < DB; ++d) tma_load_4d(to + i * box * 128 + d * S::kBlockBytes, from, full, d * 64, row, h, page);
                 }
@@ -427,101 +459,109 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             }
         }
     } else if (warp == 4) {
-        // ------------------------------------------------------------ MMA
+        // ------------------------------------------------------------ S = Q K^T
         if (lane == 0) {
-            const uint32_t t_s = tmem, t_o = t_s + S::kOCol;
             const uint32_t q_lo = umma_desc_lo(smem_u32(smem));
-            const uint32_t ring0 = smem_u32(ring);
-            const uint32_t idesc_o = tile_idesc<T>(p.dim, true);
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const int ksteps = p.dim >> 4;
-            bool ok = true, issued = false;
-            auto keys_of = [&](int j) { return min(per_tile, boxes - j * per_tile) << box_shift; };
-            // S of tile j into its buffer
-            auto score = [&](int j) {
-                const int stage = j % S::kStages;
-                if (!(ok = mbar_wait(&c.k_full[stage], (j / S::kStages) & 1, ctl, 202))) return;
+            bool ok = true;
+            int j = 0;
+            for (; j < tiles; ++j) {
+                if (!(ok = mbar_wait(&c.k_full[j % S::kStages], (j / S::kStages) & 1, ctl, 202))) break;
+                if (j > 0 && !(ok = mbar_wait(&c.s_free, (j - 1) & 1, ctl, 203))) break;
                 tc_fence_after_sync();
-                const uint32_t k_lo = umma_desc_lo(ring0 + stage * S::kStageBytes);
-                const uint32_t idesc_s = tile_idesc<T>(keys_of(j), false) | negate;
-                for (int k = 0; k < ksteps; ++k) {
-                    const uint32_t in = (k & 3) * 2, blk = k >> 2;
-                    umma_f16(t_s + (j & 1) * S::kKeys, umma_desc_join(q_lo + blk * (128 * 128 >> 4) + in, kDescHiSw128),
-                             umma_desc_join(k_lo + blk * (S::kBlockBytes >> 4) + in, kDescHiSw128), idesc_s, k > 0);
+                const uint32_t k_lo = umma_desc_lo(ring0 + (j % S::kStages) * S::kStageBytes);
+                const uint32_t idesc = tile_idesc<T>(keys_of(j), false) | negate;
+#pragma unroll
+                for (int k = 0; k < DB * 4; ++k) {
+                    if (k < ksteps)
+                        umma_f16(tmem, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
+                                 umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc, k > 0);
                 }
                 umma_commit(&c.s_full[j & 1]);
-                umma_commit(&c.k_empty[stage]);
-                issued = true;
-            };
-            if (tiles > 0) score(0);
-            if (ok && tiles > 1) score(1);
-            for (int j = 0; ok && j < tiles; ++j) {
-                const int stage = j % S::kStages;
-                if (!(ok = mbar_wait(&c.v_full[stage], (j / S::kStages) & 1, ctl, 204))) break;
+                umma_commit(&c.k_empty[j % S::kStages]);
+            }
+            if (!ok && j > 0) {  // gave up: the products already issued end before TMEM is freed (bounded)
+                umma_commit(&c.drain[0]);
+                const uint64_t t0 = global_timer_ns();
+                while (!mbar_try_wait(&c.drain[0], 0) && global_timer_ns() - t0 < 2000000000ull) {
+                }
+            }
+        }
+    } else if (warp == 5) {
+        // ------------------------------------------------------------ O += P V
+        if (lane == 0) {
+            const uint32_t t_o = tmem + S::kOCol;
+            const uint32_t idesc = tile_idesc<T>(p.dim, true);
+            bool ok = true;
+            int j = 0;
+            for (; j < tiles; ++j) {
+                if (!(ok = mbar_wait(&c.v_full[j % S::kStages], (j / S::kStages) & 1, ctl, 204))) break;
                 if (!(ok = mbar_wait(&c.p_ready[j & 1], (j >> 1) & 1, ctl, 205))) break;
                 tc_fence_after_sync();
                 // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
-                const uint32_t v_addr = ring0 + stage * S::kStageBytes + S::kPlaneBytes;
+                const uint32_t v_addr = ring0 + (j % S::kStages) * S::kStageBytes + S::kPlaneBytes;
                 const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-                for (int k = 0; k < keys_of(j) >> 4; ++k)
-                    umma_f16_ts(t_o, t_s + (j & 1) * S::kKeys + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o,
-                                (j > 0 || k > 0) ? 1u : 0u);
+                const uint32_t t_p = tmem + S::kPCol + (j & 1) * (S::kKeys / 2);
+                const int steps = keys_of(j) >> 4;
+#pragma unroll
+                for (int k = 0; k < S::kKeys / 16; ++k)
+                    if (k < steps) umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc, (j > 0 || k > 0) ? 1u : 0u);
                 umma_commit(&c.pv_done[j & 1]);
-                umma_commit(&c.v_empty[stage]);
-                if (j + 2 < tiles) {
-                    if (!(ok = mbar_wait(&c.pv_done[j & 1], (j >> 1) & 1, ctl, 203))) break;  // P(j) lies where S(j + 2) goes
-                    score(j + 2);
-                }
+                umma_commit(&c.v_empty[j % S::kStages]);
             }
-            if (!ok && issued) {
-                umma_commit(&c.drain);
+            if (!ok && j > 0) {
+                umma_commit(&c.drain[1]);
                 const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
+                while (!mbar_try_wait(&c.drain[1], 0) && global_timer_ns() - t0 < 2000000000ull) {
                 }
             }
         }
     } else {
         // ------------------------------------------------------------ softmax: thread = row = TMEM lane
         const int r = tid;
-        const int tok = r / p.group;
+        const int tok = token_of(r, inv_group);
         const bool row_live = tok < tokens;
         const int pos = row_live && c.req[tok] >= 0 ? c.pos[tok] : -1;
         const int word = row_live ? tok >> 5 : 0;
         const uint32_t bit = row_live && pos >= 0 ? 1u << (tok & 31) : 0u;
         const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-        const uint32_t t_s0 = tmem + lanes, t_o = t_s0 + S::kOCol;
+        const uint32_t t_rows = tmem + lanes, t_o = t_rows + S::kOCol;
         const float scale = fmaxf(fabsf(p.scale_log2), 1.2e-38f);  // zero would turn masked logits into NaN
         const float slack = 8.0f / scale;
         float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum
         bool ok = true;
+        const uint64_t scale2 = pair32(scale, scale);
+        auto members_of = [&](int b, uint32_t low) { return word == 0 ? low : c.more[b][word - 1]; };
+        auto ahead = c.box[0];  // the next tile's first box, fetched under this tile's exponentials
         for (int j = 0; j < tiles; ++j) {
-            const int stage = j % S::kStages;
             const int b0 = j * per_tile, n_boxes = min(per_tile, boxes - b0);
-            const uint32_t t_s = t_s0 + (j & 1) * S::kKeys;
+            const uint32_t t_p = t_rows + S::kPCol + (j & 1) * (S::kKeys / 2);
             // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees
-            uint32_t full = 0, part = 0;
-            int rem = 0;
-            bool tail = false;
-            for (int i = 0; i < n_boxes; ++i) {
-                const int seen = (c.members[b0 + i][word] & bit) ? min(max(pos + 1 - c.first[b0 + i], 0), box) : 0;
+            int seen = (members_of(b0, ahead.members) & bit) ? min(max(pos + 1 - ahead.first, 0), box) : 0;
+            uint32_t full = (1u << (seen >> 4)) - 1, part = seen & 15 ? 1u << (seen >> 4) : 0u;
+            int rem = seen & 15;
+            bool tail = ahead.dead < box;
+            for (int i = 1; i < n_boxes; ++i) {
+                seen = (members_of(b0 + i, c.box[b0 + i].members) & bit) ? min(max(pos + 1 - c.box[b0 + i].first, 0), box) : 0;
                 const int g0 = (i << box_shift) >> 4;
                 full |= ((1u << (seen >> 4)) - 1) << g0;
                 if (seen & 15) {
                     part |= 1u << (g0 + (seen >> 4));
                     rem = seen & 15;
                 }
-                tail |= c.dead[b0 + i] < box;
+                tail |= c.box[b0 + i].dead < box;
             }
             const uint32_t mine = full | part;
             const bool some = __any_sync(0xFFFFFFFFu, mine != 0);
             // keys that only part of a group's rows see, and columns that hold no key of the request
             const bool cut = __any_sync(0xFFFFFFFFu, part != 0) || tail || n_boxes < per_tile;
             if (tail) {  // value rows that no token of the window sees
-                if (!(ok = warp_wait(&c.v_full[stage], (j / S::kStages) & 1, ctl, 207))) break;
+                if (!(ok = warp_wait(&c.v_full[j % S::kStages], (j / S::kStages) & 1, ctl, 207))) break;
                 for (int i = 0; i < n_boxes; ++i) {
-                    const int rows = box - c.dead[b0 + i];
-                    uint8_t* base = ring + stage * S::kStageBytes + S::kPlaneBytes + (i * box + c.dead[b0 + i]) * 128;
-                    for (int x = r; x < rows * 8 * DB; x += 128) {
+                    const int dead = c.box[b0 + i].dead;
+                    uint8_t* base = ring + (j % S::kStages) * S::kStageBytes + S::kPlaneBytes + (i * box + dead) * 128;
+                    for (int x = r; x < (box - dead) * 8 * DB; x += 128) {
                         const int piece = x & 7, rest = x >> 3;
                         *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                     }
@@ -530,42 +570,43 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             }
             if (!(ok = warp_wait(&c.s_full[j & 1], (j >> 1) & 1, ctl, 208))) break;
             tc_fence_after_sync();
-            constexpr int kGroups = S::kKeys / 16;
-            if (!some) {  // no row of the warp selected any of it
-                const uint32_t none[16] = {};
-#pragma unroll
-                for (int q = 0; q < S::kKeys / 32; ++q) tmem_st_32x32b_x16(t_s + q * 16, none);
-                tmem_wait_st();
-                tc_fence_before_sync();
-                mbar_arrive(&c.p_ready[j & 1]);
-                continue;
-            }
             uint32_t s[S::kKeys];
-            tmem_ld_32x32b_x64(t_s, s);
-            tmem_wait_ld_regs(s);
-            if (cut) {
+            constexpr int kGroups = S::kKeys / 16;
+            if (some) {
+                tmem_ld_32x32b_x64(t_rows, s);
+                tmem_wait_ld_regs(s);
+            }
+            tc_fence_before_sync();
+            mbar_arrive(&c.s_free);
+            float top = -INFINITY;
+            if (some) {
+                if (cut) {
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g) {
+                        const int see = full >> g & 1 ? 16 : part >> g & 1 ? rem : 0;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            if (x >= see) s[g * 16 + x] = 0xFF800000u;
+                    }
+                }
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int seen = full >> g & 1 ? 16 : part >> g & 1 ? rem : 0;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        if (x >= seen) s[g * 16 + x] = 0xFF800000u;
+                    const uint32_t* v = &s[g * 16];
+                    const float a = max3f(v[0], v[1], v[2]), b = max3f(v[3], v[4], v[5]), d = max3f(v[6], v[7], v[8]), f = max3f(v[9], v[10], v[11]);
+                    const float t = fmaxf(max3f(max3f(a, b, d), f, max3f(v[12], v[13], v[14])), __uint_as_float(v[15]));
+                    top = fmaxf(top, mine >> g & 1 ? t : -INFINITY);
                 }
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const uint32_t* v = &s[g * 16];
-                const float a = max3f(v[0], v[1], v[2]), b = max3f(v[3], v[4], v[5]), d = max3f(v[6], v[7], v[8]), f = max3f(v[9], v[10], v[11]);
-                const float t = fmaxf(max3f(max3f(a, b, d), f, max3f(v[12], v[13], v[14])), __uint_as_float(v[15]));
-                top = fmaxf(top, mine >> g & 1 ? t : -INFINITY);
+            if (j > 1) {  // the weights of tile j - 2 have been used
+                if (!(ok = warp_wait(&c.pv_done[j & 1], ((j >> 1) - 1) & 1, ctl, 215))) break;
+                tc_fence_after_sync();
             }
             const bool grow = top > m + slack || (m == -INFINITY && top > m);
             if (__any_sync(0xFFFFFFFFu, grow)) {
-                const float fix = grow ? (l > 0.0f ? exp2_fast((m - top) * scale) : 1.0f) : 1.0f;
+                const float fix = grow && l > 0.0f ? exp2_fast((m - top) * scale) : 1.0f;
                 if (grow) m = top;
-                if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {
-                    if (!(ok = warp_wait(&c.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, ctl, 211))) break;  // (a sum that is not zero: j > 0)
+                if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (a sum that is not zero: j > 0)
+                    if (!(ok = warp_wait(&c.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, ctl, 211))) break;
                     tc_fence_after_sync();
                     l *= fix;
                     for (int q = 0; q < p.dim >> 4; ++q) {  // 16 columns at a time: the logits stay in registers
@@ -577,25 +618,31 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     }
                 }
             }
-            const float base = m == -INFINITY ? 0.0f : m * scale;
-            uint64_t sum[2] = {0, 0};  // of two 32-bit sums each
-            const uint64_t scale2 = pair32(scale, scale);
+            if (j + 1 < tiles) ahead = c.box[b0 + per_tile];
+            if (some) {
+                const float base = m == -INFINITY ? 0.0f : m * scale;
+                uint64_t sum[2] = {0, 0};  // of two 32-bit sums each
 #pragma unroll
-            for (int q = 0; q < S::kKeys / 32; ++q) {
-                uint32_t out[16];
+                for (int q = 0; q < S::kKeys / 32; ++q) {
+                    uint32_t out[16];
 #pragma unroll
-                for (int x = 0; x < 32; x += 2) {
-                    const int i = q * 32 + x;
-                    const float off = mine >> (i / 16) & 1 ? -base : -INFINITY;  // a group that the row does not see: all weights 0
-                    const uint64_t z = fma2(pair32(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, pair32(off, off));
-                    const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
-                    sum[x / 2 & 1] = add2(sum[x / 2 & 1], pair32(a, b));
-                    out[x / 2] = Pair16<T>::pack(a, b);
+                    for (int x = 0; x < 32; x += 2) {
+                        const int i = q * 32 + x;
+                        const float off = mine >> (i / 16) & 1 ? -base : -INFINITY;  // a group that the row does not see: all weights 0
+                        const uint64_t z = fma2(pair32(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, pair32(off, off));
+                        const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
+                        sum[x / 2 & 1] = add2(sum[x / 2 & 1], pair32(a, b));
+                        out[x / 2] = Pair16<T>::pack(a, b);
+                    }
+                    tmem_st_32x32b_x16(t_p + q * 16, out);
                 }
-                tmem_st_32x32b_x16(t_s + q * 16, out);
+                const uint64_t both = add2(sum[0], sum[1]);
+                l += lo32(both) + hi32(both);
+            } else {  // no row of the warp selected any of it
+                const uint32_t none[16] = {};
+#pragma unroll
+                for (int q = 0; q < S::kKeys / 32; ++q) tmem_st_32x32b_x16(t_p + q * 16, none);
             }
-            const uint64_t both = add2(sum[0], sum[1]);
-            l += lo32(both) + hi32(both);
             tmem_wait_st();
             tc_fence_before_sync();
             mbar_arrive(&c.p_ready[j & 1]);
@@ -631,7 +678,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             constexpr int kAtOnce = 32 / (DB * 8) > 0 ? 32 / (DB * 8) : 1;  // rows of a store
             for (int row0 = 0; row0 < 32; row0 += kAtOnce) {
                 const int row = row0 + lane / (DB * 8 < 32 ? DB * 8 : 32), piece = lane % (DB * 8 < 32 ? DB * 8 : 32);
-                const int out_row = warp * 32 + row, tk = out_row / p.group;
+                const int out_row = warp * 32 + row, tk = token_of(out_row, inv_group);
                 if (tk < tokens && piece < pieces) {
                     const uint4 v = *reinterpret_cast<const uint4*>(stash + row * (DB * 128) + ((piece ^ (row & 7)) << 4));
                     *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + (w0 + tk) * p.out_stride[0] +
