@@ -73,6 +73,12 @@ constexpr int tile_smem() {
     return 1024 + S::kQBytes + S::kStages * S::kStageBytes + static_cast<int>(sizeof(TileControl<DB>));
 }
 
+// True in one lane of the warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -182,7 +188,10 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = smem + S::kQBytes;
     TileControl<DB>& c = *reinterpret_cast<TileControl<DB>*>(ring + S::kStages * S::kStageBytes);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31;
+    // (broadcast, so that the compiler knows it to be the same for the warp: the products' descriptors then live in uniform
+    // registers and an issue takes 48 cycles instead of 79)
+    const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     const int h = blockIdx.y;
     const int64_t w0 = static_cast<int64_t>(blockIdx.x) * p.window;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(p.window), p.n_tokens - w0));
@@ -403,7 +412,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     auto keys_of = [&](int j) { return min(per_tile, boxes - j * per_tile) << box_shift; };
     if (warp == 6) {
         // ------------------------------------------------------------ copies: keys and values in whatever order stages come free
-        if (lane == 0) {
+        if (elect_one()) {
             auto copy = [&](int j, const CUtensorMap* from, uint64_t* full, uint32_t to) {
                 const int b0 = j * per_tile, n = min(per_tile, boxes - b0);
                 mbar_arrive_expect_tx(full, n * DB * box * 128);
@@ -460,7 +469,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
     } else if (warp == 4) {
         // ------------------------------------------------------------ S = Q K^T
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t q_lo = umma_desc_lo(smem_u32(smem));
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const int ksteps = p.dim >> 4;
@@ -490,7 +499,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         }
     } else if (warp == 5) {
         // ------------------------------------------------------------ O += P V
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t t_o = tmem + S::kOCol;
             const uint32_t idesc = tile_idesc<T>(p.dim, true);
             bool ok = true;
