@@ -8,9 +8,8 @@
 //                   sums give every block its place, and every (token, block) sets the token's bit there.  (A
 //                   warp that merged the tokens' lists tile by tile needed 2,600 cycles for a tile and held all
 //                   the others up.)
-//   three threads   of a warp each issue the copies (TMA), S = Q K^T into TMEM, and O += P V with P read from TMEM.
-//                   One thread for both products spent 2,300 cycles of issue and waits on a tile, and everybody
-//                   else's time with it.
+//   issuer          one thread serves in whatever order their inputs come: S = Q K^T into TMEM, O += P V with P read
+//                   from TMEM, and the copies of keys and values (TMA)
 //   softmax warps   one thread per row: S out of TMEM, maximum and sum in registers, P into TMEM.  O is rescaled
 //                   only when the maximum has grown by more than 2^8 past the reference of the exponentials; the
 //                   reference cancels in the final division.
@@ -38,10 +37,10 @@ struct TileShape {
     static constexpr int kPlaneBytes = DB * kBlockBytes;
     static constexpr int kStageBytes = 2 * kPlaneBytes;
     static constexpr int kQBytes = DB * 128 * 128;
-    static constexpr int kBoxes = 448;                  // of a plan
+    static constexpr int kBoxes = 320;                  // of a plan
     static constexpr int kMapWords = 1024;              // bitmap of 32,768 blocks at a time, in the ring before the loop
     static constexpr int kRows = 128;
-    static constexpr int kWarps = 7;                    // softmax 0-3, S 4, P V 5, copies 6
+    static constexpr int kWarps = 5;                    // softmax 0-3, issuer 4
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kPCol = kKeys, kOCol = 2 * kKeys;  // TMEM columns: S, P twice (16-bit: half as wide), O
     static constexpr int kCols = DB == 4 ? 512 : 256;
@@ -51,7 +50,7 @@ template <int DB>
 struct TileControl {
     uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2];
     // by the tile's parity: a waiter may be one tile late, not two
-    uint64_t s_free, s_full[2], p_ready[2], pv_done[2], drain[2];
+    uint64_t s_free, s_full[2], p_ready[2], pv_done[2], drain;
     // the plan, a box being a page or a half of a page of 128
     struct alignas(16) Box {
         int first;         // position of its first token
@@ -255,8 +254,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             mbar_init(&c.pv_done[i], 1);
         }
         mbar_init(&c.s_free, 128);
-        mbar_init(&c.drain[0], 1);
-        mbar_init(&c.drain[1], 1);
+        mbar_init(&c.drain, 1);
         c.abort_flag = 0;
         c.bad = 0;
         fence_mbar_init();
@@ -410,9 +408,14 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     ctl.limit_ns = p.limit_ns;
     const uint32_t ring0 = smem_u32(ring);
     auto keys_of = [&](int j) { return min(per_tile, boxes - j * per_tile) << box_shift; };
-    if (warp == 6) {
-        // ------------------------------------------------------------ copies: keys and values in whatever order stages come free
+    if (warp == S::kWarps - 1) {
+        // ------------------------------------------------------------ issuer
         if (elect_one()) {
+            const uint32_t t_o = tmem + S::kOCol;
+            const uint32_t q_lo = umma_desc_lo(smem_u32(smem));
+            const uint32_t idesc_o = tile_idesc<T>(p.dim, true);
+            const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
+            const int ksteps = p.dim >> 4;
             auto copy = [&](int j, const CUtensorMap* from, uint64_t* full, uint32_t to) {
                 const int b0 = j * per_tile, n = min(per_tile, boxes - b0);
                 mbar_arrive_expect_tx(full, n * DB * box * 128);
@@ -425,12 +428,46 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             auto is_free = [&](uint64_t* empty, int j) {
                 return j < S::kStages || mbar_test_wait(&empty[j % S::kStages], (j / S::kStages - 1) & 1);
             };
-            int k = 0, v = 0;
+            int k = 0, v = 0;        // next keys and values to copy
+            int sj = 0, pj = 0;  // next S and P V
             uint64_t since = 0;
             uint32_t idle = 0;
             bool ok = true;
-            while (v < tiles) {
+            while (pj < tiles) {
                 bool moved = false;
+                if (sj < k && mbar_test_wait(&c.k_full[sj % S::kStages], (sj / S::kStages) & 1) &&
+                    (sj == 0 || mbar_test_wait(&c.s_free, (sj - 1) & 1))) {
+                    tc_fence_after_sync();
+                    const uint32_t k_lo = umma_desc_lo(ring0 + (sj % S::kStages) * S::kStageBytes);
+                    const uint32_t idesc = tile_idesc<T>(keys_of(sj), false) | negate;
+#pragma unroll
+                    for (int k = 0; k < DB * 4; ++k) {
+                        if (k < ksteps)
+                            umma_f16(tmem, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
+                                     umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc, k > 0);
+                    }
+                    umma_commit(&c.s_full[sj & 1]);
+                    umma_commit(&c.k_empty[sj % S::kStages]);
+                    ++sj;
+                    moved = true;
+                }
+                if (pj < sj && pj < v && mbar_test_wait(&c.p_ready[pj & 1], (pj >> 1) & 1) &&
+                    mbar_test_wait(&c.v_full[pj % S::kStages], (pj / S::kStages) & 1)) {
+                    tc_fence_after_sync();
+                    // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
+                    const uint32_t v_addr = ring0 + (pj % S::kStages) * S::kStageBytes + S::kPlaneBytes;
+                    const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
+                    const uint32_t t_p = tmem + S::kPCol + (pj & 1) * (S::kKeys / 2);
+                    const int steps = keys_of(pj) >> 4;
+#pragma unroll
+                    for (int k = 0; k < S::kKeys / 16; ++k)
+                        if (k < steps)
+                            umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (pj > 0 || k > 0) ? 1u : 0u);
+                    umma_commit(&c.pv_done[pj & 1]);
+                    umma_commit(&c.v_empty[pj % S::kStages]);
+                    ++pj;
+                    moved = true;
+                }
                 if (k < tiles && is_free(c.k_empty, k)) {
                     copy(k, &map_k, &c.k_full[k % S::kStages], ring0 + (k % S::kStages) * S::kStageBytes);
                     ++k;
@@ -443,87 +480,27 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
                 if (moved) {
                     idle = 0;
-                } else {
-                    __nanosleep(40);
-                    if ((++idle & 63u) == 0u) {
-                        const uint64_t t = global_timer_ns();
-                        if (idle == 64u) since = t;
-                        if (t - since > ctl.limit_ns) report_timeout(ctl, 201);
-                        if (*ctl.abort_flag) {
-                            ok = false;
-                            break;
-                        }
+                } else if ((++idle & 255u) == 0u) {
+                    const uint64_t t = global_timer_ns();
+                    if (idle == 256u) since = t;
+                    if (t - since > ctl.limit_ns) report_timeout(ctl, 202);
+                    if (*ctl.abort_flag) {
+                        ok = false;
+                        break;
                     }
                 }
             }
-            if (!ok) {
-                // gave up: let the copies already issued land before the CTA goes away (bounded)
+            if (!ok) {  // gave up: copies and products already issued end before the CTA and its TMEM go (bounded)
+                umma_commit(&c.drain);
                 const uint64_t t0 = global_timer_ns();
+                while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
+                }
                 for (int i = max(0, k - S::kStages); i < k; ++i)
                     while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                     }
                 for (int i = max(0, v - S::kStages); i < v; ++i)
                     while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
                     }
-            }
-        }
-    } else if (warp == 4) {
-        // ------------------------------------------------------------ S = Q K^T
-        if (elect_one()) {
-            const uint32_t q_lo = umma_desc_lo(smem_u32(smem));
-            const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
-            const int ksteps = p.dim >> 4;
-            bool ok = true;
-            int j = 0;
-            for (; j < tiles; ++j) {
-                if (!(ok = mbar_wait(&c.k_full[j % S::kStages], (j / S::kStages) & 1, ctl, 202))) break;
-                if (j > 0 && !(ok = mbar_wait(&c.s_free, (j - 1) & 1, ctl, 203))) break;
-                tc_fence_after_sync();
-                const uint32_t k_lo = umma_desc_lo(ring0 + (j % S::kStages) * S::kStageBytes);
-                const uint32_t idesc = tile_idesc<T>(keys_of(j), false) | negate;
-#pragma unroll
-                for (int k = 0; k < DB * 4; ++k) {
-                    if (k < ksteps)
-                        umma_f16(tmem, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
-                                 umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc, k > 0);
-                }
-                umma_commit(&c.s_full[j & 1]);
-                umma_commit(&c.k_empty[j % S::kStages]);
-            }
-            if (!ok && j > 0) {  // gave up: the products already issued end before TMEM is freed (bounded)
-                umma_commit(&c.drain[0]);
-                const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain[0], 0) && global_timer_ns() - t0 < 2000000000ull) {
-                }
-            }
-        }
-    } else if (warp == 5) {
-        // ------------------------------------------------------------ O += P V
-        if (elect_one()) {
-            const uint32_t t_o = tmem + S::kOCol;
-            const uint32_t idesc = tile_idesc<T>(p.dim, true);
-            bool ok = true;
-            int j = 0;
-            for (; j < tiles; ++j) {
-                if (!(ok = mbar_wait(&c.v_full[j % S::kStages], (j / S::kStages) & 1, ctl, 204))) break;
-                if (!(ok = mbar_wait(&c.p_ready[j & 1], (j >> 1) & 1, ctl, 205))) break;
-                tc_fence_after_sync();
-                // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
-                const uint32_t v_addr = ring0 + (j % S::kStages) * S::kStageBytes + S::kPlaneBytes;
-                const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-                const uint32_t t_p = tmem + S::kPCol + (j & 1) * (S::kKeys / 2);
-                const int steps = keys_of(j) >> 4;
-#pragma unroll
-                for (int k = 0; k < S::kKeys / 16; ++k)
-                    if (k < steps) umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc, (j > 0 || k > 0) ? 1u : 0u);
-                umma_commit(&c.pv_done[j & 1]);
-                umma_commit(&c.v_empty[j % S::kStages]);
-            }
-            if (!ok && j > 0) {
-                umma_commit(&c.drain[1]);
-                const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain[1], 0) && global_timer_ns() - t0 < 2000000000ull) {
-                }
             }
         }
     } else {
@@ -565,18 +542,6 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             const bool some = __any_sync(0xFFFFFFFFu, mine != 0);
             // keys that only part of a group's rows see, and columns that hold no key of the request
             const bool cut = __any_sync(0xFFFFFFFFu, part != 0) || tail || n_boxes < per_tile;
-            if (tail) {  // value rows that no token of the window sees
-                if (!(ok = warp_wait(&c.v_full[j % S::kStages], (j / S::kStages) & 1, ctl, 207))) break;
-                for (int i = 0; i < n_boxes; ++i) {
-                    const int dead = c.box[b0 + i].dead;
-                    uint8_t* base = ring + (j % S::kStages) * S::kStageBytes + S::kPlaneBytes + (i * box + dead) * 128;
-                    for (int x = r; x < (box - dead) * 8 * DB; x += 128) {
-                        const int piece = x & 7, rest = x >> 3;
-                        *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                }
-                fence_proxy_async_smem();
-            }
             if (!(ok = warp_wait(&c.s_full[j & 1], (j >> 1) & 1, ctl, 208))) break;
             tc_fence_after_sync();
             uint32_t s[S::kKeys];
@@ -609,6 +574,18 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             if (j > 1) {  // the weights of tile j - 2 have been used
                 if (!(ok = warp_wait(&c.pv_done[j & 1], ((j >> 1) - 1) & 1, ctl, 215))) break;
                 tc_fence_after_sync();
+            }
+            if (tail) {  // value rows that no token of the window sees (their stage is known to be one copy behind at most, too)
+                if (!(ok = warp_wait(&c.v_full[j % S::kStages], (j / S::kStages) & 1, ctl, 207))) break;
+                for (int i = 0; i < n_boxes; ++i) {
+                    const int dead = c.box[b0 + i].dead;
+                    uint8_t* base = ring + (j % S::kStages) * S::kStageBytes + S::kPlaneBytes + (i * box + dead) * 128;
+                    for (int x = r; x < (box - dead) * 8 * DB; x += 128) {
+                        const int piece = x & 7, rest = x >> 3;
+                        *reinterpret_cast<uint4*>(base + (rest % DB) * S::kBlockBytes + (rest / DB) * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+                fence_proxy_async_smem();
             }
             const bool grow = top > m + slack || (m == -INFINITY && top > m);
             if (__any_sync(0xFFFFFFFFu, grow)) {
