@@ -499,6 +499,7 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
 /* Test hook: 0 = the kernel of ivf_kv_attend is chosen by the sizes, 1 = always the one that takes tokens singly,
  * 2 = the one that takes windows of tokens wherever it can run. */
 int ivf_debug_set_kv_attend(int kernel);
+int ivf_debug_set_kv_select(int kernel);  /* the same for ivf_kv_select */
 
 #ifdef __cplusplus
 }

@@ -29,7 +29,7 @@ EXPORTS = (
     "ivf_route_prepared",
     "ivf_pq_encode", "ivf_pq_search", "ivf_pq_residuals", "ivf_assign_candidates", "ivf_merge_shards",
     "ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend",
-    "ivf_debug_set_kv_attend",
+    "ivf_debug_set_kv_attend", "ivf_debug_set_kv_select",
     "ivf_set_deferred_host_outputs", "ivf_wait_host_outputs",
     "ivf_check", "ivf_last_error", "ivf_release_workspace", "ivf_launch_count",
     "ivf_debug_plan", "ivf_debug_span", "ivf_debug_rotation", "ivf_debug_set_rotation", "ivf_debug_set_threshold_pass", "ivf_debug_fail_next_alloc", "ivf_debug_bounds_checked", "ivf_debug_bounds_probe", "ivf_debug_set_wait_limit_ns",
@@ -679,6 +679,13 @@ def ivf_debug_wait_probe() -> None:
 def ivf_debug_set_kv_attend(kernel: int) -> None:
     """0: by the sizes; 1: always the kernel that takes tokens singly; 2: windows of tokens wherever possible."""
     rc = lib().ivf_debug_set_kv_attend(int(kernel))
+    if rc != IVF_OK:
+        _raise(rc)
+
+
+def ivf_debug_set_kv_select(kernel: int) -> None:
+    """0: by the sizes; 1: always the kernel that takes tokens singly; 2: windows of tokens wherever possible."""
+    rc = lib().ivf_debug_set_kv_select(int(kernel))
     if rc != IVF_OK:
         _raise(rc)
 

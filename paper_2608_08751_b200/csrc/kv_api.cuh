@@ -93,6 +93,64 @@ int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) 
     return IVF_OK;
 }
 
+int g_kv_select = 0;  // test hook (ivf_debug_set_kv_select): 0 = by the sizes, 1 = rows kernel, 2 = windows kernel wherever it can run
+
+template <typename T, int L>
+int kv_launch_select_rows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    auto kernel = kv_select_rows_kernel<T, L>;
+    const int smem = p.max_blocks * 4;
+    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // CTAs to a row: until the card has four for each SM, as long as each still has 64 blocks
+    unsigned ranks = 1;
+    while (ranks < 8 && p.n_tokens * p.n_kv_heads * ranks < 4 * ctx.num_sms && p.max_blocks >= static_cast<int>(ranks) * 128) ranks *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.n_tokens) * ranks, p.n_kv_heads);
+    cfg.blockDim = kSelThreads;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    g_launches.fetch_add(1);
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
+    return IVF_OK;
+}
+template <typename T, int K>
+int kv_launch_select_windows(const KvSelectParams& p, cudaStream_t stream) {
+    auto kernel = kv_select_windows_kernel<T, K>;
+    const int smem = static_cast<int>(sel_window_smem(p.max_blocks));
+    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    const dim3 grid(static_cast<unsigned>((p.n_tokens + kSelWindow - 1) / kSelWindow), p.n_kv_heads);
+    kernel<<<grid, kSelThreads, smem, stream>>>(p, (p.max_blocks + 63) / 64 * 64);
+    LAUNCH_CHECK();
+    return IVF_OK;
+}
+template <typename T>
+int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    bool windows = g_kv_select != 1 && p.max_blocks <= kSelWindowBlocks;
+    if (g_kv_select == 0) windows = windows && p.n_tokens >= 8 * static_cast<int64_t>(p.n_req);
+    if (windows) {
+        switch ((p.dim + 31) / 32) {
+            case 1: return kv_launch_select_windows<T, 1>(p, stream);
+            case 2: return kv_launch_select_windows<T, 2>(p, stream);
+            case 3: return kv_launch_select_windows<T, 3>(p, stream);
+            case 4: return kv_launch_select_windows<T, 4>(p, stream);
+            case 5: return kv_launch_select_windows<T, 5>(p, stream);
+            case 6: return kv_launch_select_windows<T, 6>(p, stream);
+            case 7: return kv_launch_select_windows<T, 7>(p, stream);
+            default: return kv_launch_select_windows<T, 8>(p, stream);
+        }
+    }
+    if (p.dim <= 16) return kv_launch_select_rows<T, 1>(p, ctx, stream);
+    if (p.dim <= 32) return kv_launch_select_rows<T, 2>(p, ctx, stream);
+    if (p.dim <= 64) return kv_launch_select_rows<T, 4>(p, ctx, stream);
+    if (p.dim <= 128) return kv_launch_select_rows<T, 8>(p, ctx, stream);
+    return kv_launch_select_rows<T, 16>(p, ctx, stream);
+}
+
 int g_kv_attend = 0;  // test hook (ivf_debug_set_kv_attend): 0 = by the sizes, 1 = rows kernel only, 2 = tile kernel wherever it can run
 
 template <typename T, int DP>
@@ -275,6 +333,7 @@ int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int
     if (n_first < 0 || n_last < 1 || n_first > n_select || n_last > n_select - n_first)
         return fail(IVF_ERR_INVALID_ARG, "n_first = %d, n_last = %d: n_last must be at least 1 and both fit n_select = %d", n_first, n_last, n_select);
     if (num_pages < 0 || num_pages > 0x7FFFFFFF) return fail(IVF_ERR_INVALID_ARG, "num_pages = %lld", (long long)num_pages);
+    if (n_tokens > kKvMaxTokens / 8) return fail(IVF_ERR_UNSUPPORTED, "at most 2^28 - 1 tokens");
     if (n_tokens == 0) return IVF_OK;
     if ((rc = kv_check_tokens(table, table_stride, n_req, max_blocks, token_req, token_pos)) != IVF_OK) return rc;
     if (max_blocks > kSelMaxBlocks) return fail(IVF_ERR_UNSUPPORTED, "max_blocks = %d: at most %d blocks of one request", max_blocks, kSelMaxBlocks);
@@ -291,13 +350,7 @@ int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int
     p.token_req = token_req, p.token_pos = token_pos, p.n_select = n_select, p.n_first = n_first, p.n_last = n_last;
     p.out = out, p.status = pctx->status;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const int smem = max_blocks * 4;
-    const dim3 grid(static_cast<unsigned>(n_tokens), n_kv_heads);
-    auto kernel = dtype == IVF_F16 ? kv_select_kernel<__half> : kv_select_kernel<__nv_bfloat16>;
-    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    kernel<<<grid, kSelThreads, smem, stream>>>(p);
-    LAUNCH_CHECK();
-    return IVF_OK;
+    return dtype == IVF_F16 ? kv_launch_select<__half>(p, *pctx, stream) : kv_launch_select<__nv_bfloat16>(p, *pctx, stream);
 }
 
 int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache,
@@ -327,6 +380,12 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
     p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = pctx->status;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     return cache->dtype == IVF_F16 ? kv_launch_attend<__half>(p, *pctx, stream) : kv_launch_attend<__nv_bfloat16>(p, *pctx, stream);
+}
+
+int ivf_debug_set_kv_select(int kernel) {
+    if (kernel < 0 || kernel > 2) return fail(IVF_ERR_INVALID_ARG, "kernel = %d", kernel);
+    g_kv_select = kernel;
+    return IVF_OK;
 }
 
 int ivf_debug_set_kv_attend(int kernel) {

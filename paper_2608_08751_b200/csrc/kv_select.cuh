@@ -5,13 +5,24 @@
 // on every launch; ties go to the lower block.  Blocks 0 .. pos / page_size are visible; the first n_first
 // and the last n_last of them are always taken, the best of the others fill up to n_select.  Ids come out
 // ascending, -1 after the last.
+//
+// Scores become 32-bit keys in shared memory (larger score, larger key) and never reach global memory; the
+// n_select-th largest key is found bit by bit from the highest bit in which the keys differ, and one ordered
+// pass writes the ids.
+//
+//   rows     (single and drafted tokens) a cluster of CTAs shares the blocks of one (token, kv head), 4-byte dot products
+//            straight from the loads; the keys meet in the first CTA's shared memory.  Bound by the codes' bytes.
+//   windows  (prompts) 16 tokens by one kv head to a CTA, scores by the integer matrix instruction, a warp selects a row.
 #pragma once
 #include "kv_common.cuh"
 
 namespace ivf {
 
 constexpr int kSelThreads = 256;
+constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelMaxBlocks = 49152;  // keys of one row in shared memory
+constexpr int kSelWindow = 16;        // tokens of a window: rows of the matrix instruction
+constexpr int kSelWindowBlocks = 2816;  // blocks that a window's keys, pages and scales have room for
 
 struct KvSelectParams {
     const void* q;
@@ -31,144 +42,453 @@ struct KvSelectParams {
 };
 
 // Larger scores get larger keys; 0 is kept for blocks that cannot be taken, all ones for those always taken.
-__device__ __forceinline__ uint32_t sel_key(float score) {
-    const uint32_t u = __float_as_uint(score + 0.0f);  // -0 counts as 0
+constexpr uint32_t kSelAlways = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t sel_key(int dot, float scale) {
+    const uint32_t u = __float_as_uint(__fmul_rn(static_cast<float>(dot), scale) + 0.0f);  // -0 counts as 0
     const uint32_t k = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    return min(max(k, 1u), 0xFFFFFFFEu);
+    return min(max(k, 1u), kSelAlways - 1);
 }
 
-// The group's coded query, dim bytes into s_code.  P: group rounded up to a power of two.
-template <typename T, int P>
-__device__ __forceinline__ void sel_query(const KvSelectParams& p, int64_t t, int h, int8_t* s_code, float* s_red) {
-    const int e = threadIdx.x;
-    float u = 0.0f;
-    if (e < p.dim) {
-        const T* src = static_cast<const T*>(p.q) + t * p.q_stride[0] + static_cast<int64_t>(h) * p.group * p.q_stride[1] + e;
-        float x[P];
+// Sum of x(o), x(o + S), x(o + 2S) ... below P by halving: the same additions as halving_sum, without an array.
+template <int P, int S, typename F>
+__device__ __forceinline__ void sel_halving(float (&r)[8], int o, F&& load) {
+    if constexpr (S >= P) {
+        load(o, r);
+    } else {
+        float b[8];
+        sel_halving<P, 2 * S>(r, o, load);
+        sel_halving<P, 2 * S>(b, o + S, load);
 #pragma unroll
-        for (int g = 0; g < P; ++g) x[g] = g < p.group ? static_cast<float>(src[g * p.q_stride[1]]) : 0.0f;
-        u = halving_sum<P>(x);
+        for (int i = 0; i < 8; ++i) r[i] = __fadd_rn(r[i], b[i]);
     }
-    float amax = fabsf(u);
+}
+
+// The coded query of (token t, kv head h) by one warp: 8 elements to a lane.  P: group rounded up to a power of two.
+template <typename T, int P>
+__device__ __forceinline__ uint2 sel_code_warp(const KvSelectParams& p, int64_t t, int h) {
+    const int e0 = (threadIdx.x & 31) * 8;
+    const T* src = static_cast<const T*>(p.q) + t * p.q_stride[0] + static_cast<int64_t>(h) * p.group * p.q_stride[1] + e0;
+    float u[8];
+    sel_halving<P, 1>(u, 0, [&](int g, float (&x)[8]) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (g < p.group && e0 < p.dim) v = *reinterpret_cast<const uint4*>(src + g * p.q_stride[1]);
+        unpack8<T>(v, x);
+    });
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(u[i]));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
-    if ((e & 31) == 0) s_red[e >> 5] = amax;
-    __syncthreads();
-    amax = 0.0f;
-    for (int w = 0; w < kSelThreads / 32; ++w) amax = fmaxf(amax, s_red[w]);
-    if (e < p.dim) s_code[e] = static_cast<int8_t>(code_of(u, code_scale(amax)));
-    __syncthreads();
+    const float scale = code_scale(amax);
+    uint32_t w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        w[k] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[k] |= static_cast<uint32_t>(code_of(u[4 * k + i], scale) & 255) << (8 * i);
+    }
+    return make_uint2(w[0], w[1]);
+}
+template <typename T>
+__device__ __forceinline__ uint2 sel_code(const KvSelectParams& p, int64_t t, int h) {
+    if (p.group <= 1) return sel_code_warp<T, 1>(p, t, h);
+    if (p.group <= 2) return sel_code_warp<T, 2>(p, t, h);
+    if (p.group <= 4) return sel_code_warp<T, 4>(p, t, h);
+    if (p.group <= 8) return sel_code_warp<T, 8>(p, t, h);
+    if (p.group <= 16) return sel_code_warp<T, 16>(p, t, h);
+    return sel_code_warp<T, 64>(p, t, h);
 }
 
-__device__ __forceinline__ int sel_block_sum(int v, int* s_red) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = v;
+// ---------------------------------------------------------------------------------------------- rows
+// Sums over the CTA of a per-thread count; s_red: two slots used in turn, so that one barrier is enough.
+__device__ __forceinline__ int sel_block_sum(int v, int (&s_red)[2][kSelWarps], int& turn) {
+    v = __reduce_add_sync(0xFFFFFFFFu, v);
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) s_red[turn][threadIdx.x >> 5] = v;
     __syncthreads();
     int s = 0;
-    for (int w = 0; w < kSelThreads / 32; ++w) s += s_red[w];
+#pragma unroll
+    for (int w = 0; w < kSelWarps; ++w) s += s_red[turn][w];
     return s;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvSelectParams p) {
-    extern __shared__ uint32_t sel_keys[];
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {  // the same place in another CTA of the cluster
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// L lanes to a block's codes, 16 bytes each (L >= dim / 16, a power of two); kDeep blocks of a lane group in flight.
+template <typename T, int L>
+__global__ void __launch_bounds__(kSelThreads) kv_select_rows_kernel(KvSelectParams p) {
+    extern __shared__ uint32_t sel_keys[];  // of the first CTA of the cluster: one key per visible block
     __shared__ __align__(16) int8_t s_code[kKvMaxDim];
-    __shared__ float s_redf[kSelThreads / 32];
-    __shared__ int s_red[kSelThreads / 32];
-    const int64_t t = blockIdx.x;
-    const int h = blockIdx.y, tid = threadIdx.x;
+    __shared__ int s_red[2][kSelWarps];
+    __shared__ int s_scan[2][kSelWarps];
+    constexpr int kDeep = 8;
+    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    const int64_t t = blockIdx.x / ranks;
+    const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t* out = p.out + (t * p.n_kv_heads + h) * p.n_select;
     const int req = p.token_req[t], pos = p.token_pos[t];
     const bool padded = req < 0 || pos < 0;
     const bool bad = req >= p.n_req || (!padded && (pos >> p.page_shift) >= p.max_blocks);
-    if (padded || bad) {
-        if (bad && tid == 0) kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
-        for (int i = tid; i < p.n_select; i += kSelThreads) out[i] = -1;
+    if (padded || bad) {  // the whole cluster
+        if (rank == 0) {
+            if (bad && tid == 0) kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
+            for (int i = tid; i < p.n_select; i += kSelThreads) out[i] = -1;
+        }
         return;
     }
-    if (p.group <= 1) sel_query<T, 1>(p, t, h, s_code, s_redf);
-    else if (p.group <= 2) sel_query<T, 2>(p, t, h, s_code, s_redf);
-    else if (p.group <= 4) sel_query<T, 4>(p, t, h, s_code, s_redf);
-    else if (p.group <= 8) sel_query<T, 8>(p, t, h, s_code, s_redf);
-    else if (p.group <= 16) sel_query<T, 16>(p, t, h, s_code, s_redf);
-    else sel_query<T, 64>(p, t, h, s_code, s_redf);
-
     const int n = (pos >> p.page_shift) + 1;
     const int32_t* row = p.table + req * p.table_stride;
-    int valid = 0;
-    for (int b = tid; b < n; b += kSelThreads) {
-        const int page = row[b];
-        uint32_t key = 0;
-        if (page >= 0 && page < p.num_pages) {
-            ++valid;
-            if (b < p.n_first || b >= n - p.n_last) {
-                key = 0xFFFFFFFFu;
-            } else {
-                const int64_t at = static_cast<int64_t>(page) * p.n_kv_heads + h;
-                const int4* c = reinterpret_cast<const int4*>(p.codes + at * p.dim);
-                int dot = 0;
-                for (int i = 0; i < p.dim / 16; ++i) {
-                    const int4 a = c[i], u = reinterpret_cast<const int4*>(s_code)[i];
-                    dot = __dp4a(a.x, u.x, dot);
-                    dot = __dp4a(a.y, u.y, dot);
-                    dot = __dp4a(a.z, u.z, dot);
-                    dot = __dp4a(a.w, u.w, dot);
-                }
-                key = sel_key(__fmul_rn(static_cast<float>(dot), p.scales[at]));
+    const uint32_t keys0 = cluster_addr(sel_keys, 0);
+
+    // group of L lanes g of this cluster takes blocks g, g + groups, ...; kDeep of them at a time
+    constexpr int kGroups = kSelThreads / L;
+    const int sub = tid % L;
+    const int step = kGroups * static_cast<int>(ranks);
+    const bool live = sub * 16 < p.dim;
+    int4 c[kDeep];
+    float sc[kDeep];
+    int page[kDeep];
+    auto fetch = [&](int b0) {
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const int b = b0 + i * step;
+            page[i] = b < n ? row[b] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const bool ok = page[i] >= 0 && page[i] < p.num_pages;
+            const int64_t at = ok ? static_cast<int64_t>(page[i]) * p.n_kv_heads + h : 0;
+            c[i] = make_int4(0, 0, 0, 0);
+            sc[i] = 0.0f;
+            if (ok && live) c[i] = *reinterpret_cast<const int4*>(p.codes + at * p.dim + sub * 16);
+            if (ok) sc[i] = p.scales[at];
+        }
+    };
+    const int first = static_cast<int>(rank) * kGroups + tid / L;
+    fetch(first);  // on its way while the query is coded
+    if (warp == 0) {
+        const uint2 w = sel_code<T>(p, t, h);
+        if (lane * 8 < p.dim) *reinterpret_cast<uint2*>(s_code + lane * 8) = w;
+    }
+    if (ranks > 1) cluster_sync();  // (the first CTA runs, so its shared memory may be written)
+    else __syncthreads();
+    int4 u = make_int4(0, 0, 0, 0);
+    if (live) u = *reinterpret_cast<const int4*>(s_code + sub * 16);
+    for (int b0 = first; b0 - tid / L < n; b0 += kDeep * step) {
+        int dot[kDeep];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) dot[i] = __dp4a(c[i].w, u.w, __dp4a(c[i].z, u.z, __dp4a(c[i].y, u.y, __dp4a(c[i].x, u.x, 0))));
+#pragma unroll
+        for (int off = L / 2; off > 0; off >>= 1) {
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) dot[i] += __shfl_xor_sync(0xFFFFFFFFu, dot[i], off);
+        }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const int b = b0 + i * step;
+            if (b < n && sub == i % L) {
+                uint32_t key = 0;
+                if (page[i] >= 0 && page[i] < p.num_pages)
+                    key = b < p.n_first || b >= n - p.n_last ? kSelAlways : sel_key(dot[i], sc[i]);
+                else if (page[i] >= p.num_pages)
+                    kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
+                cluster_store(keys0 + b * 4, key);
             }
-        } else if (page >= p.num_pages) {
-            kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
         }
-        sel_keys[b] = key;
+        fetch(b0 + kDeep * step);
     }
-    const int total = sel_block_sum(valid, s_red);
-    const int take = min(p.n_select, total);
-    // the take-th largest key: bit by bit the largest threshold that at least `take` keys reach
-    uint32_t thr = 1;
-    if (total > p.n_select) {
-        thr = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t cand = thr | (1u << bit);
-            int c = 0;
-            for (int b = tid; b < n; b += kSelThreads) c += sel_keys[b] >= cand;
-            if (sel_block_sum(c, s_red) >= take) thr = cand;
-        }
-    }
-    int above = 0;
-    for (int b = tid; b < n; b += kSelThreads) above += sel_keys[b] > thr;
-    const int equals = take - sel_block_sum(above, s_red);  // of the keys at the threshold, the lowest blocks
-    // ascending ids: each thread owns a contiguous run of blocks
-    const int per = (n + kSelThreads - 1) / kSelThreads;
-    const int b0 = min(tid * per, n), b1 = min(b0 + per, n);
-    int gt = 0, eq = 0;
-    for (int b = b0; b < b1; ++b) gt += sel_keys[b] > thr, eq += sel_keys[b] == thr && thr > 0;
-    __shared__ int s_scan[2][kSelThreads];
-    s_scan[0][tid] = gt;
-    s_scan[1][tid] = eq;
-    __syncthreads();
-    if (tid == 0) {
-        int a = 0, c = 0;
-        for (int i = 0; i < kSelThreads; ++i) {
-            const int x = s_scan[0][i], y = s_scan[1][i];
-            s_scan[0][i] = a;
-            s_scan[1][i] = c;
-            a += x;
-            c += y;
-        }
-    }
-    __syncthreads();
-    int ngt = s_scan[0][tid], neq = s_scan[1][tid];
-    for (int b = b0; b < b1; ++b) {
+    if (ranks > 1) cluster_sync();
+    else __syncthreads();
+    if (rank != 0) return;
+
+    // ---- the take-th largest key
+    int turn = 0, always = 0, valid = 0;
+    uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
+    for (int b = tid; b < n; b += kSelThreads) {
         const uint32_t k = sel_keys[b];
-        if (k > thr) out[ngt++ + min(neq, equals)] = b;
-        else if (k == thr && k > 0) {
-            if (neq < equals) out[ngt + neq] = b;
-            ++neq;
+        always += k == kSelAlways;
+        valid += k != 0;
+        if (k != 0 && k != kSelAlways) {
+            all_or |= k;
+            all_and &= k;
         }
+    }
+    __shared__ uint32_t s_bits[2][kSelWarps];
+    all_or = __reduce_or_sync(0xFFFFFFFFu, all_or);
+    all_and = __reduce_and_sync(0xFFFFFFFFu, all_and);
+    if (lane == 0) s_bits[0][warp] = all_or, s_bits[1][warp] = all_and;
+    const int n_always = sel_block_sum(always, s_red, turn), n_valid = sel_block_sum(valid, s_red, turn);
+#pragma unroll
+    for (int w = 0; w < kSelWarps; ++w) all_or |= s_bits[0][w], all_and &= s_bits[1][w];
+    const int take = min(p.n_select, n_valid);
+    const int want = take - n_always;  // of the scored ones
+    uint32_t thr = 1;                  // keys >= thr are taken, those equal to it as far as they are needed
+    int at_least = n_valid - n_always;
+    if (n_valid > p.n_select) {
+        if (want <= 0) {
+            thr = kSelAlways;
+            at_least = 0;
+        } else {
+            const int top = 31 - __clz((all_or ^ all_and) | 1u);
+            thr = all_and & ~((2u << top) - 1);
+            for (int bit = top; bit >= 0 && at_least != want; --bit) {
+                const uint32_t cand = thr | (1u << bit);
+                int cnt = 0;
+                for (int b = tid; b < n; b += kSelThreads) cnt += sel_keys[b] >= cand && sel_keys[b] != kSelAlways;
+                cnt = sel_block_sum(cnt, s_red, turn);
+                if (cnt >= want) {
+                    thr = cand;
+                    at_least = cnt;
+                }
+            }
+        }
+    }
+    const int surplus = max(0, at_least - max(want, 0));  // keys equal to thr that are not needed: the highest blocks
+    // ---- ids in ascending order: warps take contiguous parts
+    const int per = (n + kSelWarps * 32 - 1) / (kSelWarps * 32) * 32;
+    const int w0 = min(warp * per, n), w1 = min(w0 + per, n);
+    int gt = 0, eq = 0;
+    for (int b = w0 + lane; b < w1; b += 32) {
+        gt += sel_keys[b] > thr;
+        eq += sel_keys[b] == thr;
+    }
+    gt = __reduce_add_sync(0xFFFFFFFFu, gt);
+    eq = __reduce_add_sync(0xFFFFFFFFu, eq);
+    if (lane == 0) s_scan[0][warp] = gt, s_scan[1][warp] = eq;
+    __syncthreads();
+    int gt_before = 0, eq_before = 0, eq_all = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWarps; ++w) {
+        if (w < warp) gt_before += s_scan[0][w], eq_before += s_scan[1][w];
+        eq_all += s_scan[1][w];
+    }
+    const int eq_take = eq_all - surplus;
+    for (int b0 = w0; b0 < w1; b0 += 32) {
+        const int b = b0 + lane;
+        const uint32_t k = b < w1 ? sel_keys[b] : 0u;
+        const unsigned mg = __ballot_sync(0xFFFFFFFFu, k > thr), me = __ballot_sync(0xFFFFFFFFu, b < w1 && k == thr);
+        const unsigned below = (1u << lane) - 1;
+        const int g = gt_before + __popc(mg & below), e = eq_before + __popc(me & below);
+        if (k > thr) out[g + min(e, eq_take)] = b;
+        else if (b < w1 && k == thr && e < eq_take) out[g + e] = b;
+        gt_before += __popc(mg);
+        eq_before += __popc(me);
     }
     for (int i = take + tid; i < p.n_select; i += kSelThreads) out[i] = -1;
+}
+
+// ---------------------------------------------------------------------------------------------- windows
+__device__ __forceinline__ void mma_s8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+inline size_t sel_window_smem(int blocks) {
+    const int padded = (blocks + 63) / 64 * 64;
+    return static_cast<size_t>(kSelWindow + 2) * padded * 4;
+}
+
+// K: steps of 32 elements (32 * K >= dim).  A dot product may take its elements in any order: lane q of a block's four lanes
+// takes elements 8 K q .. 8 K (q + 1), so that its loads are contiguous, and the query's fragments do the same.
+template <typename T, int K>
+__global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelectParams p, int padded) {
+    extern __shared__ uint32_t sel_smem[];
+    uint32_t* keys = sel_smem;                                        // [16][padded]
+    int* s_page = reinterpret_cast<int*>(keys + kSelWindow * padded);  // [padded]
+    float* s_scale = reinterpret_cast<float*>(s_page + padded);        // [padded]
+    __shared__ __align__(16) int8_t s_code[kSelWindow][32 * K];
+    __shared__ int s_req[kSelWindow], s_pos[kSelWindow];
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kSelWindow;
+    const int tokens = static_cast<int>(min(static_cast<int64_t>(kSelWindow), p.n_tokens - t0));
+    const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid < kSelWindow) {
+        int req = -1, pos = -1;
+        if (tid < tokens) {
+            req = p.token_req[t0 + tid];
+            pos = p.token_pos[t0 + tid];
+            if (req >= p.n_req || (req >= 0 && pos >= 0 && (pos >> p.page_shift) >= p.max_blocks)) {
+                kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
+                req = -1;
+            }
+            if (pos < 0) req = -1;
+        }
+        s_req[tid] = req;
+        s_pos[tid] = pos;
+    }
+    for (int r = warp; r < kSelWindow; r += kSelWarps) {
+        if (r < tokens) {
+            const uint2 w = sel_code<T>(p, t0 + r, h);
+            if (lane * 8 < 32 * K) *reinterpret_cast<uint2*>(&s_code[r][lane * 8]) = lane * 8 < p.dim ? w : make_uint2(0, 0);
+        } else if (lane * 8 < 32 * K) {
+            *reinterpret_cast<uint2*>(&s_code[r][lane * 8]) = make_uint2(0, 0);
+        }
+    }
+    __syncthreads();
+    const int q = lane & 3, nb = lane >> 2;
+    uint32_t a[K][4];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        a[k][0] = *reinterpret_cast<const uint32_t*>(&s_code[nb][q * 8 * K + k * 8]);
+        a[k][1] = *reinterpret_cast<const uint32_t*>(&s_code[nb + 8][q * 8 * K + k * 8]);
+        a[k][2] = *reinterpret_cast<const uint32_t*>(&s_code[nb][q * 8 * K + k * 8 + 4]);
+        a[k][3] = *reinterpret_cast<const uint32_t*>(&s_code[nb + 8][q * 8 * K + k * 8 + 4]);
+    }
+    // one request after the other: mostly there is one
+    for (int r0 = 0; r0 < tokens;) {
+        const int req = s_req[r0];
+        int r1 = r0, last = -1;
+        while (r1 < tokens && s_req[r1] == req) last = max(last, s_pos[r1++]);
+        const int n = req < 0 ? 0 : (last >> p.page_shift) + 1;
+        for (int b = tid; b < n; b += kSelThreads) {
+            int page = p.table[req * p.table_stride + b];
+            float scale = 0.0f;
+            if (page >= p.num_pages) {
+                kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
+                page = -1;
+            }
+            if (page >= 0) scale = p.scales[static_cast<int64_t>(page) * p.n_kv_heads + h];
+            s_page[b] = page;
+            s_scale[b] = scale;
+        }
+        __syncthreads();
+        // two tiles of 8 blocks to a warp at a time; their codes are fetched a step ahead
+        uint32_t code[2][2 * K];
+        auto fetch = [&](int b0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int b = b0 + i * 8 + nb;
+                const int page = b < n ? s_page[b] : -1;
+                const int8_t* src = p.codes + (page >= 0 ? static_cast<int64_t>(page) * p.n_kv_heads + h : 0) * p.dim;
+                const int e0 = q * 8 * K;
+                if constexpr (K % 2 == 0) {
+#pragma unroll
+                    for (int k = 0; k < K; k += 2) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (page >= 0 && e0 + k * 8 < p.dim) v = *reinterpret_cast<const uint4*>(src + e0 + k * 8);
+                        code[i][2 * k] = v.x, code[i][2 * k + 1] = v.y, code[i][2 * k + 2] = v.z, code[i][2 * k + 3] = v.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        uint2 v = make_uint2(0, 0);
+                        if (page >= 0 && e0 + k * 8 < p.dim) v = *reinterpret_cast<const uint2*>(src + e0 + k * 8);
+                        code[i][2 * k] = v.x, code[i][2 * k + 1] = v.y;
+                    }
+                }
+            }
+        };
+        fetch(warp * 16);
+        for (int b0 = warp * 16; b0 < n; b0 += kSelWarps * 16) {
+            int c[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                mma_s8(c[0], a[k], code[0][2 * k], code[0][2 * k + 1]);
+                mma_s8(c[1], a[k], code[1][2 * k], code[1][2 * k + 1]);
+            }
+            fetch(b0 + kSelWarps * 16);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int r = nb + (x >> 1) * 8, b = b0 + i * 8 + 2 * q + (x & 1);
+                    if (r >= r0 && r < r1 && b < n) {
+                        const int seen = (s_pos[r] >> p.page_shift) + 1;
+                        uint32_t key = 0;
+                        if (b < seen && s_page[b] >= 0) key = b < p.n_first || b >= seen - p.n_last ? kSelAlways : sel_key(c[i][x], s_scale[b]);
+                        keys[r * padded + b] = key;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        // a warp selects a row
+        for (int r = r0 + warp; r < r1; r += kSelWarps) {
+            int32_t* out = p.out + ((t0 + r) * p.n_kv_heads + h) * p.n_select;
+            const uint32_t* key = keys + r * padded;
+            const int m = req < 0 ? 0 : (s_pos[r] >> p.page_shift) + 1;
+            int always = 0, valid = 0;
+            uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
+            for (int b = lane; b < m; b += 32) {
+                const uint32_t k = key[b];
+                always += k == kSelAlways;
+                valid += k != 0;
+                if (k != 0 && k != kSelAlways) {
+                    all_or |= k;
+                    all_and &= k;
+                }
+            }
+            always = __reduce_add_sync(0xFFFFFFFFu, always);
+            valid = __reduce_add_sync(0xFFFFFFFFu, valid);
+            const int take = min(p.n_select, valid), want = take - always;
+            uint32_t thr = 1;
+            int at_least = valid - always;
+            if (valid > p.n_select) {
+                if (want <= 0) {
+                    thr = kSelAlways;
+                    at_least = 0;
+                } else {
+                    all_or = __reduce_or_sync(0xFFFFFFFFu, all_or);
+                    all_and = __reduce_and_sync(0xFFFFFFFFu, all_and);
+                    const int top = 31 - __clz((all_or ^ all_and) | 1u);
+                    thr = all_and & ~((2u << top) - 1);
+                    for (int bit = top; bit >= 0 && at_least != want; --bit) {
+                        const uint32_t cand = thr | (1u << bit);
+                        int cnt = 0;
+                        for (int b = lane; b < m; b += 32) cnt += key[b] >= cand && key[b] != kSelAlways;
+                        cnt = __reduce_add_sync(0xFFFFFFFFu, cnt);
+                        if (cnt >= want) {
+                            thr = cand;
+                            at_least = cnt;
+                        }
+                    }
+                }
+            }
+            int spare = 0;  // keys equal to thr that are taken
+            if (at_least > max(want, 0)) {
+                int eq = 0;
+                for (int b = lane; b < m; b += 32) eq += key[b] == thr;
+                spare = __reduce_add_sync(0xFFFFFFFFu, eq) - (at_least - max(want, 0));
+            } else {
+                spare = 0x7FFFFFFF;
+            }
+            int gt_before = 0, eq_before = 0;
+            for (int b0 = 0; b0 < m; b0 += 32) {
+                const int b = b0 + lane;
+                const uint32_t k = b < m ? key[b] : 0u;
+                const unsigned mg = __ballot_sync(0xFFFFFFFFu, k > thr), me = __ballot_sync(0xFFFFFFFFu, b < m && k == thr);
+                const unsigned below = (1u << lane) - 1;
+                const int g = gt_before + __popc(mg & below), e = eq_before + __popc(me & below);
+                if (k > thr) out[g + min(e, spare)] = b;
+                else if (b < m && k == thr && e < spare) out[g + e] = b;
+                gt_before += __popc(mg);
+                eq_before += __popc(me);
+            }
+            for (int i = take + lane; i < p.n_select; i += 32) out[i] = -1;
+        }
+        __syncthreads();
+        r0 = r1;
+    }
 }
 
 }  // namespace ivf

@@ -259,6 +259,14 @@ def _request_table(blocks, pages, seed, columns=None):
     return table
 
 
+@pytest.fixture(params=["by size", "single tokens", "windows"])
+def select_kernel(request):
+    """Every selection test runs with the kernel chosen by the sizes and with either forced."""
+    B.ivf_debug_set_kv_select(["by size", "single tokens", "windows"].index(request.param))
+    yield request.param
+    B.ivf_debug_set_kv_select(0)
+
+
 SELECT = [
     # contexts, fresh, kv, group, dim, page, take, first, last, type
     ([1], 1, 1, 1, 16, 16, 1, 0, 1, "bf16"), ([17], 3, 2, 3, 64, 16, 2, 0, 1, "fp16"), ([1000, 1, 64, 65], 1, 2, 4, 128, 16, 8, 1, 2, "bf16"),
@@ -275,7 +283,7 @@ def _step(contexts, fresh):
 
 
 @pytest.mark.parametrize("contexts,fresh,kv,group,dim,page,take,first,last,kind", SELECT)
-def test_selection_equals_the_plain_form(contexts, fresh, kv, group, dim, page, take, first, last, kind):
+def test_selection_equals_the_plain_form(select_kernel, contexts, fresh, kv, group, dim, page, take, first, last, kind):
     if first + last > take:
         first = take - last
     g = _gen(dim + take)
@@ -302,7 +310,7 @@ def test_selection_equals_the_plain_form(contexts, fresh, kv, group, dim, page, 
 
 @pytest.mark.parametrize("n_blocks,take", [(50, 8), (700, 64), (5000, 33), (20000, 1000)])
 @pytest.mark.parametrize("fresh", [1, 20])
-def test_ties_go_to_the_lower_block(n_blocks, take, fresh):
+def test_ties_go_to_the_lower_block(select_kernel, n_blocks, take, fresh):
     # few distinct scores: nearly every place in the list is decided by the tie rule; zero scales of both signs too
     g = _gen(n_blocks)
     page, dim = 16, 32
@@ -322,7 +330,7 @@ def test_ties_go_to_the_lower_block(n_blocks, take, fresh):
     assert (_np(got)[0, 0] == list(range(take - 1)) + [pos[0] // page]).all()
 
 
-def test_selection_skips_what_is_out_of_range():
+def test_selection_skips_what_is_out_of_range(select_kernel):
     codes, scales = torch.ones(8, 1, 32, dtype=torch.int8, device="cuda"), torch.ones(8, 1, device="cuda")
     q = torch.ones(4, 1, 32, device="cuda", dtype=torch.bfloat16)
     table = np.array([[0, 1, 2, 8, 3], [4, 5, -1, -1, -1]])
