@@ -56,6 +56,20 @@ int kv_check_tokens(const int32_t* table, int64_t table_stride, int n_req, int m
     return IVF_OK;
 }
 
+// Raises a kernel's limit of dynamic shared memory, once for a device and size: asking each time costs a call half a
+// microsecond.  `seen` belongs to one kernel.
+struct KvSmemSeen {
+    std::atomic<int> bytes[kMaxDevices];
+};
+template <typename K>
+int kv_allow_smem(K kernel, int bytes, const DeviceCtx& ctx, KvSmemSeen& seen) {
+    std::atomic<int>& known = seen.bytes[&ctx - g_ctx];
+    if (bytes <= 32 * 1024 || bytes <= known.load(std::memory_order_relaxed)) return IVF_OK;
+    CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    known.store(bytes, std::memory_order_relaxed);
+    return IVF_OK;
+}
+
 template <typename T>
 int kv_launch_append(const KvAppendParams& p, int num_sms, cudaStream_t stream) {
     int lg = 2;
@@ -99,7 +113,8 @@ template <typename T, int L>
 int kv_launch_select_rows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     auto kernel = kv_select_rows_kernel<T, L>;
     const int smem = p.max_blocks * 4;
-    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static KvSmemSeen seen;
+    if (int rc = kv_allow_smem(kernel, smem, ctx, seen)) return rc;
     // CTAs to a row: until the card has four for each SM, as long as each still has 64 blocks
     unsigned ranks = 1;
     while (ranks < 8 && p.n_tokens * p.n_kv_heads * ranks < 4 * ctx.num_sms && p.max_blocks >= static_cast<int>(ranks) * 128) ranks *= 2;
@@ -119,10 +134,11 @@ int kv_launch_select_rows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStr
     return IVF_OK;
 }
 template <typename T, int K>
-int kv_launch_select_windows(const KvSelectParams& p, cudaStream_t stream) {
+int kv_launch_select_windows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     auto kernel = kv_select_windows_kernel<T, K>;
     const int smem = static_cast<int>(sel_window_smem(p.max_blocks));
-    if (smem > 40 * 1024) CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static KvSmemSeen seen;
+    if (int rc = kv_allow_smem(kernel, smem, ctx, seen)) return rc;
     const dim3 grid(static_cast<unsigned>((p.n_tokens + kSelWindow - 1) / kSelWindow), p.n_kv_heads);
     kernel<<<grid, kSelThreads, smem, stream>>>(p, (p.max_blocks + 63) / 64 * 64);
     LAUNCH_CHECK();
@@ -134,14 +150,14 @@ int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t
     if (g_kv_select == 0) windows = windows && p.n_tokens >= 8 * static_cast<int64_t>(p.n_req);
     if (windows) {
         switch ((p.dim + 31) / 32) {
-            case 1: return kv_launch_select_windows<T, 1>(p, stream);
-            case 2: return kv_launch_select_windows<T, 2>(p, stream);
-            case 3: return kv_launch_select_windows<T, 3>(p, stream);
-            case 4: return kv_launch_select_windows<T, 4>(p, stream);
-            case 5: return kv_launch_select_windows<T, 5>(p, stream);
-            case 6: return kv_launch_select_windows<T, 6>(p, stream);
-            case 7: return kv_launch_select_windows<T, 7>(p, stream);
-            default: return kv_launch_select_windows<T, 8>(p, stream);
+            case 1: return kv_launch_select_windows<T, 1>(p, ctx, stream);
+            case 2: return kv_launch_select_windows<T, 2>(p, ctx, stream);
+            case 3: return kv_launch_select_windows<T, 3>(p, ctx, stream);
+            case 4: return kv_launch_select_windows<T, 4>(p, ctx, stream);
+            case 5: return kv_launch_select_windows<T, 5>(p, ctx, stream);
+            case 6: return kv_launch_select_windows<T, 6>(p, ctx, stream);
+            case 7: return kv_launch_select_windows<T, 7>(p, ctx, stream);
+            default: return kv_launch_select_windows<T, 8>(p, ctx, stream);
         }
     }
     if (p.dim <= 16) return kv_launch_select_rows<T, 1>(p, ctx, stream);
@@ -155,7 +171,8 @@ int g_kv_attend = 0;  // test hook (ivf_debug_set_kv_attend): 0 = by the sizes, 
 
 template <typename T, int DP>
 int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
-    CUDA_TRY(cudaFuncSetAttribute(kv_attend_rows_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DP>::kSmem));
+    static KvSmemSeen seen;
+    if (int rc = kv_allow_smem(kv_attend_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
     dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_kv_heads, (p.group + 15) / 16);
     if (p.done) {
         const int64_t most = std::max(1, 2 * ctx.num_sms / p.n_kv_heads);
@@ -191,8 +208,9 @@ bool kv_make_map(CUtensorMap* map, const KvPlane& c, const KvAttendParams& p, bo
 }
 
 template <typename T, int DB>
-int kv_launch_tile(const KvAttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t stream) {
-    CUDA_TRY(cudaFuncSetAttribute(kv_attend_tile_kernel<T, DB>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_smem<DB>()));
+int kv_launch_tile(const KvAttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, const DeviceCtx& ctx, cudaStream_t stream) {
+    static KvSmemSeen seen;
+    if (int rc = kv_allow_smem(kv_attend_tile_kernel<T, DB>, tile_smem<DB>(), ctx, seen)) return rc;
     const dim3 grid(static_cast<unsigned>((p.n_tokens + p.window - 1) / p.window), p.n_kv_heads);
     kv_attend_tile_kernel<T, DB><<<grid, TileShape<DB>::kThreads, tile_smem<DB>(), stream>>>(mk, mv, p);
     LAUNCH_CHECK();
@@ -215,8 +233,8 @@ int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     if (!tile) return kv_launch_rows<T>(p, ctx, stream);
     const int64_t windows = (p.n_tokens + p.window - 1) / p.window;
     WS(WS_KV_DONE, static_cast<size_t>(windows) * p.n_kv_heads, p.done);
-    const int rc = p.dim <= 64 ? kv_launch_tile<T, 1>(p, mk, mv, stream) : p.dim <= 128 ? kv_launch_tile<T, 2>(p, mk, mv, stream)
-                                                                                       : kv_launch_tile<T, 4>(p, mk, mv, stream);
+    const int rc = p.dim <= 64 ? kv_launch_tile<T, 1>(p, mk, mv, ctx, stream) : p.dim <= 128 ? kv_launch_tile<T, 2>(p, mk, mv, ctx, stream)
+                                                                                       : kv_launch_tile<T, 4>(p, mk, mv, ctx, stream);
     return rc != IVF_OK ? rc : kv_launch_rows<T>(p, ctx, stream);
 }
 
@@ -253,8 +271,8 @@ int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int pa
     p.max_tokens = max_tokens, p.touched_page = touched_page, p.touched_fill = touched_fill, p.max_touched = max_touched;
     p.used = used, p.status = pctx->status;
     const size_t smem = 3 * (static_cast<size_t>(n_req) + 1) * sizeof(int);
-    if (smem > 48 * 1024)
-        CUDA_TRY(cudaFuncSetAttribute(kv_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static KvSmemSeen seen;
+    if (int rc = kv_allow_smem(kv_tables_kernel, static_cast<int>(smem), *pctx, seen)) return rc;
     const int64_t items = (static_cast<int64_t>(n_req) * max_blocks) / 8 + max_tokens + max_touched;
     int64_t grid = (items + kTabThreads - 1) / kTabThreads;
     if (grid > pctx->num_sms) grid = pctx->num_sms;

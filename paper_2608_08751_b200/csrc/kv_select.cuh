@@ -6,9 +6,10 @@
 // and the last n_last of them are always taken, the best of the others fill up to n_select.  Ids come out
 // ascending, -1 after the last.
 //
-// Scores become 32-bit keys in shared memory (larger score, larger key) and never reach global memory; the
-// n_select-th largest key is found bit by bit from the highest bit in which the keys differ, and one ordered
-// pass writes the ids.
+// Scores become 32-bit keys in shared memory (larger score, larger key) and never reach global memory.  The largest keys
+// of parts of a row give a lower bound of its n_select-th largest key; what reaches it, a few more keys than are wanted,
+// goes on a short list in block order, and among those the threshold is found bit by bit.  (Bit by bit over
+// the whole row took 4,700 instructions of a warp for a row of 512 blocks.)
 //
 //   rows     (single and drafted tokens) a cluster of CTAs shares the blocks of one (token, kv head), 4-byte dot products
 //            straight from the loads; the keys meet in the first CTA's shared memory.  Bound by the codes' bytes.
@@ -22,7 +23,8 @@ constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelMaxBlocks = 49152;  // keys of one row in shared memory
 constexpr int kSelWindow = 16;        // tokens of a window: rows of the matrix instruction
-constexpr int kSelWindowBlocks = 2816;  // blocks that a window's keys, pages and scales have room for
+constexpr int kSelWindowList = 192;     // of a row's short list
+constexpr int kSelWindowBlocks = 2688;  // blocks that a window's keys, pages and scales have room for
 
 struct KvSelectParams {
     const void* q;
@@ -99,18 +101,105 @@ __device__ __forceinline__ uint2 sel_code(const KvSelectParams& p, int64_t t, in
     return sel_code_warp<T, 64>(p, t, h);
 }
 
-// ---------------------------------------------------------------------------------------------- rows
-// Sums over the CTA of a per-thread count; s_red: two slots used in turn, so that one barrier is enough.
-__device__ __forceinline__ int sel_block_sum(int v, int (&s_red)[2][kSelWarps], int& turn) {
-    v = __reduce_add_sync(0xFFFFFFFFu, v);
-    turn ^= 1;
-    if ((threadIdx.x & 31) == 0) s_red[turn][threadIdx.x >> 5] = v;
-    __syncthreads();
-    int s = 0;
+// ---------------------------------------------------------------------------------------------- from keys to ids, by a warp
+// The k-th largest of the 64 numbers that the lanes hold two of each, rounded down to its upper 16 bits; 0 if there are
+// fewer than k above 0.
+__device__ __forceinline__ uint32_t sel_kth_of_64(uint32_t a, uint32_t b, int k) {
+    uint32_t t = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) s += s_red[turn][w];
-    return s;
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t cand = t | (1u << bit);
+        if (__popc(__ballot_sync(0xFFFFFFFFu, a >= cand)) + __popc(__ballot_sync(0xFFFFFFFFu, b >= cand)) >= k) t = cand;
+    }
+    return t;
 }
+
+// The largest scored keys of key[b0 .. b1), of even and of odd groups of 32.
+__device__ __forceinline__ void sel_two_largest(const uint32_t* key, int b0, int b1, uint32_t& a, uint32_t& b) {
+    a = b = 0;
+    for (int i = b0 + (threadIdx.x & 31); i < b1; i += 64) {
+        const uint32_t x = key[i], y = i + 32 < b1 ? key[i + 32] : 0u;
+        if (x != kSelAlways) a = max(a, x);
+        if (y != kSelAlways) b = max(b, y);
+    }
+}
+
+// Writes the ids of the n_select largest of m keys in their order (all of them where there are fewer), -1 after the last.  Keys
+// of 0 do not count, those always taken come first; equal keys go to the earlier.  id: the keys' blocks, null: 0, 1, 2 ...
+__device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, int m, int n_select, int32_t* out) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kHeld = 4;
+    uint32_t held[kHeld];  // short lists stay in registers
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < m ? key[i * 32 + lane] : 0u;
+    const bool in_regs = m <= kHeld * 32;
+    int always = 0, valid = 0;
+    uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
+    auto look = [&](uint32_t k) {
+        always += k == kSelAlways;
+        valid += k != 0;
+        if (k != 0 && k != kSelAlways) {
+            all_or |= k;
+            all_and &= k;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) look(held[i]);
+    for (int b = kHeld * 32 + lane; b < m; b += 32) look(key[b]);
+    always = __reduce_add_sync(0xFFFFFFFFu, always);
+    valid = __reduce_add_sync(0xFFFFFFFFu, valid);
+    const int take = min(n_select, valid), want = take - always;
+    uint32_t thr = 1;  // larger keys are taken, and of those equal to it the first `spare`
+    int spare = 0x7FFFFFFF;
+    if (valid > n_select) {
+        int at_least = valid - always;
+        if (want <= 0) {
+            thr = kSelAlways;
+            at_least = always;
+        } else {
+            all_or = __reduce_or_sync(0xFFFFFFFFu, all_or);
+            all_and = __reduce_and_sync(0xFFFFFFFFu, all_and);
+            const int top = 31 - __clz((all_or ^ all_and) | 1u);
+            thr = all_and & ~((2u << top) - 1);
+            for (int bit = top; bit >= 0 && at_least != want; --bit) {
+                const uint32_t cand = thr | (1u << bit);
+                int cnt = 0;
+                if (in_regs) {
+#pragma unroll
+                    for (int i = 0; i < kHeld; ++i) cnt += held[i] >= cand;
+                } else {
+                    for (int b = lane; b < m; b += 32) cnt += key[b] >= cand;
+                }
+                cnt = __reduce_add_sync(0xFFFFFFFFu, cnt) - always;
+                if (cnt >= want) {
+                    thr = cand;
+                    at_least = cnt;
+                }
+            }
+        }
+        const int surplus = at_least - (want <= 0 ? take : want);
+        if (surplus > 0) {
+            int eq = 0;
+            for (int b = lane; b < m; b += 32) eq += key[b] == thr;
+            spare = __reduce_add_sync(0xFFFFFFFFu, eq) - surplus;
+        }
+    }
+    int gt_before = 0, eq_before = 0;
+    for (int b0 = 0; b0 < m; b0 += 32) {
+        const int b = b0 + lane;
+        const uint32_t k = b < m ? key[b] : 0u;
+        const unsigned mg = __ballot_sync(0xFFFFFFFFu, k > thr), me = __ballot_sync(0xFFFFFFFFu, k == thr);
+        const unsigned below = (1u << lane) - 1;
+        const int g = gt_before + __popc(mg & below), e = eq_before + __popc(me & below);
+        if (k > thr || (k == thr && e < spare)) out[g + min(e, spare)] = id ? id[b] : b;
+        gt_before += __popc(mg);
+        eq_before += __popc(me);
+    }
+    for (int i = take + lane; i < n_select; i += 32) out[i] = -1;
+}
+
+// ---------------------------------------------------------------------------------------------- rows
+constexpr int kSelList = 1024;  // of a row's short list
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -136,12 +225,14 @@ __device__ __forceinline__ void cluster_sync() {
 
 // L lanes to a block's codes, 16 bytes each (L >= dim / 16, a power of two); kDeep blocks of a lane group in flight.
 template <typename T, int L>
-__global__ void __launch_bounds__(kSelThreads) kv_select_rows_kernel(KvSelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelectParams p) {
     extern __shared__ uint32_t sel_keys[];  // of the first CTA of the cluster: one key per visible block
     __shared__ __align__(16) int8_t s_code[kKvMaxDim];
-    __shared__ int s_red[2][kSelWarps];
-    __shared__ int s_scan[2][kSelWarps];
-    constexpr int kDeep = 8;
+    __shared__ uint32_t s_bound[kSelWarps];
+    __shared__ int s_count[kSelWarps];
+    __shared__ uint32_t s_key[kSelList];
+    __shared__ int s_id[kSelList];
+    constexpr int kDeep = 4;
     const uint32_t rank = cluster_rank(), ranks = cluster_size();
     const int64_t t = blockIdx.x / ranks;
     const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -165,27 +256,32 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_rows_kernel(KvSelectPar
     const int sub = tid % L;
     const int step = kGroups * static_cast<int>(ranks);
     const bool live = sub * 16 < p.dim;
-    int4 c[kDeep];
-    float sc[kDeep];
-    int page[kDeep];
-    auto fetch = [&](int b0) {
+    // two steps are under way: the codes of the next, and the pages of the one after it
+    struct Step {
+        int4 code[kDeep];
+        float scale[kDeep];
+        int page[kDeep];
+    };
+    auto pages_of = [&](int b0, int (&page)[kDeep]) {
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) page[i] = b0 + i * step < n ? row[b0 + i * step] : -1;
+    };
+    auto codes_of = [&](Step& s) {
 #pragma unroll
         for (int i = 0; i < kDeep; ++i) {
-            const int b = b0 + i * step;
-            page[i] = b < n ? row[b] : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < kDeep; ++i) {
-            const bool ok = page[i] >= 0 && page[i] < p.num_pages;
-            const int64_t at = ok ? static_cast<int64_t>(page[i]) * p.n_kv_heads + h : 0;
-            c[i] = make_int4(0, 0, 0, 0);
-            sc[i] = 0.0f;
-            if (ok && live) c[i] = *reinterpret_cast<const int4*>(p.codes + at * p.dim + sub * 16);
-            if (ok) sc[i] = p.scales[at];
+            const bool ok = s.page[i] >= 0 && s.page[i] < p.num_pages;
+            const int64_t at = ok ? static_cast<int64_t>(s.page[i]) * p.n_kv_heads + h : 0;
+            s.code[i] = make_int4(0, 0, 0, 0);
+            s.scale[i] = 0.0f;
+            if (ok && live) s.code[i] = *reinterpret_cast<const int4*>(p.codes + at * p.dim + sub * 16);
+            if (ok) s.scale[i] = p.scales[at];
         }
     };
     const int first = static_cast<int>(rank) * kGroups + tid / L;
-    fetch(first);  // on its way while the query is coded
+    Step now, next;
+    pages_of(first, now.page);
+    pages_of(first + kDeep * step, next.page);
+    codes_of(now);  // on its way while the query is coded
     if (warp == 0) {
         const uint2 w = sel_code<T>(p, t, h);
         if (lane * 8 < p.dim) *reinterpret_cast<uint2*>(s_code + lane * 8) = w;
@@ -194,10 +290,11 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_rows_kernel(KvSelectPar
     else __syncthreads();
     int4 u = make_int4(0, 0, 0, 0);
     if (live) u = *reinterpret_cast<const int4*>(s_code + sub * 16);
-    for (int b0 = first; b0 - tid / L < n; b0 += kDeep * step) {
+    auto finish = [&](const Step& s, int b0) {
         int dot[kDeep];
 #pragma unroll
-        for (int i = 0; i < kDeep; ++i) dot[i] = __dp4a(c[i].w, u.w, __dp4a(c[i].z, u.z, __dp4a(c[i].y, u.y, __dp4a(c[i].x, u.x, 0))));
+        for (int i = 0; i < kDeep; ++i)
+            dot[i] = __dp4a(s.code[i].w, u.w, __dp4a(s.code[i].z, u.z, __dp4a(s.code[i].y, u.y, __dp4a(s.code[i].x, u.x, 0))));
 #pragma unroll
         for (int off = L / 2; off > 0; off >>= 1) {
 #pragma unroll
@@ -208,93 +305,71 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_rows_kernel(KvSelectPar
             const int b = b0 + i * step;
             if (b < n && sub == i % L) {
                 uint32_t key = 0;
-                if (page[i] >= 0 && page[i] < p.num_pages)
-                    key = b < p.n_first || b >= n - p.n_last ? kSelAlways : sel_key(dot[i], sc[i]);
-                else if (page[i] >= p.num_pages)
+                if (s.page[i] >= 0 && s.page[i] < p.num_pages)
+                    key = b < p.n_first || b >= n - p.n_last ? kSelAlways : sel_key(dot[i], s.scale[i]);
+                else if (s.page[i] >= p.num_pages)
                     kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
                 cluster_store(keys0 + b * 4, key);
             }
         }
-        fetch(b0 + kDeep * step);
+    };
+    for (int b0 = first; b0 - tid / L < n; b0 += 2 * kDeep * step) {
+        codes_of(next);
+        Step later;
+        pages_of(b0 + 2 * kDeep * step, later.page);
+        finish(now, b0);
+        now = later;
+        codes_of(now);
+        pages_of(b0 + 3 * kDeep * step, later.page);
+        finish(next, b0 + kDeep * step);
+        next = later;
     }
     if (ranks > 1) cluster_sync();
     else __syncthreads();
     if (rank != 0) return;
 
-    // ---- the take-th largest key
-    int turn = 0, always = 0, valid = 0;
-    uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
-    for (int b = tid; b < n; b += kSelThreads) {
-        const uint32_t k = sel_keys[b];
-        always += k == kSelAlways;
-        valid += k != 0;
-        if (k != 0 && k != kSelAlways) {
-            all_or |= k;
-            all_and &= k;
-        }
-    }
-    __shared__ uint32_t s_bits[2][kSelWarps];
-    all_or = __reduce_or_sync(0xFFFFFFFFu, all_or);
-    all_and = __reduce_and_sync(0xFFFFFFFFu, all_and);
-    if (lane == 0) s_bits[0][warp] = all_or, s_bits[1][warp] = all_and;
-    const int n_always = sel_block_sum(always, s_red, turn), n_valid = sel_block_sum(valid, s_red, turn);
-#pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) all_or |= s_bits[0][w], all_and &= s_bits[1][w];
-    const int take = min(p.n_select, n_valid);
-    const int want = take - n_always;  // of the scored ones
-    uint32_t thr = 1;                  // keys >= thr are taken, those equal to it as far as they are needed
-    int at_least = n_valid - n_always;
-    if (n_valid > p.n_select) {
-        if (want <= 0) {
-            thr = kSelAlways;
-            at_least = 0;
-        } else {
-            const int top = 31 - __clz((all_or ^ all_and) | 1u);
-            thr = all_and & ~((2u << top) - 1);
-            for (int bit = top; bit >= 0 && at_least != want; --bit) {
-                const uint32_t cand = thr | (1u << bit);
-                int cnt = 0;
-                for (int b = tid; b < n; b += kSelThreads) cnt += sel_keys[b] >= cand && sel_keys[b] != kSelAlways;
-                cnt = sel_block_sum(cnt, s_red, turn);
-                if (cnt >= want) {
-                    thr = cand;
-                    at_least = cnt;
-                }
-            }
-        }
-    }
-    const int surplus = max(0, at_least - max(want, 0));  // keys equal to thr that are not needed: the highest blocks
-    // ---- ids in ascending order: warps take contiguous parts
-    const int per = (n + kSelWarps * 32 - 1) / (kSelWarps * 32) * 32;
+    // ---- the short list: every warp takes a part of the row.  At least ceil(n_select / 8) scored keys of each part reach
+    // the smallest of the parts' bounds, so at least n_select of the row do
+    const int per = (n + kSelThreads - 1) / kSelThreads * 32;
     const int w0 = min(warp * per, n), w1 = min(w0 + per, n);
-    int gt = 0, eq = 0;
-    for (int b = w0 + lane; b < w1; b += 32) {
-        gt += sel_keys[b] > thr;
-        eq += sel_keys[b] == thr;
-    }
-    gt = __reduce_add_sync(0xFFFFFFFFu, gt);
-    eq = __reduce_add_sync(0xFFFFFFFFu, eq);
-    if (lane == 0) s_scan[0][warp] = gt, s_scan[1][warp] = eq;
+    uint32_t a, b;
+    sel_two_largest(sel_keys, w0, w1, a, b);
+    const uint32_t bound_w = sel_kth_of_64(a, b, (p.n_select + kSelWarps - 1) / kSelWarps);
+    if (lane == 0) s_bound[warp] = bound_w;
     __syncthreads();
-    int gt_before = 0, eq_before = 0, eq_all = 0;
+    uint32_t bound = s_bound[0];
+#pragma unroll
+    for (int w = 1; w < kSelWarps; ++w) bound = min(bound, s_bound[w]);
+    bound = max(bound, 1u);
+    int count = 0;
+    for (int i = w0 + lane; i < w1; i += 32) count += sel_keys[i] >= bound;
+    count = __reduce_add_sync(0xFFFFFFFFu, count);
+    if (lane == 0) s_count[warp] = count;
+    __syncthreads();
+    int before = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < kSelWarps; ++w) {
-        if (w < warp) gt_before += s_scan[0][w], eq_before += s_scan[1][w];
-        eq_all += s_scan[1][w];
+        if (w < warp) before += s_count[w];
+        total += s_count[w];
     }
-    const int eq_take = eq_all - surplus;
-    for (int b0 = w0; b0 < w1; b0 += 32) {
-        const int b = b0 + lane;
-        const uint32_t k = b < w1 ? sel_keys[b] : 0u;
-        const unsigned mg = __ballot_sync(0xFFFFFFFFu, k > thr), me = __ballot_sync(0xFFFFFFFFu, b < w1 && k == thr);
-        const unsigned below = (1u << lane) - 1;
-        const int g = gt_before + __popc(mg & below), e = eq_before + __popc(me & below);
-        if (k > thr) out[g + min(e, eq_take)] = b;
-        else if (b < w1 && k == thr && e < eq_take) out[g + e] = b;
-        gt_before += __popc(mg);
-        eq_before += __popc(me);
+    if (total <= kSelList) {
+        for (int i0 = w0; i0 < w1; i0 += 32) {
+            const int i = i0 + lane;
+            const uint32_t k = i < w1 ? sel_keys[i] : 0u;
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, k >= bound);
+            if (k >= bound) {
+                const int at = before + __popc(m & ((1u << lane) - 1));
+                s_key[at] = k;
+                s_id[at] = i;
+            }
+            before += __popc(m);
+        }
     }
-    for (int i = take + tid; i < p.n_select; i += kSelThreads) out[i] = -1;
+    __syncthreads();
+    if (warp == 0) {
+        if (total <= kSelList) sel_finish(s_key, s_id, total, p.n_select, out);
+        else sel_finish(sel_keys, nullptr, n, p.n_select, out);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- windows
@@ -318,6 +393,8 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
     float* s_scale = reinterpret_cast<float*>(s_page + padded);        // [padded]
     __shared__ __align__(16) int8_t s_code[kSelWindow][32 * K];
     __shared__ int s_req[kSelWindow], s_pos[kSelWindow];
+    __shared__ uint32_t s_key[kSelWarps][kSelWindowList];
+    __shared__ int s_id[kSelWarps][kSelWindowList];
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kSelWindow;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(kSelWindow), p.n_tokens - t0));
     const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -427,64 +504,25 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
             int32_t* out = p.out + ((t0 + r) * p.n_kv_heads + h) * p.n_select;
             const uint32_t* key = keys + r * padded;
             const int m = req < 0 ? 0 : (s_pos[r] >> p.page_shift) + 1;
-            int always = 0, valid = 0;
-            uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
-            for (int b = lane; b < m; b += 32) {
-                const uint32_t k = key[b];
-                always += k == kSelAlways;
-                valid += k != 0;
-                if (k != 0 && k != kSelAlways) {
-                    all_or |= k;
-                    all_and &= k;
-                }
-            }
-            always = __reduce_add_sync(0xFFFFFFFFu, always);
-            valid = __reduce_add_sync(0xFFFFFFFFu, valid);
-            const int take = min(p.n_select, valid), want = take - always;
-            uint32_t thr = 1;
-            int at_least = valid - always;
-            if (valid > p.n_select) {
-                if (want <= 0) {
-                    thr = kSelAlways;
-                    at_least = 0;
-                } else {
-                    all_or = __reduce_or_sync(0xFFFFFFFFu, all_or);
-                    all_and = __reduce_and_sync(0xFFFFFFFFu, all_and);
-                    const int top = 31 - __clz((all_or ^ all_and) | 1u);
-                    thr = all_and & ~((2u << top) - 1);
-                    for (int bit = top; bit >= 0 && at_least != want; --bit) {
-                        const uint32_t cand = thr | (1u << bit);
-                        int cnt = 0;
-                        for (int b = lane; b < m; b += 32) cnt += key[b] >= cand && key[b] != kSelAlways;
-                        cnt = __reduce_add_sync(0xFFFFFFFFu, cnt);
-                        if (cnt >= want) {
-                            thr = cand;
-                            at_least = cnt;
-                        }
-                    }
-                }
-            }
-            int spare = 0;  // keys equal to thr that are taken
-            if (at_least > max(want, 0)) {
-                int eq = 0;
-                for (int b = lane; b < m; b += 32) eq += key[b] == thr;
-                spare = __reduce_add_sync(0xFFFFFFFFu, eq) - (at_least - max(want, 0));
-            } else {
-                spare = 0x7FFFFFFF;
-            }
-            int gt_before = 0, eq_before = 0;
-            for (int b0 = 0; b0 < m; b0 += 32) {
+            uint32_t x, y;
+            sel_two_largest(key, 0, m, x, y);
+            const uint32_t bound = max(sel_kth_of_64(x, y, p.n_select), 1u);
+            int total = 0;
+            for (int b0 = 0; b0 < m && total <= kSelWindowList - 32; b0 += 32) {
                 const int b = b0 + lane;
                 const uint32_t k = b < m ? key[b] : 0u;
-                const unsigned mg = __ballot_sync(0xFFFFFFFFu, k > thr), me = __ballot_sync(0xFFFFFFFFu, b < m && k == thr);
-                const unsigned below = (1u << lane) - 1;
-                const int g = gt_before + __popc(mg & below), e = eq_before + __popc(me & below);
-                if (k > thr) out[g + min(e, spare)] = b;
-                else if (b < m && k == thr && e < spare) out[g + e] = b;
-                gt_before += __popc(mg);
-                eq_before += __popc(me);
+                const unsigned in = __ballot_sync(0xFFFFFFFFu, k >= bound);
+                if (k >= bound) {
+                    const int at = total + __popc(in & ((1u << lane) - 1));
+                    s_key[warp][at] = k;
+                    s_id[warp][at] = b;
+                }
+                total += __popc(in);
             }
-            for (int i = take + lane; i < p.n_select; i += 32) out[i] = -1;
+            __syncwarp();
+            if (total <= kSelWindowList - 32) sel_finish(s_key[warp], s_id[warp], total, p.n_select, out);
+            else sel_finish(key, nullptr, m, p.n_select, out);
+            __syncwarp();
         }
         __syncthreads();
         r0 = r1;
