@@ -173,13 +173,29 @@ template <typename T, int DP>
 int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     static KvSmemSeen seen;
     if (int rc = kv_allow_smem(kv_attend_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
-    dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_kv_heads, (p.group + 15) / 16);
-    if (p.done) {
-        const int64_t most = std::max(1, 2 * ctx.num_sms / p.n_kv_heads);
-        if (p.n_tokens > most) grid.x = static_cast<unsigned>(most);
+    const int z = (p.group + 15) / 16;
+    unsigned ranks = 1, x = static_cast<unsigned>(p.n_tokens);
+    if (p.done) {  // what the tile kernel left: a few CTAs look for it
+        x = static_cast<unsigned>(std::min<int64_t>(p.n_tokens, std::max(1, 2 * ctx.num_sms / p.n_kv_heads)));
+    } else {
+        // CTAs to a token: until the card has eight for each SM, as long as each warp still has a piece
+        const int pieces = p.n_select << (p.page_shift - 4);
+        while (ranks < 8 && p.n_tokens * p.n_kv_heads * z * ranks < 8 * ctx.num_sms && pieces >= static_cast<int>(ranks) * 2 * kRowsWarps) ranks *= 2;
+        x *= ranks;
     }
-    kv_attend_rows_kernel<T, DP><<<grid, kRowsThreads, RowsShape<DP>::kSmem, stream>>>(p);
-    LAUNCH_CHECK();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(x, p.n_kv_heads, z);
+    cfg.blockDim = kRowsThreads;
+    cfg.dynamicSmemBytes = RowsShape<DP>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    g_launches.fetch_add(1);
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, kv_attend_rows_kernel<T, DP>, p));
     return IVF_OK;
 }
 template <typename T>
@@ -385,6 +401,7 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
     if (n_tokens == 0) return IVF_OK;
     if ((rc = kv_check_tokens(table, table_stride, n_req, max_blocks, token_req, token_pos)) != IVF_OK) return rc;
     if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("out", out, out_stride, 2)) != IVF_OK) return rc;
+    if (n_tokens > kKvMaxTokens / 8) return fail(IVF_ERR_UNSUPPORTED, "at most 2^28 - 1 tokens");
     if (!selected) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
     DeviceCtx* pctx = nullptr;
     if ((rc = get_ctx(&pctx)) != IVF_OK) return rc;

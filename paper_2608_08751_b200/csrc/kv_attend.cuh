@@ -69,15 +69,16 @@ __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uin
 }
 
 // ---------------------------------------------------------------------------------------------- rows
-// One CTA per (token, kv head, 16 query heads of its group).  The group's heads are the 16 rows of the matrix
+// A cluster of CTAs per (token, kv head, 16 query heads of its group).  The group's heads are the 16 rows of the matrix
 // product, the keys come in pieces of 16 tokens.  Each warp takes pieces of its own through a ring of its own
-// and keeps its own running maximum, sum and output; the warps meet once, at the end.
+// and keeps its own running maximum, sum and output; the warps meet once, at the end, and then the cluster's CTAs,
+// through each other's shared memory.
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = kRowsWarps * 32;
 
 template <int DP>
 struct RowsShape {
-    static constexpr int kStages = DP == 256 ? 3 : 4;
+    static constexpr int kStages = DP == 64 ? 4 : 3;  // two CTAs on an SM (one for wide heads)
     static constexpr int kPlaneBytes = 16 * DP * 2;         // 16 tokens
     static constexpr int kStageBytes = 2 * kPlaneBytes;     // keys and values
     static constexpr int kRing = kRowsWarps * kStages * kStageBytes;
@@ -94,7 +95,7 @@ __device__ __forceinline__ uint32_t rows_addr(uint32_t base, int r, int c) {
 }
 
 template <typename T, int DP>
-__device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64_t t, uint8_t* rows_smem, int* s_page, int* s_first, int& s_n) {
+__device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64_t t, const int rank, const int ranks, uint8_t* rows_smem, int* s_page, int* s_first, int& s_n) {
     using S = RowsShape<DP>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y, g0 = blockIdx.z * 16;
@@ -146,6 +147,7 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
     const int pieces = s_n * per;
     const uint32_t ring = smem0 + warp * (S::kStages * S::kStageBytes);
     const int ksteps = p.dim >> 4;
+    const int first = rank * kRowsWarps + warp, stride = ranks * kRowsWarps;  // this warp's pieces
 
     auto fetch = [&](int piece, int stage) {
         if (piece < pieces) {
@@ -157,14 +159,19 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
             const T* ks = static_cast<const T*>(p.kc.base) + page * p.kc.page_stride + h * p.kc.head_stride;
             const T* vs = static_cast<const T*>(p.vc.base) + page * p.vc.page_stride + h * p.vc.head_stride;
             if (seen >= 0) {
-                const int chunks = p.dim >> 3;
-                for (int i = lane; i < 16 * (DP / 8); i += 32) {
-                    const int r = i / (DP / 8), c = i % (DP / 8);
-                    if (c < chunks) {
+                // a lane keeps its column, its rows follow at a fixed distance
+                constexpr int kLanes = DP / 8 < 32 ? DP / 8 : 32, kRowsAtOnce = 32 / kLanes;
+                const int c = lane % kLanes, r0 = lane / kLanes;
+                const T* kp = ks + (tok0 + r0) * p.kc.token_stride + c * 8;
+                const T* vp = vs + (tok0 + r0) * p.vc.token_stride + c * 8;
+                if (c * 8 < p.dim) {
+#pragma unroll
+                    for (int r = r0; r < 16; r += kRowsAtOnce) {
                         const bool ok = r <= seen;  // what lies past the token is never read: it may hold anything
-                        const int64_t tok = ok ? tok0 + r : 0;
-                        cp_async16(rows_addr<DP>(kb, r, c), ks + tok * p.kc.token_stride + c * 8, ok);
-                        cp_async16(rows_addr<DP>(vb, r, c), vs + tok * p.vc.token_stride + c * 8, ok);
+                        cp_async16(rows_addr<DP>(kb, r, c), ok ? kp : ks, ok);
+                        cp_async16(rows_addr<DP>(vb, r, c), ok ? vp : vs, ok);
+                        kp += kRowsAtOnce * p.kc.token_stride;
+                        vp += kRowsAtOnce * p.vc.token_stride;
                     }
                 }
             }
@@ -181,12 +188,12 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 
 #pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s) fetch(warp + s * kRowsWarps, s);
+    for (int s = 0; s < S::kStages - 1; ++s) fetch(first + s * stride, s);
     int stage = 0;
-    for (int piece = warp; piece < pieces; piece += kRowsWarps) {
+    for (int piece = first; piece < pieces; piece += stride) {
         cp_async_wait<S::kStages - 2>();
         __syncwarp();
-        fetch(piece + (S::kStages - 1) * kRowsWarps, stage == 0 ? S::kStages - 1 : stage - 1);
+        fetch(piece + (S::kStages - 1) * stride, stage == 0 ? S::kStages - 1 : stage - 1);
         const int e = piece / per;
         const int seen = pos - s_first[e] - (piece % per) * 16;
         const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + S::kPlaneBytes;
@@ -279,28 +286,71 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
         }
     }
     __syncthreads();
+    // the CTA's sum over its warps: into the first warp's rows, or to the end where the CTA is alone
+    const bool alone = ranks == 1;
     for (int i = tid; i < rows * (DP / 8); i += kRowsThreads) {
         const int r = i / (DP / 8), c = i % (DP / 8);
         if (c * 8 >= p.dim) continue;
-        float top = -INFINITY, sum = 0.0f, w[kRowsWarps], acc[8];
+        float top = -INFINITY, sum = 0.0f, acc[8] = {};
 #pragma unroll
         for (int k = 0; k < kRowsWarps; ++k) top = fmaxf(top, s_o[(k * 16 + r) * kRow + DP]);
         const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
-#pragma unroll
         for (int k = 0; k < kRowsWarps; ++k) {
             const float* src = s_o + (k * 16 + r) * kRow;
-            w[k] = exp2_fast(src[DP] - base);
-            sum += w[k] * src[DP + 1];
+            const float w = exp2_fast(src[DP] - base);
+            sum += w * src[DP + 1];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += w[k] * src[c * 8 + j];
+            for (int j = 0; j < 8; ++j) acc[j] += w * src[c * 8 + j];
         }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // nothing seen: zeros
+        if (alone) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // nothing seen: zeros
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] *= inv;
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + (head0 + r) * p.out_stride[1] + c * 8) = pack8<T>(acc);
-        if (c == 0 && p.lse) p.lse[t * n_heads + head0 + r] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+            for (int j = 0; j < 8; ++j) acc[j] *= inv;
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + (head0 + r) * p.out_stride[1] + c * 8) = pack8<T>(acc);
+            if (c == 0 && p.lse) p.lse[t * n_heads + head0 + r] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+        } else {
+            float* dst = s_o + r * kRow + c * 8;
+            *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            *reinterpret_cast<float4*>(dst + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            if (c == 0) *reinterpret_cast<float2*>(s_o + r * kRow + DP + 4) = make_float2(top, sum);  // (apart from the warps' own)
+        }
+    }
+    if (!alone) {
+        // the CTAs share out the rows and read each other's
+        cluster_sync();
+        const int pieces_all = rows * (DP / 8);
+        for (int i = rank * kRowsThreads + tid; i < pieces_all; i += ranks * kRowsThreads) {
+            const int r = i / (DP / 8), c = i % (DP / 8);
+            if (c * 8 >= p.dim) continue;
+            float2 ml[8];
+            float top = -INFINITY, sum = 0.0f, acc[8] = {};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                ml[k] = make_float2(-INFINITY, 0.0f);
+                if (k < ranks) ml[k] = cluster_load2(cluster_addr(s_o + r * kRow + DP + 4, k));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k < ranks) {
+                    const uint32_t src = cluster_addr(s_o + r * kRow + c * 8, k);
+                    const float4 lo = cluster_load4(src), hi = cluster_load4(src + 16);
+                    const float w = exp2_fast(ml[k].x - base);
+                    sum += w * ml[k].y;
+                    acc[0] += w * lo.x, acc[1] += w * lo.y, acc[2] += w * lo.z, acc[3] += w * lo.w;
+                    acc[4] += w * hi.x, acc[5] += w * hi.y, acc[6] += w * hi.z, acc[7] += w * hi.w;
+                }
+            }
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] *= inv;
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + (head0 + r) * p.out_stride[1] + c * 8) = pack8<T>(acc);
+            if (c == 0 && p.lse) p.lse[t * n_heads + head0 + r] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+        }
+        cluster_sync();  // nobody leaves while its rows are read
     }
     __syncthreads();  // the next token's lists and ring lie over this one's
 }
@@ -311,7 +361,8 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
     __shared__ int s_page[kKvMaxSelect], s_first[kKvMaxSelect];
     __shared__ int s_n;
     if (p.done == nullptr) {
-        attend_rows<T, DP>(p, blockIdx.x, rows_smem, s_page, s_first, s_n);
+        const int ranks = static_cast<int>(cluster_size());
+        attend_rows<T, DP>(p, blockIdx.x / ranks, static_cast<int>(cluster_rank()), ranks, rows_smem, s_page, s_first, s_n);
         return;
     }
     // what the tile kernel left: 32 tokens are looked at at a time
@@ -319,7 +370,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
         const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
         unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && p.done[mine / p.window * p.n_kv_heads + blockIdx.y] == 0);
         for (; left; left &= left - 1)
-            attend_rows<T, DP>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, rows_smem, s_page, s_first, s_n);
+            attend_rows<T, DP>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
     }
 }
 

@@ -201,28 +201,6 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
 // ---------------------------------------------------------------------------------------------- rows
 constexpr int kSelList = 1024;  // of a row's short list
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {  // the same place in another CTA of the cluster
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t v) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // L lanes to a block's codes, 16 bytes each (L >= dim / 16, a power of two); kDeep blocks of a lane group in flight.
 template <typename T, int L>
 __global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelectParams p) {
