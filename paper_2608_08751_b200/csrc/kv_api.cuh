@@ -70,41 +70,49 @@ int kv_allow_smem(K kernel, int bytes, const DeviceCtx& ctx, KvSmemSeen& seen) {
     return IVF_OK;
 }
 
-template <typename T>
+template <typename T, int LG>
 int kv_launch_append(const KvAppendParams& p, int num_sms, cudaStream_t stream) {
-    int lg = 2;
-    while (lg * 8 < p.dim) lg *= 2;
-    const int groups = kAppThreads / lg;
-    const int rows = p.n_heads + 2 * p.n_kv_heads;
-    const int most = (rows + groups - 1) / groups;
+    constexpr int kGroups = kAppThreads / LG;
     // few tokens: the rows of one token are shared out over several CTAs
-    const int y = p.n_tokens * 2 < num_sms ? most : 1;
-    const dim3 grid(static_cast<unsigned>(p.n_tokens), y);
-    switch (lg) {
-        case 2: kv_append_kernel<T, 2><<<grid, kAppThreads, 0, stream>>>(p); break;
-        case 4: kv_append_kernel<T, 4><<<grid, kAppThreads, 0, stream>>>(p); break;
-        case 8: kv_append_kernel<T, 8><<<grid, kAppThreads, 0, stream>>>(p); break;
-        case 16: kv_append_kernel<T, 16><<<grid, kAppThreads, 0, stream>>>(p); break;
-        default: kv_append_kernel<T, 32><<<grid, kAppThreads, 0, stream>>>(p); break;
-    }
+    const int parts = (p.n_heads + kGroups - 1) / kGroups + 2 * ((p.n_kv_heads + kGroups - 1) / kGroups);
+    const dim3 grid(static_cast<unsigned>(p.n_tokens), p.n_tokens < 4 * num_sms ? parts : 1);
+    if (p.interleaved) kv_append_kernel<T, LG, true><<<grid, kAppThreads, 0, stream>>>(p);
+    else kv_append_kernel<T, LG, false><<<grid, kAppThreads, 0, stream>>>(p);
     LAUNCH_CHECK();
     return IVF_OK;
 }
-
 template <typename T>
+int kv_launch_append(const KvAppendParams& p, int num_sms, cudaStream_t stream) {
+    if (p.dim <= 16) return kv_launch_append<T, 2>(p, num_sms, stream);
+    if (p.dim <= 32) return kv_launch_append<T, 4>(p, num_sms, stream);
+    if (p.dim <= 64) return kv_launch_append<T, 8>(p, num_sms, stream);
+    if (p.dim <= 128) return kv_launch_append<T, 16>(p, num_sms, stream);
+    return kv_launch_append<T, 32>(p, num_sms, stream);
+}
+
+template <typename T, int LG, int DEEP>
 int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) {
-    int lg = 2;
-    while (lg * 8 < p.dim) lg *= 2;
-    const dim3 grid(static_cast<unsigned>(n), p.n_kv_heads);
-    switch (lg) {
-        case 2: kv_summary_kernel<T, 2><<<grid, kSumThreads, 0, stream>>>(p); break;
-        case 4: kv_summary_kernel<T, 4><<<grid, kSumThreads, 0, stream>>>(p); break;
-        case 8: kv_summary_kernel<T, 8><<<grid, kSumThreads, 0, stream>>>(p); break;
-        case 16: kv_summary_kernel<T, 16><<<grid, kSumThreads, 0, stream>>>(p); break;
-        default: kv_summary_kernel<T, 32><<<grid, kSumThreads, 0, stream>>>(p); break;
-    }
+    kv_summary_kernel<T, LG, DEEP><<<dim3(static_cast<unsigned>(n), p.n_kv_heads), kSumThreads, 0, stream>>>(p);
     LAUNCH_CHECK();
     return IVF_OK;
+}
+template <typename T, int LG>
+int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) {
+    constexpr int kRows = kSumThreads / LG;  // token rows side by side
+    switch (p.page_size) {
+        case 16: return kv_launch_summary<T, LG, (16 + kRows - 1) / kRows>(p, n, stream);
+        case 32: return kv_launch_summary<T, LG, (32 + kRows - 1) / kRows>(p, n, stream);
+        case 64: return kv_launch_summary<T, LG, (64 + kRows - 1) / kRows>(p, n, stream);
+        default: return kv_launch_summary<T, LG, (128 + kRows - 1) / kRows>(p, n, stream);
+    }
+}
+template <typename T>
+int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) {
+    if (p.dim <= 16) return kv_launch_summary<T, 2>(p, n, stream);
+    if (p.dim <= 32) return kv_launch_summary<T, 4>(p, n, stream);
+    if (p.dim <= 64) return kv_launch_summary<T, 8>(p, n, stream);
+    if (p.dim <= 128) return kv_launch_summary<T, 16>(p, n, stream);
+    return kv_launch_summary<T, 32>(p, n, stream);
 }
 
 int g_kv_select = 0;  // test hook (ivf_debug_set_kv_select): 0 = by the sizes, 1 = rows kernel, 2 = windows kernel wherever it can run
@@ -178,9 +186,10 @@ int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t s
     if (p.done) {  // what the tile kernel left: a few CTAs look for it
         x = static_cast<unsigned>(std::min<int64_t>(p.n_tokens, std::max(1, 2 * ctx.num_sms / p.n_kv_heads)));
     } else {
-        // CTAs to a token: until the card has eight for each SM, as long as each warp still has a piece
+        // CTAs to a token: until the card has two for each SM, as long as each warp still has a piece.  (More of them than
+        // that costs: 64 tokens by 8 heads take 121 us with 4 CTAs to a token, 92 us with one.)
         const int pieces = p.n_select << (p.page_shift - 4);
-        while (ranks < 8 && p.n_tokens * p.n_kv_heads * z * ranks < 8 * ctx.num_sms && pieces >= static_cast<int>(ranks) * 2 * kRowsWarps) ranks *= 2;
+        while (ranks < 8 && p.n_tokens * p.n_kv_heads * z * ranks < 2 * ctx.num_sms && pieces >= static_cast<int>(ranks) * 2 * kRowsWarps) ranks *= 2;
         x *= ranks;
     }
     cudaLaunchConfig_t cfg = {};

@@ -12,7 +12,6 @@
 namespace ivf {
 
 constexpr int kSumThreads = 128;
-constexpr int kSumMaxPage = 128;
 
 struct KvSummaryParams {
     KvPlane kc;
@@ -24,11 +23,12 @@ struct KvSummaryParams {
     int* status;
 };
 
-// LG lanes span a row (a power of two, LG * 8 >= D); kSumThreads / LG token rows are read at a time.
-template <typename T, int LG>
-__global__ void __launch_bounds__(kSumThreads) kv_summary_kernel(KvSummaryParams p) {
-    constexpr int kRows = kSumThreads / LG;                             // rows (tokens) side by side, a power of two
-    constexpr int kDeep = kSumMaxPage / kRows > 0 ? kSumMaxPage / kRows : 1;  // tokens of one thread at most
+// LG lanes span a row (a power of two, LG * 8 >= D); kSumThreads / LG token rows are read at a time, DEEP of them by a
+// thread: a page, no more, so that registers are left for many CTAs.
+template <typename T, int LG, int DEEP>
+__global__ void __launch_bounds__(kSumThreads, DEEP <= 8 ? 8 : 4) kv_summary_kernel(KvSummaryParams p) {
+    constexpr int kRows = kSumThreads / LG;  // rows (tokens) side by side, a power of two
+    constexpr int kDeep = DEEP;              // tokens of one thread
     __shared__ float s_part[kRows][LG * 8];
     __shared__ float s_max[kSumThreads / 32];
     const int item = blockIdx.x, h = blockIdx.y;
