@@ -117,18 +117,18 @@ int kv_launch_summary(const KvSummaryParams& p, int64_t n, cudaStream_t stream) 
 
 int g_kv_select = 0;  // test hook (ivf_debug_set_kv_select): 0 = by the sizes, 1 = rows kernel, 2 = windows kernel wherever it can run
 
-template <typename T, int L>
+template <typename T, int L, int NP>
 int kv_launch_select_rows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
-    auto kernel = kv_select_rows_kernel<T, L>;
+    auto kernel = kv_select_rows_kernel<T, L, NP>;
     const int smem = p.max_blocks * 4;
     static KvSmemSeen seen;
     if (int rc = kv_allow_smem(kernel, smem, ctx, seen)) return rc;
-    // CTAs to a row: until the card has four for each SM, as long as each still has 64 blocks
-    unsigned ranks = 1;
-    while (ranks < 8 && p.n_tokens * p.n_kv_heads * ranks < 4 * ctx.num_sms && p.max_blocks >= static_cast<int>(ranks) * 128) ranks *= 2;
+    // CTAs to a row: as many as live on the card at a time, as long as each still has 64 blocks
+    const int64_t rows = p.n_tokens * p.n_kv_heads;
+    const unsigned ranks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>({8, kSelRowCtas * ctx.num_sms / rows, p.max_blocks / 64})));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.n_tokens) * ranks, p.n_kv_heads);
-    cfg.blockDim = kSelThreads;
+    cfg.blockDim = kSelRowThreads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -168,11 +168,9 @@ int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t
             default: return kv_launch_select_windows<T, 8>(p, ctx, stream);
         }
     }
-    if (p.dim <= 16) return kv_launch_select_rows<T, 1>(p, ctx, stream);
-    if (p.dim <= 32) return kv_launch_select_rows<T, 2>(p, ctx, stream);
-    if (p.dim <= 64) return kv_launch_select_rows<T, 4>(p, ctx, stream);
-    if (p.dim <= 128) return kv_launch_select_rows<T, 8>(p, ctx, stream);
-    return kv_launch_select_rows<T, 16>(p, ctx, stream);
+    if (p.dim <= 64) return kv_launch_select_rows<T, 4, 1>(p, ctx, stream);
+    if (p.dim <= 128) return kv_launch_select_rows<T, 4, 2>(p, ctx, stream);
+    return kv_launch_select_rows<T, 8, 2>(p, ctx, stream);
 }
 
 int g_kv_attend = 0;  // test hook (ivf_debug_set_kv_attend): 0 = by the sizes, 1 = rows kernel only, 2 = tile kernel wherever it can run

@@ -92,7 +92,7 @@ __device__ __forceinline__ uint2 sel_code_warp(const KvSelectParams& p, int64_t 
     return make_uint2(w[0], w[1]);
 }
 template <typename T>
-__device__ __forceinline__ uint2 sel_code(const KvSelectParams& p, int64_t t, int h) {
+__device__ __noinline__ uint2 sel_code(const KvSelectParams& p, int64_t t, int h) {
     if (p.group <= 1) return sel_code_warp<T, 1>(p, t, h);
     if (p.group <= 2) return sel_code_warp<T, 2>(p, t, h);
     if (p.group <= 4) return sel_code_warp<T, 4>(p, t, h);
@@ -128,7 +128,7 @@ __device__ __forceinline__ void sel_two_largest(const uint32_t* key, int b0, int
 // of 0 do not count, those always taken come first; equal keys go to the earlier.  id: the keys' blocks, null: 0, 1, 2 ...
 __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, int m, int n_select, int32_t* out) {
     const int lane = threadIdx.x & 31;
-    constexpr int kHeld = 4;
+    constexpr int kHeld = 8;
     uint32_t held[kHeld];  // short lists stay in registers
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < m ? key[i * 32 + lane] : 0u;
@@ -199,15 +199,18 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
 }
 
 // ---------------------------------------------------------------------------------------------- rows
+constexpr int kSelRowThreads = 128, kSelRowWarps = kSelRowThreads / 32;
+constexpr int kSelRowCtas = 6;  // on an SM
 constexpr int kSelList = 1024;  // of a row's short list
 
-// L lanes to a block's codes, 16 bytes each (L >= dim / 16, a power of two); kDeep blocks of a lane group in flight.
-template <typename T, int L>
-__global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelectParams p) {
+// L lanes to a block's codes, NP pieces of 16 bytes each (16 L NP >= dim); four blocks of a lane group are in flight, their
+// pages are fetched a step ahead.  Few lanes to a block: what is not a load is paid once for a block and lane.
+template <typename T, int L, int NP>
+__global__ void __launch_bounds__(kSelRowThreads, kSelRowCtas) kv_select_rows_kernel(KvSelectParams p) {
     extern __shared__ uint32_t sel_keys[];  // of the first CTA of the cluster: one key per visible block
     __shared__ __align__(16) int8_t s_code[kKvMaxDim];
-    __shared__ uint32_t s_bound[kSelWarps];
-    __shared__ int s_count[kSelWarps];
+    __shared__ uint32_t s_bound[kSelRowWarps];
+    __shared__ int s_count[kSelRowWarps];
     __shared__ uint32_t s_key[kSelList];
     __shared__ int s_id[kSelList];
     constexpr int kDeep = 4;
@@ -215,13 +218,17 @@ __global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelect
     const int64_t t = blockIdx.x / ranks;
     const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t* out = p.out + (t * p.n_kv_heads + h) * p.n_select;
+    if (warp == 0) {  // first of all: behind the codes its loads would wait for them
+        const uint2 w = sel_code<T>(p, t, h);
+        if (lane * 8 < p.dim) *reinterpret_cast<uint2*>(s_code + lane * 8) = w;
+    }
     const int req = p.token_req[t], pos = p.token_pos[t];
     const bool padded = req < 0 || pos < 0;
     const bool bad = req >= p.n_req || (!padded && (pos >> p.page_shift) >= p.max_blocks);
     if (padded || bad) {  // the whole cluster
         if (rank == 0) {
             if (bad && tid == 0) kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
-            for (int i = tid; i < p.n_select; i += kSelThreads) out[i] = -1;
+            for (int i = tid; i < p.n_select; i += kSelRowThreads) out[i] = -1;
         }
         return;
     }
@@ -229,95 +236,90 @@ __global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelect
     const int32_t* row = p.table + req * p.table_stride;
     const uint32_t keys0 = cluster_addr(sel_keys, 0);
 
-    // group of L lanes g of this cluster takes blocks g, g + groups, ...; kDeep of them at a time
-    constexpr int kGroups = kSelThreads / L;
+    // lane group g of the cluster takes blocks g, g + step, ...; kDeep of them at a time
+    constexpr int kGroups = kSelRowThreads / L;
     const int sub = tid % L;
     const int step = kGroups * static_cast<int>(ranks);
-    const bool live = sub * 16 < p.dim;
-    // two steps are under way: the codes of the next, and the pages of the one after it
-    struct Step {
-        int4 code[kDeep];
-        float scale[kDeep];
-        int page[kDeep];
-    };
-    auto pages_of = [&](int b0, int (&page)[kDeep]) {
+    static_assert(kDeep == 4 && L >= kDeep, "a lane of the group finishes a block");
+    int4 code[kDeep][NP];
+    int page[kDeep], ahead[kDeep];
+    auto pages_of = [&](int b0, int (&to)[kDeep]) {
 #pragma unroll
-        for (int i = 0; i < kDeep; ++i) page[i] = b0 + i * step < n ? row[b0 + i * step] : -1;
+        for (int i = 0; i < kDeep; ++i) to[i] = b0 + i * step < n ? row[b0 + i * step] : -1;
     };
-    auto codes_of = [&](Step& s) {
+    const int8_t* codes = p.codes + static_cast<int64_t>(h) * p.dim + sub * 16;
+    const int64_t page_bytes = static_cast<int64_t>(p.n_kv_heads) * p.dim;
+    auto codes_of = [&]() {
 #pragma unroll
         for (int i = 0; i < kDeep; ++i) {
-            const bool ok = s.page[i] >= 0 && s.page[i] < p.num_pages;
-            const int64_t at = ok ? static_cast<int64_t>(s.page[i]) * p.n_kv_heads + h : 0;
-            s.code[i] = make_int4(0, 0, 0, 0);
-            s.scale[i] = 0.0f;
-            if (ok && live) s.code[i] = *reinterpret_cast<const int4*>(p.codes + at * p.dim + sub * 16);
-            if (ok) s.scale[i] = p.scales[at];
-        }
-    };
-    const int first = static_cast<int>(rank) * kGroups + tid / L;
-    Step now, next;
-    pages_of(first, now.page);
-    pages_of(first + kDeep * step, next.page);
-    codes_of(now);  // on its way while the query is coded
-    if (warp == 0) {
-        const uint2 w = sel_code<T>(p, t, h);
-        if (lane * 8 < p.dim) *reinterpret_cast<uint2*>(s_code + lane * 8) = w;
-    }
-    if (ranks > 1) cluster_sync();  // (the first CTA runs, so its shared memory may be written)
-    else __syncthreads();
-    int4 u = make_int4(0, 0, 0, 0);
-    if (live) u = *reinterpret_cast<const int4*>(s_code + sub * 16);
-    auto finish = [&](const Step& s, int b0) {
-        int dot[kDeep];
+            const bool ok = page[i] >= 0 && page[i] < p.num_pages;
+            const int8_t* src = codes + (ok ? page[i] * page_bytes : 0);
 #pragma unroll
-        for (int i = 0; i < kDeep; ++i)
-            dot[i] = __dp4a(s.code[i].w, u.w, __dp4a(s.code[i].z, u.z, __dp4a(s.code[i].y, u.y, __dp4a(s.code[i].x, u.x, 0))));
-#pragma unroll
-        for (int off = L / 2; off > 0; off >>= 1) {
-#pragma unroll
-            for (int i = 0; i < kDeep; ++i) dot[i] += __shfl_xor_sync(0xFFFFFFFFu, dot[i], off);
-        }
-#pragma unroll
-        for (int i = 0; i < kDeep; ++i) {
-            const int b = b0 + i * step;
-            if (b < n && sub == i % L) {
-                uint32_t key = 0;
-                if (s.page[i] >= 0 && s.page[i] < p.num_pages)
-                    key = b < p.n_first || b >= n - p.n_last ? kSelAlways : sel_key(dot[i], s.scale[i]);
-                else if (s.page[i] >= p.num_pages)
-                    kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
-                cluster_store(keys0 + b * 4, key);
+            for (int k = 0; k < NP; ++k) {
+                code[i][k] = make_int4(0, 0, 0, 0);
+                if (ok && (sub + k * L) * 16 < p.dim) code[i][k] = *reinterpret_cast<const int4*>(src + k * L * 16);
             }
         }
     };
-    for (int b0 = first; b0 - tid / L < n; b0 += 2 * kDeep * step) {
-        codes_of(next);
-        Step later;
-        pages_of(b0 + 2 * kDeep * step, later.page);
-        finish(now, b0);
-        now = later;
-        codes_of(now);
-        pages_of(b0 + 3 * kDeep * step, later.page);
-        finish(next, b0 + kDeep * step);
-        next = later;
+    const int first = static_cast<int>(rank) * kGroups + tid / L;
+    pages_of(first, page);
+    pages_of(first + kDeep * step, ahead);
+    codes_of();
+    if (ranks > 1) cluster_sync();  // (the first CTA runs, so its shared memory may be written)
+    else __syncthreads();
+    int4 u[NP];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        u[k] = make_int4(0, 0, 0, 0);
+        if ((sub + k * L) * 16 < p.dim) u[k] = *reinterpret_cast<const int4*>(s_code + (sub + k * L) * 16);
+    }
+    for (int b0 = first; b0 - tid / L < n; b0 += kDeep * step) {
+        // lane `sub` of the group finishes block `sub` of the four
+        const int mine = sub == 0 ? page[0] : sub == 1 ? page[1] : sub == 2 ? page[2] : page[3];
+        const bool there = sub < kDeep && mine >= 0 && mine < p.num_pages;
+        const float scale = there ? p.scales[static_cast<int64_t>(mine) * p.n_kv_heads + h] : 0.0f;
+        int dot[kDeep];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            dot[i] = 0;
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+                dot[i] = __dp4a(code[i][k].w, u[k].w, __dp4a(code[i][k].z, u[k].z, __dp4a(code[i][k].y, u[k].y, __dp4a(code[i][k].x, u[k].x, dot[i]))));
+        }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) page[i] = ahead[i];
+        codes_of();
+        pages_of(b0 + 2 * kDeep * step, ahead);
+        // sums over the group, each lane keeping its own block's: lanes apart by 1 exchange odd and even blocks, by 2 the pairs
+        const int e0 = sub & 1 ? dot[0] : dot[1], e1 = sub & 1 ? dot[2] : dot[3];
+        int k0 = (sub & 1 ? dot[1] : dot[0]) + __shfl_xor_sync(0xFFFFFFFFu, e0, 1), k1 = (sub & 1 ? dot[3] : dot[2]) + __shfl_xor_sync(0xFFFFFFFFu, e1, 1);
+        int sum = (sub & 2 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, sub & 2 ? k0 : k1, 2);
+#pragma unroll
+        for (int off = 4; off < L; off <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+        const int b = b0 + sub * step;
+        if (sub < kDeep && b < n) {
+            uint32_t key = 0;
+            if (there) key = b < p.n_first || b >= n - p.n_last ? kSelAlways : sel_key(sum, scale);
+            else if (mine >= p.num_pages) kv_report(p.status, kKvStatusBadId, KV_SITE_SELECT);
+            cluster_store(keys0 + b * 4, key);
+        }
     }
     if (ranks > 1) cluster_sync();
     else __syncthreads();
     if (rank != 0) return;
 
-    // ---- the short list: every warp takes a part of the row.  At least ceil(n_select / 8) scored keys of each part reach
+    // ---- the short list: every warp takes a part of the row.  At least ceil(n_select / 4) scored keys of each part reach
     // the smallest of the parts' bounds, so at least n_select of the row do
-    const int per = (n + kSelThreads - 1) / kSelThreads * 32;
+    const int per = (n + kSelRowThreads - 1) / kSelRowThreads * 32;
     const int w0 = min(warp * per, n), w1 = min(w0 + per, n);
     uint32_t a, b;
     sel_two_largest(sel_keys, w0, w1, a, b);
-    const uint32_t bound_w = sel_kth_of_64(a, b, (p.n_select + kSelWarps - 1) / kSelWarps);
+    const uint32_t bound_w = sel_kth_of_64(a, b, (p.n_select + kSelRowWarps - 1) / kSelRowWarps);
     if (lane == 0) s_bound[warp] = bound_w;
     __syncthreads();
     uint32_t bound = s_bound[0];
 #pragma unroll
-    for (int w = 1; w < kSelWarps; ++w) bound = min(bound, s_bound[w]);
+    for (int w = 1; w < kSelRowWarps; ++w) bound = min(bound, s_bound[w]);
     bound = max(bound, 1u);
     int count = 0;
     for (int i = w0 + lane; i < w1; i += 32) count += sel_keys[i] >= bound;
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(kSelThreads, 3) kv_select_rows_kernel(KvSelect
     __syncthreads();
     int before = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) {
+    for (int w = 0; w < kSelRowWarps; ++w) {
         if (w < warp) before += s_count[w];
         total += s_count[w];
     }
