@@ -366,7 +366,7 @@ inline size_t sel_window_smem(int blocks) {
 // K: steps of 32 elements (32 * K >= dim).  A dot product may take its elements in any order: lane q of a block's four lanes
 // takes elements 8 K q .. 8 K (q + 1), so that its loads are contiguous, and the query's fragments do the same.
 template <typename T, int K>
-__global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelectParams p, int padded) {
+__global__ void __launch_bounds__(kSelThreads, 4) kv_select_windows_kernel(KvSelectParams p, int padded) {
     extern __shared__ uint32_t sel_smem[];
     uint32_t* keys = sel_smem;                                        // [16][padded]
     int* s_page = reinterpret_cast<int*>(keys + kSelWindow * padded);  // [padded]
@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
         int r1 = r0, last = -1;
         while (r1 < tokens && s_req[r1] == req) last = max(last, s_pos[r1++]);
         const int n = req < 0 ? 0 : (last >> p.page_shift) + 1;
+        bool gaps = false;  // blocks without a page
         for (int b = tid; b < n; b += kSelThreads) {
             int page = p.table[req * p.table_stride + b];
             float scale = 0.0f;
@@ -425,10 +426,12 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
                 page = -1;
             }
             if (page >= 0) scale = p.scales[static_cast<int64_t>(page) * p.n_kv_heads + h];
+            gaps |= page < 0;
             s_page[b] = page;
             s_scale[b] = scale;
         }
-        __syncthreads();
+        gaps = __syncthreads_or(gaps);
+        const bool keep[2] = {nb >= r0 && nb < r1, nb + 8 >= r0 && nb + 8 < r1};
         // two tiles of 8 blocks to a warp at a time; their codes are fetched a step ahead
         uint32_t code[2][2 * K];
         auto fetch = [&](int b0) {
@@ -467,13 +470,14 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int r = nb + (x >> 1) * 8, b = b0 + i * 8 + 2 * q + (x & 1);
-                    if (r >= r0 && r < r1 && b < n) {
-                        const int seen = (s_pos[r] >> p.page_shift) + 1;
-                        uint32_t key = 0;
-                        if (b < seen && s_page[b] >= 0) key = b < p.n_first || b >= seen - p.n_last ? kSelAlways : sel_key(c[i][x], s_scale[b]);
-                        keys[r * padded + b] = key;
+                for (int y = 0; y < 2; ++y) {
+                    const int b = b0 + i * 8 + 2 * q + y;
+                    if (b < n) {
+                        const float scale = s_scale[b];
+                        uint32_t lo = sel_key(c[i][y], scale), hi = sel_key(c[i][y + 2], scale);
+                        if (gaps && s_page[b] < 0) lo = hi = 0;
+                        if (keep[0]) keys[nb * padded + b] = lo;
+                        if (keep[1]) keys[(nb + 8) * padded + b] = hi;
                     }
                 }
             }
@@ -482,8 +486,13 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_windows_kernel(KvSelect
         // a warp selects a row
         for (int r = r0 + warp; r < r1; r += kSelWarps) {
             int32_t* out = p.out + ((t0 + r) * p.n_kv_heads + h) * p.n_select;
-            const uint32_t* key = keys + r * padded;
+            uint32_t* key = keys + r * padded;
             const int m = req < 0 ? 0 : (s_pos[r] >> p.page_shift) + 1;
+            for (int i = lane; i < p.n_first + p.n_last; i += 32) {  // those always taken, as far as they are there
+                const int b = i < p.n_first ? i : m - 1 - (i - p.n_first);
+                if (b >= 0 && b < m && key[b] != 0) key[b] = kSelAlways;
+            }
+            __syncwarp();
             uint32_t x, y;
             sel_two_largest(key, 0, m, x, y);
             const uint32_t bound = max(sel_kth_of_64(x, y, p.n_select), 1u);
