@@ -155,7 +155,11 @@ int kv_launch_select_windows(const KvSelectParams& p, const DeviceCtx& ctx, cuda
 template <typename T>
 int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     bool windows = g_kv_select != 1 && p.max_blocks <= kSelWindowBlocks;
-    if (g_kv_select == 0) windows = windows && p.n_tokens >= 8 * static_cast<int64_t>(p.n_req);
+    // Single tokens read a row's codes once for each token, windows once for 16; a window starts slower, and takes the requests
+    // in it one after the other.  256 blocks of d = 128, rows / windows: 16 tokens by 8 heads 13 / 19 us, 256 by 4
+    // heads 23 / 19, 256 by 8 heads 33 / 19, 512 by 8 heads of 32 requests 54 / 21, but 64 by 8 heads of 32 requests 15 / 47.
+    if (g_kv_select == 0)
+        windows = windows && p.n_tokens * p.n_kv_heads >= 6 * ctx.num_sms && p.n_tokens >= 2 * static_cast<int64_t>(p.n_req);
     if (windows) {
         switch ((p.dim + 31) / 32) {
             case 1: return kv_launch_select_windows<T, 1>(p, ctx, stream);
@@ -248,7 +252,12 @@ int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     CUtensorMap mk, mv;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
     bool tile = g_kv_attend != 1 && p.dim >= 64 && p.max_blocks < kTileMaxBlocks && p.num_pages > 0;
-    if (g_kv_attend == 0) tile = tile && p.n_tokens >= 2 * p.n_req && p.n_tokens * p.group >= 128;
+    // Windows pay where there is work for the whole card and tokens enough beyond one to a request to fill some; what they do
+    // not take is left to the rows.  16 blocks of 64 keys, d = 128, rows / windows: 64 tokens by 4 heads of a group of 8
+    // 31 / 43 us, 256 tokens 86 / 43, 512 tokens of 32 requests 152 / 43; by 8 heads without groups (128 tokens to a
+    // window) 128 tokens of 8 requests 85 / 307, 256 tokens of one 146 / 107.
+    const int64_t parts = (p.group + 15) / 16;
+    if (g_kv_attend == 0) tile = tile && p.n_tokens * p.n_kv_heads * parts >= 4 * ctx.num_sms && p.n_tokens - p.n_req + 1 >= 2 * p.window;
     if (tile) {
         if (int rc = get_encode()) return rc;
         tile = kv_make_map(&mk, p.kc, p, bf16) && kv_make_map(&mv, p.vc, p, bf16);

@@ -133,6 +133,7 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) held[i] = i * 32 + lane < m ? key[i * 32 + lane] : 0u;
     const bool in_regs = m <= kHeld * 32;
+    const int used = (m + 31) / 32;  // a list is mostly much shorter than what there is room for
     int always = 0, valid = 0;
     uint32_t all_or = 0, all_and = 0xFFFFFFFFu;
     auto look = [&](uint32_t k) {
@@ -144,7 +145,10 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
         }
     };
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) look(held[i]);
+    for (int i = 0; i < kHeld; ++i) {
+        if (i >= used) break;
+        look(held[i]);
+    }
     for (int b = kHeld * 32 + lane; b < m; b += 32) look(key[b]);
     always = __reduce_add_sync(0xFFFFFFFFu, always);
     valid = __reduce_add_sync(0xFFFFFFFFu, valid);
@@ -166,7 +170,10 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
                 int cnt = 0;
                 if (in_regs) {
 #pragma unroll
-                    for (int i = 0; i < kHeld; ++i) cnt += held[i] >= cand;
+                    for (int i = 0; i < kHeld; ++i) {
+                        if (i >= used) break;
+                        cnt += held[i] >= cand;
+                    }
                 } else {
                     for (int b = lane; b < m; b += 32) cnt += key[b] >= cand;
                 }

@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import argparse
 import json
+import math
 
 import numpy as np
 import torch
@@ -297,9 +298,64 @@ def candidates_case(args):
                       "ms_per_call": ms, "vectors_per_s": args.n / (ms / 1e3), "algorithmic_GBps": nbytes / (ms / 1e3) / 1e9}))
 
 
+def kv_case(args):
+    """The block-cache operators as a server runs them, for one attention layer: prompts in chunks, then single
+    tokens, every step the five calls; random queries, keys and values stand in for the model.  Prints the time of a
+    step and what the layer's attention reads against a cache that is read whole."""
+    dev, kind, page, heads, kv_heads, d, take = "cuda", torch.bfloat16, 64, 32, 8, 128, 32
+    n, total = args.requests, args.context + args.decode_steps
+    columns = -(-total // page)
+    pages = n * columns
+    g = torch.Generator(device=dev)
+    g.manual_seed(0)
+    k_cache, v_cache = (torch.empty(pages, kv_heads, page, d, dtype=kind, device=dev) for _ in range(2))
+    codes = torch.empty(pages, kv_heads, d, dtype=torch.int8, device=dev)
+    scales = torch.empty(pages, kv_heads, device=dev)
+    free = torch.randperm(pages, device=dev, generator=g).to(torch.int32)
+    table = torch.full((n, columns), -1, dtype=torch.int32, device=dev)
+    cached = torch.zeros(n, dtype=torch.int32, device=dev)
+    angle = torch.arange(total, device=dev)[:, None] * torch.exp(torch.arange(0, d, 2, device=dev) * (-math.log(10000.0) / d))[None]
+    rotary = torch.cat([angle.cos(), angle.sin()], 1).float().contiguous()
+    weight = torch.ones(d, device=dev)
+    taken = 0
+
+    def step(fresh, tokens):
+        nonlocal taken
+        qkv = torch.randn(tokens, (heads + 2 * kv_heads) * d, device=dev, generator=g).to(kind)
+        q, k, v = (x.view(tokens, -1, d) for x in qkv.split([heads * d, kv_heads * d, kv_heads * d], 1))
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        plan = B.ivf_kv_tables(cached, fresh, free[taken:], table, page, tokens)
+        q = B.ivf_kv_append(q, k, v, k_cache, v_cache, plan.token_pos, plan.token_slot, rotary=rotary, q_weight=weight, k_weight=weight)
+        B.ivf_kv_summarize(k_cache, plan.touched_page, plan.touched_fill, codes, scales)
+        chosen = B.ivf_kv_select(q, codes, scales, table, plan.token_req, plan.token_pos, page, take, n_first=1, n_last=2)
+        out, _ = B.ivf_kv_attend(q, k_cache, v_cache, table, plan.token_req, plan.token_pos, chosen, d ** -0.5)
+        e1.record()
+        cached.copy_(plan.kv_lens)
+        taken += int(plan.used)
+        B.ivf_check()
+        return e0.elapsed_time(e1), out
+
+    prompt_ms = []
+    for at in range(0, args.context, args.chunk):
+        size = min(args.chunk, args.context - at)
+        for r in range(n):
+            fresh = torch.zeros(n, dtype=torch.int32, device=dev)
+            fresh[r] = size
+            prompt_ms.append(step(fresh, size)[0])
+    one = torch.ones(n, dtype=torch.int32, device=dev)
+    decode_ms = [step(one, n) for _ in range(args.decode_steps)]
+    assert all(torch.isfinite(out.float()).all() for _, out in decode_ms)
+    decode_ms = sorted(ms for ms, _ in decode_ms)
+    seen = min(take * page, args.context)
+    print(json.dumps({"op": "kv", "requests": n, "context": args.context, "heads": heads, "kv_heads": kv_heads, "d": d, "page": page, "take": take,
+                      "prompt_chunk_us": 1e3 * sorted(prompt_ms)[len(prompt_ms) // 2], "decode_step_us": 1e3 * decode_ms[len(decode_ms) // 2],
+                      "keys_read_share": seen / args.context}))
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--op", default="assign", choices=["assign", "route", "update", "stream", "serve", "pq", "candidates", "build"])
+    ap.add_argument("--op", default="assign", choices=["assign", "route", "update", "stream", "serve", "pq", "candidates", "build", "kv"])
     ap.add_argument("--train-rows", type=int, default=1 << 20, dest="train_rows", help="sample size of --op build")
     ap.add_argument("--pq-m", type=int, default=32, dest="pq_m")
     ap.add_argument("--n-rerank", type=int, default=512, dest="n_rerank")
@@ -312,6 +368,10 @@ def main():
     ap.add_argument("--d", type=int, default=128)
     ap.add_argument("--k", type=int, default=64)
     ap.add_argument("--dtype", default="u8", choices=["u8", "f32", "i8"])
+    ap.add_argument("--requests", type=int, default=8, help="--op kv: requests served")
+    ap.add_argument("--context", type=int, default=32768, help="--op kv: prompt tokens of a request, fed in chunks")
+    ap.add_argument("--chunk", type=int, default=2048, help="--op kv: tokens of a prompt chunk")
+    ap.add_argument("--decode-steps", type=int, default=32, dest="decode_steps", help="--op kv: single-token steps after the prompts")
     ap.add_argument("--reps", type=int, default=3)
     ap.add_argument("--dependent-launch", type=int, default=-1, help="kernel-family mask of dependent launches (0 = none)")
     ap.add_argument("--crossing-cost", type=int, default=-1, help="span-partition crossing cost in units (0 = equal counts)")
@@ -336,6 +396,8 @@ def main():
         return candidates_case(args)
     if args.op == "build":
         return build_case(args)
+    if args.op == "kv":
+        return kv_case(args)
     if args.dtype == "i8":
         x, c = synth.spacev_like(args.n, args.nlist, seed=0, d=args.d)
     elif args.dtype == "u8":
