@@ -531,7 +531,14 @@ def ivf_kv_tables(cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.T
     [n_req, max_blocks] int32 is extended in place by pages from the front of free_pages; the plan of the
     new tokens comes back (or is written into `plan`, an earlier call's)."""
     got = (_kv or _bind()).kv_tables(cached, fresh, free_pages, table, page_size, max_tokens, max_touched, plan)
-    return KvPlan._make(got) if plan is None else plan
+    if plan is None:
+        plan = KvPlan._make(got)
+    if not table.shape[0]:  # no requests: the library has nothing to do, the padding is still due
+        for t in (plan.token_start, plan.touched_fill, plan.used):
+            t.zero_()
+        for t in (plan.token_req, plan.token_pos, plan.token_slot, plan.touched_page):
+            t.fill_(-1)
+    return plan
 
 
 def ivf_kv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,

@@ -72,7 +72,9 @@ __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uin
 // A cluster of CTAs per (token, kv head, 16 query heads of its group).  The group's heads are the 16 rows of the matrix
 // product, the keys come in pieces of 16 tokens.  Each warp takes pieces of its own through a ring of its own
 // and keeps its own running maximum, sum and output; the warps meet once, at the end, and then the cluster's CTAs,
-// through each other's shared memory.
+// through each other's shared memory.  Bound by the selected pages' bytes: 64 tokens by 8 heads of 32 pages, 537 MB, in
+// 92 us (5.8 TB/s, 0.90 of a copy's rate); one token by 4 heads of 96, 3 MB, in 9.3 us, a chain of waits: request, block,
+// page, keys, and two meetings.
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = kRowsWarps * 32;
 

@@ -12,8 +12,11 @@
 // the whole row took 4,700 instructions of a warp for a row of 512 blocks.)
 //
 //   rows     (single and drafted tokens) a cluster of CTAs shares the blocks of one (token, kv head), 4-byte dot products
-//            straight from the loads; the keys meet in the first CTA's shared memory.  Bound by the codes' bytes.
+//            straight from the loads; the keys meet in the first CTA's shared memory.  32 requests of up to 4,096 blocks by 8
+//            heads: 89 MB of codes in 38 us, of which the scores take 15 (at the memory's rate), what comes before and
+//            after them (the query's code, the short list) the rest; 2,048 blocks of one request 10 us.
 //   windows  (prompts) 16 tokens by one kv head to a CTA, scores by the integer matrix instruction, a warp selects a row.
+//            Bound by the selection's instructions (2,600 of a warp for a row of 512 blocks): 16,384 rows in 60 us.
 #pragma once
 #include "kv_common.cuh"
 

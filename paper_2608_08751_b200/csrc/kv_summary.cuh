@@ -5,7 +5,9 @@
 // additions and the correctly rounded divisions make the codes the same whole numbers on every launch.
 //
 // Bound by memory: fill * D keys are read once, D + 4 bytes written.  One CTA per (page, head): D / 8 lanes
-// span a token row with 16-byte loads, all loads of a thread are independent.
+// span a token row with 16-byte loads, all loads of a thread are independent, and ten CTAs an SM keep enough of them
+// under way (8,192 pages of 64 tokens by 8 heads of 128: 1.08 GB in 195 us, 5.5 TB/s; with room for 128 tokens in
+// every thread's registers 260 us).
 #pragma once
 #include "kv_common.cuh"
 
@@ -26,7 +28,7 @@ struct KvSummaryParams {
 // LG lanes span a row (a power of two, LG * 8 >= D); kSumThreads / LG token rows are read at a time, DEEP of them by a
 // thread: a page, no more, so that registers are left for many CTAs.
 template <typename T, int LG, int DEEP>
-__global__ void __launch_bounds__(kSumThreads, DEEP <= 8 ? 8 : 4) kv_summary_kernel(KvSummaryParams p) {
+__global__ void __launch_bounds__(kSumThreads, DEEP <= 8 ? 10 : 5) kv_summary_kernel(KvSummaryParams p) {
     constexpr int kRows = kSumThreads / LG;  // rows (tokens) side by side, a power of two
     constexpr int kDeep = DEEP;              // tokens of one thread
     __shared__ float s_part[kRows][LG * 8];

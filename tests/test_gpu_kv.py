@@ -120,6 +120,13 @@ def test_tables_shortages_are_cut_and_flagged(what):
     _same_tables(t, plan, R.tables(cached, fresh, 64, free, table, tokens, touched))
 
 
+def test_tables_of_no_request():
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    plan = B.ivf_kv_tables(none, none, none, torch.zeros(0, 4, dtype=torch.int32, device="cuda"), 16, 3)
+    B.ivf_check()
+    assert _np(plan.token_start).tolist() == [0] and int(plan.used) == 0 and (plan.token_slot == -1).all() and (plan.token_req == -1).all()
+
+
 # ---------------------------------------------------------------------------------------------- append
 
 def _cache(pages, heads, page, dim, kind, layout="head", fill=math.nan):
