@@ -372,7 +372,11 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             boxes += found * halves;
             if (halves == 2 && boxes > 0 && base + S::kMapWords * 32 > last_block) {
                 __syncthreads();
-                if (c.box[boxes - 1].first > last_pos) --boxes;  // the last block's second half is empty
+                if (c.box[boxes - 1].first > last_pos) {  // the last block's second half is empty: the next request gets its place
+                    --boxes;
+                    __syncthreads();
+                    if (tid == 0) c.box[boxes].members = c.more[boxes][0] = c.more[boxes][1] = c.more[boxes][2] = 0;
+                }
             }
             __syncthreads();
         }

@@ -435,6 +435,9 @@ PROMPT = [
     ([300], 64, 1, 7, 256, 32, 4, "bf16", "head", True), ([260], 80, 1, 20, 64, 16, 5, "fp16", "head", False),
     ([700] * 9, 17, 1, 8, 128, 64, 5, "bf16", "head", True), ([200], 40, 1, 64, 128, 64, 2, "bf16", "head", False),
     ([150], 150, 1, 2, 16, 16, 4, "fp16", "head", False),
+    # several requests in a window, pages of two boxes whose last half is empty
+    ([704, 190, 333], 61, 2, 7, 64, 128, 4, "fp16", "head", True), ([300, 420, 1000], 50, 1, 1, 128, 128, 3, "bf16", "token", True),
+    ([130, 270], 40, 1, 4, 256, 128, 2, "bf16", "both", False),
 ]
 
 
