@@ -16,7 +16,7 @@
 //            heads: 89 MB of codes in 38 us, of which the scores take 15 (at the memory's rate), what comes before and
 //            after them (the query's code, the short list) the rest; 2,048 blocks of one request 10 us.
 //   windows  (prompts) 16 tokens by one kv head to a CTA, scores by the integer matrix instruction, a warp selects a row.
-//            Bound by the selection's instructions (2,600 of a warp for a row of 512 blocks): 16,384 rows in 60 us.
+//            Bound by the selection's instructions (about 2,500 of a warp for a row of 512 blocks): 16,384 rows in 57 us.
 #pragma once
 #include "kv_common.cuh"
 
@@ -242,6 +242,7 @@ __global__ void __launch_bounds__(kSelRowThreads, kSelRowCtas) kv_select_rows_ke
         }
         return;
     }
+    if (ranks > 1) cluster_arrive();
     const int n = (pos >> p.page_shift) + 1;
     const int32_t* row = p.table + req * p.table_stride;
     const uint32_t keys0 = cluster_addr(sel_keys, 0);
@@ -275,14 +276,14 @@ __global__ void __launch_bounds__(kSelRowThreads, kSelRowCtas) kv_select_rows_ke
     pages_of(first, page);
     pages_of(first + kDeep * step, ahead);
     codes_of();
-    if (ranks > 1) cluster_sync();  // (the first CTA runs, so its shared memory may be written)
-    else __syncthreads();
+    __syncthreads();
     int4 u[NP];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
         u[k] = make_int4(0, 0, 0, 0);
         if ((sub + k * L) * 16 < p.dim) u[k] = *reinterpret_cast<const int4*>(s_code + (sub + k * L) * 16);
     }
+    if (ranks > 1) cluster_wait();  // the first CTA runs, so its shared memory may be written
     for (int b0 = first; b0 - tid / L < n; b0 += kDeep * step) {
         // lane `sub` of the group finishes block `sub` of the four
         const int mine = sub == 0 ? page[0] : sub == 1 ? page[1] : sub == 2 ? page[2] : page[3];
@@ -503,13 +504,9 @@ __global__ void __launch_bounds__(kSelThreads, 4) kv_select_windows_kernel(KvSel
                 if (b >= 0 && b < m && key[b] != 0) key[b] = kSelAlways;
             }
             __syncwarp();
-            uint32_t x, y;
-            sel_two_largest(key, 0, m, x, y);
-            const uint32_t bound = max(sel_kth_of_64(x, y, p.n_select), 1u);
+            uint32_t x = 0, y = 0, bound;
             int total = 0;
-            for (int b0 = 0; b0 < m && total <= kSelWindowList - 32; b0 += 32) {
-                const int b = b0 + lane;
-                const uint32_t k = b < m ? key[b] : 0u;
+            auto enlist = [&](uint32_t k, int b) {
                 const unsigned in = __ballot_sync(0xFFFFFFFFu, k >= bound);
                 if (k >= bound) {
                     const int at = total + __popc(in & ((1u << lane) - 1));
@@ -517,6 +514,25 @@ __global__ void __launch_bounds__(kSelThreads, 4) kv_select_windows_kernel(KvSel
                     s_id[warp][at] = b;
                 }
                 total += __popc(in);
+            };
+            constexpr int kHeld = 16;  // a row of up to 512 keys stays in registers between the bound and the list
+            if (m <= kHeld * 32) {
+                uint32_t held[kHeld];
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i) {
+                    held[i] = i * 32 + lane < m ? key[i * 32 + lane] : 0u;
+                    const uint32_t k = held[i] == kSelAlways ? 0u : held[i];
+                    if (i & 1) y = max(y, k);
+                    else x = max(x, k);
+                }
+                bound = max(sel_kth_of_64(x, y, p.n_select), 1u);
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i)
+                    if (i * 32 < m && total <= kSelWindowList - 32) enlist(held[i], i * 32 + lane);
+            } else {
+                sel_two_largest(key, 0, m, x, y);
+                bound = max(sel_kth_of_64(x, y, p.n_select), 1u);
+                for (int b0 = 0; b0 < m && total <= kSelWindowList - 32; b0 += 32) enlist(b0 + lane < m ? key[b0 + lane] : 0u, b0 + lane);
             }
             __syncwarp();
             if (total <= kSelWindowList - 32) sel_finish(s_key[warp], s_id[warp], total, p.n_select, out);
