@@ -370,7 +370,8 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 }
             });
             boxes += found * halves;
-            if (halves == 2 && boxes > 0 && base + S::kMapWords * 32 > last_block) {
+            // (of this request's own boxes: one that found none must leave the last box of the request before it)
+            if (halves == 2 && found > 0 && base + S::kMapWords * 32 > last_block) {
                 __syncthreads();
                 if (c.box[boxes - 1].first > last_pos) {  // the last block's second half is empty: the next request gets its place
                     --boxes;

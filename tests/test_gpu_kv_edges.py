@@ -1,0 +1,48 @@
+"""Block-cache operators at their edges, against the plain 64-bit forms; tolerances as in test_gpu_kv.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as R
+from paper_2608_08751_b200 import binding as B
+from test_gpu_kv import _attend_case, _check_attend, _gen, _i32, _np, kernel  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _against_plain(case, scale, kind, dim):
+    kc, vc, table, req, pos, q, sel = case
+    got, lse = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), scale, want_lse=True)
+    B.ivf_check()
+    _check_attend(got, lse, R.attend(_np(q), np.nan_to_num(_np(kc)), np.nan_to_num(_np(vc)), table, req, pos, sel, scale), kind, dim)
+    return got
+
+
+# ---------------------------------------------------------------------------------------------- requests that share a window
+
+# A page of 128 is two boxes of a window's plan, and a last one that nobody sees is given back: the box of the request
+# that has it, not of one before it.
+@pytest.mark.parametrize("dim,kind", [(64, "fp16"), (128, "bf16"), (256, "bf16")])
+@pytest.mark.parametrize("contexts,group,empty", [
+    ([501, 8], 8, [1]), ([8, 501], 8, [0]), ([501, 9, 8], 4, [1, 2]), ([8, 501, 9], 4, [0, 2]), ([700, 8, 501], 4, [1]), ([9, 8], 8, [0, 1]),
+])
+def test_a_request_with_no_block_leaves_its_neighbours_alone(kernel, contexts, group, empty, dim, kind):  # noqa: F811
+    case = _attend_case(contexts, 8, 1, group, dim, 128, 4, kind, "head", seed=len(contexts) + dim)
+    req, sel = case[3], case[6]
+    for b, c in enumerate(contexts):
+        sel[req == b] = -1 if b in empty else [0, (c - 1) // 128, -1, -1] if c > 128 else [0, -1, -1, -1]
+    got = _against_plain(case, 1 / math.sqrt(dim), kind, dim)
+    assert (got[torch.from_numpy(np.isin(req, empty)).cuda()] == 0).all()
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("contexts,empty", [([501, 8], 1), ([8, 501], 0)])
+def test_a_request_without_pages_leaves_its_neighbours_alone(kernel, contexts, empty, page):  # noqa: F811
+    kc, vc, table, req, pos, q, _ = _attend_case(contexts, 8, 2, 8, 64, page, 4, "bf16", "head", seed=page)
+    table[empty] = -1  # it found no free page
+    codes = torch.randint(-127, 128, (kc.shape[0], 2, 64), device="cuda", generator=_gen(1)).to(torch.int8)
+    sel = _np(B.ivf_kv_select(q, codes, torch.ones(kc.shape[0], 2, device="cuda"), _i32(table), _i32(req), _i32(pos), page, 4))
+    assert (sel[req == empty] == -1).all() and (sel[req != empty][:, :, 0] == 0).all()
+    _against_plain((kc, vc, table, req, pos, q, sel), 0.125, "bf16", 64)
