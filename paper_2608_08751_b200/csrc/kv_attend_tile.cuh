@@ -283,7 +283,8 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         int before = 0;
         for (int t0 = 0; t0 < tokens; t0 += 32) {
             const int t = t0 + lane;
-            const unsigned m = __ballot_sync(0xFFFFFFFFu, t > 0 && t < tokens && c.req[t] != c.req[t - 1]);
+            // the requests as given, as they were counted: a token that is padding by its position stays inside its segment
+            const unsigned m = __ballot_sync(0xFFFFFFFFu, t > 0 && t < tokens && p.token_req[w0 + t] != p.token_req[w0 + t - 1]);
             c.seg[t] = before + __popc(m & (0xFFFFFFFFu >> (31 - lane)));
             before += __popc(m);
         }

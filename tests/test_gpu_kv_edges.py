@@ -46,3 +46,17 @@ def test_a_request_without_pages_leaves_its_neighbours_alone(kernel, contexts, e
     sel = _np(B.ivf_kv_select(q, codes, torch.ones(kc.shape[0], 2, device="cuda"), _i32(table), _i32(req), _i32(pos), page, 4))
     assert (sel[req == empty] == -1).all() and (sel[req != empty][:, :, 0] == 0).all()
     _against_plain((kc, vc, table, req, pos, q, sel), 0.125, "bf16", 64)
+
+
+# ---------------------------------------------------------------------------------------------- padding inside a window
+
+# A token is padding by its request or by its position; either way the window's other tokens keep their places.
+@pytest.mark.parametrize("page", [32, 128])
+@pytest.mark.parametrize("group,fresh", [(8, 8), (2, 32), (1, 60)])
+@pytest.mark.parametrize("by_pos,by_req", [([3], []), ([3], [5]), ([0, 9], [12]), ([15], [])])
+def test_padding_by_position_inside_a_shared_window(kernel, by_pos, by_req, group, fresh, page):  # noqa: F811
+    case = _attend_case([400, 260], fresh, 2, group, 64, page, 3, "bf16", "head", seed=fresh + page)
+    req, pos = case[3], case[4]
+    pos[by_pos], req[by_req] = -1, -1
+    got = _against_plain(case, 0.125, "bf16", 64)
+    assert (got[by_pos + by_req] == 0).all()
