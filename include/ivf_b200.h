@@ -489,6 +489,8 @@ int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int
  * natural logarithm of the softmax's sum.
  *   selected        [n_tokens][n_kv_heads][n_select] as ivf_kv_select gives them: ascending without repeats, -1 after the
  *                   last; a user's own choice is fine.  A block past the token's own is ignored.
+ *   out             may be q itself with q's strides (the tokens are then taken singly); it must not share memory with q, the
+ *                   caches or `selected` in any other way
  * A token that sees nothing (padding, or no block selected) gets zeros and an out_lse of -infinity.  What pages hold past
  * a request's last token is never used, whatever it is.
  */

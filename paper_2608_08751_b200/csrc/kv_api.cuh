@@ -244,6 +244,19 @@ int kv_launch_tile(const KvAttendParams& p, const CUtensorMap& mk, const CUtenso
     return IVF_OK;
 }
 
+// Whether `out` has an element of `q`'s memory.  Rows of one buffer in turn (the same token stride) are told apart, other
+// tensors by their ranges.
+bool kv_out_over_q(const KvAttendParams& p) {
+    const int64_t heads = static_cast<int64_t>(p.group) * p.n_kv_heads;
+    const int64_t q_row = (heads - 1) * p.q_stride[1] + p.dim, o_row = (heads - 1) * p.out_stride[1] + p.dim;
+    const int64_t q0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(p.q)) / 2, o0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(p.out)) / 2;
+    if (q0 + (p.n_tokens - 1) * p.q_stride[0] + q_row <= o0 || o0 + (p.n_tokens - 1) * p.out_stride[0] + o_row <= q0) return false;
+    const int64_t step = p.q_stride[0];
+    if (step == 0 || step != p.out_stride[0]) return true;
+    const int64_t after = ((o0 - q0) % step + step) % step;  // of an output row behind the start of a query row
+    return after < q_row || after + o_row > step;
+}
+
 template <typename T>
 int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     p.done = nullptr;
@@ -257,6 +270,9 @@ int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     // 31 / 43 us, 256 tokens 86 / 43, 512 tokens of 32 requests 152 / 43; by 8 heads without groups (128 tokens to a
     // window) 128 tokens of 8 requests 85 / 307, 256 tokens of one 146 / 107.
     const int64_t parts = (p.group + 15) / 16;
+    // A window may be taken twice, and the second time needs its queries: an output in their place goes by the rows alone, which
+    // read a row before they write it.
+    tile = tile && !kv_out_over_q(p);
     if (g_kv_attend == 0) tile = tile && p.n_tokens * p.n_kv_heads * parts >= 4 * ctx.num_sms && p.n_tokens - p.n_req + 1 >= 2 * p.window;
     if (tile) {
         if (int rc = get_encode()) return rc;

@@ -60,3 +60,36 @@ def test_padding_by_position_inside_a_shared_window(kernel, by_pos, by_req, grou
     pos[by_pos], req[by_req] = -1, -1
     got = _against_plain(case, 0.125, "bf16", 64)
     assert (got[by_pos + by_req] == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------- output over the queries
+
+@pytest.mark.parametrize("group,fresh", [(4, 64), (20, 40), (8, 1)])
+def test_output_in_place_of_the_queries(kernel, group, fresh):  # noqa: F811
+    kc, vc, table, req, pos, q, sel = _attend_case([640, 300], fresh, 2, group, 128, 64, 4, "bf16", "head", seed=group)
+    n = len(req)
+    for h in range(2):  # one block that the odd tokens of the first request do not see
+        for t in np.flatnonzero(req == 0):
+            sel[t, h] = [0, 2, 5, 9] if t % 2 else [0, 3, 5, 9]
+    vc[int(table[0, 3]), :, 7] = math.inf
+    want = R.attend(_np(q), np.nan_to_num(_np(kc)), np.nan_to_num(_np(vc), posinf=1e30), table, req, pos, sel, 0.1)
+    clean = [t for t in range(n) if req[t] == 1 or t % 2]
+    got, lse = B.ivf_kv_attend(q.clone(), kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1, want_lse=True)
+    over = q.clone()
+    same, lse2 = B.ivf_kv_attend(over, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1, out=over, want_lse=True)
+    B.ivf_check()
+    assert same.data_ptr() == over.data_ptr()
+    for x, y in ((got, lse), (same, lse2)):
+        _check_attend(x[clean], y[clean], tuple(w[clean] for w in want), "bf16", 128)
+
+
+def test_output_beside_the_queries(kernel):  # noqa: F811
+    # rows of one buffer in turn: the same numbers as apart
+    kc, vc, table, req, pos, q, sel = _attend_case([640, 300], 64, 2, 4, 128, 64, 4, "bf16", "head", seed=8)
+    both = torch.zeros(len(req), 2, 8, 128, dtype=q.dtype, device="cuda")
+    both[:, 0] = q
+    args = (kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1)
+    want, _ = B.ivf_kv_attend(q, *args)
+    got, _ = B.ivf_kv_attend(both[:, 0], *args, out=both[:, 1])
+    B.ivf_check()
+    assert torch.equal(got, want) and torch.equal(both[:, 0], q)
