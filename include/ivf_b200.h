@@ -401,8 +401,9 @@ int ivf_pq_search(const void* queries, int64_t nq, int d, ivf_dtype qtype, const
  *
  *   ivf_kv_tables -> ivf_kv_append -> ivf_kv_summarize -> ivf_kv_select -> ivf_kv_attend
  *
- * on one stream.  The calls return without waiting and may be captured in a CUDA graph (after a first call of the
- * same sizes, which sizes the workspace).  Sums, norms, scores
+ * on one stream.  The calls return without waiting.  They use none of the library's workspace: steps on other streams need no
+ * order between them, and a step may be captured in a CUDA graph (after a first call of any size on the device) whatever is
+ * called between its replays.  Sums, norms, scores
  * and softmax statistics are held in 32 bits.
  */
 typedef struct ivf_kv_cache {

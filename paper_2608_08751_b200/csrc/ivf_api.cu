@@ -137,7 +137,7 @@ void timing_end(int idx, cudaStream_t stream) {
 // ------------------------------------------------------------------ workspace
 enum WsSlot {
     WS_X16, WS_C16, WS_XN, WS_SCAL, WS_BITS, WS_PART, WS_PARTMETA, WS_FAIL, WS_FBKEYS, WS_TAU, WS_SKETCH, WS_OUT_IDS0, WS_OUT_IDS1, WS_OUT_DISTS0, WS_OUT_DISTS1,
-    WS_UCNT, WS_UOFF, WS_UCUR, WS_UPERM, WS_IDS, WS_CHUNK0, WS_CHUNK1, WS_PQ_CHUNKS, WS_PQ_GCAND, WS_PQ_GCOUNT, WS_PQ_CBT, WS_UPARTS, WS_KV_DONE, WS_NUM
+    WS_UCNT, WS_UOFF, WS_UCUR, WS_UPERM, WS_IDS, WS_CHUNK0, WS_CHUNK1, WS_PQ_CHUNKS, WS_PQ_GCAND, WS_PQ_GCOUNT, WS_PQ_CBT, WS_UPARTS, WS_NUM
 };
 struct Buf {
     void* p = nullptr;

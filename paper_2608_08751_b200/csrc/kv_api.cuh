@@ -185,7 +185,7 @@ int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t s
     if (int rc = kv_allow_smem(kv_attend_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
     const int z = (p.group + 15) / 16;
     unsigned ranks = 1, x = static_cast<unsigned>(p.n_tokens);
-    if (p.done) {  // what the tile kernel left: a few CTAs look for it
+    if (p.window) {  // what the tile kernel left: a few CTAs look for it
         x = static_cast<unsigned>(std::min<int64_t>(p.n_tokens, std::max(1, 2 * ctx.num_sms / p.n_kv_heads)));
     } else {
         // CTAs to a token: until the card has two for each SM, as long as each warp still has a piece.  (More of them than
@@ -258,9 +258,9 @@ bool kv_out_over_q(const KvAttendParams& p) {
 }
 
 template <typename T>
-int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
-    p.done = nullptr;
-    p.window = 128 / p.group;
+int kv_launch_attend(KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    const int window = 128 / p.group;
+    p.window = 0;
     p.limit_ns = g_wait_limit_ns.load();
     CUtensorMap mk, mv;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -273,14 +273,13 @@ int kv_launch_attend(KvAttendParams& p, DeviceCtx& ctx, cudaStream_t stream) {
     // A window may be taken twice, and the second time needs its queries: an output in their place goes by the rows alone, which
     // read a row before they write it.
     tile = tile && !kv_out_over_q(p);
-    if (g_kv_attend == 0) tile = tile && p.n_tokens * p.n_kv_heads * parts >= 4 * ctx.num_sms && p.n_tokens - p.n_req + 1 >= 2 * p.window;
+    if (g_kv_attend == 0) tile = tile && p.n_tokens * p.n_kv_heads * parts >= 4 * ctx.num_sms && p.n_tokens - p.n_req + 1 >= 2 * window;
     if (tile) {
         if (int rc = get_encode()) return rc;
         tile = kv_make_map(&mk, p.kc, p, bf16) && kv_make_map(&mv, p.vc, p, bf16);
     }
     if (!tile) return kv_launch_rows<T>(p, ctx, stream);
-    const int64_t windows = (p.n_tokens + p.window - 1) / p.window;
-    WS(WS_KV_DONE, static_cast<size_t>(windows) * p.n_kv_heads, p.done);
+    p.window = window;
     const int rc = p.dim <= 64 ? kv_launch_tile<T, 1>(p, mk, mv, ctx, stream) : p.dim <= 128 ? kv_launch_tile<T, 2>(p, mk, mv, ctx, stream)
                                                                                        : kv_launch_tile<T, 4>(p, mk, mv, ctx, stream);
     return rc != IVF_OK ? rc : kv_launch_rows<T>(p, ctx, stream);

@@ -25,12 +25,18 @@ struct KvAttendParams {
     int64_t out_stride[2];
     float* lse;  // [n_tokens][n_heads] or null
     int* status;
-    // windows of `window` tokens that the tile kernel has finished (flag 1) or left to the rows kernel (flag 0);
-    // null where the rows kernel runs alone
-    uint8_t* done;  // [windows][n_kv_heads]
-    int window;
+    int window;          // tokens of a window of the tile kernel; 0 where the rows kernel runs alone
     uint64_t limit_ns;
 };
+
+// What the tile kernel leaves to the rows kernel it marks in the output itself: the first four bytes of a token's row, one mark
+// for each kv head and 16 query heads of its group.  No finished row can hold it: both halves are NaN in either type, and a
+// finished window is finite.  (No memory of the library's own: calls of several streams and captured graphs share nothing.)
+constexpr uint32_t kKvLeft = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t* kv_mark(const KvAttendParams& p, int64_t t, int h, int part) {
+    return reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + t * p.out_stride[0] +
+                                       (static_cast<int64_t>(h) * p.group + part * 16) * p.out_stride[1]);
+}
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -362,15 +368,16 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
     extern __shared__ __align__(128) uint8_t rows_smem[];
     __shared__ int s_page[kKvMaxSelect], s_first[kKvMaxSelect];
     __shared__ int s_n;
-    if (p.done == nullptr) {
+    if (p.window == 0) {
         const int ranks = static_cast<int>(cluster_size());
         attend_rows<T, DP>(p, blockIdx.x / ranks, static_cast<int>(cluster_rank()), ranks, rows_smem, s_page, s_first, s_n);
         return;
     }
-    // what the tile kernel left: 32 tokens are looked at at a time
+    // what the tile kernel left: 32 tokens are looked at at a time (a mark is read by every warp before the first barrier
+    // that its token's row is written behind)
     for (int64_t t0 = blockIdx.x; t0 < p.n_tokens; t0 += static_cast<int64_t>(gridDim.x) * 32) {
         const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
-        unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && p.done[mine / p.window * p.n_kv_heads + blockIdx.y] == 0);
+        unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && *kv_mark(p, mine, blockIdx.y, blockIdx.z) == kKvLeft);
         for (; left; left &= left - 1)
             attend_rows<T, DP>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
     }

@@ -27,7 +27,7 @@
 // What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
 // value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
 // such a window, one whose tokens belong to many requests and one whose plan is too long is left to the rows
-// kernel by its flag.
+// kernel by marks in its output rows.
 #pragma once
 #include "kv_attend.cuh"
 
@@ -200,7 +200,10 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     const int h = blockIdx.y;
     const int64_t w0 = static_cast<int64_t>(blockIdx.x) * p.window;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(p.window), p.n_tokens - w0));
-    uint8_t* done = p.done + static_cast<int64_t>(blockIdx.x) * p.n_kv_heads + h;
+    auto leave = [&]() {  // to the rows kernel
+        const int parts = (p.group + 15) / 16;
+        for (int i = tid; i < tokens * parts; i += S::kThreads) *kv_mark(p, w0 + i / parts, h, i % parts) = kKvLeft;
+    };
 
     // ---- queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits; they come
     // while the plan is built
@@ -243,7 +246,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     const int segments = __syncthreads_count(change) + 1;
     if (segments > 1 && segments * 8 > tokens) {
         cp_async_wait<0>();
-        if (tid == 0) *done = 0;
+        leave();
         return;
     }
 
@@ -385,7 +388,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     }
     if (boxes < 0) {  // more than the plan holds: a tile would serve a few of its rows only
         cp_async_wait<0>();
-        if (tid == 0) *done = 0;
+        leave();
         return;
     }
     for (int b = tid; b < boxes; b += S::kThreads) {
@@ -696,7 +699,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         tc_fence_after_sync();
         tmem_dealloc(tmem, S::kCols);
     }
-    if (tid == 0) *done = c.bad ? 0 : 1;
+    if (c.bad) leave();  // (over what other threads wrote before the barrier)
 }
 
 }  // namespace ivf

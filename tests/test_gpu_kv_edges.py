@@ -93,3 +93,68 @@ def test_output_beside_the_queries(kernel):  # noqa: F811
     got, _ = B.ivf_kv_attend(both[:, 0], *args, out=both[:, 1])
     B.ivf_check()
     assert torch.equal(got, want) and torch.equal(both[:, 0], q)
+
+
+# ---------------------------------------------------------------------------------------------- graphs and streams
+
+def _mixed_windows(seed, requests, fresh, group=8, page=64):
+    """Prompt chunks of which some windows are finished and some left: several requests, a value that is not finite."""
+    case = _attend_case([700 + 13 * i for i in range(requests)], fresh, 2, group, 128, page, 4, "bf16", "head", seed=seed, shared=True)
+    table, vc = case[2], case[1]
+    vc[int(table[0, 3]), :, 5] = math.inf
+    kc, vc, table, req, pos, q, sel = case
+    return (q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1)
+
+
+def _same(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_a_graph_outlives_larger_calls(kernel):  # noqa: F811
+    small, large = _mixed_windows(1, 9, 24), _mixed_windows(2, 6, 400)
+    first = B.ivf_kv_attend(*small)[0]
+    want = first.clone()
+    assert want.isfinite().any() and not want.isfinite().all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, _ = B.ivf_kv_attend(*small)
+    B.ivf_kv_attend(*large)
+    B.ivf_release_workspace()
+    spoil = torch.full((1 << 22,), 1, dtype=torch.uint8, device="cuda")  # takes over what may have been given back
+    for fill in (0, 1, 255):
+        out.view(torch.uint8).fill_(fill)
+        spoil.fill_(fill)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(out, want)
+    B.ivf_check()
+
+
+def test_two_streams_without_order(kernel):  # noqa: F811
+    cases = [_mixed_windows(3, 12, 20), _mixed_windows(4, 2, 300)]
+    want = [B.ivf_kv_attend(*c)[0].clone() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[torch.empty_like(w) for _ in range(20)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for c, s, o in zip(cases, streams, outs):
+            with torch.cuda.stream(s):
+                B.ivf_kv_attend(*c, out=o[i])
+    torch.cuda.synchronize()
+    B.ivf_check()
+    for w, o in zip(want, outs):
+        assert all(_same(x, w) for x in o)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_stale_outputs_are_not_taken_for_marks(kernel, kind):  # noqa: F811
+    # an output buffer full of the bytes that mark a row, of a call that finishes every window
+    case = _attend_case([640], 128, 2, 20, 64, 64, 4, kind, "head", seed=6, shared=True)
+    kc, vc, table, req, pos, q, sel = case
+    out = torch.full_like(q, math.nan)
+    out.view(torch.int16).fill_(-1)
+    got, _ = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1, out=out)
+    want, _ = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1)
+    B.ivf_check()
+    assert _same(got, want) and got.isfinite().all()
