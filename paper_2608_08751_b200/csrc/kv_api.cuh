@@ -321,8 +321,8 @@ int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int pa
     static KvSmemSeen seen;
     if (int rc = kv_allow_smem(kv_tables_kernel, static_cast<int>(smem), *pctx, seen)) return rc;
     const int64_t items = (static_cast<int64_t>(n_req) * max_blocks) / 8 + max_tokens + max_touched;
-    int64_t grid = (items + kTabThreads - 1) / kTabThreads;
-    if (grid > pctx->num_sms) grid = pctx->num_sms;
+    // (the lengths and counts are written even where there is room for nothing else)
+    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>((items + kTabThreads - 1) / kTabThreads, pctx->num_sms));
     kv_tables_kernel<<<static_cast<unsigned>(grid), kTabThreads, smem, stream>>>(p);
     LAUNCH_CHECK();
     return IVF_OK;

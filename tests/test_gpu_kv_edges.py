@@ -158,3 +158,19 @@ def test_stale_outputs_are_not_taken_for_marks(kernel, kind):  # noqa: F811
     want, _ = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1)
     B.ivf_check()
     assert _same(got, want) and got.isfinite().all()
+
+
+# ---------------------------------------------------------------------------------------------- tables: no room
+
+def test_tables_without_room_for_tokens_or_blocks():
+    # nothing but the table, the lengths and the counts to write
+    table = torch.full((1, 4), 9, dtype=torch.int32, device="cuda")
+    plan = B.ivf_kv_tables(_i32([20]), _i32([0]), _i32([5, 6]), table, 16, 0, max_touched=0)
+    B.ivf_check()
+    assert _np(plan.kv_lens).tolist() == [20] and _np(plan.token_start).tolist() == [0, 0] and int(plan.used) == 0
+    assert _np(table).tolist() == [[9, 9, -1, -1]]
+    plan = B.ivf_kv_tables(_i32([20]), _i32([30]), _i32([5, 6]), table, 16, 0, max_touched=0)
+    with pytest.raises(B.IvfError) as e:
+        B.ivf_check()
+    assert e.value.code == B.IVF_ERR_NO_PAGES
+    assert _np(table).tolist() == [[9, 9, 5, 6]] and int(plan.used) == 2 and _np(plan.token_start).tolist() == [0, 30]
