@@ -4,7 +4,8 @@
 // now_b = ceil((cached_b + fresh_b) / p) pages.  With exclusive prefix sums over the requests of the new
 // tokens, of the new pages now_b - old_b and of the touched blocks, every output element follows by itself:
 // table[b][j] = free[pages_before_b + j - old_b] for old_b <= j < now_b, and for new token i of request b
-// pos = cached_b + i, slot = page(pos / p) * p + pos % p.
+// pos = cached_b + i, slot = page(pos / p) * p + pos % p.  The sums are taken in 64 bits and held at 2^31 - 1 where they are
+// stored: no list is as long, so what lies behind such a sum has no place in any.
 //
 // One launch, no workspace, no atomics: every CTA scans all lengths itself (they are 8 bytes a request and
 // come from L2) and keeps the three prefix sums in shared memory; then the CTAs share out the table rows,
@@ -49,6 +50,13 @@ __device__ __forceinline__ TabLengths tab_lengths(const KvTablesParams& p, int b
     return l;
 }
 
+// Blocks that hold new tokens of a request.
+__device__ __forceinline__ int tab_touched(const KvTablesParams& p, const TabLengths& l) {
+    return l.fresh > 0 ? l.now_blocks - (l.cached >> p.page_shift) : 0;
+}
+
+__device__ __forceinline__ int tab_held(int64_t sum) { return static_cast<int>(min(sum, static_cast<int64_t>(0x7FFFFFFF))); }
+
 // Last index i in [0, n) with start[i] <= x (start ascends, start[0] == 0): skips entries of empty requests.
 __device__ __forceinline__ int tab_find(const int* start, int n, int x) {
     int lo = 0, hi = n;  // start[lo] <= x < start[hi]
@@ -73,62 +81,63 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(KvTablesParams p
     int* s_tok = tab_smem;                // [n_req + 1] first token of each request
     int* s_page = s_tok + p.n_req + 1;    // [n_req + 1] new pages before it
     int* s_touch = s_page + p.n_req + 1;  // [n_req + 1] touched blocks before it
-    __shared__ int s_warp[3][kTabThreads / 32];
+    __shared__ int64_t s_warp[3][kTabThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     // ---- prefix sums: each thread owns a contiguous run of requests
     const int per = (p.n_req + kTabThreads - 1) / kTabThreads;
     const int b0 = min(tid * per, p.n_req), b1 = min(b0 + per, p.n_req);
-    int sum[3] = {0, 0, 0};
+    int64_t sum[3] = {0, 0, 0};
     bool bad = false, cramped = false;
     for (int b = b0; b < b1; ++b) {
         const TabLengths l = tab_lengths(p, b);
-        s_tok[b] = sum[0];
-        s_page[b] = sum[1];
-        s_touch[b] = sum[2];
         sum[0] += l.fresh;
         sum[1] += l.now_blocks - l.old_blocks;
-        sum[2] += l.fresh > 0 ? l.now_blocks - (l.cached >> p.page_shift) : 0;
+        sum[2] += tab_touched(p, l);
         bad |= l.bad;
         cramped |= l.now_blocks > p.max_blocks;
         if (blockIdx.x == 0) p.kv_lens[b] = l.cached + l.fresh;
     }
-    int incl[3];
+    int64_t incl[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         incl[k] = sum[k];
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const int v = __shfl_up_sync(0xFFFFFFFFu, incl[k], off);
+            const int64_t v = __shfl_up_sync(0xFFFFFFFFu, incl[k], off);
             if (lane >= off) incl[k] += v;
         }
         if (lane == 31) s_warp[k][warp] = incl[k];
     }
     __syncthreads();
-    int base[3], total[3];
+    int64_t base[3], total[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         base[k] = incl[k] - sum[k];
         total[k] = 0;
         for (int w = 0; w < kTabThreads / 32; ++w) {
-            const int v = s_warp[k][w];
+            const int64_t v = s_warp[k][w];
             if (w < warp) base[k] += v;
             total[k] += v;
         }
     }
     for (int b = b0; b < b1; ++b) {
-        s_tok[b] += base[0];
-        s_page[b] += base[1];
-        s_touch[b] += base[2];
+        const TabLengths l = tab_lengths(p, b);
+        s_tok[b] = tab_held(base[0]);
+        s_page[b] = tab_held(base[1]);
+        s_touch[b] = tab_held(base[2]);
         if (blockIdx.x == 0) p.token_start[b] = s_tok[b];
+        base[0] += l.fresh;
+        base[1] += l.now_blocks - l.old_blocks;
+        base[2] += tab_touched(p, l);
     }
     if (tid == 0) {
-        s_tok[p.n_req] = total[0];
-        s_page[p.n_req] = total[1];
-        s_touch[p.n_req] = total[2];
+        s_tok[p.n_req] = tab_held(total[0]);
+        s_page[p.n_req] = tab_held(total[1]);
+        s_touch[p.n_req] = tab_held(total[2]);
         if (blockIdx.x == 0) {
-            p.token_start[p.n_req] = total[0];
-            *p.used = total[1];
+            p.token_start[p.n_req] = s_tok[p.n_req];
+            *p.used = s_page[p.n_req];
             if (total[1] > p.n_free || total[0] > p.max_tokens || total[2] > p.max_touched)
                 kv_report(p.status, kKvStatusNoPages, KV_SITE_TABLES);
         }
@@ -149,7 +158,7 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(KvTablesParams p
         if (t < total[0]) {
             req = tab_find(s_tok, p.n_req, static_cast<int>(t));
             const TabLengths l = tab_lengths(p, req);
-            pos = l.cached + static_cast<int>(t) - s_tok[req];
+            pos = l.cached + (static_cast<int>(t) - s_tok[req]);
             const int page = tab_page(p, req, pos >> p.page_shift, l.old_blocks, s_page[req]);
             if (page >= 0) slot = (static_cast<int64_t>(page) << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
         }
@@ -163,7 +172,7 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(KvTablesParams p
         if (w < total[2]) {
             const int b = tab_find(s_touch, p.n_req, static_cast<int>(w));
             const TabLengths l = tab_lengths(p, b);
-            const int j = (l.cached >> p.page_shift) + static_cast<int>(w) - s_touch[b];
+            const int j = (l.cached >> p.page_shift) + (static_cast<int>(w) - s_touch[b]);
             page = tab_page(p, b, j, l.old_blocks, s_page[b]);
             fill = page >= 0 ? min(1 << p.page_shift, l.cached + l.fresh - (j << p.page_shift)) : 0;
         }

@@ -174,3 +174,39 @@ def test_tables_without_room_for_tokens_or_blocks():
         B.ivf_check()
     assert e.value.code == B.IVF_ERR_NO_PAGES
     assert _np(table).tolist() == [[9, 9, 5, 6]] and int(plan.used) == 2 and _np(plan.token_start).tolist() == [0, 30]
+
+
+# ---------------------------------------------------------------------------------------------- tables: long sums
+
+def test_tables_of_lengths_whose_sum_passes_31_bits():
+    # each length is fine by itself; the sums are not, and nothing is read or written by a sum that went round
+    page, most = 16, 2 ** 31 - 1
+    lengths = [(0, 1_500_000_000), (40, 1_500_000_000), (17, 1_500_000_000), (5, 3)]
+    table = torch.full((4, 6), 77, dtype=torch.int32, device="cuda")
+    plan = B.ivf_kv_tables(_i32([c for c, _ in lengths]), _i32([f for _, f in lengths]), _i32([3, 4]), table, page, 40, max_touched=5)
+    with pytest.raises(B.IvfError) as e:
+        B.ivf_check()
+    assert e.value.code == B.IVF_ERR_NO_PAGES and "ivf_kv_tables" in str(e.value)
+    assert _np(plan.token_start).tolist() == [0, 1_500_000_000, most, most, most]
+    assert int(plan.used) == sum(R.ceil_div(c + f, page) - R.ceil_div(c, page) for c, f in lengths)
+    assert _np(plan.kv_lens).tolist() == [c + f for c, f in lengths]
+    assert _np(plan.token_req).tolist() == [0] * 40 and _np(plan.token_pos).tolist() == list(range(40))
+    assert _np(plan.token_slot).tolist() == [48 + i for i in range(16)] + [64 + i for i in range(16)] + [-1] * 8
+    assert _np(plan.touched_page).tolist() == [3, 4, -1, -1, -1] and _np(plan.touched_fill).tolist() == [16, 16, 0, 0, 0]
+    assert _np(table).tolist() == [[3, 4, -1, -1, -1, -1], [77, 77, 77, -1, -1, -1], [77, 77, -1, -1, -1, -1], [77, -1, -1, -1, -1, -1]]
+
+
+@pytest.mark.parametrize("n", [2, 3, 1500])
+def test_tables_of_sums_that_come_round_to_a_small_number(n):
+    # 32-bit sums of these are 0, 1 and so on again: still too few tokens
+    long = 2 ** 31 - 200
+    cached, fresh = [5] * n, [long] * n
+    table = torch.full((n, 3), 8, dtype=torch.int32, device="cuda")
+    plan = B.ivf_kv_tables(_i32(cached), _i32(fresh), _i32([1]), table, 128, 600)
+    with pytest.raises(B.IvfError) as e:
+        B.ivf_check()
+    assert e.value.code == B.IVF_ERR_NO_PAGES
+    assert (plan.token_req == 0).all() and _np(plan.token_pos).tolist() == list(range(5, 605))
+    assert _np(plan.token_start)[:3].tolist() == [0, long, 2 ** 31 - 1]
+    assert int(plan.used) == min(2 ** 31 - 1, n * (R.ceil_div(long + 5, 128) - 1))
+    assert _np(plan.token_slot).tolist() == [8 * 128 + i for i in range(5, 128)] + [128 + i for i in range(128)] + [-1] * (600 - 251)
