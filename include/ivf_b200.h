@@ -434,7 +434,9 @@ typedef struct ivf_kv_cache {
  *   used            [1] pages taken from free_pages
  * Where pages, columns, tokens or touched blocks do not suffice the surplus gets -1 (`used` still says what was
  * asked for) and the status word IVF_ERR_NO_PAGES.  A negative length counts as 0 for the whole request and sets
- * IVF_ERR_BAD_ID.  Sums past 2^31 - 1 (token_start, used) are held there.  The call may be repeated on the same arrays.  n_req == 0 enqueues nothing.
+ * IVF_ERR_BAD_ID.  Sums past 2^31 - 1 (token_start, used) are held there.  The call may be repeated on the same arrays.
+ * The table and the plan must not lie over cached, fresh or free_pages (refused): copy kv_lens before it becomes the next
+ * step's `cached` in the same plan.  n_req == 0 enqueues nothing.
  */
 int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int page_size, const int32_t* free_pages, int n_free,
                   int32_t* table, int64_t table_stride, int max_blocks, int32_t* kv_lens, int32_t* token_start,

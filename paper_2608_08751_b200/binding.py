@@ -529,7 +529,7 @@ def ivf_kv_tables(cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.T
                   max_tokens: int, max_touched: int | None = None, plan: KvPlan | None = None) -> KvPlan:
     """Block tables, positions and cache slots of a step from the request lengths (int32 [n_req] each): `table`
     [n_req, max_blocks] int32 is extended in place by pages from the front of free_pages; the plan of the
-    new tokens comes back (or is written into `plan`, an earlier call's)."""
+    new tokens comes back (or is written into `plan`, an earlier call's, whose kv_lens must then not be `cached`)."""
     got = (_kv or _bind()).kv_tables(cached, fresh, free_pages, table, page_size, max_tokens, max_touched, plan)
     if plan is None:
         plan = KvPlan._make(got)

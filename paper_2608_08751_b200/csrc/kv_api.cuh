@@ -45,6 +45,14 @@ int kv_check_cache(const ivf_kv_cache* c, bool keys, bool values) {
     if (values && (rc = kv_check_rows("value cache", c->v, c->v_stride, 3)) != IVF_OK) return rc;
     return IVF_OK;
 }
+// Whether `bytes` at `p` share memory with one of `n` rows of `row` bytes, `step` apart.
+bool kv_over_rows(const void* p, int64_t bytes, const void* rows, int64_t row, int64_t step, int64_t n) {
+    const int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(p)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(rows));
+    if (bytes <= 0 || row <= 0 || n < 1 || at + bytes <= 0 || at >= (n - 1) * step + row) return false;
+    if (at < 0) return true;
+    const int64_t k = at / step;
+    return at - k * step < row || (k + 1 < n && at + bytes > (k + 1) * step);
+}
 KvPlane kv_plane(void* base, const int64_t* s) { return KvPlane{base, s[0], s[1], s[2]}; }
 
 // The table and the tokens' request and position, as select and attend take them.
@@ -307,6 +315,16 @@ int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int pa
     if (!cached || !fresh || !table || !kv_lens || !token_start || !used || (n_free > 0 && !free_pages) ||
         (max_tokens > 0 && (!token_req || !token_pos || !token_slot)) || (max_touched > 0 && (!touched_page || !touched_fill)))
         return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    // Every block of threads reads the lengths and the free list throughout, so nothing may be written over them: a plan's
+    // kv_lens cannot be the `cached` of a call that fills the same plan.
+    struct { const void* p; int64_t bytes; } out[] = {
+        {kv_lens, 4ll * n_req}, {token_start, 4ll * n_req + 4}, {token_req, 4 * max_tokens}, {token_pos, 4 * max_tokens}, {token_slot, 8 * max_tokens},
+        {touched_page, 4 * max_touched}, {touched_fill, 4 * max_touched}, {used, 4}}, in[] = {{cached, 4ll * n_req}, {fresh, 4ll * n_req}, {free_pages, 4ll * n_free}};
+    for (const auto& i : in) {
+        bool over = kv_over_rows(i.p, i.bytes, table, 4ll * max_blocks, 4 * table_stride, n_req);
+        for (const auto& o : out) over |= kv_over_rows(i.p, i.bytes, o.p, o.bytes, o.bytes, 1);
+        if (over) return fail(IVF_ERR_INVALID_ARG, "the table and the plan must not lie over cached, fresh or free_pages");
+    }
     DeviceCtx* pctx = nullptr;
     if (int rc = get_ctx(&pctx)) return rc;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
