@@ -64,17 +64,18 @@ int kv_check_tokens(const int32_t* table, int64_t table_stride, int n_req, int m
     return IVF_OK;
 }
 
-// Raises a kernel's limit of dynamic shared memory, once for a device and size: asking each time costs a call half a
-// microsecond.  `seen` belongs to one kernel.
+// Allows a kernel the most dynamic shared memory that any call of it takes, once for a device (asking each time costs a call
+// half a microsecond).  The same number from every thread: the limit can also be lowered, and with each call's own size the
+// smaller of two first calls could undo the larger.  `seen` belongs to one kernel.
 struct KvSmemSeen {
-    std::atomic<int> bytes[kMaxDevices];
+    std::atomic<bool> device[kMaxDevices];
 };
 template <typename K>
-int kv_allow_smem(K kernel, int bytes, const DeviceCtx& ctx, KvSmemSeen& seen) {
-    std::atomic<int>& known = seen.bytes[&ctx - g_ctx];
-    if (bytes <= 32 * 1024 || bytes <= known.load(std::memory_order_relaxed)) return IVF_OK;
-    CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    known.store(bytes, std::memory_order_relaxed);
+int kv_allow_smem(K kernel, int most, const DeviceCtx& ctx, KvSmemSeen& seen) {
+    std::atomic<bool>& known = seen.device[&ctx - g_ctx];
+    if (known.load(std::memory_order_acquire)) return IVF_OK;
+    CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    known.store(true, std::memory_order_release);
     return IVF_OK;
 }
 
@@ -130,7 +131,7 @@ int kv_launch_select_rows(const KvSelectParams& p, const DeviceCtx& ctx, cudaStr
     auto kernel = kv_select_rows_kernel<T, L, NP>;
     const int smem = p.max_blocks * 4;
     static KvSmemSeen seen;
-    if (int rc = kv_allow_smem(kernel, smem, ctx, seen)) return rc;
+    if (int rc = kv_allow_smem(kernel, kSelMaxBlocks * 4, ctx, seen)) return rc;
     // CTAs to a row: as many as live on the card at a time, as long as each still has 64 blocks
     const int64_t rows = p.n_tokens * p.n_kv_heads;
     const unsigned ranks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>({8, kSelRowCtas * ctx.num_sms / rows, p.max_blocks / 64})));
@@ -154,7 +155,7 @@ int kv_launch_select_windows(const KvSelectParams& p, const DeviceCtx& ctx, cuda
     auto kernel = kv_select_windows_kernel<T, K>;
     const int smem = static_cast<int>(sel_window_smem(p.max_blocks));
     static KvSmemSeen seen;
-    if (int rc = kv_allow_smem(kernel, smem, ctx, seen)) return rc;
+    if (int rc = kv_allow_smem(kernel, static_cast<int>(sel_window_smem(kSelWindowBlocks)), ctx, seen)) return rc;
     const dim3 grid(static_cast<unsigned>((p.n_tokens + kSelWindow - 1) / kSelWindow), p.n_kv_heads);
     kernel<<<grid, kSelThreads, smem, stream>>>(p, (p.max_blocks + 63) / 64 * 64);
     LAUNCH_CHECK();
@@ -335,9 +336,10 @@ int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int pa
     p.kv_lens = kv_lens, p.token_start = token_start, p.token_req = token_req, p.token_pos = token_pos, p.token_slot = token_slot;
     p.max_tokens = max_tokens, p.touched_page = touched_page, p.touched_fill = touched_fill, p.max_touched = max_touched;
     p.used = used, p.status = pctx->status;
-    const size_t smem = 3 * (static_cast<size_t>(n_req) + 1) * sizeof(int);
+    auto smem_of = [](int requests) { return 3 * (requests + 1) * static_cast<int>(sizeof(int)); };
+    const int smem = smem_of(n_req);
     static KvSmemSeen seen;
-    if (int rc = kv_allow_smem(kv_tables_kernel, static_cast<int>(smem), *pctx, seen)) return rc;
+    if (int rc = kv_allow_smem(kv_tables_kernel, smem_of(kTabMaxReq), *pctx, seen)) return rc;
     const int64_t items = (static_cast<int64_t>(n_req) * max_blocks) / 8 + max_tokens + max_touched;
     // (the lengths and counts are written even where there is room for nothing else)
     const int64_t grid = std::max<int64_t>(1, std::min<int64_t>((items + kTabThreads - 1) / kTabThreads, pctx->num_sms));

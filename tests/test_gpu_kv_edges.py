@@ -1,5 +1,7 @@
 """Block-cache operators at their edges, against the plain 64-bit forms; tolerances as in test_gpu_kv.py."""
 import math
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -210,3 +212,50 @@ def test_tables_of_sums_that_come_round_to_a_small_number(n):
     assert _np(plan.token_start)[:3].tolist() == [0, long, 2 ** 31 - 1]
     assert int(plan.used) == min(2 ** 31 - 1, n * (R.ceil_div(long + 5, 128) - 1))
     assert _np(plan.token_slot).tolist() == [8 * 128 + i for i in range(5, 128)] + [128 + i for i in range(128)] + [-1] * (600 - 251)
+
+
+# ---------------------------------------------------------------------------------------------- threads
+
+_THREADS = """
+import ctypes, sys, threading
+import torch
+from paper_2608_08751_b200 import binding as B
+L = B.lib()
+i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+stream = torch.cuda.current_stream().cuda_stream
+s64 = lambda *v: (ctypes.c_int64 * len(v))(*v)
+failed = []
+zero = torch.zeros(1 << 16, dtype=torch.int32, device="cuda")
+for dtype in (B.IVF_F16, B.IVF_BF16):
+    for kernel in (1, 2):
+        B.ivf_debug_set_kv_select(kernel)
+        for dim in ((64, 128, 256) if kernel == 1 else range(32, 257, 32)):
+            q = torch.zeros(1, 1, dim, dtype=torch.float16, device="cuda")
+            codes, scales = torch.zeros(1, 1, dim, dtype=torch.int8, device="cuda"), torch.zeros(1, 1, device="cuda")
+            def call(blocks):
+                table, out = zero[:blocks], torch.empty(1, dtype=torch.int32, device="cuda")
+                rc = L.ivf_kv_select(q.data_ptr(), s64(dim, dim), dtype, 1, 1, 1, dim, codes.data_ptr(), scales.data_ptr(), 1, table.data_ptr(), blocks, 1,
+                                     blocks, 16, zero.data_ptr(), zero.data_ptr(), 1, 0, 1, out.data_ptr(), stream)
+                if rc:
+                    failed.append((dtype, kernel, dim, blocks, L.ivf_last_error()))
+            small, large = (12000, 49152) if kernel == 1 else (700, 2688)
+            gate = threading.Barrier(4)
+            def first(blocks):
+                gate.wait()
+                call(blocks)
+            threads = [threading.Thread(target=first, args=(b,)) for b in (small, large, small, large)]
+            [t.start() for t in threads]
+            [t.join() for t in threads]
+            for b in (large, small, large):
+                call(b)
+torch.cuda.synchronize()
+B.ivf_check()
+print(len(failed), failed[:3])
+sys.exit(1 if failed else 0)
+"""
+
+
+def test_first_calls_of_several_host_threads():
+    # each thread's first launch of a kernel asks for another amount of shared memory
+    run = subprocess.run([sys.executable, "-c", _THREADS], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stdout + run.stderr
