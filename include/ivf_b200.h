@@ -465,7 +465,8 @@ int ivf_kv_append(const void* q, const int64_t q_stride[2], const void* k, const
  * Summaries of cache pages: for pages[i] and every kv head the mean of its first fills[i] keys, coded as
  * scale = max|mean| / 127, code = round(mean / scale).
  *   codes           [num_pages][n_kv_heads][head_dim] int8, scales [num_pages][n_kv_heads] float32; only the
- *                   listed pages are written.  Page -1 or fill 0 is padding.
+ *                   listed pages are written.  Page -1 or fill 0 is padding.  A mean that is not finite, or so small that the
+ *                   scale is below the normal numbers, gives a scale and codes of 0.
  * The mean is summed in a fixed order: the codes are the same on every call.  cache->v is not used.
  */
 int ivf_kv_summarize(const ivf_kv_cache* cache, const int32_t* pages, const int32_t* fills, int64_t n, int8_t* codes,
@@ -478,7 +479,7 @@ int ivf_kv_summarize(const ivf_kv_cache* cache, const int32_t* pages, const int3
  * Visible are blocks 0 .. token_pos / page_size with a page in the table.  The first n_first and the last n_last (>= 1) blocks are
  * always taken; the others by the score of the kv head's group: the sum of its query heads, coded like a summary,
  * times the block's codes (an exact whole number) times its scale, rounded once to 32 bits.  Equal scores go to the
- * lower block, so the result is the same on every call.  n_select <= 1024, max_blocks <= 49152.  A negative
+ * lower block, so the result is the same on every call (a query that is not finite scores 0 everywhere).  n_select <= 1024, max_blocks <= 49152.  A negative
  * request or position is padding: all -1.
  */
 int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int64_t n_tokens, int n_heads, int n_kv_heads,

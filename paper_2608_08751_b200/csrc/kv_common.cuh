@@ -86,8 +86,14 @@ __device__ __forceinline__ float halving_sum(float (&x)[N]) {
     return x[0];
 }
 
+// Largest magnitude so far: NaN stays NaN (fmaxf would drop it, and the row would be coded as if the number were not there).
+__device__ __forceinline__ float max_magnitude(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
 // Row of 32-bit numbers with largest magnitude `amax` -> codes in [-127, 127] and a scale; a scale below the
-// normal range, and a scale that is not finite, becomes 0 and all codes 0.
+// normal range, and a scale that is not finite (NaN too), becomes 0 and all codes 0.
 __device__ __forceinline__ float code_scale(float amax) {
     const float s = __fmul_rn(amax, 1.0f / 127.0f);
     return s >= 1.17549435e-38f && s <= 3.4e38f ? s : 0.0f;

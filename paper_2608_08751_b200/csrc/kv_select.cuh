@@ -81,9 +81,9 @@ __device__ __forceinline__ uint2 sel_code_warp(const KvSelectParams& p, int64_t 
     });
     float amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(u[i]));
+    for (int i = 0; i < 8; ++i) amax = max_magnitude(amax, u[i]);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
+    for (int off = 16; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
     const float scale = code_scale(amax);
     uint32_t w[2];
 #pragma unroll

@@ -84,14 +84,14 @@ __global__ void __launch_bounds__(kSumThreads, DEEP <= 8 ? 10 : 5) kv_summary_ke
 #pragma unroll
             for (int r = 0; r < kRows; ++r) x[r] = r < live_rows ? s_part[r][e] : 0.0f;
             mean[c] = __fdiv_rn(halving_sum<kRows>(x), static_cast<float>(fill));
-            amax = fmaxf(amax, fabsf(mean[c]));
+            amax = max_magnitude(amax, mean[c]);
         }
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
+    for (int off = 16; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
     if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
     __syncthreads();
-    amax = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+    amax = max_magnitude(max_magnitude(s_max[0], s_max[1]), max_magnitude(s_max[2], s_max[3]));
     const float scale = code_scale(amax);
     const int64_t at = static_cast<int64_t>(page) * p.n_kv_heads + h;
 #pragma unroll

@@ -9,7 +9,7 @@ import torch
 
 import kv_reference as R
 from paper_2608_08751_b200 import binding as B
-from test_gpu_kv import _attend_case, _check_attend, _gen, _i32, _np, kernel  # noqa: F401
+from test_gpu_kv import _attend_case, _cache, _check_attend, _gen, _i32, _np, kernel, select_kernel  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -259,3 +259,36 @@ def test_first_calls_of_several_host_threads():
     # each thread's first launch of a kernel asks for another amount of shared memory
     run = subprocess.run([sys.executable, "-c", _THREADS], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0, run.stdout + run.stderr
+
+
+# ---------------------------------------------------------------------------------------------- summaries and queries that are not finite
+
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_a_block_without_a_finite_mean_has_no_summary(what):
+    kc = _cache(3, 2, 16, 64, "bf16", fill=1.0)
+    kc[1, 0, 4, 17] = what
+    codes, scales = torch.full((3, 2, 64), 99, dtype=torch.int8, device="cuda"), torch.full((3, 2), 5.0, device="cuda")
+    B.ivf_kv_summarize(kc, _i32([0, 1, 2]), _i32([16, 9, 4]), codes, scales)
+    B.ivf_check()
+    assert (codes[1, 0] == 0).all() and float(scales[1, 0]) == 0.0
+    codes[1, 0], scales[1, 0] = codes[1, 1], scales[1, 1]
+    assert (codes == 127).all() and (scales == scales[0, 0]).all() and float(scales[0, 0]) > 0
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_a_query_that_is_not_finite_prefers_no_block(select_kernel, fresh, what):  # noqa: F811
+    n_blocks, dim = 300, 96
+    g = _gen(3)
+    codes = torch.randint(-127, 128, (n_blocks, 2, dim), device="cuda", generator=g).to(torch.int8)
+    q = torch.randn(fresh, 6, dim, device="cuda", generator=g).to(torch.bfloat16)
+    q[0, 1, 40] = what  # a head of the first group
+    pos = np.arange(n_blocks * 16 - fresh, n_blocks * 16)
+    table = np.arange(n_blocks)[None]
+    scales = torch.rand(n_blocks, 2, device="cuda", generator=g) + 0.1
+    got = _np(B.ivf_kv_select(q, codes, scales, _i32(table), _i32([0] * fresh), _i32(pos), 16, 8, n_first=1, n_last=2))
+    B.ivf_check()
+    assert got[0, 0].tolist() == [0, 1, 2, 3, 4, 5, pos[0] // 16 - 1, pos[0] // 16]
+    q[0, :3] = 0  # no preference either, and a number for the plain form
+    want = R.select(_np(q), _np(codes), scales.cpu().numpy(), table, np.zeros(fresh, np.int64), pos, 16, 8, 1, 2)
+    assert (got == want).all()
