@@ -10,6 +10,7 @@ import torch
 import kv_reference as R
 from paper_2608_08751_b200 import binding as B
 from test_gpu_kv import _attend_case, _cache, _check_attend, _gen, _i32, _np, kernel, select_kernel  # noqa: F401
+from test_gpu_kv import test_append_matches_the_formula as check_append
 
 pytestmark = pytest.mark.gpu
 
@@ -292,3 +293,17 @@ def test_a_query_that_is_not_finite_prefers_no_block(select_kernel, fresh, what)
     q[0, :3] = 0  # no preference either, and a number for the plain form
     want = R.select(_np(q), _np(codes), scales.cpu().numpy(), table, np.zeros(fresh, np.int64), pos, 16, 8, 1, 2)
     assert (got == want).all()
+
+
+# ---------------------------------------------------------------------------------------------- append
+
+@pytest.mark.parametrize("n,kv,group,dim,rot,pairs,page,kind,layout,weights", [
+    # from 592 tokens on a block of threads takes a whole token, several rows to a lane group
+    (640, 8, 4, 128, 128, False, 64, "bf16", "head", True), (640, 8, 4, 128, 64, True, 32, "fp16", "token", True),
+    (601, 8, 2, 256, 256, False, 16, "fp16", "both", True), (593, 12, 1, 256, 128, True, 64, "bf16", "token", True),
+    (700, 5, 7, 96, 96, True, 128, "bf16", "head", False), (1000, 3, 20, 80, 32, False, 32, "fp16", "head", True),
+    (592, 1, 64, 64, 64, True, 16, "bf16", "head", True), (591, 8, 4, 128, 128, True, 64, "bf16", "head", True),
+    (600, 16, 1, 16, 16, True, 16, "fp16", "both", True), (800, 40, 1, 48, 0, False, 16, "bf16", "token", True),
+])
+def test_append_of_prompts(n, kv, group, dim, rot, pairs, page, kind, layout, weights):
+    check_append(n, kv, group, dim, rot, pairs, page, kind, layout, weights)
