@@ -452,9 +452,9 @@ int ivf_kv_tables(const int32_t* cached, const int32_t* fresh, int n_req, int pa
  *                   rot_dim entries (a multiple of 16; 0: no rotation) of a head are rotated in pairs
  *                   (i, i + rot_dim/2), or (2i, 2i + 1) with interleaved != 0
  *   q_out           rotated queries (may be q itself with q's strides); keys and values go to token_slot
- * A token whose position is negative is padding: zeros in q_out and nothing written; a negative slot writes
- * nothing to the cache.  A position or slot past its range counts as padding and sets IVF_ERR_BAD_ID.  Two
- * tokens must not have the same slot.
+ * A token whose position is negative is padding: zeros in q_out and nothing written.  A negative slot writes nothing to the
+ * cache; the queries of such a token are turned like any other's.  A position or a slot past its range counts as a negative one
+ * and sets IVF_ERR_BAD_ID.  Two tokens must not have the same slot.
  */
 int ivf_kv_append(const void* q, const int64_t q_stride[2], const void* k, const int64_t k_stride[2], const void* v,
                   const int64_t v_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, const int32_t* token_pos,

@@ -307,3 +307,17 @@ def test_a_query_that_is_not_finite_prefers_no_block(select_kernel, fresh, what)
 ])
 def test_append_of_prompts(n, kv, group, dim, rot, pairs, page, kind, layout, weights):
     check_append(n, kv, group, dim, rot, pairs, page, kind, layout, weights)
+
+
+def test_append_rotates_the_query_of_a_token_without_a_place():
+    # a slot past the cache is one that writes nothing, as a negative slot is; a position past the angles is padding
+    x = torch.randn(4, 2, 64, device="cuda", generator=_gen(2)).to(torch.bfloat16)
+    kc, vc = _cache(2, 2, 16, 64, "bf16", fill=0.0), _cache(2, 2, 16, 64, "bf16", fill=0.0)
+    rotary = torch.randn(4, 32, device="cuda", generator=_gen(3))
+    places = [torch.tensor(s, device="cuda") for s in ([0, 1, 2, 3], [0, 32, -1, 3])]
+    good = B.ivf_kv_append(x, x, x, kc, vc, _i32([0, 1, 2, 3]), places[0], rotary=rotary)
+    B.ivf_check()
+    got = B.ivf_kv_append(x, x, x, kc, vc, _i32([0, 1, 2, 4]), places[1], rotary=rotary)
+    with pytest.raises(B.IvfError):
+        B.ivf_check()
+    assert torch.equal(got[:3], good[:3]) and (got[3] == 0).all()
