@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -78,9 +79,12 @@ int type16(const at::Tensor& t, const char* name) {
     refuse(PyExc_TypeError, "%s must be float16 or bfloat16, got %s", name, c10::toString(t.scalar_type()));
 }
 
+// Neither mode of differentiation is dropped without a word.
 void no_grad(const at::Tensor& t, const char* name) {
     if (t.requires_grad() && c10::GradMode::is_enabled())
         refuse(PyExc_ValueError, "%s requires grad: the block-cache operators compute no gradients", name);
+    if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
+        refuse(PyExc_ValueError, "%s carries a forward-mode tangent: the block-cache operators compute no gradients", name);
 }
 
 // A contiguous CUDA tensor of this type, device and shape.

@@ -321,3 +321,17 @@ def test_append_rotates_the_query_of_a_token_without_a_place():
     with pytest.raises(B.IvfError):
         B.ivf_check()
     assert torch.equal(got[:3], good[:3]) and (got[3] == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------- autograd
+
+def test_forward_mode_tangents_are_refused():
+    import torch.autograd.forward_ad as fwad
+    kc, vc, table, req, pos, q, sel = _attend_case([40], 1, 1, 2, 64, 16, 2, "bf16", "head", seed=1)
+    with fwad.dual_level():
+        dual = fwad.make_dual(q, torch.ones_like(q))
+        with pytest.raises(ValueError, match="gradient"):
+            B.ivf_kv_attend(dual, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), 0.1)
+        with pytest.raises(ValueError, match="gradient"):
+            B.ivf_kv_summarize(fwad.make_dual(kc, torch.ones_like(kc)), _i32([0]), _i32([1]), torch.zeros(kc.shape[0], 1, 64, dtype=torch.int8, device="cuda"),
+                               torch.zeros(kc.shape[0], 1, device="cuda"))
