@@ -86,6 +86,10 @@ void no_grad(const at::Tensor& t, const char* name) {
     if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
         refuse(PyExc_ValueError, "%s carries a forward-mode tangent: the block-cache operators compute no gradients", name);
 }
+// A tensor that the call writes into: whoever saved it for a backward pass finds out.  (Inference tensors count nothing.)
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 
 // A contiguous CUDA tensor of this type, device and shape.
 void* dense(const at::Tensor& t, const char* name, at::ScalarType type, c10::Device dev, std::initializer_list<int64_t> shape) {
@@ -224,7 +228,9 @@ PyObject* kv_tables(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     auto i32 = [&](int i) { return static_cast<int32_t*>(out[i].data_ptr()); };
     check(f_tables(cached, fresh_, static_cast<int>(n), page, free_p, static_cast<int>(free_t.numel()), tb.p, tb.stride, tb.columns, i32(0), i32(1),
                    i32(2), i32(3), static_cast<int64_t*>(out[4].data_ptr()), tokens, i32(5), i32(6), touched, i32(7), stream_of(dev)));
+    written(table);
     if (given(a[7])) {
+        for (const at::Tensor& t : out) written(t);
         Py_INCREF(a[7]);
         return a[7];
     }
@@ -273,6 +279,9 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     const c10::cuda::CUDAGuard guard(dev);
     check(f_append(qp, qs, kp, ks, vp, vs, n, static_cast<int>(heads), &c, pos, slot, rotary, static_cast<int>(n_pos), static_cast<int>(rot), pairs,
                    qw, kw, eps, op, os, stream_of(dev)));
+    written(kc);
+    written(vc);
+    if (given(a[12])) written(out);
     return THPVariable_Wrap(out);
     END
 }
@@ -292,6 +301,8 @@ PyObject* kv_summarize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     auto* scales = as<float>(dense(tensor(a[4], "scales"), "scales", at::kFloat, dev, {c.num_pages, c.n_kv_heads}));
     const c10::cuda::CUDAGuard guard(dev);
     check(f_summarize(&c, pp, fp, n, codes, scales, stream_of(dev)));
+    written(tensor(a[3], "codes"));
+    written(tensor(a[4], "scales"));
     Py_RETURN_NONE;
     END
 }
@@ -321,6 +332,7 @@ PyObject* kv_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     const c10::cuda::CUDAGuard guard(dev);
     check(f_select(qp, qs, static_cast<ivf_dtype>(type), n, static_cast<int>(heads), static_cast<int>(kv), static_cast<int>(d), codes, scales, pages,
                    tb.p, tb.stride, tb.n, tb.columns, page, req, pos, take, first, last, op, stream_of(dev)));
+    if (given(a[10])) written(out);
     return THPVariable_Wrap(out);
     END
 }
@@ -354,6 +366,7 @@ PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     check(f_attend(qp, qs, n, static_cast<int>(heads), &c, tb.p, tb.stride, tb.n, tb.columns, req, pos, sel,
                    static_cast<int>(std::min<int64_t>(st.size(2), INT32_MAX)), scale, op, os,
                    want && lse.numel() ? lse.data_ptr<float>() : nullptr, stream_of(dev)));
+    if (given(a[8])) written(out);
     PyObject* r = PyTuple_New(2);
     if (!r) return nullptr;
     PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(out));

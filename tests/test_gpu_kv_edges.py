@@ -335,3 +335,36 @@ def test_forward_mode_tangents_are_refused():
         with pytest.raises(ValueError, match="gradient"):
             B.ivf_kv_summarize(fwad.make_dual(kc, torch.ones_like(kc)), _i32([0]), _i32([1]), torch.zeros(kc.shape[0], 1, 64, dtype=torch.int8, device="cuda"),
                                torch.zeros(kc.shape[0], 1, device="cuda"))
+
+
+def test_tensors_written_in_place_count_a_version():
+    kc, vc = _cache(4, 1, 16, 64, "bf16", fill=0.0), _cache(4, 1, 16, 64, "bf16", fill=0.0)
+    table, x = torch.full((1, 4), -1, dtype=torch.int32, device="cuda"), torch.ones(3, 1, 64, device="cuda", dtype=torch.bfloat16)
+    codes, scales = torch.zeros(4, 1, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, 1, device="cuda")
+    before = table._version
+    plan = B.ivf_kv_tables(_i32([0]), _i32([3]), _i32([0, 1]), table, 16, 3)
+    assert table._version > before
+    old = [t._version for t in plan]
+    B.ivf_kv_tables(_i32([0]), _i32([3]), _i32([0, 1]), table, 16, 3, plan=plan)
+    assert all(t._version > v for t, v in zip(plan, old))
+    q, old = torch.empty_like(x), (kc._version, vc._version)
+    old_q = q._version
+    B.ivf_kv_append(x, x, x, kc, vc, plan.token_pos, plan.token_slot, q_out=q)
+    assert kc._version > old[0] and vc._version > old[1] and q._version > old_q
+    old = (codes._version, scales._version, kc._version)
+    B.ivf_kv_summarize(kc, plan.touched_page, plan.touched_fill, codes, scales)
+    assert codes._version > old[0] and scales._version > old[1] and kc._version == old[2]
+    sel = torch.empty(3, 1, 2, dtype=torch.int32, device="cuda")
+    old = sel._version
+    B.ivf_kv_select(q, codes, scales, table, plan.token_req, plan.token_pos, 16, 2, out=sel)
+    assert sel._version > old
+    out, old = torch.empty_like(q), q._version
+    old_out = out._version
+    B.ivf_kv_attend(q, kc, vc, table, plan.token_req, plan.token_pos, sel, 0.1, out=out)
+    assert out._version > old_out and q._version == old
+    B.ivf_check()
+    with torch.inference_mode():  # its tensors count no versions
+        y = torch.ones(3, 1, 64, device="cuda", dtype=torch.bfloat16)
+        z = torch.empty_like(y)
+    B.ivf_kv_append(y, y, y, kc, vc, plan.token_pos, plan.token_slot, q_out=z)
+    B.ivf_check()
