@@ -404,7 +404,7 @@ int ivf_pq_search(const void* queries, int64_t nq, int d, ivf_dtype qtype, const
  * on one stream.  The calls return without waiting.  They use none of the library's workspace: steps on other streams need no
  * order between them, and a step may be captured in a CUDA graph (after a first call of any size on the device) whatever is
  * called between its replays.  Sums, norms, scores
- * and softmax statistics are held in 32 bits.
+ * and softmax statistics are held in 32 bits; the softmax weights meet the values in 16 (see ivf_kv_attend).
  */
 typedef struct ivf_kv_cache {
     void* k;                /* element (page, kv head, token, i) at k + page*k_stride[0] + head*k_stride[1] + token*k_stride[2] + i */
@@ -495,6 +495,9 @@ int ivf_kv_select(const void* q, const int64_t q_stride[2], ivf_dtype dtype, int
  *                   last; a user's own choice is fine.  A block past the token's own is ignored.
  *   out             may be q itself with q's strides (the tokens are then taken singly); it must not share memory with q, the
  *                   caches or `selected` in any other way
+ * The weights are rounded to the cache's type, relative to a maximum, before they meet the values: an output is off by up to
+ * 2^-8 (IVF_BF16) or 2^-11 (IVF_F16) of the weighted mean of |v| beside its own rounding.  Tokens taken singly with up to 8 query
+ * heads to a kv head keep 16 or 22 bits of each weight.  The sum that divides them, and out_lse, are of the unrounded ones.
  * A token that sees nothing (padding, or no block selected) gets zeros and an out_lse of -infinity.  What pages hold past
  * a request's last token is never used, whatever it is.
  */

@@ -188,10 +188,11 @@ int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t
 
 int g_kv_attend = 0;  // test hook (ivf_debug_set_kv_attend): 0 = by the sizes, 1 = rows kernel only, 2 = tile kernel wherever it can run
 
-template <typename T, int DP>
+template <typename T, int DP, bool SPLIT>
 int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    auto kernel = kv_attend_rows_kernel<T, DP, SPLIT>;
     static KvSmemSeen seen;
-    if (int rc = kv_allow_smem(kv_attend_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
+    if (int rc = kv_allow_smem(kernel, RowsShape<DP>::kSmem, ctx, seen)) return rc;
     const int z = (p.group + 15) / 16;
     unsigned ranks = 1, x = static_cast<unsigned>(p.n_tokens);
     if (p.window) {  // what the tile kernel left: a few CTAs look for it
@@ -215,14 +216,18 @@ int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t s
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     g_launches.fetch_add(1);
-    CUDA_TRY(cudaLaunchKernelEx(&cfg, kv_attend_rows_kernel<T, DP>, p));
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
     return IVF_OK;
+}
+template <typename T, bool SPLIT>
+int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
+    if (p.dim <= 64) return kv_launch_rows<T, 64, SPLIT>(p, ctx, stream);
+    if (p.dim <= 128) return kv_launch_rows<T, 128, SPLIT>(p, ctx, stream);
+    return kv_launch_rows<T, 256, SPLIT>(p, ctx, stream);
 }
 template <typename T>
 int kv_launch_rows(const KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
-    if (p.dim <= 64) return kv_launch_rows<T, 64>(p, ctx, stream);
-    if (p.dim <= 128) return kv_launch_rows<T, 128>(p, ctx, stream);
-    return kv_launch_rows<T, 256>(p, ctx, stream);
+    return p.group <= 8 ? kv_launch_rows<T, true>(p, ctx, stream) : kv_launch_rows<T, false>(p, ctx, stream);
 }
 
 // A page of one head (64 tokens of it at most), 64 columns wide, with the 128-byte swizzle.

@@ -2,7 +2,10 @@
 //
 // out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), s_j = scale * q . k_j, over the tokens j of the selected
 // blocks at positions <= pos; lse = m + log(sum).  One pass over the keys with a running maximum and sum, both
-// in 32 bits; the exponentials are rounded to the cache's 16-bit type only as operands of the second product.
+// in 32 bits.  As operands of the second product the exponentials take the cache's 16-bit type, since the matrix instruction
+// wants one type for both: each is off by up to 2^-8 (bfloat16) or 2^-11 (float16) of itself, an output by as much of the
+// weighted mean of |v|.  Where it costs nothing, in the rows kernel for up to 8 query heads to a kv head, they are carried in two
+// parts, rounding and rest (2^-16, 2^-22).
 #pragma once
 #include "kv_common.cuh"
 
@@ -43,6 +46,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+__device__ __forceinline__ bool is_finite(float x) { return x - x == 0.0f; }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
     const int n = ok ? 16 : 0;  // the rest is filled with zeros
@@ -102,7 +107,11 @@ __device__ __forceinline__ uint32_t rows_addr(uint32_t base, int r, int c) {
     return base + r * (DP * 2) + ((c ^ (r & 7)) << 4);
 }
 
-template <typename T, int DP>
+//
+// SPLIT: at most 8 query heads.  The product's other 8 rows then take the second parts of the weights, and their sums are added at
+// the end.  (With rows of their own the second parts are a second product: 64 tokens by 8 heads of a group of 16 take
+// 121 us with it, 110 without, at the rate of the matrix instruction; so larger groups go without.)
+template <typename T, int DP, bool SPLIT>
 __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64_t t, const int rank, const int ranks, uint8_t* rows_smem, int* s_page, int* s_first, int& s_n) {
     using S = RowsShape<DP>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -220,11 +229,12 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
             }
         }
         // row lane / 4 (and + 8): tokens 2 (lane % 4), + 1, + 8, + 9
+        constexpr int kR = SPLIT ? 1 : 2;
         float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 2 * kR; ++i) {
                 const int tok = n * 8 + (lane & 3) * 2 + (i & 1);
                 sc[n][i] = tok <= seen ? sc[n][i] * p.scale_log2 : -INFINITY;
                 top[i >> 1] = fmaxf(top[i >> 1], sc[n][i]);
@@ -232,7 +242,7 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
         }
         float fix[2], base[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < kR; ++r) {
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], 1));
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], 2));
             const float mn = fmaxf(m[r], top[r]);
@@ -241,18 +251,23 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
             m[r] = mn;
         }
         float add[2] = {0.0f, 0.0f};
+        uint32_t pf[4];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sc[n][i] = exp2_fast(sc[n][i] - base[i >> 1]);
-                add[i >> 1] += sc[n][i];
+            for (int r = 0; r < kR; ++r) {
+                const float w0 = exp2_fast(sc[n][2 * r] - base[r]), w1 = exp2_fast(sc[n][2 * r + 1] - base[r]);
+                add[r] += w0 + w1;
+                pf[2 * n + r] = Pair16<T>::pack(w0, w1);
+                if (SPLIT) {
+                    const float2 first = Pair16<T>::unpack(pf[2 * n]);
+                    pf[2 * n + 1] = Pair16<T>::pack(w0 - first.x, w1 - first.y);
+                }
             }
         }
-        l[0] = l[0] * fix[0] + add[0];
-        l[1] = l[1] * fix[1] + add[1];
-        const uint32_t pf[4] = {Pair16<T>::pack(sc[0][0], sc[0][1]), Pair16<T>::pack(sc[0][2], sc[0][3]),
-                                Pair16<T>::pack(sc[1][0], sc[1][1]), Pair16<T>::pack(sc[1][2], sc[1][3])};
+        if (SPLIT) fix[1] = fix[0];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) l[r] = l[r] * fix[r] + add[r];
         if (__any_sync(0xFFFFFFFFu, fix[0] != 1.0f || fix[1] != 1.0f)) {
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i) {
@@ -270,6 +285,13 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
                 mma16816<T>(o[2 * n], pf, b[0], b[1]);
                 mma16816<T>(o[2 * n + 1], pf, b[2], b[3]);
             }
+        }
+    }
+    if (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) {  // an infinite value is infinite with the first parts; with the second ones it may be 0 * inf
+            o[i][0] += is_finite(o[i][0]) ? o[i][2] : 0.0f;
+            o[i][1] += is_finite(o[i][1]) ? o[i][3] : 0.0f;
         }
     }
     cp_async_wait<0>();
@@ -363,14 +385,14 @@ __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64
     __syncthreads();  // the next token's lists and ring lie over this one's
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool SPLIT>
 __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendParams p) {
     extern __shared__ __align__(128) uint8_t rows_smem[];
     __shared__ int s_page[kKvMaxSelect], s_first[kKvMaxSelect];
     __shared__ int s_n;
     if (p.window == 0) {
         const int ranks = static_cast<int>(cluster_size());
-        attend_rows<T, DP>(p, blockIdx.x / ranks, static_cast<int>(cluster_rank()), ranks, rows_smem, s_page, s_first, s_n);
+        attend_rows<T, DP, SPLIT>(p, blockIdx.x / ranks, static_cast<int>(cluster_rank()), ranks, rows_smem, s_page, s_first, s_n);
         return;
     }
     // what the tile kernel left: 32 tokens are looked at at a time (a mark is read by every warp before the first barrier
@@ -379,7 +401,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
         const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
         unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && *kv_mark(p, mine, blockIdx.y, blockIdx.z) == kKvLeft);
         for (; left; left &= left - 1)
-            attend_rows<T, DP>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
+            attend_rows<T, DP, SPLIT>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
     }
 }
 

@@ -98,6 +98,59 @@ def test_output_beside_the_queries(kernel):  # noqa: F811
     assert torch.equal(got, want) and torch.equal(both[:, 0], q)
 
 
+# ---------------------------------------------------------------------------------------------- weights of single tokens
+
+# For up to 8 query heads to a kv head a weight w (the largest is 1) meets the values as two 16-bit parts.  With u = 2^-8 or 2^-11 the first is within u w of it, the
+# second within u of that rest, or within 2^-25 where float16 has no finer steps: u^2 w + 2^-25 in all, which is
+# u^2 + 2^-25 / (smallest weight) of the weighted mean of |v|.  Each product of 16 tokens joins the sums in 32 bits with an
+# error of 2^-22 of them at most; a warp takes every fourth piece of 16 tokens, two products each.  The rest as in
+# test_gpu_kv.py: the output's own rounding, the logits', 2^-20.  (Weights of one part miss this by far.)
+@pytest.mark.parametrize("contexts,fresh,kv,group,dim,page,take,kind", [
+    ([20], 1, 2, 8, 128, 64, 2, "bf16"), ([33, 7], 2, 2, 7, 64, 16, 3, "fp16"), ([18] * 40, 1, 4, 4, 256, 32, 2, "bf16"),
+    ([50], 3, 1, 3, 96, 128, 1, "fp16"), ([16] * 70, 1, 8, 2, 128, 64, 1, "bf16"), ([900], 1, 2, 8, 128, 64, 12, "bf16"),
+])
+def test_weights_of_single_tokens_keep_their_bits(contexts, fresh, kv, group, dim, page, take, kind):
+    kc, vc, table, req, pos, q, sel = _attend_case(contexts, fresh, kv, group, dim, page, take, kind, "head", seed=take)
+    scale = 0.3 / math.sqrt(dim)  # many weights of much the same size
+    B.ivf_debug_set_kv_attend(1)
+    try:
+        got, _ = B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), scale)
+    finally:
+        B.ivf_debug_set_kv_attend(0)
+    B.ivf_check()
+    keys = np.nan_to_num(_np(kc))
+    out, _, size, unit = R.attend(_np(q), keys, np.nan_to_num(_np(vc)), table, req, pos, sel, scale)
+    least = np.ones(q.shape[:2])
+    for t in range(len(req)):
+        for h in range(kv):
+            k = np.concatenate([keys[table[req[t], b], h, : max(0, min(page, pos[t] + 1 - b * page))] for b in sel[t, h] if b >= 0])
+            z = _np(q)[t, h * group: (h + 1) * group] @ k.T * scale
+            least[t, h * group: (h + 1) * group] = np.exp(z.min(1) - z.max(1))
+    u = R.UNIT[kind]
+    parts = u * u + (2.0 ** -25 / least if kind == "fp16" else 0 * least) + 2 * R.ceil_div(take * page, 64) * 2.0 ** -22
+    tol = u * np.abs(out) + (parts + 2 * dim * 2.0 ** -24 * unit + 2.0 ** -20)[..., None] * size + R.TINY[kind]
+    d = np.abs(_np(got) - out)
+    assert (d <= tol).all(), (d / tol).max()
+
+
+@pytest.mark.parametrize("group", [3, 8, 9, 20])
+@pytest.mark.parametrize("dim,kind", [(64, "fp16"), (128, "bf16"), (256, "bf16")])
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_infinite_values_of_tokens_that_are_seen(kernel, fresh, group, dim, kind):  # noqa: F811
+    kc, vc, table, req, pos, q, sel = _attend_case([200], fresh, 1, group, dim, 32, 7, kind, "head", seed=group)
+    vc[int(table[0, 1]), 0, 3, :16] = math.inf
+    vc[int(table[0, 1]), 0, 4, 16:32] = -math.inf
+    scale = 0.1 / math.sqrt(dim)
+    got = _np(B.ivf_kv_attend(q, kc, vc, _i32(table), _i32(req), _i32(pos), _i32(sel), scale)[0])
+    B.ivf_check()
+    seen = (sel[:, 0] == 1).any(1)
+    assert seen.any()
+    assert (got[seen, :, :16] == math.inf).all() and (got[seen, :, 16:32] == -math.inf).all()
+    want = R.attend(_np(q), np.nan_to_num(_np(kc)), np.nan_to_num(_np(vc), posinf=0, neginf=0), table, req, pos, sel, scale)
+    got[seen, :, :32] = want[0][seen, :, :32]
+    _check_attend(torch.from_numpy(got), None, want, kind, dim)
+
+
 # ---------------------------------------------------------------------------------------------- graphs and streams
 
 def _mixed_windows(seed, requests, fresh, group=8, page=64):
