@@ -395,13 +395,18 @@ __global__ void __launch_bounds__(kRowsThreads) kv_attend_rows_kernel(KvAttendPa
         attend_rows<T, DP, SPLIT>(p, blockIdx.x / ranks, static_cast<int>(cluster_rank()), ranks, rows_smem, s_page, s_first, s_n);
         return;
     }
-    // what the tile kernel left: 32 tokens are looked at at a time (a mark is read by every warp before the first barrier
-    // that its token's row is written behind)
-    for (int64_t t0 = blockIdx.x; t0 < p.n_tokens; t0 += static_cast<int64_t>(gridDim.x) * 32) {
-        const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x & 31) * gridDim.x;
-        unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && *kv_mark(p, mine, blockIdx.y, blockIdx.z) == kKvLeft);
-        for (; left; left &= left - 1)
-            attend_rows<T, DP, SPLIT>(p, t0 + static_cast<int64_t>(__ffs(left) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
+    // what the tile kernel left: each thread looks at one token of the CTA's (its own CTA alone writes that token's row, behind
+    // the barrier)
+    __shared__ unsigned s_left[kRowsWarps];
+    for (int64_t t0 = blockIdx.x; t0 < p.n_tokens; t0 += static_cast<int64_t>(gridDim.x) * kRowsThreads) {
+        const int64_t mine = t0 + static_cast<int64_t>(threadIdx.x) * gridDim.x;
+        const unsigned left = __ballot_sync(0xFFFFFFFFu, mine < p.n_tokens && *kv_mark(p, mine, blockIdx.y, blockIdx.z) == kKvLeft);
+        if ((threadIdx.x & 31) == 0) s_left[threadIdx.x >> 5] = left;
+        if (!__syncthreads_or(left != 0)) continue;
+        for (int w = 0; w < kRowsWarps; ++w)
+            for (unsigned rest = s_left[w]; rest; rest &= rest - 1)
+                attend_rows<T, DP, SPLIT>(p, t0 + static_cast<int64_t>(w * 32 + __ffs(rest) - 1) * gridDim.x, 0, 1, rows_smem, s_page, s_first, s_n);
+        __syncthreads();  // the next round's words lie over these
     }
 }
 

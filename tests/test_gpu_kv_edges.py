@@ -216,6 +216,29 @@ def test_stale_outputs_are_not_taken_for_marks(kernel, kind):  # noqa: F811
     assert _same(got, want) and got.isfinite().all()
 
 
+def test_more_rows_left_than_one_look():
+    # nearly every window is left (requests of four tokens): several rounds of looking, and the same arithmetic as by themselves
+    n_req, kv, dim = 330, 40, 64
+    g = _gen(7)
+    kc, vc = (torch.randn(n_req, kv, 16, dim, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    req, pos = np.repeat(np.arange(n_req), 4), np.tile(np.arange(4), n_req)
+    req[500:540], pos[500:540] = 3, np.arange(4).repeat(10)  # and some that are not
+    q = torch.randn(len(req), kv * 2, dim, device="cuda", generator=g).to(torch.bfloat16)
+    sel = torch.zeros(len(req), kv, 2, dtype=torch.int32, device="cuda")
+    sel[:, :, 1] = -1
+    args = (q, kc, vc, _i32(np.arange(n_req)).view(-1, 1), _i32(req), _i32(pos), sel, 0.1)
+    got = []
+    try:
+        for forced in (1, 2):
+            B.ivf_debug_set_kv_attend(forced)
+            got.append(B.ivf_kv_attend(*args)[0])
+    finally:
+        B.ivf_debug_set_kv_attend(0)
+    B.ivf_check()
+    assert torch.equal(got[0][:448], got[1][:448]) and torch.equal(got[0][640:], got[1][640:])
+    assert got[1].isfinite().all() and (got[0] - got[1]).abs().max() < 0.1
+
+
 # ---------------------------------------------------------------------------------------------- tables: no room
 
 def test_tables_without_room_for_tokens_or_blocks():
