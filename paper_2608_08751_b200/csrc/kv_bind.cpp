@@ -107,7 +107,7 @@ void* dense(const at::Tensor& t, const char* name, at::ScalarType type, c10::Dev
 
 // A CUDA tensor whose last axis is contiguous.
 void* strided(const at::Tensor& t, const char* name, int dim, at::ScalarType type, c10::Device dev, int64_t* stride = nullptr) {
-    if (t.dim() != dim || !t.is_cuda() || t.device() != dev || t.scalar_type() != type || (t.numel() && t.stride(dim - 1) != 1))
+    if (t.dim() != dim || !t.is_cuda() || t.device() != dev || t.scalar_type() != type || (t.numel() && t.size(dim - 1) > 1 && t.stride(dim - 1) != 1))
         refuse(PyExc_ValueError, "%s must be a %d-D CUDA tensor of %s on %s with a contiguous last axis", name, dim, c10::toString(type),
                dev.str().c_str());
     if (stride)

@@ -444,3 +444,26 @@ def test_tensors_written_in_place_count_a_version():
         z = torch.empty_like(y)
     B.ivf_kv_append(y, y, y, kc, vc, plan.token_pos, plan.token_slot, q_out=z)
     B.ivf_check()
+
+
+# ---------------------------------------------------------------------------------------------- axes of one element
+
+def test_axes_of_one_element_may_carry_any_stride():
+    # a table of one column cut out of a wider tensor crosswise, caches and queries of one head or token likewise
+    n, dim = 5, 64
+    kc, vc, table, req, pos, q, sel = _attend_case([16] * n, 1, 1, 1, dim, 16, 1, "bf16", "head", seed=4)
+    one = _i32(table[:, :1])
+    want, _ = B.ivf_kv_attend(q, kc, vc, one, _i32(req), _i32(pos), _i32(sel), 0.1)
+    for odd in (torch.as_strided(one, (n, 1), (1, 7)), torch.as_strided(one, (n, 1), (1, 0))):
+        got, _ = B.ivf_kv_attend(q, kc, vc, odd, _i32(req), _i32(pos), _i32(sel), 0.1)
+        assert torch.equal(got, want)
+        codes = torch.ones(kc.shape[0], 1, dim, dtype=torch.int8, device="cuda")
+        ids = B.ivf_kv_select(q, codes, torch.ones(kc.shape[0], 1, device="cuda"), odd, _i32(req), _i32(pos), 16, 2)
+        assert _np(ids)[:, 0].tolist() == [[0, -1]] * n
+        plan = B.ivf_kv_tables(_i32([1] * n), _i32([1] * n), _i32([0]), odd, 16, n)
+        assert _np(plan.token_slot).tolist() == [int(p) * 16 + 1 for p in table[:, 0]]
+    wide = torch.zeros(n, 3, dim, dtype=q.dtype, device="cuda")
+    wide[:, :1] = q
+    got, _ = B.ivf_kv_attend(torch.as_strided(wide, (n, 1, dim), (3 * dim, 5, 1)), kc, vc, one, _i32(req), _i32(pos), _i32(sel), 0.1)
+    assert torch.equal(got, want)
+    B.ivf_check()
