@@ -278,7 +278,7 @@ int kv_launch_attend(KvAttendParams& p, const DeviceCtx& ctx, cudaStream_t strea
     p.limit_ns = g_wait_limit_ns.load();
     CUtensorMap mk, mv;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    bool tile = g_kv_attend != 1 && p.dim >= 64 && p.max_blocks < kTileMaxBlocks && p.num_pages > 0;
+    bool tile = g_kv_attend != 1 && p.dim >= 64 && p.num_pages > 0;
     // Windows pay where there is work for the whole card and tokens enough beyond one to a request to fill some; what they do
     // not take is left to the rows.  16 blocks of 64 keys, d = 128, rows / windows: 64 tokens by 4 heads of a group of 8
     // 31 / 43 us, 256 tokens 86 / 43, 512 tokens of 32 requests 152 / 43; by 8 heads without groups (128 tokens to a

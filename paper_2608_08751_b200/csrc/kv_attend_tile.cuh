@@ -99,17 +99,6 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, ui
         ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-        : "memory");
-}
 // 16 columns, the wait included.
 __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
@@ -130,9 +119,6 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
 // Two 32-bit numbers in one 64-bit register pair: sm_100 multiplies and adds them in one instruction.
 __device__ __forceinline__ uint64_t pair32(float a, float b) {
     uint64_t d;
@@ -181,9 +167,6 @@ __device__ __forceinline__ uint32_t tile_idesc(int n, bool b_mn) {
     return (1u << 4) | (UmmaType<T>::kFormat << 7) | (UmmaType<T>::kFormat << 10) | (b_mn ? 1u << 16 : 0u) |
            (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
-
-constexpr uint32_t kNoKey = 0xFFFFFFFFu;
-constexpr int kTileMaxBlocks = 1 << 24;  // block number and segment share a key
 
 template <typename T, int DB>
 __global__ void __launch_bounds__(TileShape<DB>::kThreads, TileShape<DB>::kCtas)
@@ -369,7 +352,7 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 for (int half = 0; half < halves; ++half) {
                     atomicOr(tok < 32 ? &c.box[at + half].members : &c.more[at + half][(tok >> 5) - 1], 1u << (tok & 31));
                     c.box[at + half].first = first + half * 64;
-                    c.box[at + half].dead = max(0, min(box, last_pos + 1 - first - half * 64));
+                    c.box[at + half].dead = max(0, min(box - 1, last_pos - first - half * 64) + 1);
                     c.box[at + half].page = c.req[tok];  // whose page: looked up below
                 }
             });
@@ -538,13 +521,14 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         for (int j = 0; j < tiles; ++j) {
             const int b0 = j * per_tile, n_boxes = min(per_tile, boxes - b0);
             const uint32_t t_p = t_rows + S::kPCol + (j & 1) * (S::kKeys / 2);
-            // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees
-            int seen = (members_of(b0, ahead.members) & bit) ? min(max(pos + 1 - ahead.first, 0), box) : 0;
+            // groups of 16 keys that the row sees: whole ones, and one whose first `rem` keys it sees (a position may be
+            // 2^31 - 1: one is added after the minimum)
+            int seen = (members_of(b0, ahead.members) & bit) ? max(min(pos - ahead.first, box - 1) + 1, 0) : 0;
             uint32_t full = (1u << (seen >> 4)) - 1, part = seen & 15 ? 1u << (seen >> 4) : 0u;
             int rem = seen & 15;
             bool tail = ahead.dead < box;
             for (int i = 1; i < n_boxes; ++i) {
-                seen = (members_of(b0 + i, c.box[b0 + i].members) & bit) ? min(max(pos + 1 - c.box[b0 + i].first, 0), box) : 0;
+                seen = (members_of(b0 + i, c.box[b0 + i].members) & bit) ? max(min(pos - c.box[b0 + i].first, box - 1) + 1, 0) : 0;
                 const int g0 = (i << box_shift) >> 4;
                 full |= ((1u << (seen >> 4)) - 1) << g0;
                 if (seen & 15) {

@@ -467,3 +467,22 @@ def test_axes_of_one_element_may_carry_any_stride():
     got, _ = B.ivf_kv_attend(torch.as_strided(wide, (n, 1, dim), (3 * dim, 5, 1)), kc, vc, one, _i32(req), _i32(pos), _i32(sel), 0.1)
     assert torch.equal(got, want)
     B.ivf_check()
+
+
+# ---------------------------------------------------------------------------------------------- the longest requests
+
+@pytest.mark.parametrize("dim,fresh", [(64, 1), (128, 40)])
+def test_positions_up_to_the_last_number(kernel, dim, fresh):  # noqa: F811
+    # a request whose last token has position 2^31 - 1, in a table of 2^24 columns
+    page, columns = 128, 1 << 24
+    g = _gen(dim)
+    kc, vc = (torch.randn(5, 1, page, dim, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    table = np.full((1, columns), -1, np.int32)
+    blocks = [0, 7, columns // 2, columns - 2, columns - 1]
+    table[0, blocks] = [3, 1, 4, 0, 2]
+    pos = np.arange(2 ** 31 - fresh, 2 ** 31)
+    req = np.zeros(fresh, np.int64)
+    sel = np.tile(np.array(blocks)[None, None], (fresh, 1, 1))
+    sel[::3, 0] = [0, 7, columns // 2, columns - 1, -1]
+    q = torch.randn(fresh, 4, dim, device="cuda", generator=g).to(torch.bfloat16)
+    _against_plain((kc, vc, table, req, pos, q, sel), 0.125, "bf16", dim)
