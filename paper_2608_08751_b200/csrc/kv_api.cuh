@@ -165,7 +165,8 @@ template <typename T>
 int kv_launch_select(const KvSelectParams& p, const DeviceCtx& ctx, cudaStream_t stream) {
     bool windows = g_kv_select != 1 && p.max_blocks <= kSelWindowBlocks;
     // Single tokens read a row's codes once for each token, windows once for 16; a window starts slower, and takes the requests
-    // in it one after the other.  256 blocks of d = 128, rows / windows: 16 tokens by 8 heads 13 / 19 us, 256 by 4
+    // in it one after the other.  (Heads wider than 192 spill there and still win: 4,096 tokens by 4 heads of 512 blocks, d = 256,
+    // windows 100 us, rows 299; d = 224 117 and 326; d = 128 66 and 242.)  256 blocks of d = 128, rows / windows: 16 tokens by 8 heads 13 / 19 us, 256 by 4
     // heads 23 / 19, 256 by 8 heads 33 / 19, 512 by 8 heads of 32 requests 54 / 21, but 64 by 8 heads of 32 requests 15 / 47.
     if (g_kv_select == 0)
         windows = windows && p.n_tokens * p.n_kv_heads >= 6 * ctx.num_sms && p.n_tokens >= 2 * static_cast<int64_t>(p.n_req);

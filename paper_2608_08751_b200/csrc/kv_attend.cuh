@@ -84,7 +84,7 @@ __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uin
 // product, the keys come in pieces of 16 tokens.  Each warp takes pieces of its own through a ring of its own
 // and keeps its own running maximum, sum and output; the warps meet once, at the end, and then the cluster's CTAs,
 // through each other's shared memory.  Bound by the selected pages' bytes: 64 tokens by 8 heads of 32 pages, 537 MB, in
-// 92 us (5.8 TB/s, 0.90 of a copy's rate); one token by 4 heads of 96, 3 MB, in 9.3 us, a chain of waits: request, block,
+// 92 us (5.8 TB/s, 0.90 of a copy's rate); one token by 4 heads of 96, 3 MB, in 9.1 us, a chain of waits: request, block,
 // page, keys, and two meetings.
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = kRowsWarps * 32;
@@ -109,8 +109,8 @@ __device__ __forceinline__ uint32_t rows_addr(uint32_t base, int r, int c) {
 
 //
 // SPLIT: at most 8 query heads.  The product's other 8 rows then take the second parts of the weights, and their sums are added at
-// the end.  (With rows of their own the second parts are a second product: 64 tokens by 8 heads of a group of 16 take
-// 121 us with it, 110 without, at the rate of the matrix instruction; so larger groups go without.)
+// the end.  (With rows of their own the second parts are a second product: 64 tokens by 8 heads of a group of 16 took
+// 121 us with it, next to the first or apart from it, 110 without; so larger groups go without.)
 template <typename T, int DP, bool SPLIT>
 __device__ __forceinline__ void attend_rows(const KvAttendParams& p, const int64_t t, const int rank, const int ranks, uint8_t* rows_smem, int* s_page, int* s_first, int& s_n) {
     using S = RowsShape<DP>;

@@ -20,9 +20,10 @@
 //
 // 4,096 tokens of two requests by 4 heads of a group of 8, d = 128, 16 of up to 512 blocks of 64: 160 us, 430 TFLOP/s of
 // useful products.  The 16 tokens of a window select 23 blocks between them, so 1.45 times the useful work is done.  A
-// tile takes a CTA 1.24 us, nearly all of it one softmax warp's dependent instructions (2,300 cycles, half of
-// them exponentials at the rate of the unit that two CTAs share); the products take 350 of them.  5 us of a CTA's 37 go
-// into queries and plan, 3 into the output, partly under the other CTA's work.
+// tile takes a CTA 1.24 us, nearly all of it one softmax warp's dependent instructions (2,300 cycles; the products take 350 of
+// them, and no unit is full: issue slots 34 %, tensor pipe 32 %, exponentials 28 %).  5 us of a CTA's 37 go
+// into queries and plan, 3 into the output, partly under the other CTA's work.  (Weights in two parts, as the rows kernel has
+// them, were right and took 219 us in place of 163: the parts are made in the same warps.)
 //
 // What a page holds past the window's last token may be anything: those value rows are zeroed in shared memory.  A
 // value that is not finite at a token that only some rows see turns the other rows' sums into NaN (0 * NaN);
@@ -43,7 +44,11 @@ struct TileShape {
     static constexpr int kPlaneBytes = DB * kBlockBytes;
     static constexpr int kStageBytes = 2 * kPlaneBytes;
     static constexpr int kQBytes = DB * 128 * 128;
-    static constexpr int kBoxes = 320;                  // of a plan
+    // Of a plan: as many as fit beside two CTAs' tiles on an SM.  Windows win where they fit (2,048 tokens of one request by 4 heads
+    // of a group of 8, windows / rows kernel): 64 blocks of 64 keys a token, 90 to a window 263 / 1,958 us; 16 blocks a
+    // token that hardly agree, 170 to a window 402 / 567.  What does not fit costs the plan on top of the rows: 537 blocks to
+    // a window 1,973 / 1,976, 256 blocks of 16 keys a token, 346 to a window 2,178 / 2,078.
+    static constexpr int kBoxes = 320;
     static constexpr int kMapWords = 1024;              // bitmap of 32,768 blocks at a time, in the ring before the loop
     static constexpr int kRows = 128;
     static constexpr int kWarps = 5;                    // softmax 0-3, issuer 4

@@ -13,8 +13,10 @@
 //
 //   rows     (single and drafted tokens) a cluster of CTAs shares the blocks of one (token, kv head), 4-byte dot products
 //            straight from the loads; the keys meet in the first CTA's shared memory.  32 requests of up to 4,096 blocks by 8
-//            heads: 89 MB of codes in 38 us, of which the scores take 15 (at the memory's rate), what comes before and
-//            after them (the query's code, the short list) the rest; 2,048 blocks of one request 10 us.
+//            heads: 89 MB of codes in 37 us from call to call (14 at a copy's rate).  Stamps in the kernel: all CTAs run after
+//            1.7 us, the last query is coded at 6.8, the scores are there at 19 on average and at 27 for the longest
+//            rows (contexts are ragged, each row has the same three CTAs), the short list takes 4 more and the ids 2; the rest is
+//            the change of kernels.  2,048 blocks of one request 11 us.
 //   windows  (prompts) 16 tokens by one kv head to a CTA, scores by the integer matrix instruction, a warp selects a row.
 //            Bound by the selection's instructions (about 2,500 of a warp for a row of 512 blocks): 16,384 rows in 57 us.
 #pragma once
@@ -26,8 +28,14 @@ constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelMaxBlocks = 49152;  // keys of one row in shared memory
 constexpr int kSelWindow = 16;        // tokens of a window: rows of the matrix instruction
-constexpr int kSelWindowList = 192;     // of a row's short list
-constexpr int kSelWindowBlocks = 2688;  // blocks that a window's keys, pages and scales have room for
+// A row's short list.  What does not fit goes bit by bit over the whole row.  4,096 tokens by 4 heads of 512 random blocks,
+// windows / rows kernel: 16 blocks a token 66 / 242 us, 48 70 / 250, 64 (of which the bound lets 227 through) 127 / 254, 256
+// 117 / 299.
+constexpr int kSelWindowList = 192;
+// Blocks that a window's keys, pages and scales have room for in shared memory: not where the kernels cross.  Windows / rows
+// kernel by blocks of a request (16 a token): 512 66 / 244 us, 1,024 139 / 348, 2,048 297 / 582, 2,688 358 / 735.
+// The room is taken by the table's columns, not by the blocks in use: 512 blocks in a table of 1,024 columns 92 us, of 2,688 137.
+constexpr int kSelWindowBlocks = 2688;
 
 struct KvSelectParams {
     const void* q;
@@ -211,7 +219,10 @@ __device__ __forceinline__ void sel_finish(const uint32_t* key, const int* id, i
 // ---------------------------------------------------------------------------------------------- rows
 constexpr int kSelRowThreads = 128, kSelRowWarps = kSelRowThreads / 32;
 constexpr int kSelRowCtas = 6;  // on an SM
-constexpr int kSelList = 1024;  // of a row's short list
+// A row's short list.  Above 256 blocks a token there is no bound, and rows longer than the list go bit by bit: 32 requests by 8 heads
+// of 2,048 blocks, 64 blocks a token 37 us, 128 39, 256 and 512 55.  (A table of more columns than 8,192 costs CTAs on an SM:
+// 512 blocks in 2,048 columns 21 us, in 16,384 31, in 49,152 66.)
+constexpr int kSelList = 1024;
 
 // L lanes to a block's codes, NP pieces of 16 bytes each (16 L NP >= dim); four blocks of a lane group are in flight, their
 // pages are fetched a step ahead.  Few lanes to a block: what is not a load is paid once for a block and lane.

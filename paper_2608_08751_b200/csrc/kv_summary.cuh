@@ -7,7 +7,8 @@
 // Bound by memory: fill * D keys are read once, D + 4 bytes written.  One CTA per (page, head): D / 8 lanes
 // span a token row with 16-byte loads, all loads of a thread are independent, and ten CTAs an SM keep enough of them
 // under way (8,192 pages of 64 tokens by 8 heads of 128: 1.08 GB in 195 us, 5.5 TB/s; with room for 128 tokens in
-// every thread's registers 260 us).
+// every thread's registers 260 us).  Wide heads with pages of 128 tokens do not fit the registers and spill: the same bytes by
+// heads of 256 at 3.5 TB/s, of 192 at 3.1; with pages of 64 at 5.2.
 #pragma once
 #include "kv_common.cuh"
 
