@@ -396,7 +396,8 @@ int ivf_pq_search(const void* queries, int64_t nq, int d, ivf_dtype qtype, const
  * A cache holds pages of `page_size` tokens (16, 32, 64 or 128); block j of a request is the page that its
  * row of the block table names.  Element types are IVF_F16 and IVF_BF16, head_dim a multiple of 16 up to 256,
  * n_heads a multiple of n_kv_heads with at most 64 query heads to a kv head.  Strides are in elements,
- * non-negative multiples of 8; the head_dim axis is contiguous; base addresses are 16-byte aligned.  All
+ * non-negative multiples of 8; the head_dim axis is contiguous; base addresses are 16-byte aligned.  What is read may be
+ * expanded (a stride of 0); a tensor that is written with two elements in one place is refused.  All
  * arrays are device memory.  A step of a server is
  *
  *   ivf_kv_tables -> ivf_kv_append -> ivf_kv_summarize -> ivf_kv_select -> ivf_kv_attend

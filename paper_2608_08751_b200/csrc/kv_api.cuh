@@ -32,6 +32,23 @@ int kv_check_rows(const char* what, const void* p, const int64_t* stride, int n)
             return fail(IVF_ERR_INVALID_ARG, "%s: stride %lld must be a non-negative multiple of 8 elements", what, (long long)stride[i]);
     return IVF_OK;
 }
+// A tensor that is written: no two elements in one place.  Axes of one element do not count, the others lie within each other.
+int kv_check_apart(const char* what, const int64_t* stride, std::initializer_list<int64_t> size, int dim) {
+    std::pair<int64_t, int64_t> axis[3];
+    int n = 0, i = 0;
+    for (int64_t s : size) {
+        if (s > 1) axis[n++] = {stride[i], s};
+        ++i;
+    }
+    std::sort(axis, axis + n);
+    int64_t span = dim;
+    for (i = 0; i < n; ++i) {
+        if (axis[i].first < span)
+            return fail(IVF_ERR_INVALID_ARG, "%s is written: its stride of %lld elements must not be below %lld", what, (long long)axis[i].first, (long long)span);
+        span += (axis[i].second - 1) * axis[i].first;
+    }
+    return IVF_OK;
+}
 int kv_check_cache(const ivf_kv_cache* c, bool keys, bool values) {
     if (!c) return fail(IVF_ERR_INVALID_ARG, "null cache descriptor");
     if (c->dtype != IVF_F16 && c->dtype != IVF_BF16)
@@ -369,7 +386,10 @@ int ivf_kv_append(const void* q, const int64_t q_stride[2], const void* k, const
     if (!(eps >= 0.0f)) return fail(IVF_ERR_INVALID_ARG, "eps must not be negative");
     if (n_tokens == 0) return IVF_OK;
     if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("k", k, k_stride, 2)) != IVF_OK ||
-        (rc = kv_check_rows("v", v, v_stride, 2)) != IVF_OK || (rc = kv_check_rows("q_out", q_out, q_out_stride, 2)) != IVF_OK)
+        (rc = kv_check_rows("v", v, v_stride, 2)) != IVF_OK || (rc = kv_check_rows("q_out", q_out, q_out_stride, 2)) != IVF_OK ||
+        (rc = kv_check_apart("q_out", q_out_stride, {n_tokens, n_heads}, cache->head_dim)) != IVF_OK ||
+        (rc = kv_check_apart("key cache", cache->k_stride, {cache->num_pages, cache->n_kv_heads, cache->page_size}, cache->head_dim)) != IVF_OK ||
+        (rc = kv_check_apart("value cache", cache->v_stride, {cache->num_pages, cache->n_kv_heads, cache->page_size}, cache->head_dim)) != IVF_OK)
         return rc;
     if (!token_pos || !token_slot || (rot_dim > 0 && !rotary)) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
     if (kv_misaligned(rotary, 16) || kv_misaligned(q_weight, 16) || kv_misaligned(k_weight, 16))
@@ -457,7 +477,9 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
     if (!(scale - scale == 0.0f)) return fail(IVF_ERR_INVALID_ARG, "scale must be finite");
     if (n_tokens == 0) return IVF_OK;
     if ((rc = kv_check_tokens(table, table_stride, n_req, max_blocks, token_req, token_pos)) != IVF_OK) return rc;
-    if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("out", out, out_stride, 2)) != IVF_OK) return rc;
+    if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("out", out, out_stride, 2)) != IVF_OK ||
+        (rc = kv_check_apart("out", out_stride, {n_tokens, n_heads}, cache->head_dim)) != IVF_OK)
+        return rc;
     if (n_tokens > kKvMaxTokens / 8) return fail(IVF_ERR_UNSUPPORTED, "at most 2^28 - 1 tokens");
     if (!selected) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
     DeviceCtx* pctx = nullptr;

@@ -36,3 +36,44 @@ def test_tables_neighbours_are_not_refused():
     assert not refused(tokens=0, req=PLACES["cached"], pos=PLACES["cached"], slot=PLACES["cached"])
     assert not refused(stride=512, free=PLACES["table"] + 32, nf=16)  # between two rows
     assert not refused(stride=512, n=2, free=PLACES["table"] + 2048 + 32, nf=100, lens=P + 40000, start=P + 41000)  # behind the last one
+
+
+def _s(*v):
+    return (ctypes.c_int64 * len(v))(*v)
+
+
+def _cache(ks=(4096, 1024, 64), vs=(4096, 1024, 64), pages=10, kv=2):
+    return ctypes.byref(B._KvCache(P, P, _s(*ks), _s(*vs), pages, 16, kv, 64, B.IVF_BF16))
+
+
+def _append(n=4, heads=4, out=(256, 64), cache=None):
+    return B.lib().ivf_kv_append(P, _s(0, 0), P, _s(0, 0), P, _s(0, 0), n, heads, cache or _cache(), P, P, None, 0, 0, 0, None, None, 1e-6, P, _s(*out), None)
+
+
+def _attend(n=4, heads=4, out=(256, 64), cache=None):
+    return B.lib().ivf_kv_attend(P, _s(0, 0), n, heads, cache or _cache(), P, 8, 2, 8, P, P, P, 4, 1.0, P, _s(*out), None, None)
+
+
+def _written(rc):
+    return rc == B.IVF_ERR_INVALID_ARG and b"is written" in B.lib().ivf_last_error()
+
+
+def test_written_tensors_with_two_elements_in_one_place():
+    for call in (_append, _attend):
+        for out in ((0, 64), (256, 0), (248, 64), (256, 56), (64, 192)):
+            assert _written(call(out=out)), (call, out)
+    for bad in ((0, 1024, 64), (4096, 0, 64), (4096, 1024, 0), (4096, 1016, 64), (2040, 1024, 64)):
+        assert _written(_append(cache=_cache(ks=bad))) and _written(_append(cache=_cache(vs=bad))), bad
+
+
+def test_what_is_only_read_may_be_expanded():
+    import torch
+    if torch.cuda.is_available():
+        return  # (these are host addresses)
+    # what follows the argument checks needs a device: any other answer will do.  Axes of one element, heads outside of
+    # tokens, and a token axis outside of pages are fine
+    assert not _written(_attend(cache=_cache(ks=(0, 0, 0), vs=(0, 0, 0))))
+    for call in (_append, _attend):
+        assert not _written(call()) and not _written(call(n=1, out=(0, 64))) and not _written(call(n=4, heads=2, out=(64, 256)))
+    assert not _written(_append(cache=_cache(ks=(2048, 64, 128), vs=(128, 64, 1280))))
+    assert not _written(_append(cache=_cache(ks=(0, 1024, 64), vs=(0, 1024, 64), pages=1)))
