@@ -110,6 +110,8 @@ void* strided(const at::Tensor& t, const char* name, int dim, at::ScalarType typ
     if (t.dim() != dim || !t.is_cuda() || t.device() != dev || t.scalar_type() != type || (t.numel() && t.size(dim - 1) > 1 && t.stride(dim - 1) != 1))
         refuse(PyExc_ValueError, "%s must be a %d-D CUDA tensor of %s on %s with a contiguous last axis", name, dim, c10::toString(type),
                dev.str().c_str());
+    for (int i = 1; i < dim; ++i)  // the library takes these as 32-bit numbers
+        if (t.size(i) > INT32_MAX) refuse(PyExc_ValueError, "%s: axis %d has %lld elements", name, i, static_cast<long long>(t.size(i)));
     if (stride)
         for (int i = 0; i < dim - 1; ++i) stride[i] = t.size(i) > 1 ? t.stride(i) : 0;  // an axis of one element may carry any stride
     no_grad(t, name);
@@ -146,6 +148,7 @@ Table table_of(const at::Tensor& t, c10::Device dev) {
     Table r;
     int64_t s;
     r.p = static_cast<int32_t*>(strided(t, "table", 2, at::kInt, dev, &s));
+    if (t.size(0) > INT32_MAX) refuse(PyExc_ValueError, "table: at most 2^31 - 1 rows");
     r.n = static_cast<int>(t.size(0));
     r.columns = static_cast<int>(t.size(1));
     r.stride = r.n > 1 ? s : r.columns;

@@ -486,3 +486,17 @@ def test_positions_up_to_the_last_number(kernel, dim, fresh):  # noqa: F811
     sel[::3, 0] = [0, 7, columns // 2, columns - 1, -1]
     q = torch.randn(fresh, 4, dim, device="cuda", generator=g).to(torch.bfloat16)
     _against_plain((kc, vc, table, req, pos, q, sel), 0.125, "bf16", dim)
+
+
+# ---------------------------------------------------------------------------------------------- axes that are too long
+
+def test_axes_past_32_bits_are_refused():
+    # expanded, so that they cost no memory; cut to 32 bits the head count would be 4
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1, 2 ** 32 + 4, 64)
+    codes, scales = torch.zeros(1, 4, 64, dtype=torch.int8, device="cuda"), torch.zeros(1, 4, device="cuda")
+    with pytest.raises(ValueError, match="axis 1"):
+        B.ivf_kv_select(q, codes, scales, _i32([[0]]), _i32([0]), _i32([0]), 16, 1)
+    kc = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1, 1, 2 ** 32 + 16, 64)
+    with pytest.raises(ValueError, match="axis 2"):
+        B.ivf_kv_summarize(kc, _i32([0]), _i32([1]), codes[:, :1].contiguous(), scales[:, :1].contiguous())
+    B.ivf_check()
