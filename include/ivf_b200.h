@@ -71,7 +71,7 @@ typedef enum {
     IVF_ERR_DEVICE_TIMEOUT = -5, /* a bounded device-side wait expired; results are invalid       */
     IVF_ERR_BAD_ID = -6,         /* an id, page, position or length was out of range and skipped  */
     IVF_ERR_BOUNDS = -7,         /* checked build only: an index check inside a kernel failed     */
-    IVF_ERR_NO_PAGES = -8        /* ivf_kv_tables: too few free pages, columns, tokens or blocks  */
+    IVF_ERR_NO_PAGES = -8        /* ivf_kv_tables, ivf_kv_fork: too few free pages, columns, ...  */
 } ivf_status;
 
 /*
@@ -506,10 +506,79 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
                   const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_req,
                   const int32_t* token_pos, const int32_t* selected, int n_select, float scale, void* out,
                   const int64_t out_stride[2], float* out_lse, void* stream);
+/*
+ * Attention of each request's new tokens over its whole cache (a prompt's chunk, one token, a few drafted ones):
+ * out = softmax(z) V for every query head, out_lse as in ivf_kv_attend, with the logits
+ *   z = scale * q.k;  cap > 0:  z = cap * tanh(scale * q.k / cap);  slopes:  z - slopes[head] * |p - key|
+ * of the keys that a token at position p of its request sees: key < kv_lens[b], and key <= p or key < prefix[b], and
+ * (window > 0) p - key < window.
+ *   token_start     [n_req + 1] as ivf_kv_tables gives it: request b has rows token_start[b] .. token_start[b + 1] - 1 of q and out.
+ *                   Rows from n_tokens on do not exist; rows that belong to no request get zeros and an out_lse of -infinity
+ *   kv_lens         [n_req] tokens in the cache, the new ones among them: they are the last ones.  n_req <= 16384
+ *   slopes          [n_heads] float32, or NULL: no bias.  prefix [n_req], or NULL: none (a negative one counts as 0)
+ *   out             must not share memory with q (refused), the caches or the workspace
+ *   workspace       what ivf_kv_attend_chunk_workspace says for the same sizes, 16-byte aligned.  It is written and read by this call alone;
+ *                   two calls that may run at the same time need one each
+ * The tokens of a request with fewer tokens in the cache than new ones see nothing (zeros; -infinity); one whose rows of token_start
+ * descend has none.  Both set IVF_ERR_BAD_ID, as a page past the cache and a length past the table's columns do; a page that is missing (-1), and what lies past the
+ * columns, is not seen.  What pages hold past a request's last token, or before every window, is never used; a value that is not
+ * finite reaches only the tokens that see it.  The weights are rounded as in ivf_kv_attend.  The result is the same on every call.
+ */
+int ivf_kv_attend_chunk_workspace(int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, int n_req, int64_t* bytes);
+int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_tokens, int n_heads, const ivf_kv_cache* cache,
+                        const int32_t* table, int64_t table_stride, int n_req, int max_blocks, const int32_t* token_start,
+                        const int32_t* kv_lens, float scale, float cap, const float* slopes, int window, const int32_t* prefix, void* out,
+                        const int64_t out_stride[2], float* out_lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The pages' life.  Nothing is counted from step to step: the pages that are held are those of the table's rows, so a request ends when
+ * its row is left out, and the list of free pages is made anew.  The plans below name pages to be copied; ivf_kv_copy does it in each
+ * layer's cache, on the same stream, before the next tokens are appended.
+ *
+ * ivf_kv_fork: out_table's row i [n_new][max_blocks] holds the first keep[i] tokens (keep NULL: all) of row parent[i] of the table
+ * [n_old][max_blocks]; parent -1: an empty row.  Rows may have the same parent.  Blocks that the kept tokens fill are shared.  A
+ * block that they fill in part will be appended to, so it has one holder: the page stays with the lowest row that ends in it, unless some
+ * row shares it as filled; every other such row gets a page of its own,
+ *   copy_from, copy_to, copy_fill  [n_new] and copies the first copy_fill[i] tokens of page copy_from[i] onto page copy_to[i]; -1, -1, 0
+ *                   where a row needs no copy
+ *   out_lens        [n_new] tokens of each row (keep, or the parent's length)
+ *   free_pages      [num_pages] the pages that no row holds, ascending, those taken for copies left out; -1 behind them.  Copies take the
+ *                   lowest ones in row order.  n_free [1] how many they are
+ * Columns of out_table behind a row's blocks get -1.  Where pages do not suffice the rows of the surplus copies get -1 in their last block
+ * (and no copy) and the status word IVF_ERR_NO_PAGES.  A parent past the table, a length or a keep that is negative, past the parent's or past the
+ * columns gives an empty row, a page past num_pages counts as missing (-1); both set IVF_ERR_BAD_ID.  The outputs must not lie over the
+ * inputs (refused).  n_old, n_new <= 16384.
+ *
+ * ivf_kv_compact: with n_held pages held, the held pages from number n_held on move into the holes below it, the highest into the lowest
+ * hole, max_moves of them at most (the highest first); afterwards, if all are made, pages n_held and up are free.
+ *   out_table       [n_req][max_blocks] the table with the new numbers, -1 behind a row's blocks; may be the table itself
+ *   copy_from, copy_to  [max_moves] the moves, -1 behind them; no page is in both lists.  n_held [1]
+ *
+ * workspace: what ivf_kv_pages_workspace says for the same sizes (n_new or n_req rows), 16-byte aligned; 0 bytes for small ones.
+ */
+int ivf_kv_pages_workspace(int n_new, int max_blocks, int64_t num_pages, int64_t* bytes);
+int ivf_kv_fork(const int32_t* table, int64_t table_stride, const int32_t* kv_lens, int n_old, int max_blocks, const int32_t* parent,
+                const int32_t* keep, int n_new, int64_t num_pages, int page_size, int32_t* out_table, int64_t out_stride, int32_t* out_lens,
+                int32_t* copy_from, int32_t* copy_to, int32_t* copy_fill, int32_t* free_pages, int32_t* n_free, void* workspace,
+                int64_t workspace_bytes, void* stream);
+int ivf_kv_compact(const int32_t* table, int64_t table_stride, const int32_t* kv_lens, int n_req, int max_blocks, int64_t num_pages,
+                   int page_size, int32_t* out_table, int64_t out_stride, int32_t* copy_from, int32_t* copy_to, int64_t max_moves,
+                   int32_t* n_held, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Copies pages inside a layer's cache: the first copy_fill[i] tokens (NULL: all) of page copy_from[i] onto page copy_to[i], for every kv head of
+ * keys and values, and the page's summary (codes, scales of ivf_kv_summarize; NULL: none).  A page -1 in either list, or a fill of 0 or
+ * less, is padding.  A page past the cache or a fill past the page size is skipped and sets IVF_ERR_BAD_ID.  A page that is copied to must not be
+ * in the list twice nor be copied from in the same call.
+ */
+int ivf_kv_copy(const ivf_kv_cache* cache, const int32_t* copy_from, const int32_t* copy_to, const int32_t* copy_fill, int64_t n, int8_t* codes,
+                float* scales, void* stream);
+
 /* Test hook: 0 = the kernel of ivf_kv_attend is chosen by the sizes, 1 = always the one that takes tokens singly,
  * 2 = the one that takes windows of tokens wherever it can run. */
 int ivf_debug_set_kv_attend(int kernel);
 int ivf_debug_set_kv_select(int kernel);  /* the same for ivf_kv_select */
+int ivf_debug_set_kv_chunk(int kernel);   /* the same for ivf_kv_attend_chunk: 1 = tiles of 16 rows, 2 = tiles of 128 or 256 wherever they can run */
 
 #ifdef __cplusplus
 }

@@ -29,7 +29,8 @@ EXPORTS = (
     "ivf_route_prepared",
     "ivf_pq_encode", "ivf_pq_search", "ivf_pq_residuals", "ivf_assign_candidates", "ivf_merge_shards",
     "ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend",
-    "ivf_debug_set_kv_attend", "ivf_debug_set_kv_select",
+    "ivf_kv_attend_chunk", "ivf_kv_attend_chunk_workspace", "ivf_kv_fork", "ivf_kv_compact", "ivf_kv_pages_workspace", "ivf_kv_copy",
+    "ivf_debug_set_kv_attend", "ivf_debug_set_kv_select", "ivf_debug_set_kv_chunk",
     "ivf_set_deferred_host_outputs", "ivf_wait_host_outputs",
     "ivf_check", "ivf_last_error", "ivf_release_workspace", "ivf_launch_count",
     "ivf_debug_plan", "ivf_debug_span", "ivf_debug_rotation", "ivf_debug_set_rotation", "ivf_debug_set_threshold_pass", "ivf_debug_fail_next_alloc", "ivf_debug_bounds_checked", "ivf_debug_bounds_probe", "ivf_debug_set_wait_limit_ns",
@@ -109,6 +110,12 @@ def lib() -> ctypes.CDLL:
     L.ivf_kv_summarize.argtypes = [cache, vp, vp, i64, vp, vp, vp]
     L.ivf_kv_select.argtypes = [vp, vp, i32, i64, i32, i32, i32, vp, vp, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp]
     L.ivf_kv_attend.argtypes = [vp, vp, i64, i32, cache, vp, i64, i32, i32, vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp]
+    L.ivf_kv_attend_chunk_workspace.argtypes = [i64, i32, cache, i32, ctypes.POINTER(i64)]
+    L.ivf_kv_attend_chunk.argtypes = [vp, vp, i64, i32, cache, vp, i64, i32, i32, vp, vp, ctypes.c_float, ctypes.c_float, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+    L.ivf_kv_pages_workspace.argtypes = [i32, i32, i64, ctypes.POINTER(i64)]
+    L.ivf_kv_fork.argtypes = [vp, i64, vp, i32, i32, vp, vp, i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.ivf_kv_compact.argtypes = [vp, i64, vp, i32, i32, i64, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp]
+    L.ivf_kv_copy.argtypes = [cache, vp, vp, vp, i64, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("ivf_last_error", "ivf_launch_count"):
             getattr(L, name).restype = i32
@@ -507,7 +514,8 @@ def _bind():
         loader = importlib.machinery.ExtensionFileLoader("_kv_bind", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kv_bind", loader))
         loader.exec_module(module)
-        names = ("ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend", "ivf_last_error")
+        names = ("ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend", "ivf_kv_attend_chunk",
+                 "ivf_kv_attend_chunk_workspace", "ivf_kv_fork", "ivf_kv_compact", "ivf_kv_pages_workspace", "ivf_kv_copy", "ivf_last_error")
         module.init(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in names), IvfError)
         _kv = module
     return _kv
@@ -571,6 +579,58 @@ def ivf_kv_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
     """(out [n, heads, d] in q's type, lse float32 [n, heads] or None): attention of each token over its selected blocks
     (int32 [n, kv_heads, n_select]), positions up to its own."""
     return (_kv or _bind()).kv_attend(q, k_cache, v_cache, table, token_req, token_pos, selected, scale, out, want_lse)
+
+
+def ivf_kv_attend_chunk(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, token_start: torch.Tensor,
+                        kv_lens: torch.Tensor, scale: float, cap: float = 0.0, slopes: torch.Tensor | None = None, window: int = 0,
+                        prefix: torch.Tensor | None = None, out: torch.Tensor | None = None, want_lse: bool = False):
+    """(out [n, heads, d] in q's type, lse float32 [n, heads] or None): attention of each request's new tokens (rows token_start[b] to
+    token_start[b + 1], its last ones of kv_lens[b]) over its whole cache: keys up to a token's own, and those below prefix[b],
+    that lie less than `window` (0: any distance) before it; logits cap * tanh(scale q.k / cap) (cap 0: scale q.k) less
+    slopes[head] times the distance."""
+    return (_kv or _bind()).kv_attend_chunk(q, k_cache, v_cache, table, token_start, kv_lens, scale, cap, slopes, window, prefix, out, want_lse)
+
+
+class KvFork(NamedTuple):
+    """What ivf_kv_fork gives: the next step's table, the copies that it asks for, and the pages that nobody holds."""
+    table: torch.Tensor       # int32 [n_new, max_blocks]
+    kv_lens: torch.Tensor     # int32 [n_new]
+    copy_from: torch.Tensor   # int32 [n_new], -1: the row needs no copy
+    copy_to: torch.Tensor     # int32 [n_new]
+    copy_fill: torch.Tensor   # int32 [n_new]
+    free_pages: torch.Tensor  # int32 [num_pages], -1 after the last
+    n_free: torch.Tensor      # int32 [1]
+
+
+def ivf_kv_fork(table: torch.Tensor, kv_lens: torch.Tensor, parent: torch.Tensor, keep: torch.Tensor | None, num_pages: int, page_size: int,
+                fork: KvFork | None = None) -> KvFork:
+    """The table whose row i holds the first keep[i] tokens (None: all) of row parent[i] (-1: an empty row): filled blocks are
+    shared, a partly filled one stays with its lowest row unless a row shares it as filled, the others take a page of their own, which
+    ivf_kv_copy then fills in each layer.  Written into `fork`, an earlier call's, if given."""
+    got = (_kv or _bind()).kv_fork(table, kv_lens, parent, keep, num_pages, page_size, fork)
+    return KvFork._make(got) if fork is None else fork
+
+
+class KvMoves(NamedTuple):
+    """What ivf_kv_compact gives."""
+    table: torch.Tensor      # int32 [n_req, max_blocks]
+    copy_from: torch.Tensor  # int32 [max_moves], -1 after the last
+    copy_to: torch.Tensor    # int32 [max_moves]
+    n_held: torch.Tensor     # int32 [1]
+
+
+def ivf_kv_compact(table: torch.Tensor, kv_lens: torch.Tensor, num_pages: int, page_size: int, max_moves: int | None = None,
+                   out: torch.Tensor | None = None) -> KvMoves:
+    """The table (written in place, or into `out`) after the held pages with the highest numbers, at most max_moves of them, have moved
+    to the lowest holes below the number of held pages; ivf_kv_copy then moves their contents in each layer."""
+    return KvMoves._make((_kv or _bind()).kv_compact(table, kv_lens, num_pages, page_size, max_moves, out))
+
+
+def ivf_kv_copy(k_cache: torch.Tensor, v_cache: torch.Tensor, copy_from: torch.Tensor, copy_to: torch.Tensor, copy_fill: torch.Tensor | None = None,
+                codes: torch.Tensor | None = None, scales: torch.Tensor | None = None) -> None:
+    """Copies the first copy_fill[i] tokens (None: all) of page copy_from[i] onto page copy_to[i], for every kv head of both caches, and the
+    pages' summaries if given.  -1 in either list: nothing."""
+    (_kv or _bind()).kv_copy(k_cache, v_cache, copy_from, copy_to, copy_fill, codes, scales)
 
 
 def ivf_check(device=None) -> None:
@@ -693,6 +753,13 @@ def ivf_debug_set_kv_attend(kernel: int) -> None:
 def ivf_debug_set_kv_select(kernel: int) -> None:
     """0: by the sizes; 1: always the kernel that takes tokens singly; 2: windows of tokens wherever possible."""
     rc = lib().ivf_debug_set_kv_select(int(kernel))
+    if rc != IVF_OK:
+        _raise(rc)
+
+
+def ivf_debug_set_kv_chunk(kernel: int) -> None:
+    """0: by the sizes; 1: always tiles of 16 rows; 2: tiles of 128 or 256 rows wherever possible."""
+    rc = lib().ivf_debug_set_kv_chunk(int(kernel))
     if rc != IVF_OK:
         _raise(rc)
 

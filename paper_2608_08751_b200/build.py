@@ -17,10 +17,13 @@ _CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libivf_b200.so")
 CHECKED_LIB_PATH = os.path.join(_PKG, "libivf_b200_checked.so")
 BIND_PATH = os.path.join(_PKG, "_kv_bind.so")
-_SOURCES = ["ivf_api.cu"]
-_HEADERS = ["ptx.cuh", "check.cuh", "scales.cuh", "fused_topk.cuh", "merge.cuh", "prep.cuh", "update.cuh", "pq.cuh",
-            "candidates.cuh", "kv_common.cuh", "kv_tables.cuh", "kv_append.cuh", "kv_summary.cuh", "kv_select.cuh",
-            "kv_attend.cuh", "kv_attend_tile.cuh", "kv_api.cuh"]
+_COMMON = ["ptx.cuh", "check.cuh", "kv_common.cuh", "kv_attend.cuh", "kv_attend_tile.cuh", "kv_host.cuh", "kv_check.cuh"]
+_UNITS = {  # translation units, and the headers that each includes beside the common ones
+    "ivf_api.cu": ["scales.cuh", "fused_topk.cuh", "merge.cuh", "prep.cuh", "update.cuh", "pq.cuh", "candidates.cuh", "kv_tables.cuh",
+                   "kv_append.cuh", "kv_summary.cuh", "kv_select.cuh", "kv_api.cuh"],
+    "kv_whole.cu": ["kv_chunk.cuh", "kv_pages.cuh"],
+}
+_CHECKED = {"ivf_api.cu"}  # units whose kernels have index checks to switch on
 
 
 def _nvcc() -> str:
@@ -30,27 +33,47 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def _deps(unit: str) -> list[str]:
+    return [os.path.join(_CSRC, f) for f in [unit, *_UNITS[unit], *_COMMON]] + [os.path.join(_ROOT, "include", "ivf_b200.h")]
+
+
+def _newer(deps: list[str], path: str) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
+
+
 def _stale(path: str = LIB_PATH) -> bool:
-    if not os.path.exists(path):
-        return True
-    t = os.path.getmtime(path)
-    deps = [os.path.join(_CSRC, f) for f in _SOURCES + _HEADERS] + [os.path.join(_ROOT, "include", "ivf_b200.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+    return any(_newer(_deps(unit), path) for unit in _UNITS)
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
+    """Compiles the units side by side (those whose objects are older than their sources) and links them."""
     out = CHECKED_LIB_PATH if checked else LIB_PATH
     if not force and not _stale(out):
         return out
-    tmp = out + f".{os.getpid()}.tmp"
+    folder = os.path.join(_PKG, "build")
+    os.makedirs(folder, exist_ok=True)
     cmd = [_nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(_ROOT, "include")]
-    if checked:
-        cmd += ["-DIVF_CHECK_BOUNDS"]
+           "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include")]
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(_CSRC, s) for s in _SOURCES] + ["-o", tmp]
-    subprocess.check_call(cmd)
+    objects, running = [], []
+    for unit in _UNITS:
+        other = checked and unit in _CHECKED
+        obj = os.path.join(folder, unit.removesuffix(".cu") + ("_checked.o" if other else ".o"))
+        objects.append(obj)
+        if force or _newer(_deps(unit), obj):
+            tmp = obj + f".{os.getpid()}.tmp.o"
+            running.append((subprocess.Popen(cmd + (["-DIVF_CHECK_BOUNDS"] if other else []) + ["-c", os.path.join(_CSRC, unit), "-o", tmp]), tmp, obj))
+    failed = None
+    for process, tmp, obj in running:
+        if process.wait() == 0:
+            os.replace(tmp, obj)
+        else:
+            failed = process.args
+    if failed:
+        raise subprocess.CalledProcessError(1, failed)
+    tmp = out + f".{os.getpid()}.tmp"
+    subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", *objects, "-o", tmp])
     os.replace(tmp, out)
     return out
 

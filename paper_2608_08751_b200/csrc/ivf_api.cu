@@ -25,6 +25,7 @@
 #include "kv_append.cuh"
 #include "kv_attend.cuh"
 #include "kv_attend_tile.cuh"
+#include "kv_host.cuh"
 #include "kv_select.cuh"
 #include "kv_summary.cuh"
 #include "kv_tables.cuh"
@@ -1449,8 +1450,9 @@ int ivf_check(void* stream) {
         CUDA_TRY(cudaMemset(ctx->status, 0, sizeof h));
         if (h[0] == IVF_ERR_DEVICE_TIMEOUT)
             return fail(IVF_ERR_DEVICE_TIMEOUT, "a device-side wait expired (wait site %d, block %d)", h[1], h[2]);
-        if (h[1] >= KV_SITE_TABLES && h[1] <= KV_SITE_ATTEND && (h[0] == IVF_ERR_BAD_ID || h[0] == IVF_ERR_NO_PAGES)) {
-            static const char* const names[] = {"ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend"};
+        if (h[1] >= KV_SITE_TABLES && h[1] <= KV_SITE_COPY && (h[0] == IVF_ERR_BAD_ID || h[0] == IVF_ERR_NO_PAGES)) {
+            static const char* const names[] = {"ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend", "ivf_kv_attend_chunk",
+                                                "ivf_kv_fork", "ivf_kv_compact", "ivf_kv_copy"};
             return fail(h[0], h[0] == IVF_ERR_NO_PAGES ? "%s had too few free pages, table columns, tokens or touched blocks"
                                                        : "%s skipped a length, position, slot, page or block out of range", names[h[1] - KV_SITE_TABLES]);
         }

@@ -28,6 +28,12 @@ decltype(&ivf_kv_append) f_append = nullptr;
 decltype(&ivf_kv_summarize) f_summarize = nullptr;
 decltype(&ivf_kv_select) f_select = nullptr;
 decltype(&ivf_kv_attend) f_attend = nullptr;
+decltype(&ivf_kv_attend_chunk) f_chunk = nullptr;
+decltype(&ivf_kv_attend_chunk_workspace) f_chunk_workspace = nullptr;
+decltype(&ivf_kv_fork) f_fork = nullptr;
+decltype(&ivf_kv_compact) f_compact = nullptr;
+decltype(&ivf_kv_pages_workspace) f_pages_workspace = nullptr;
+decltype(&ivf_kv_copy) f_copy = nullptr;
 decltype(&ivf_last_error) f_last_error = nullptr;
 PyObject* g_error = nullptr;  // IvfError
 
@@ -382,11 +388,179 @@ PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     END
 }
 
-// (addresses of tables, append, summarize, select, attend, last_error; the error class)
-PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+// Scratch memory of one call: the allocator hands it out again to later work of the same stream only, and a captured graph keeps its own.
+at::Tensor scratch(int64_t bytes, c10::Device dev) { return fresh({bytes}, at::kByte, dev); }
+
+// (q, k_cache, v_cache, table, token_start, kv_lens, scale, cap, slopes, window, prefix, out, want_lse) -> (out, lse or None)
+PyObject* kv_attend_chunk(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    NEEDS(13)
+    BEGIN
+    const at::Tensor &q = tensor(a[0], "q"), &kc = tensor(a[1], "k_cache"), &vc = tensor(a[2], "v_cache");
+    const ivf_kv_cache c = cache_of(kc, &vc);
+    const c10::Device dev = kc.device();
+    int64_t qs[2], os[2];
+    const void* qp = strided(q, "q", 3, kc.scalar_type(), dev, qs);
+    const int64_t n = q.size(0), heads = q.size(1), d = q.size(2);
+    if (d != c.head_dim) refuse(PyExc_ValueError, "head_dim mismatch between q and the caches");
+    const Table tb = table_of(tensor(a[3], "table"), dev);
+    const auto* start = as<int32_t>(dense(tensor(a[4], "token_start"), "token_start", at::kInt, dev, {tb.n + int64_t{1}}));
+    const auto* lens = as<int32_t>(dense(tensor(a[5], "kv_lens"), "kv_lens", at::kInt, dev, {tb.n}));
+    const float scale = real(a[6]), cap = real(a[7]);
+    const auto* slopes = given(a[8]) ? as<float>(dense(tensor(a[8], "slopes"), "slopes", at::kFloat, dev, {heads})) : nullptr;
+    const int window = small(a[9], "window");
+    const auto* prefix = given(a[10]) ? as<int32_t>(dense(tensor(a[10], "prefix"), "prefix", at::kInt, dev, {tb.n})) : nullptr;
+    const at::Tensor out = given(a[11]) ? tensor(a[11], "out") : fresh({n, heads, d}, kc.scalar_type(), dev);
+    void* op = strided(out, "out", 3, kc.scalar_type(), dev, os);
+    same_shape(out, q, "out and q");
+    const int want = PyObject_IsTrue(a[12]);
+    if (want < 0) return nullptr;
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor lse, work;
+    if (want) lse = fresh({n, heads}, at::kFloat, dev);
+    int64_t bytes = 0;
+    check(f_chunk_workspace(n, static_cast<int>(heads), &c, tb.n, &bytes));
+    if (bytes) work = scratch(bytes, dev);
+    check(f_chunk(qp, qs, n, static_cast<int>(heads), &c, tb.p, tb.stride, tb.n, tb.columns, start, lens, scale, cap, slopes, window, prefix, op, os,
+                  want && lse.numel() ? lse.data_ptr<float>() : nullptr, bytes ? work.data_ptr() : nullptr, bytes, stream_of(dev)));
+    if (given(a[11])) written(out);
+    PyObject* r = PyTuple_New(2);
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(out));
+    if (want) PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(lse));
+    else {
+        Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(r, 1, Py_None);
+    }
+    return r;
+    END
+}
+
+// (table, kv_lens, parent, keep, num_pages, page_size, fork or None) -> the seven tensors of a fork
+PyObject* kv_fork(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     NEEDS(7)
-    void* f[6];
-    for (int i = 0; i < 6; ++i) {
+    BEGIN
+    const at::Tensor& table = tensor(a[0], "table");
+    const c10::Device dev = table.device();
+    const Table tb = table_of(table, dev);
+    const auto* lens = as<int32_t>(dense(tensor(a[1], "kv_lens"), "kv_lens", at::kInt, dev, {tb.n}));
+    const at::Tensor& pt = tensor(a[2], "parent");
+    const int64_t n = pt.numel();
+    if (n > INT32_MAX) refuse(PyExc_ValueError, "parent: at most 2^31 - 1 rows");
+    const auto* parent = as<int32_t>(dense(pt, "parent", at::kInt, dev, {n}));
+    const auto* keep = given(a[3]) ? as<int32_t>(dense(tensor(a[3], "keep"), "keep", at::kInt, dev, {n})) : nullptr;
+    const int64_t pages = whole(a[4], "num_pages");
+    const int page = small(a[5], "page_size");
+    if (pages < 0 || pages > INT32_MAX) refuse(PyExc_ValueError, "num_pages = %lld is out of range", static_cast<long long>(pages));
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor out[7];
+    int64_t stride = tb.columns;
+    if (given(a[6])) {
+        if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != 7) refuse(PyExc_TypeError, "fork must be what an earlier call returned");
+        for (int i = 0; i < 7; ++i) out[i] = tensor(PyTuple_GET_ITEM(a[6], i), "fork");
+        strided(out[0], "fork.table", 2, at::kInt, dev, &stride);
+        if (out[0].size(0) != n || out[0].size(1) != tb.columns) refuse(PyExc_ValueError, "fork.table must have a row for each parent and the table's columns");
+        if (n <= 1) stride = tb.columns;
+        static const char* const names[] = {"", "fork.kv_lens", "fork.copy_from", "fork.copy_to", "fork.copy_fill"};
+        for (int i = 1; i < 5; ++i) dense(out[i], names[i], at::kInt, dev, {n});
+        dense(out[5], "fork.free_pages", at::kInt, dev, {pages});
+        dense(out[6], "fork.n_free", at::kInt, dev, {1});
+    } else {
+        out[0] = fresh({n, tb.columns}, at::kInt, dev);
+        const at::Tensor buf = fresh({4 * (4 * n + pages + 1)}, at::kByte, dev);
+        for (int i = 1; i < 5; ++i) out[i] = part(buf, 4 * (i - 1) * n, n, at::kInt);
+        out[5] = part(buf, 16 * n, pages, at::kInt);
+        out[6] = part(buf, 16 * n + 4 * pages, 1, at::kInt);
+    }
+    int64_t bytes = 0;
+    at::Tensor work;
+    check(f_pages_workspace(static_cast<int>(n), tb.columns, pages, &bytes));
+    if (bytes) work = scratch(bytes, dev);
+    auto i32 = [&](int i) { return out[i].numel() ? static_cast<int32_t*>(out[i].data_ptr()) : nullptr; };
+    check(f_fork(tb.p, tb.stride, lens, tb.n, tb.columns, parent, keep, static_cast<int>(n), pages, page, i32(0), stride, i32(1), i32(2), i32(3), i32(4),
+                 i32(5), i32(6), bytes ? work.data_ptr() : nullptr, bytes, stream_of(dev)));
+    if (given(a[6])) {
+        for (const at::Tensor& t : out) written(t);
+        Py_INCREF(a[6]);
+        return a[6];
+    }
+    PyObject* r = PyTuple_New(7);
+    for (int i = 0; r && i < 7; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
+    return r;
+    END
+}
+
+// (table, kv_lens, num_pages, page_size, max_moves or None, out or None) -> (table, copy_from, copy_to, n_held)
+PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    NEEDS(6)
+    BEGIN
+    const at::Tensor& table = tensor(a[0], "table");
+    const c10::Device dev = table.device();
+    const Table tb = table_of(table, dev);
+    const auto* lens = as<int32_t>(dense(tensor(a[1], "kv_lens"), "kv_lens", at::kInt, dev, {tb.n}));
+    const int64_t pages = whole(a[2], "num_pages");
+    const int page = small(a[3], "page_size");
+    if (pages < 0 || pages > INT32_MAX) refuse(PyExc_ValueError, "num_pages = %lld is out of range", static_cast<long long>(pages));
+    const int64_t moves = given(a[4]) ? whole(a[4], "max_moves") : pages;
+    if (moves < 0 || moves > INT32_MAX) refuse(PyExc_ValueError, "max_moves = %lld is out of range", static_cast<long long>(moves));
+    const at::Tensor out = given(a[5]) ? tensor(a[5], "out") : table;
+    const Table to = table_of(out, dev);
+    if (to.n != tb.n || to.columns != tb.columns) refuse(PyExc_ValueError, "out must have the table's shape");
+    const c10::cuda::CUDAGuard guard(dev);
+    const at::Tensor buf = fresh({4 * (2 * moves + 1)}, at::kByte, dev);
+    const at::Tensor lists[3] = {part(buf, 0, moves, at::kInt), part(buf, 4 * moves, moves, at::kInt), part(buf, 8 * moves, 1, at::kInt)};
+    int64_t bytes = 0;
+    at::Tensor work;
+    check(f_pages_workspace(tb.n, tb.columns, pages, &bytes));
+    if (bytes) work = scratch(bytes, dev);
+    auto i32 = [&](int i) { return lists[i].numel() ? static_cast<int32_t*>(lists[i].data_ptr()) : nullptr; };
+    check(f_compact(tb.p, tb.stride, lens, tb.n, tb.columns, pages, page, to.p, to.stride, i32(0), i32(1), moves, i32(2), bytes ? work.data_ptr() : nullptr,
+                    bytes, stream_of(dev)));
+    written(out);
+    PyObject* r = PyTuple_New(4);
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(out));
+    for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(r, i + 1, THPVariable_Wrap(lists[i]));
+    return r;
+    END
+}
+
+// (k_cache, v_cache, copy_from, copy_to, copy_fill or None, codes or None, scales or None)
+PyObject* kv_copy(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    NEEDS(7)
+    BEGIN
+    const at::Tensor &kc = tensor(a[0], "k_cache"), &vc = tensor(a[1], "v_cache");
+    const ivf_kv_cache c = cache_of(kc, &vc);
+    const c10::Device dev = kc.device();
+    const at::Tensor& from = tensor(a[2], "copy_from");
+    const int64_t n = from.numel();
+    const auto* fp = as<int32_t>(dense(from, "copy_from", at::kInt, dev, {n}));
+    const auto* tp = as<int32_t>(dense(tensor(a[3], "copy_to"), "copy_to", at::kInt, dev, {n}));
+    const auto* fill = given(a[4]) ? as<int32_t>(dense(tensor(a[4], "copy_fill"), "copy_fill", at::kInt, dev, {n})) : nullptr;
+    if (given(a[5]) != given(a[6])) refuse(PyExc_ValueError, "codes and scales: both or neither");
+    int8_t* codes = nullptr;
+    float* scales = nullptr;
+    if (given(a[5])) {
+        codes = as<int8_t>(dense(tensor(a[5], "codes"), "codes", at::kChar, dev, {c.num_pages, c.n_kv_heads, c.head_dim}));
+        scales = as<float>(dense(tensor(a[6], "scales"), "scales", at::kFloat, dev, {c.num_pages, c.n_kv_heads}));
+    }
+    const c10::cuda::CUDAGuard guard(dev);
+    check(f_copy(&c, fp, tp, fill, n, codes, scales, stream_of(dev)));
+    written(kc);
+    written(vc);
+    if (given(a[5])) {
+        written(tensor(a[5], "codes"));
+        written(tensor(a[6], "scales"));
+    }
+    Py_RETURN_NONE;
+    END
+}
+
+// (addresses of the library's functions in the order below; the error class)
+PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    constexpr int kFunctions = 12;
+    NEEDS(kFunctions + 1)
+    void* f[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
         f[i] = PyLong_AsVoidPtr(a[i]);
         if (!f[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null function address");
@@ -398,14 +572,21 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     f_summarize = reinterpret_cast<decltype(f_summarize)>(f[2]);
     f_select = reinterpret_cast<decltype(f_select)>(f[3]);
     f_attend = reinterpret_cast<decltype(f_attend)>(f[4]);
-    f_last_error = reinterpret_cast<decltype(f_last_error)>(f[5]);
-    Py_INCREF(a[6]);
-    Py_XSETREF(g_error, a[6]);
+    f_chunk = reinterpret_cast<decltype(f_chunk)>(f[5]);
+    f_chunk_workspace = reinterpret_cast<decltype(f_chunk_workspace)>(f[6]);
+    f_fork = reinterpret_cast<decltype(f_fork)>(f[7]);
+    f_compact = reinterpret_cast<decltype(f_compact)>(f[8]);
+    f_pages_workspace = reinterpret_cast<decltype(f_pages_workspace)>(f[9]);
+    f_copy = reinterpret_cast<decltype(f_copy)>(f[10]);
+    f_last_error = reinterpret_cast<decltype(f_last_error)>(f[11]);
+    Py_INCREF(a[kFunctions]);
+    Py_XSETREF(g_error, a[kFunctions]);
     Py_RETURN_NONE;
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(kv_tables), METHOD(kv_append), METHOD(kv_summarize), METHOD(kv_select), METHOD(kv_attend), METHOD(init),
+PyMethodDef methods[] = {METHOD(kv_tables), METHOD(kv_append), METHOD(kv_summarize), METHOD(kv_select), METHOD(kv_attend), METHOD(kv_attend_chunk),
+                         METHOD(kv_fork), METHOD(kv_compact), METHOD(kv_copy), METHOD(init),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

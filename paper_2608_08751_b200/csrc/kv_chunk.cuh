@@ -1,0 +1,631 @@
+// Attention of each request's new tokens over its whole cache.
+//
+// out = sum_k exp(z_k - m) v_k / sum_k exp(z_k - m) over the keys k that a token at position p of its request sees:
+//   z_k = scale * q . k,  with a cap  z_k = cap * tanh(scale * q . k / cap),  with a bias  z_k - slope_head * |p - k|
+//   seen: k < the request's length, k <= p or k < its prefix, and p - k < the window.  Always an interval [lo, hi).
+// One pass over the keys with a running maximum and sum, both in 32 bits; the exponentials take the cache's 16-bit type as
+// operands of the second product (off by up to 2^-8 or 2^-11 of themselves), the sum that divides them is of the unrounded ones.
+//
+// How the work is shared out.  An item is a tile of new tokens of one request and one kv head: the tile's tokens by the
+// head's group of query heads are the rows of one matrix product.  Only the device knows the lengths, and they are ragged,
+// so the grid is as many CTAs as live on the card and each takes an equal, contiguous span of the line of all items, an item
+// being as long as the keys it reads and a constant for its start and end.  Lengths, prefixes and windows make hi and lo
+// of a request's tiles piecewise linear, so every place on the line follows from sums in closed form and one scan over the
+// requests, which each CTA does for itself.  Where a span begins or ends inside an item its CTA leaves the rows' sums in
+// the workspace (two items at most), and a second kernel joins them.  Every order is fixed: a call gives the same bits each time.
+//
+// A value that is not finite at a key that only some rows of a tile see would reach the others as 0 * inf.  In pieces that not
+// all rows see such values are looked for, taken out of the product, and added at the end to the rows that do see them.
+#pragma once
+#include "kv_attend.cuh"
+
+namespace ivf {
+
+constexpr int kChunkMaxCtas = 2 * 148;
+constexpr int kChunkGrain = 64;     // spans end at multiples of this many keys
+
+struct ChunkDesc {  // of the item that a CTA's span ends in
+    int parts;      // CTAs that have a part of it; 0: the span ends with an item
+    int token, tokens, hv;
+};
+
+struct ChunkParams {
+    const void* q;
+    int64_t q_stride[2];
+    int64_t n_tokens;
+    int group, n_kv_heads, dim;
+    KvPlane kc, vc;
+    int64_t num_pages;
+    const int32_t* table;
+    int64_t table_stride;
+    int n_req, max_blocks, page_shift;
+    const int32_t *token_start, *kv_lens, *prefix;  // prefix may be null
+    int window;            // 0: none
+    float scale_log2;      // scale * log2(e)
+    float cap_in, cap_out; // with a cap: z in base 2 = cap_out * tanh(x), 2 x log2(e) = cap_in * (q . k); cap_out 0: none
+    const float* slopes;   // [n_heads] or null
+    void* out;
+    int64_t out_stride[2];
+    float* lse;  // [n_tokens][n_heads] or null
+    int* status;
+    int tile_tokens;       // tokens of a tile
+    int part_heads, parts; // query heads of a tile's rows, and how many such parts a group has
+    int item_cost;         // of an item's start and end, in keys
+    int least;             // keys of a span, at least
+    ChunkDesc* desc;       // [CTAs]
+    float* slots;          // [2 * CTAs][rows * (dim + 2)]: sums, then maxima, then totals
+    uint64_t limit_ns;
+};
+
+// ------------------------------------------------------------------ the line of items
+struct ChunkReq {
+    int start, fresh;  // its first token, its tokens in this call
+    int base;          // position of the first
+    int len, far;      // tokens in the cache; keys that the table has columns for
+    int prefix, tiles;
+    bool blind;        // its lengths make no sense: its tokens see nothing
+    int64_t j_hi, j_lo;  // tiles before these end at the prefix, begin at key 0
+};
+
+__device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, bool report) {
+    ChunkReq r;
+    const int s0 = p.token_start[b], s1 = p.token_start[b + 1], len = p.kv_lens[b];
+    const bool none = s0 < 0 || s1 < s0;
+    const int given = none ? 0 : s1 - s0;
+    r.blind = len < given || len < 0;
+    const int64_t room = static_cast<int64_t>(p.max_blocks) << p.page_shift;
+    if (report && (none || r.blind || len > room)) kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
+    r.start = s0;
+    r.fresh = static_cast<int>(max(min(static_cast<int64_t>(s0) + given, p.n_tokens) - s0, static_cast<int64_t>(0)));
+    r.len = r.blind ? 0 : len;
+    r.base = r.blind ? 0 : len - given;
+    r.far = static_cast<int>(min(static_cast<int64_t>(r.len), room));
+    r.prefix = p.prefix ? max(0, min(p.prefix[b], r.len)) : 0;
+    r.tiles = (r.fresh + p.tile_tokens - 1) / p.tile_tokens;
+    // tile j ends at max(base + (j + 1) T, prefix) and begins at max(base + j T - window + 1, 0)
+    const unsigned T = p.tile_tokens;
+    const int a = r.prefix - r.base, c = p.window - 1 - r.base;
+    r.j_hi = a <= 0 ? 0 : (static_cast<unsigned>(a) - 1) / T;
+    r.j_lo = p.window <= 0 ? r.tiles : c < 0 ? 0 : static_cast<unsigned>(c) / T + 1;
+    return r;
+}
+__device__ __forceinline__ int chunk_hi(const ChunkParams& p, const ChunkReq& r, int j) {  // one past the last key that the tile sees
+    const int last = min((j + 1) * p.tile_tokens, r.fresh);
+    return r.blind ? 0 : max(r.base + last, r.prefix);
+}
+__device__ __forceinline__ int chunk_lo(const ChunkParams& p, const ChunkReq& r, int j) {
+    return r.blind || p.window <= 0 ? 0 : max(r.base + j * p.tile_tokens - p.window + 1, 0);
+}
+__device__ __forceinline__ int64_t chunk_weight(const ChunkParams& p, const ChunkReq& r, int j) {
+    return static_cast<int64_t>(chunk_hi(p, r, j)) - chunk_lo(p, r, j) + p.item_cost;
+}
+// Weights of the tiles before tile i of one head.
+__device__ __forceinline__ int64_t chunk_before(const ChunkParams& p, const ChunkReq& r, int64_t i) {
+    const int64_t cost = i * p.item_cost;
+    if (r.blind || i == 0) return cost;
+    const int64_t n = i == r.tiles ? i - 1 : i, T = p.tile_tokens;  // the last tile may be short
+    const int64_t a = min(r.j_hi, n);
+    int64_t sum = a * r.prefix + (n - a) * r.base + T * ((n * (n + 1) - a * (a + 1)) / 2);
+    if (n < i) sum += chunk_hi(p, r, static_cast<int>(n));
+    const int64_t c = min(r.j_lo, i);
+    sum -= (i - c) * (static_cast<int64_t>(r.base) - p.window + 1) + T * ((i * (i - 1) - c * (c - 1)) / 2);
+    return sum + cost;
+}
+
+// A CTA's place on the line.
+struct ChunkCursor {
+    int b, hv, tile;
+    int64_t off;   // inside the item
+    int64_t left;  // of the span
+};
+template <int THREADS>
+struct ChunkPlan {
+    int64_t warp_sum[THREADS / 32];
+    int64_t total;
+    ChunkCursor at;
+};
+__device__ __forceinline__ int64_t chunk_span(int64_t total, int ctas, int c) { return total / ctas * c + total % ctas * c / ctas; }
+
+// All threads: the CTA's cursor (left = 0: nothing to do) and the number of CTAs that take part.
+template <int THREADS>
+__device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPlan<THREADS>& s, int& ctas) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.n_req + THREADS - 1) / THREADS;
+    const int b0 = min(tid * per, p.n_req), b1 = min(b0 + per, p.n_req);
+    const int hvs = p.n_kv_heads * p.parts;
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        const ChunkReq r = chunk_req(p, b, blockIdx.x == 0);
+        mine += hvs * chunk_before(p, r, r.tiles);
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) s.warp_sum[warp] = upto;
+    if (tid == 0) s.at.left = 0;
+    __syncthreads();
+    int64_t total = 0;
+    upto -= mine;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) upto += s.warp_sum[w];
+        total += s.warp_sum[w];
+    }
+    ctas = static_cast<int>(max(min(total / p.least, static_cast<int64_t>(gridDim.x)), static_cast<int64_t>(1)));
+    const int c = blockIdx.x;
+    if (c < ctas) {
+        const int64_t u0 = chunk_span(total, ctas, c), u1 = chunk_span(total, ctas, c + 1);
+        if (u0 >= upto && u0 < upto + mine) {
+            int64_t rest = u0 - upto;
+            for (int b = b0; b < b1; ++b) {
+                const ChunkReq r = chunk_req(p, b, false);
+                const int64_t one = chunk_before(p, r, r.tiles);
+                if (rest >= one * hvs) {
+                    rest -= one * hvs;
+                    continue;
+                }
+                s.at.b = b;
+                s.at.hv = static_cast<int>(rest / one);
+                rest -= s.at.hv * one;
+                int lo = 0, hi = r.tiles;  // before(lo) <= rest < before(hi)
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (chunk_before(p, r, mid) <= rest) lo = mid;
+                    else hi = mid;
+                }
+                s.at.tile = lo;
+                s.at.off = rest - chunk_before(p, r, lo);
+                s.at.left = u1 - u0;
+                break;
+            }
+        }
+    }
+    if (tid == 0) s.total = total;
+    __syncthreads();
+    return s.at;
+}
+
+// One item, or the part of it that a span has.
+struct ChunkItem {
+    ChunkReq r;
+    int hv, token, tokens;  // first token of the tile, and how many
+    int pos;                // position of the first
+    int lo, hi;             // keys that some row sees
+    int k0, k1;             // of them this part's
+    bool first, last;       // the part begins, ends the item
+    int64_t rest;           // of the item behind the part
+};
+__device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const ChunkCursor& at) {
+    ChunkItem it;
+    it.r = chunk_req(p, at.b, false);
+    const int64_t w = chunk_weight(p, it.r, at.tile), take = min(at.left, w - at.off);
+    it.hv = at.hv;
+    it.token = it.r.start + at.tile * p.tile_tokens;
+    it.tokens = min(p.tile_tokens, it.r.fresh - at.tile * p.tile_tokens);
+    it.pos = it.r.base + at.tile * p.tile_tokens;
+    it.lo = chunk_lo(p, it.r, at.tile);
+    it.hi = min(chunk_hi(p, it.r, at.tile), it.r.far);
+    it.lo = min(it.lo, it.hi);
+    it.first = at.off == 0;
+    it.last = at.off + take == w;
+    it.rest = w - at.off - take;
+    auto cut = [&](int64_t off) {  // a place in the item as a key
+        const int64_t k = (it.lo + max(off - p.item_cost, static_cast<int64_t>(0))) / kChunkGrain * kChunkGrain;
+        return static_cast<int>(max(static_cast<int64_t>(it.lo), min(k, static_cast<int64_t>(it.hi))));
+    };
+    it.k0 = it.first ? it.lo : cut(at.off);
+    it.k1 = it.last ? it.hi : cut(at.off + take);
+    return it;
+}
+__device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkCursor& at) {
+    ChunkReq r = chunk_req(p, at.b, false);
+    const int64_t take = min(at.left, chunk_weight(p, r, at.tile) - at.off);
+    at.left -= take;
+    at.off = 0;
+    if (++at.tile < r.tiles) return;
+    at.tile = 0;
+    if (++at.hv < p.n_kv_heads * p.parts) return;
+    at.hv = 0;
+    if (at.left > 0)  // (weights left: there is a request with tokens)
+        do r = chunk_req(p, ++at.b, false);
+        while (r.tiles == 0 && at.b < p.n_req - 1);
+}
+// The CTAs that take part in an item whose rest lies behind this CTA's span.
+__device__ __forceinline__ int chunk_parts(int64_t total, int ctas, int c, int64_t rest) {
+    const int64_t end = chunk_span(total, ctas, c + 1) + rest;  // of the item
+    int last = c, past = ctas;  // span(last) < end <= span(past)
+    while (past - last > 1) {
+        const int mid = (last + past) >> 1;
+        if (chunk_span(total, ctas, mid) < end) last = mid;
+        else past = mid;
+    }
+    return past - c;
+}
+
+// Keys that a token at position pos sees.
+__device__ __forceinline__ void chunk_sees(const ChunkParams& p, const ChunkReq& r, int pos, bool live, int& lo, int& hi) {
+    live = live && !r.blind;
+    lo = live && p.window > 0 ? max(pos - p.window + 1, 0) : 0;
+    hi = live ? min(max(pos + 1, r.prefix), r.far) : 0;
+}
+
+// Tokens that belong to no request: zeros.
+template <typename T>
+__device__ __forceinline__ void chunk_padding(const ChunkParams& p, int threads) {
+    const int n_heads = p.group * p.n_kv_heads;
+    const int64_t before = max(static_cast<int64_t>(0), min(static_cast<int64_t>(p.token_start[0]), p.n_tokens));
+    const int64_t from = max(before, min(static_cast<int64_t>(p.token_start[p.n_req]), p.n_tokens));
+    const int64_t pad = before + p.n_tokens - from;
+    if (pad == 0) return;
+    const int pieces = p.dim / 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * threads + threadIdx.x; i < pad * n_heads * pieces; i += static_cast<int64_t>(gridDim.x) * threads) {
+        const int c = static_cast<int>(i % pieces);
+        const int64_t row = i / pieces, at = row / n_heads, t = at < before ? at : from + at - before;
+        const int head = static_cast<int>(row % n_heads);
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + c * 8) = make_uint4(0, 0, 0, 0);
+        if (c == 0 && p.lse) p.lse[t * n_heads + head] = -INFINITY;
+    }
+}
+
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// A product as a logit in base 2, before the bias.  tanh(x) = 1 - 2 / (1 + exp(2 x)): off by a few 2^-24 of the cap.
+__device__ __forceinline__ float chunk_logit(const ChunkParams& p, float s) {
+    if (p.cap_out == 0.0f) return s * p.scale_log2;
+    return fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(s * p.cap_in)), p.cap_out);
+}
+
+// The numbers of `v` (two 16-bit ones to a word) that are not finite; `clean` gets zeros in their places.
+template <typename T>
+__device__ __forceinline__ bool odd_pair(uint32_t v, uint32_t& clean) {
+    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    const bool lo = (v & kExp) == kExp, hi = (v >> 16 & kExp) == kExp;
+    clean = (lo ? 0u : v & 0xFFFFu) | (hi ? 0u : v & 0xFFFF0000u);
+    return lo || hi;
+}
+template <typename T>
+__device__ __forceinline__ bool take_out_odd(uint4& v) {
+    const bool a = odd_pair<T>(v.x, v.x), b = odd_pair<T>(v.y, v.y), c = odd_pair<T>(v.z, v.z), d = odd_pair<T>(v.w, v.w);
+    return a || b || c || d;
+}
+// What was taken out of the products, for eight columns of a row that sees keys [lo, hi): added to its sums.  Keys [k0, k1) were this
+// part's; those of [clear0, clear1) stayed in the products.
+template <typename T>
+__device__ __noinline__ void add_odd(const ChunkParams& p, int b, int h, int lo, int hi, int k0, int k1, int clear0, int clear1, int column, float (&acc)[8]) {
+    for (int k = max(lo, k0); k < min(hi, k1); ++k) {
+        if (k >= clear0 && k < clear1) {
+            k = clear1 - 1;
+            continue;
+        }
+        const int page = p.table[b * p.table_stride + (k >> p.page_shift)];
+        if (page < 0 || page >= p.num_pages) continue;
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.vc.base) + page * p.vc.page_stride + h * p.vc.head_stride +
+                                                        (k & ((1 << p.page_shift) - 1)) * p.vc.token_stride + column);
+        float f[8];
+        unpack8<T>(v, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!is_finite(f[i])) acc[i] += f[i];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- rows
+// Tiles of 16 rows: single and drafted tokens.  As in ivf_kv_attend's kernel of that name each of four warps takes pieces of 16 keys
+// through a ring of its own and the warps meet at an item's end.
+template <int DP>
+struct ChunkRowsControl {
+    ChunkPlan<kRowsThreads> plan;
+    int odd;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __grid_constant__ ChunkParams p) {
+    using S = RowsShape<DP>;
+    extern __shared__ __align__(128) uint8_t rows_smem[];
+    __shared__ ChunkRowsControl<DP> c;
+    pdl_trigger();  // (the kernel that joins the parts waits for this one's end by itself)
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int ctas;
+    ChunkCursor at = chunk_plan<kRowsThreads>(p, c.plan, ctas);
+    chunk_padding<T>(p, kRowsThreads);
+    const uint32_t smem0 = smem_u32(rows_smem);
+    const uint32_t s_q = smem0 + S::kSmem - S::kQBytes;
+    const uint32_t ring = smem0 + warp * (S::kStages * S::kStageBytes);
+    const int ksteps = p.dim >> 4;
+    const int n_heads = p.group * p.n_kv_heads;
+    ChunkDesc tail = {0, 0, 0, 0};
+
+    for (; at.left > 0; chunk_next(p, at)) {
+        const ChunkItem it = chunk_item(p, at);
+        const int h = it.hv / p.parts, g0 = it.hv % p.parts * p.part_heads;
+        const int heads = min(p.part_heads, p.group - g0);
+        const int head0 = h * p.group + g0;
+        const int32_t* pages = p.table + at.b * p.table_stride;
+        auto row_token = [&](int r) { return r / p.part_heads; };
+        auto row_live = [&](int r) { return row_token(r) < it.tokens && r % p.part_heads < heads; };
+
+        if (tid == 0) c.odd = 0;
+        for (int i = tid; i < 16 * (DP / 8); i += kRowsThreads) {
+            const int r = i / (DP / 8), col = i % (DP / 8);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (row_live(r) && col * 8 < p.dim)
+                v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + static_cast<int64_t>(it.token + row_token(r)) * p.q_stride[0] +
+                                                    static_cast<int64_t>(head0 + r % p.part_heads) * p.q_stride[1] + col * 8);
+            *reinterpret_cast<uint4*>(rows_smem + (rows_addr<DP>(s_q, r, col) - smem0)) = v;
+        }
+        __syncthreads();
+
+        // keys that all rows see: those of the first and of the last token
+        int all_lo, all_hi, skip;
+        chunk_sees(p, it.r, it.pos, true, skip, all_hi);
+        chunk_sees(p, it.r, it.pos + it.tokens - 1, true, all_lo, skip);
+        const int piece0 = it.k0 >> 4, pieces = it.k1 > it.k0 ? ((it.k1 + 15) >> 4) - piece0 : 0;
+        const int mine = pieces > warp ? (pieces - warp + kRowsWarps - 1) / kRowsWarps : 0;
+        auto page_of = [&](int j) {  // of this warp's piece j
+            const int block = ((piece0 + warp + j * kRowsWarps) << 4) >> p.page_shift;
+            int page = -1;
+            if (j < mine) page = pages[block];
+            if (page >= p.num_pages) {
+                kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
+                page = -1;
+            }
+            return page;
+        };
+        int page_now = page_of(lane), page_next = page_of(32 + lane);
+        uint32_t there = 0;  // by stage: the piece has a page
+
+        auto fetch = [&](int j, int stage) {
+            if (j > 0 && (j & 31) == 0) {
+                page_now = page_next;
+                page_next = page_of(j + 32 + lane);
+            }
+            const int64_t page = __shfl_sync(0xFFFFFFFFu, page_now, j & 31);
+            there = page >= 0 ? there | 1u << stage : there & ~(1u << stage);
+            if (page >= 0) {
+                const int key0 = (piece0 + warp + j * kRowsWarps) << 4;
+                const int tok0 = key0 & ((1 << p.page_shift) - 1);
+                const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + S::kPlaneBytes;
+                const T* ks = static_cast<const T*>(p.kc.base) + page * p.kc.page_stride + h * p.kc.head_stride;
+                const T* vs = static_cast<const T*>(p.vc.base) + page * p.vc.page_stride + h * p.vc.head_stride;
+                constexpr int kLanes = DP / 8 < 32 ? DP / 8 : 32, kRowsAtOnce = 32 / kLanes;
+                const int col = lane % kLanes, r0 = lane / kLanes;
+                const T* kp = ks + (tok0 + r0) * p.kc.token_stride + col * 8;
+                const T* vp = vs + (tok0 + r0) * p.vc.token_stride + col * 8;
+                if (col * 8 < p.dim) {
+#pragma unroll
+                    for (int r = r0; r < 16; r += kRowsAtOnce) {
+                        const bool ok = key0 + r >= it.k0 && key0 + r < it.k1;  // what no row sees is never read: it may hold anything
+                        cp_async16(rows_addr<DP>(kb, r, col), ok ? kp : ks, ok);
+                        cp_async16(rows_addr<DP>(vb, r, col), ok ? vp : vs, ok);
+                        kp += kRowsAtOnce * p.kc.token_stride;
+                        vp += kRowsAtOnce * p.vc.token_stride;
+                    }
+                }
+            }
+            cp_async_commit();
+        };
+
+        uint32_t qf[DP / 16][4];
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) ldsm4(qf[k], rows_addr<DP>(s_q, lane & 15, 2 * k + (lane >> 4)));
+        float o[DP / 8][4];
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        int lo[2], hi[2], pos[2];
+        float slope[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int row = (lane >> 2) + r * 8;
+            pos[r] = it.pos + row_token(row);
+            chunk_sees(p, it.r, pos[r], row_live(row), lo[r], hi[r]);
+            slope[r] = p.slopes && row_live(row) ? p.slopes[head0 + row % p.part_heads] * 1.4426950408889634f : 0.0f;
+        }
+
+#pragma unroll
+        for (int s = 0; s < S::kStages - 1; ++s) fetch(s, s);
+        int stage = 0;
+        for (int j = 0; j < mine; ++j) {
+            cp_async_wait<S::kStages - 2>();
+            __syncwarp();
+            fetch(j + S::kStages - 1, stage == 0 ? S::kStages - 1 : stage - 1);
+            const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + S::kPlaneBytes;
+            const bool has = there >> stage & 1;
+            if (++stage == S::kStages) stage = 0;
+            if (!has) continue;
+            const int key0 = (piece0 + warp + j * kRowsWarps) << 4;
+            float sc[2][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[0][i] = sc[1][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                if (k < ksteps) {
+                    uint32_t b[4];  // tokens 0-7 and 8-15, columns 16k .. 16k + 15
+                    ldsm4(b, rows_addr<DP>(kb, (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
+                    mma16816<T>(sc[0], qf[k], b[0], b[1]);
+                    mma16816<T>(sc[1], qf[k], b[2], b[3]);
+                }
+            }
+            if (it.tokens > 1 && (key0 < all_lo || key0 + 16 > all_hi)) {  // not all rows see all of it
+                bool odd = false;
+                for (int i = lane; i < 16 * (DP / 8); i += 32) {
+                    const int r = i / (DP / 8), col = i % (DP / 8);
+                    uint4* at_v = reinterpret_cast<uint4*>(rows_smem + (rows_addr<DP>(vb, r, col) - smem0));
+                    uint4 v = *at_v;
+                    if (col * 8 < p.dim && take_out_odd<T>(v)) {
+                        *at_v = v;
+                        odd = true;
+                    }
+                }
+                if (odd) c.odd = 1;
+                __syncwarp();
+            }
+            // row lane / 4 (and + 8): keys 2 (lane % 4), + 1, + 8, + 9
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i >> 1, key = key0 + n * 8 + (lane & 3) * 2 + (i & 1);
+                    float z = chunk_logit(p, sc[n][i]);
+                    if (p.slopes) z = fmaf(-slope[r], fabsf(static_cast<float>(pos[r] - key)), z);
+                    z = key >= lo[r] && key < hi[r] && key >= it.k0 && key < it.k1 ? z : -INFINITY;
+                    sc[n][i] = z;
+                    top[r] = fmaxf(top[r], z);
+                }
+            }
+            float fix[2], base[2], add[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                top[r] = fmaxf(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], 1));
+                top[r] = fmaxf(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], 2));
+                const float mn = fmaxf(m[r], top[r]);
+                base[r] = mn == -INFINITY ? 0.0f : mn;
+                fix[r] = exp2_fast(m[r] - base[r]);
+                m[r] = mn;
+            }
+            uint32_t pf[4];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float w0 = exp2_fast(sc[n][2 * r] - base[r]), w1 = exp2_fast(sc[n][2 * r + 1] - base[r]);
+                    add[r] += w0 + w1;
+                    pf[2 * n + r] = Pair16<T>::pack(w0, w1);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) l[r] = l[r] * fix[r] + add[r];
+            if (__any_sync(0xFFFFFFFFu, fix[0] != 1.0f || fix[1] != 1.0f)) {
+#pragma unroll
+                for (int i = 0; i < DP / 8; ++i) {
+                    o[i][0] *= fix[0];
+                    o[i][1] *= fix[0];
+                    o[i][2] *= fix[1];
+                    o[i][3] *= fix[1];
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < DP / 16; ++n) {
+                if (n < ksteps) {
+                    uint32_t b[4];
+                    ldsm4_t(b, rows_addr<DP>(vb, lane & 15, 2 * n + (lane >> 4)));
+                    mma16816<T>(o[2 * n], pf, b[0], b[1]);
+                    mma16816<T>(o[2 * n + 1], pf, b[2], b[3]);
+                }
+            }
+        }
+        cp_async_wait<0>();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 1);
+            l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 2);
+        }
+        // the warps meet: rows of DP + 8 floats, the last ones maximum and sum
+        __syncthreads();
+        float* s_o = reinterpret_cast<float*>(rows_smem);
+        constexpr int kRow = DP + 8;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float* dst = s_o + (warp * 16 + (lane >> 2) + r * 8) * kRow;
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i)
+                *reinterpret_cast<float2*>(dst + i * 8 + (lane & 3) * 2) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
+            if ((lane & 3) == 0) {
+                dst[DP] = m[r];
+                dst[DP + 1] = l[r];
+            }
+        }
+        __syncthreads();
+        const bool whole = it.first && it.last;
+        float* slot = p.slots + static_cast<int64_t>(2 * blockIdx.x + (it.first ? 1 : 0)) * 16 * (p.dim + 2);
+        for (int i = tid; i < 16 * (DP / 8); i += kRowsThreads) {
+            const int r = i / (DP / 8), col = i % (DP / 8);
+            if (col * 8 >= p.dim || !row_live(r)) continue;
+            float best = -INFINITY, sum = 0.0f, acc[8] = {};
+#pragma unroll
+            for (int k = 0; k < kRowsWarps; ++k) best = fmaxf(best, s_o[(k * 16 + r) * kRow + DP]);
+            const float base = best == -INFINITY ? 0.0f : best;
+#pragma unroll
+            for (int k = 0; k < kRowsWarps; ++k) {
+                const float* src = s_o + (k * 16 + r) * kRow;
+                const float w = exp2_fast(src[DP] - base);
+                sum += w * src[DP + 1];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) acc[x] += w * src[col * 8 + x];
+            }
+            if (c.odd) {
+                int from, to;
+                chunk_sees(p, it.r, it.pos + row_token(r), true, from, to);
+                add_odd<T>(p, at.b, h, from, to, it.k0, it.k1, (all_lo + 15) & ~15, all_hi & ~15, col * 8, acc);
+            }
+            if (whole) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // nothing seen: zeros
+#pragma unroll
+                for (int x = 0; x < 8; ++x) acc[x] *= inv;
+                const int64_t t = it.token + row_token(r);
+                const int head = head0 + r % p.part_heads;
+                *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + col * 8) = pack8<T>(acc);
+                if (col == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+            } else {
+                float* dst = slot + r * p.dim + col * 8;
+                *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                *reinterpret_cast<float4*>(dst + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                if (col == 0) {
+                    slot[16 * p.dim + r] = best;
+                    slot[16 * p.dim + 16 + r] = sum;
+                }
+            }
+        }
+        if (it.first && !it.last && tid == 0)
+            tail = ChunkDesc{chunk_parts(c.plan.total, ctas, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
+        __syncthreads();  // the next item's queries and ring lie over this one's
+    }
+    if (tid == 0) p.desc[blockIdx.x] = tail;
+}
+
+// Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.
+constexpr int kJoinThreads = 128;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const ChunkParams p, int rows) {
+    pdl_wait();
+    const int c = blockIdx.x;
+    const ChunkDesc d = p.desc[c];
+    if (d.parts == 0) return;
+    const int h = d.hv / p.parts, g0 = d.hv % p.parts * p.part_heads;
+    const int heads = min(p.part_heads, p.group - g0), n_heads = p.group * p.n_kv_heads;
+    const int quads = p.dim / 4;
+    const int64_t step = static_cast<int64_t>(rows) * (p.dim + 2);
+    auto part = [&](int k) { return p.slots + (k == 0 ? 2 * c + 1 : 2 * (c + k)) * step; };
+    for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < d.tokens * p.part_heads * quads; i += gridDim.y * kJoinThreads) {
+        const int r = i / quads, col = i % quads;
+        if (r % p.part_heads >= heads) continue;
+        float best = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < d.parts; ++k) best = fmaxf(best, part(k)[rows * p.dim + r]);
+        const float base = best == -INFINITY ? 0.0f : best;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int k = 0; k < d.parts; ++k) {
+            const float* src = part(k);
+            const float4 v = *reinterpret_cast<const float4*>(src + r * p.dim + col * 4);
+            const float w = exp2_fast(src[rows * p.dim + r] - base);
+            sum += w * src[rows * p.dim + rows + r];
+            acc.x += w * v.x, acc.y += w * v.y, acc.z += w * v.z, acc.w += w * v.w;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int64_t t = d.token + r / p.part_heads;
+        const int head = h * p.group + g0 + r % p.part_heads;
+        const uint2 v = make_uint2(Pair16<T>::pack(acc.x * inv, acc.y * inv), Pair16<T>::pack(acc.z * inv, acc.w * inv));
+        *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + col * 4) = v;
+        if (col == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+}  // namespace ivf

@@ -17,7 +17,7 @@ namespace ivf {
 constexpr int kKvStatusBadId = -6;
 constexpr int kKvStatusNoPages = -8;
 // status[1] of a block-cache call: which operator met the first bad value
-enum KvSite { KV_SITE_TABLES = 601, KV_SITE_APPEND, KV_SITE_SUMMARIZE, KV_SITE_SELECT, KV_SITE_ATTEND };
+enum KvSite { KV_SITE_TABLES = 601, KV_SITE_APPEND, KV_SITE_SUMMARIZE, KV_SITE_SELECT, KV_SITE_ATTEND, KV_SITE_CHUNK, KV_SITE_FORK, KV_SITE_COMPACT, KV_SITE_COPY };
 
 constexpr int kKvMaxDim = 256;
 constexpr int kKvMaxGroup = 64;     // query heads per kv head

@@ -75,7 +75,7 @@ struct WaitCtl {
 
 constexpr int kStatusTimeout = -5;
 
-__device__ __noinline__ void report_timeout(const WaitCtl& ctl, int where) {
+static __device__ __noinline__ void report_timeout(const WaitCtl& ctl, int where) {
     *ctl.abort_flag = 1;
     if (atomicCAS(ctl.status, 0, kStatusTimeout) == 0) {
         ctl.status[1] = where;
