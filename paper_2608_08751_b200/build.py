@@ -21,7 +21,7 @@ _COMMON = ["ptx.cuh", "check.cuh", "kv_common.cuh", "kv_attend.cuh", "kv_attend_
 _UNITS = {  # translation units, and the headers that each includes beside the common ones
     "ivf_api.cu": ["scales.cuh", "fused_topk.cuh", "merge.cuh", "prep.cuh", "update.cuh", "pq.cuh", "candidates.cuh", "kv_tables.cuh",
                    "kv_append.cuh", "kv_summary.cuh", "kv_select.cuh", "kv_api.cuh"],
-    "kv_whole.cu": ["kv_chunk.cuh", "kv_pages.cuh"],
+    "kv_whole.cu": ["kv_chunk.cuh", "kv_chunk_tile.cuh", "kv_pages.cuh"],
 }
 _CHECKED = {"ivf_api.cu"}  # units whose kernels have index checks to switch on
 

@@ -21,8 +21,7 @@
 
 namespace ivf {
 
-constexpr int kChunkMaxCtas = 2 * 148;
-constexpr int kChunkGrain = 64;     // spans end at multiples of this many keys
+constexpr int kChunkMaxSms = 148;  // CTAs that a call may use: two on each of so many SMs, one of the kernel of large tiles
 
 struct ChunkDesc {  // of the item that a CTA's span ends in
     int parts;      // CTAs that have a part of it; 0: the span ends with an item
@@ -52,8 +51,10 @@ struct ChunkParams {
     int part_heads, parts; // query heads of a tile's rows, and how many such parts a group has
     int item_cost;         // of an item's start and end, in keys
     int least;             // keys of a span, at least
+    int grain;             // items are cut at multiples of this many keys (a power of two)
+    int rows;              // of a slot: tile_tokens * part_heads, and one more if that is odd
     ChunkDesc* desc;       // [CTAs]
-    float* slots;          // [2 * CTAs][rows * (dim + 2)]: sums, then maxima, then totals
+    float* slots;          // [2 * CTAs][rows * (dim + 2)]: sums, then maxima, then totals; row = token of the tile * part_heads + head
     uint64_t limit_ns;
 };
 
@@ -213,7 +214,7 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const Chun
     it.last = at.off + take == w;
     it.rest = w - at.off - take;
     auto cut = [&](int64_t off) {  // a place in the item as a key
-        const int64_t k = (it.lo + max(off - p.item_cost, static_cast<int64_t>(0))) / kChunkGrain * kChunkGrain;
+        const int64_t k = (it.lo + max(off - p.item_cost, static_cast<int64_t>(0))) & -static_cast<int64_t>(p.grain);
         return static_cast<int>(max(static_cast<int64_t>(it.lo), min(k, static_cast<int64_t>(it.hi))));
     };
     it.k0 = it.first ? it.lo : cut(at.off);
@@ -544,7 +545,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
         }
         __syncthreads();
         const bool whole = it.first && it.last;
-        float* slot = p.slots + static_cast<int64_t>(2 * blockIdx.x + (it.first ? 1 : 0)) * 16 * (p.dim + 2);
+        float* slot = p.slots + static_cast<int64_t>(2 * blockIdx.x + (it.first ? 1 : 0)) * p.rows * (p.dim + 2);
         for (int i = tid; i < 16 * (DP / 8); i += kRowsThreads) {
             const int r = i / (DP / 8), col = i % (DP / 8);
             if (col * 8 >= p.dim || !row_live(r)) continue;
@@ -578,8 +579,8 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
                 *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
                 *reinterpret_cast<float4*>(dst + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
                 if (col == 0) {
-                    slot[16 * p.dim + r] = best;
-                    slot[16 * p.dim + 16 + r] = sum;
+                    slot[p.rows * p.dim + r] = best;
+                    slot[p.rows * (p.dim + 1) + r] = sum;
                 }
             }
         }
@@ -593,7 +594,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
 // Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.
 constexpr int kJoinThreads = 128;
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const ChunkParams p, int rows) {
+__global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const ChunkParams p) {
     pdl_wait();
     const int c = blockIdx.x;
     const ChunkDesc d = p.desc[c];
@@ -601,22 +602,22 @@ __global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const Chunk
     const int h = d.hv / p.parts, g0 = d.hv % p.parts * p.part_heads;
     const int heads = min(p.part_heads, p.group - g0), n_heads = p.group * p.n_kv_heads;
     const int quads = p.dim / 4;
-    const int64_t step = static_cast<int64_t>(rows) * (p.dim + 2);
+    const int64_t step = static_cast<int64_t>(p.rows) * (p.dim + 2);
     auto part = [&](int k) { return p.slots + (k == 0 ? 2 * c + 1 : 2 * (c + k)) * step; };
     for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < d.tokens * p.part_heads * quads; i += gridDim.y * kJoinThreads) {
         const int r = i / quads, col = i % quads;
         if (r % p.part_heads >= heads) continue;
         float best = -INFINITY, sum = 0.0f;
 #pragma unroll 4
-        for (int k = 0; k < d.parts; ++k) best = fmaxf(best, part(k)[rows * p.dim + r]);
+        for (int k = 0; k < d.parts; ++k) best = fmaxf(best, part(k)[p.rows * p.dim + r]);
         const float base = best == -INFINITY ? 0.0f : best;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (int k = 0; k < d.parts; ++k) {
             const float* src = part(k);
             const float4 v = *reinterpret_cast<const float4*>(src + r * p.dim + col * 4);
-            const float w = exp2_fast(src[rows * p.dim + r] - base);
-            sum += w * src[rows * p.dim + rows + r];
+            const float w = exp2_fast(src[p.rows * p.dim + r] - base);
+            sum += w * src[p.rows * (p.dim + 1) + r];
             acc.x += w * v.x, acc.y += w * v.y, acc.z += w * v.z, acc.w += w * v.w;
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;

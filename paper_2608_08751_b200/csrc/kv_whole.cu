@@ -14,6 +14,7 @@
 #include <utility>
 
 #include "kv_chunk.cuh"
+#include "kv_chunk_tile.cuh"
 #include "kv_host.cuh"
 #include "kv_pages.cuh"
 
@@ -82,18 +83,34 @@ int allow_smem(K kernel, int most, const KvHostCtx& ctx, SmemSeen& seen) {
 std::atomic<int> g_kv_chunk{0};  // test hook (ivf_debug_set_kv_chunk): 0 = by the sizes, 1 = rows kernel only, 2 = tile kernel wherever it can run
 
 struct ChunkShape {
-    int rows, part_heads, parts, tile_tokens;
+    int streams;  // of 128 rows; 0: the kernel of 16 rows
+    int part_heads, parts, tile_tokens, ctas;
+    int rows;  // of a slot: an even number, so that slots and their rows of sums start at multiples of 16 bytes
 };
-ChunkShape chunk_shape(int group) {
+ChunkShape chunk_shape(int group, int dim, bool tile) {
     ChunkShape s;
-    s.rows = 16;
-    s.part_heads = std::min(group, s.rows);
-    s.parts = (group + s.rows - 1) / s.rows;
-    s.tile_tokens = group > s.rows ? 1 : s.rows / group;
+    s.streams = !tile ? 0 : dim > 128 ? 1 : 2;
+    const int rows = tile ? 128 : 16;
+    s.part_heads = std::min(group, rows);
+    s.parts = (group + rows - 1) / rows;
+    s.tile_tokens = (group > rows ? 1 : rows / group) * std::max(s.streams, 1);
+    s.rows = (s.tile_tokens * s.part_heads + 1) / 2 * 2;
+    s.ctas = (!tile && dim <= 128 ? 2 : 1) * kChunkMaxSms;
     return s;
 }
 int64_t chunk_bytes(const ChunkShape& s, int dim) {
-    return kChunkMaxCtas * (static_cast<int64_t>(sizeof(ChunkDesc)) + 2ll * s.rows * (dim + 2) * sizeof(float));
+    return s.ctas * (static_cast<int64_t>(sizeof(ChunkDesc)) + 2ll * s.rows * (dim + 2) * sizeof(float));
+}
+// Large tiles read the keys once for up to 256 rows, small ones once for 16.
+bool chunk_tiles_pay(int64_t n_tokens, int n_req, int group, int dim) {
+    const int kernel = g_kv_chunk.load();
+    if (kernel == 1 || dim < 64) return false;
+    return kernel == 2 || n_tokens * group > 32ll * std::max(n_req, 1);
+}
+int64_t chunk_workspace(int64_t n_tokens, int n_req, int group, int dim) {
+    int64_t bytes = chunk_bytes(chunk_shape(group, dim, false), dim);
+    if (chunk_tiles_pay(n_tokens, n_req, group, dim)) bytes = std::max(bytes, chunk_bytes(chunk_shape(group, dim, true), dim));
+    return bytes;
 }
 
 template <typename T, int DP>
@@ -102,16 +119,41 @@ int launch_chunk_rows(const ChunkParams& p, int ctas, const KvHostCtx& ctx, cuda
     if (int rc = allow_smem(kv_chunk_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
     return launch(false, kv_chunk_rows_kernel<T, DP>, dim3(ctas), kRowsThreads, RowsShape<DP>::kSmem, stream, p);
 }
+template <typename T, int DB, bool PLAIN>
+int launch_chunk_tile(const ChunkParams& p, const CUtensorMap& mk, const CUtensorMap& mv, int ctas, const KvHostCtx& ctx, cudaStream_t stream) {
+    static SmemSeen seen;
+    if (int rc = allow_smem(kv_chunk_tile_kernel<T, DB, PLAIN>, chunk_tile_smem<DB>(), ctx, seen)) return rc;
+    return launch(false, kv_chunk_tile_kernel<T, DB, PLAIN>, dim3(ctas), ChunkTileShape<DB>::kThreads, chunk_tile_smem<DB>(), stream, mk, mv, p);
+}
+template <typename T, int DB>
+int launch_chunk_tile(const ChunkParams& p, const CUtensorMap& mk, const CUtensorMap& mv, int ctas, const KvHostCtx& ctx, cudaStream_t stream) {
+    return p.cap_out == 0.0f && !p.slopes ? launch_chunk_tile<T, DB, true>(p, mk, mv, ctas, ctx, stream) : launch_chunk_tile<T, DB, false>(p, mk, mv, ctas, ctx, stream);
+}
 template <typename T>
-int launch_chunk(ChunkParams& p, const ChunkShape& s, const KvHostCtx& ctx, cudaStream_t stream) {
-    const int ctas = std::min(kChunkMaxCtas, (p.dim > 128 ? 1 : 2) * ctx.num_sms);
-    p.item_cost = 64;
-    p.least = 256;
-    int rc = p.dim <= 64 ? launch_chunk_rows<T, 64>(p, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_rows<T, 128>(p, ctas, ctx, stream)
-                                                                                        : launch_chunk_rows<T, 256>(p, ctas, ctx, stream);
+int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStream_t stream) {
+    CUtensorMap mk, mv;
+    const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+    const int page = 1 << p.page_shift;
+    // (an expanded cache has no tensor map: small tiles)
+    const bool tile = chunk_tiles_pay(p.n_tokens, p.n_req, p.group, p.dim) && p.num_pages > 0 &&
+                      kv_host_map(&mk, p.kc, p.dim, page, p.n_kv_heads, p.num_pages, bf16) && kv_host_map(&mv, p.vc, p.dim, page, p.n_kv_heads, p.num_pages, bf16);
+    const ChunkShape s = chunk_shape(p.group, p.dim, tile);
+    const int ctas = s.ctas / kChunkMaxSms * std::min(ctx.num_sms, kChunkMaxSms);
+    p.tile_tokens = s.tile_tokens, p.part_heads = s.part_heads, p.parts = s.parts, p.rows = s.rows;
+    p.desc = static_cast<ChunkDesc*>(workspace);
+    p.slots = reinterpret_cast<float*>(p.desc + s.ctas);
+    p.item_cost = tile ? 384 : 64;
+    p.least = tile ? 1024 : 256;
+    p.grain = tile ? 128 : 64;
+    int rc;
+    if (tile)
+        rc = p.dim <= 64 ? launch_chunk_tile<T, 1>(p, mk, mv, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_tile<T, 2>(p, mk, mv, ctas, ctx, stream)
+                                                                                              : launch_chunk_tile<T, 4>(p, mk, mv, ctas, ctx, stream);
+    else
+        rc = p.dim <= 64 ? launch_chunk_rows<T, 64>(p, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_rows<T, 128>(p, ctas, ctx, stream)
+                                                                                         : launch_chunk_rows<T, 256>(p, ctas, ctx, stream);
     if (rc != IVF_OK) return rc;
-    const int quads = s.rows * p.dim / 4;
-    return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (quads + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, stream, p, s.rows);
+    return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (p.rows * p.dim / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, stream, p);
 }
 
 // Whether rows of `a` (heads by tokens) may share memory with rows of `b`.
@@ -178,7 +220,7 @@ int ivf_kv_attend_chunk_workspace(int64_t n_tokens, int n_heads, const ivf_kv_ca
     int rc = kv_check_dim(cache->head_dim);
     if (rc == IVF_OK) rc = kv_check_heads(n_heads, cache->n_kv_heads);
     if (rc != IVF_OK) return rc;
-    *bytes = n_tokens == 0 ? 0 : chunk_bytes(chunk_shape(n_heads / cache->n_kv_heads), cache->head_dim);
+    *bytes = n_tokens == 0 ? 0 : chunk_workspace(n_tokens, n_req, n_heads / cache->n_kv_heads, cache->head_dim);
     return IVF_OK;
 }
 
@@ -204,8 +246,7 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
         return rc;
     if (rows_meet(q, q_stride, out, out_stride, n_tokens, n_heads, cache->head_dim))
         return fail(IVF_ERR_INVALID_ARG, "out must not share memory with q: rows are read again by other blocks of threads");
-    const ChunkShape s = chunk_shape(n_heads / cache->n_kv_heads);
-    const int64_t need = chunk_bytes(s, cache->head_dim);
+    const int64_t need = chunk_workspace(n_tokens, n_req, n_heads / cache->n_kv_heads, cache->head_dim);
     if (!workspace || workspace_bytes < need || kv_misaligned(workspace, 16))
         return fail(IVF_ERR_INVALID_ARG, "workspace: %lld bytes, 16-byte aligned, are needed (ivf_kv_attend_chunk_workspace)", (long long)need);
     KvHostCtx ctx;
@@ -223,12 +264,9 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
     p.cap_in = cap > 0.0f ? 2.0f * log2e * scale / cap : 0.0f;
     p.cap_out = cap * log2e;
     p.slopes = slopes, p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = ctx.status;
-    p.tile_tokens = s.tile_tokens, p.part_heads = s.part_heads, p.parts = s.parts;
-    p.desc = static_cast<ChunkDesc*>(workspace);
-    p.slots = reinterpret_cast<float*>(p.desc + kChunkMaxCtas);
     p.limit_ns = ctx.limit_ns;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    return cache->dtype == IVF_F16 ? launch_chunk<__half>(p, s, ctx, stream) : launch_chunk<__nv_bfloat16>(p, s, ctx, stream);
+    return cache->dtype == IVF_F16 ? launch_chunk<__half>(p, workspace, ctx, stream) : launch_chunk<__nv_bfloat16>(p, workspace, ctx, stream);
 }
 
 int ivf_debug_set_kv_chunk(int kernel) {
