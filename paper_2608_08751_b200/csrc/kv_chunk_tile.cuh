@@ -3,9 +3,8 @@
 // An item's rows are one or two streams of 128 (tokens by query heads of a kv head's group).  Both streams go over the same keys, each
 // fetched once, a tile of keys at a time:
 //
-//   softmax warps   four to a stream, one thread per row: S out of TMEM, maximum and sum in registers, P over S in TMEM.  O is rescaled
-//                   only when the maximum has grown by more than 2^8 past the reference of the exponentials; the reference
-//                   cancels in the final division
+//   softmax warps   a thread per row: S out of TMEM, maximum and sum in registers, P over S in TMEM.  O is rescaled only when the maximum has
+//                   grown by more than 2^8 past the reference of the exponentials; the reference cancels in the final division
 //   issuer          one thread: S = Q K^T into TMEM, O += P V with P from TMEM.  While one stream's rows are in its softmax
 //                   warps the other stream's products run
 //   copier          the tiles' pages, looked up a tile ahead, by TMA
@@ -13,9 +12,9 @@
 //   cleaner         value rows that no row of the item may look at become zeros, and in tiles that not all rows see values that are not
 //                   finite are taken out
 //
-// Heads of up to 128: two streams, 128 keys to a tile, S and P of a stream share 128 columns (64 of P lie over S), so the
-// product S(j + 1) of a stream follows its P(j) V.  Wider heads: O takes half of TMEM, so one stream, 64 keys to a tile, two S
-// and S(j + 1) before P(j) V.
+// A tile is 64 keys.  A stream has two S, P lies over its S, and S(j + 1) is issued before P(j) V: the softmax warps find the next
+// logits ready.  TMEM holds it exactly: two streams of two S (256 columns) and of O (256).  Heads wider than 128 take all of the second half
+// for one stream's O; it has two threads to a row then, 32 keys each, which tell each other their maxima through shared memory.
 #pragma once
 #include "kv_chunk.cuh"
 #include "kv_attend_tile.cuh"
@@ -26,20 +25,19 @@ namespace ivf {
 template <int DB>
 struct ChunkTileShape {
     static constexpr int kStreams = DB == 4 ? 1 : 2;
-    static constexpr int kScores = DB == 4 ? 2 : 1;  // S buffers of a stream
-    static constexpr int kKeys = DB == 4 ? 64 : 128;
-    static constexpr int kStages = 2;                // of keys, and of values
+    static constexpr int kHalves = DB == 4 ? 2 : 1;  // threads of a row
+    static constexpr int kKeys = 64;
+    static constexpr int kMine = kKeys / kHalves;    // keys of a softmax thread
+    static constexpr int kStages = DB == 4 ? 2 : 4;  // of keys, and of values
     static constexpr int kBlockBytes = kKeys * 128;  // 64 columns of all keys
     static constexpr int kPlaneBytes = DB * kBlockBytes;
     static constexpr int kQBytes = DB * 128 * 128;   // of a stream
-    static constexpr int kSoftWarps = 4 * kStreams;
-    // Two streams: the softmax warps hold 128 logits a thread; three warpgroups are launched with 168 registers a thread (64,512 in all)
-    // and share them anew, 2 * 128 * 208 + 128 * 88.
-    static constexpr bool kShare = kStreams == 2;
+    static constexpr int kSoftWarps = 8;
+    static constexpr int kRowThreads = 128 * kHalves;  // of a stream
     static constexpr int kWarps = kSoftWarps + 4;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kOCol = 256, kCols = 512;
-    static constexpr int kHoles = 8;                 // tiles whose missing pages are remembered
+    static constexpr int kHoles = 16;                // tiles whose missing pages are remembered
     static constexpr int kItems = 4;                 // items that are planned ahead
 };
 
@@ -63,8 +61,9 @@ struct ChunkTileControl {
     ChunkTileItem item[S::kItems];
     uint64_t item_full[S::kItems], item_empty[S::kItems];
     uint64_t k_full[S::kStages], v_full[S::kStages], k_empty[S::kStages], v_empty[S::kStages], v_clean[S::kStages];
-    uint64_t q_full[S::kStreams], s_full[S::kStreams * S::kScores], p_ready[S::kStreams * S::kScores], pv_done[S::kStreams], o_full[S::kStreams], o_free[S::kStreams];
-    uint64_t drain;
+    uint64_t q_full[S::kStreams], s_full[S::kStreams * 2], p_ready[S::kStreams * 2], pv_done[S::kStreams], o_full[S::kStreams], o_free[S::kStreams];
+    uint64_t halves[S::kStreams * 4], drain;
+    float told[S::kStreams * 4][2][2][32];  // by warp pair, turn and half: maxima of a tile, at last the sums
     ChunkPlan<S::kThreads> plan;
     uint32_t holes[S::kHoles];  // by tile: groups of 16 keys without a page
     int odd[4];                 // by item: a value that is not finite was taken out
@@ -114,7 +113,7 @@ template <typename T, int DB, bool PLAIN>
 __global__ void __launch_bounds__(ChunkTileShape<DB>::kThreads, 1)
 kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkParams p) {
     using S = ChunkTileShape<DB>;
-    constexpr int kKeys = S::kKeys, kStreams = S::kStreams, kScores = S::kScores, kStages = S::kStages;
+    constexpr int kKeys = S::kKeys, kStreams = S::kStreams, kStages = S::kStages;
     extern __shared__ uint8_t tile_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* k_ring = smem + kStreams * S::kQBytes;
@@ -132,19 +131,20 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             mbar_init(&c.v_clean[i], 1);
         }
         for (int i = 0; i < kStreams; ++i) {
-            mbar_init(&c.q_full[i], 128);
+            mbar_init(&c.q_full[i], S::kRowThreads);
             mbar_init(&c.pv_done[i], 1);
             mbar_init(&c.o_full[i], 1);
-            mbar_init(&c.o_free[i], 128);
+            mbar_init(&c.o_free[i], S::kRowThreads);
         }
-        for (int i = 0; i < kStreams * kScores; ++i) {
+        for (int i = 0; i < kStreams * 2; ++i) {
             mbar_init(&c.s_full[i], 1);
-            mbar_init(&c.p_ready[i], 128);
+            mbar_init(&c.p_ready[i], S::kRowThreads);
         }
         for (int i = 0; i < S::kItems; ++i) {
             mbar_init(&c.item_full[i], 1);
             mbar_init(&c.item_empty[i], S::kWarps - 1);
         }
+        for (int i = 0; i < kStreams * 4; ++i) mbar_init(&c.halves[i], 2);
         mbar_init(&c.drain, 1);
         c.abort_flag = 0;
         fence_mbar_init();
@@ -167,80 +167,78 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     ctl.limit_ns = p.limit_ns;
     const int per = p.tile_tokens / kStreams;  // tokens of a stream
     bool ok = true;
-    // (inside the branches: where they meet again the compiler goes by the smaller number)
-    auto take = [] {
-        if (S::kShare) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    };
-    auto give = [] {
-        if (S::kShare) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    };
-
     if (warp == S::kSoftWarps) {
         // ------------------------------------------------------------ issuer
-        give();
         if (elect_one()) {
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const uint32_t idesc_s = tile_idesc<T>(kKeys, false) | negate, idesc_o = tile_idesc<T>(p.dim, true);
             const int ksteps = p.dim >> 4;
             const uint32_t k0_lo = umma_desc_lo(smem_u32(k_ring)), q0_lo = umma_desc_lo(smem_u32(smem));
-            int tiles = 0;                      // copied tiles before this item
-            int done[2] = {0, 0};               // tiles of a stream so far
-            int items[2] = {0, 0};              // items with tiles of a stream so far
+            const uint32_t v0_lo = ((smem_u32(v_ring) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
+            int tiles = 0;         // copied tiles before this item
+            int done[2] = {0, 0};  // tiles of a stream before this item
+            int items[2] = {0, 0}; // items with tiles of a stream so far
             for (int seq = 0;; ++seq) {
                 if (!(ok = mbar_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
                 const ChunkTileItem& t = c.item[seq % S::kItems];
                 if (t.tokens == 0) break;
-                auto scores = [&](int s, int j) {  // S of a stream and tile
-                    const int n = tiles + j - t.first, d = done[s] + j - t.from[s];
-                    if (!(ok = ok && mbar_wait(&c.k_full[n % kStages], (n / kStages) & 1, ctl, 241))) return;
-                    if (j == t.from[s] && !(ok = mbar_wait(&c.q_full[s], items[s] & 1, ctl, 242))) return;
+                // (in registers, and counted from the part's first tile: read from shared memory at each use they cost the products more than
+                // the products cost)
+                const int count = t.end - t.first;
+                int from[kStreams], to[kStreams];
+#pragma unroll
+                for (int s = 0; s < kStreams; ++s) from[s] = t.from[s] - t.first, to[s] = t.to[s] - t.first;
+                auto scores = [&](int s, int i) {  // S of a stream and tile
+                    const int n = tiles + i, d = done[s] + i - from[s];
+                    if (!(ok = mbar_wait(&c.k_full[n % kStages], (n / kStages) & 1, ctl, 241))) return;
+                    if (i == from[s] && !(ok = mbar_wait(&c.q_full[s], items[s] & 1, ctl, 242))) return;
                     tc_fence_after_sync();
                     const uint32_t k_lo = k0_lo + (n % kStages) * (S::kPlaneBytes >> 4), q_lo = q0_lo + s * (S::kQBytes >> 4);
-                    const uint32_t to = tmem + (kScores == 2 ? (d & 1) * kKeys : s * kKeys);
+                    const uint32_t at = tmem + (s * 2 + (d & 1)) * kKeys;
 #pragma unroll
                     for (int k = 0; k < DB * 4; ++k)
                         if (k < ksteps)
-                            umma_f16(to, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
+                            umma_f16(at, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
                                      umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc_s, k > 0);
-                    umma_commit(&c.s_full[kScores == 2 ? d & 1 : s]);
+                    umma_commit(&c.s_full[s * 2 + (d & 1)]);
                 };
-                auto outputs = [&](int s, int j) {  // O of a stream, by a tile
-                    const int n = tiles + j - t.first, d = done[s] + j - t.from[s];
-                    if (!(ok = ok && mbar_wait(&c.v_clean[n % kStages], (n / kStages) & 1, ctl, 243))) return;
-                    if (j == t.from[s] && items[s] > 0 && !(ok = mbar_wait(&c.o_free[s], (items[s] - 1) & 1, ctl, 244))) return;
-                    if (!(ok = mbar_wait(&c.p_ready[kScores == 2 ? d & 1 : s], kScores == 2 ? (d >> 1) & 1 : d & 1, ctl, 245))) return;
+                auto outputs = [&](int s, int i) {  // O of a stream, by a tile
+                    const int n = tiles + i, d = done[s] + i - from[s];
+                    if (!(ok = mbar_wait(&c.v_clean[n % kStages], (n / kStages) & 1, ctl, 243))) return;
+                    if (i == from[s] && items[s] > 0 && !(ok = mbar_wait(&c.o_free[s], (items[s] - 1) & 1, ctl, 244))) return;
+                    if (!(ok = mbar_wait(&c.p_ready[s * 2 + (d & 1)], (d >> 1) & 1, ctl, 245))) return;
                     tc_fence_after_sync();
                     // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
-                    const uint32_t v_addr = smem_u32(v_ring) + (n % kStages) * S::kPlaneBytes;
-                    const uint32_t v_lo = ((v_addr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-                    const uint32_t t_p = tmem + (kScores == 2 ? (d & 1) * kKeys : s * kKeys), t_o = tmem + S::kOCol + s * (DB * 64);
+                    const uint32_t v_lo = v0_lo + (n % kStages) * (S::kPlaneBytes >> 4);
+                    const uint32_t t_p = tmem + (s * 2 + (d & 1)) * kKeys, t_o = tmem + S::kOCol + s * (DB * 64);
 #pragma unroll
                     for (int k = 0; k < kKeys / 16; ++k)
-                        umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (j > t.from[s] || k > 0) ? 1u : 0u);
-                    if (kScores == 2) umma_commit(&c.pv_done[s]);
-                    if (j == t.to[s] - 1) umma_commit(&c.o_full[s]);
+                        umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (i > from[s] || k > 0) ? 1u : 0u);
+                    umma_commit(&c.pv_done[s]);
+                    if (i == to[s] - 1) umma_commit(&c.o_full[s]);
                 };
-                for (int j = t.first - 1; ok && j < t.end; ++j) {
-                    const bool more = j + 1 < t.end;
-                    if (kScores == 2 && more) {
-                        if (j + 1 >= t.from[0] && j + 1 < t.to[0]) scores(0, j + 1);
-                        if (ok) umma_commit(&c.k_empty[(tiles + j + 1 - t.first) % kStages]);
-                    }
+                // (S(i + 1) goes where P(i - 1) was, whose product was issued before it: a thread's products run in order)
+                for (int i = -1; ok && i < count; ++i) {
+                    if (i + 1 < count) {
 #pragma unroll
-                    for (int s = 0; s < kStreams; ++s) {
-                        if (ok && j >= t.from[s] && j < t.to[s]) outputs(s, j);
-                        if (ok && s == kStreams - 1 && j >= t.first) umma_commit(&c.v_empty[(tiles + j - t.first) % kStages]);
-                        if (ok && kScores == 1 && more && j + 1 >= t.from[s] && j + 1 < t.to[s]) scores(s, j + 1);
+                        for (int s = 0; s < kStreams; ++s)
+                            if (ok && i + 1 >= from[s] && i + 1 < to[s]) scores(s, i + 1);
+                        if (ok) umma_commit(&c.k_empty[(tiles + i + 1) % kStages]);
                     }
-                    if (ok && kScores == 1 && more) umma_commit(&c.k_empty[(tiles + j + 1 - t.first) % kStages]);
-                }
-                tiles += t.end - t.first;
+                    if (i >= 0) {
 #pragma unroll
-                for (int s = 0; s < kStreams; ++s) {
-                    done[s] += t.to[s] - t.from[s];
-                    items[s] += t.to[s] > t.from[s];
+                        for (int s = 0; s < kStreams; ++s)
+                            if (ok && i >= from[s] && i < to[s]) outputs(s, i);
+                        if (ok) umma_commit(&c.v_empty[(tiles + i) % kStages]);
+                    }
                 }
                 if (!ok) break;
+                tiles += count;
+#pragma unroll
+                for (int s = 0; s < kStreams; ++s) {
+                    done[s] += to[s] - from[s];
+                    items[s] += to[s] > from[s];
+                }
                 mbar_arrive(&c.item_empty[seq % S::kItems]);
             }
             if (!ok) {  // gave up: products already issued end before the CTA and its TMEM go (bounded)
@@ -252,7 +250,6 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         }
     } else if (warp == S::kSoftWarps + 1) {
         // ------------------------------------------------------------ copier
-        give();
         const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
         const int boxes = kKeys >> box_shift;
         int n = 0;  // tiles so far
@@ -260,24 +257,31 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
             const ChunkTileItem& t = c.item[seq % S::kItems];
             if (t.tokens == 0) break;
-            const int h = t.h;
+            const int h = t.h, first = t.first, count = t.end - t.first, k0 = t.k0, k1 = t.k1;
             const int32_t* pages = p.table + t.b * p.table_stride;
-            auto page_of = [&](int j) {  // of this lane's box in tile j; -1: none
-                const int key = j * kKeys + (lane << box_shift);
-                int page = -1;
-                if (lane < boxes && j < t.end && key < t.k1 && key + box > t.k0) page = pages[key >> p.page_shift];
+            // each lane knows the page of one of 32 boxes, and has asked for that of the box 32 further on: the table answers while
+            // those are copied (asked for a tile ahead and looked at at once, it held every tile up by its latency)
+            auto entry = [&](int i) {
+                const int key = first * kKeys + (i << box_shift);
+                return key < k1 && key + box > k0 ? pages[key >> p.page_shift] : -1;
+            };
+            auto checked = [&](int page) {
                 if (page >= p.num_pages) {
                     kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
                     page = -1;
                 }
                 return max(page, -1);
             };
-            int next = page_of(t.first);
-            for (int j = t.first; j < t.end; ++j, ++n) {
-                const int page = next;
-                next = page_of(j + 1);
+            int page = checked(entry(lane)), ahead = entry(32 + lane);
+            int at_box = 0;  // the tile's first box, among the 32
+            for (int i = 0; i < count; ++i, ++n, at_box += boxes) {
+                if (at_box == 32) {
+                    page = checked(ahead);
+                    ahead = entry(i * boxes + 32 + lane);
+                    at_box = 0;
+                }
                 const int stage = n % kStages;
-                const unsigned none = __ballot_sync(0xFFFFFFFFu, page < 0);
+                const unsigned none = __ballot_sync(0xFFFFFFFFu, page < 0) >> at_box;
                 for (int plane = 0; plane < 2; ++plane) {
                     uint64_t* empty = plane ? &c.v_empty[stage] : &c.k_empty[stage];
                     uint64_t* full = plane ? &c.v_full[stage] : &c.k_full[stage];
@@ -293,9 +297,9 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     }
                     const uint32_t to = smem_u32(plane ? v_ring : k_ring) + stage * S::kPlaneBytes;
                     for (int b = 0; b < boxes; ++b) {
-                        const int pg = __shfl_sync(0xFFFFFFFFu, page, b);  // (page -1 lies outside the map: zeros)
+                        const int pg = __shfl_sync(0xFFFFFFFFu, page, at_box + b);  // (page -1 lies outside the map: zeros)
                         if (lane == 0) {
-                            const int row = ((j * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
+                            const int row = (((first + i) * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
 #pragma unroll
                             for (int d = 0; d < DB; ++d)
                                 tma_load_4d(to + b * box * 128 + d * S::kBlockBytes, plane ? &map_v : &map_k, full, d * 64, row, h, pg);
@@ -317,19 +321,19 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         }
     } else if (warp == S::kSoftWarps + 2) {
         // ------------------------------------------------------------ cleaner
-        give();
         int n = 0, items = 0;
         for (int seq = 0; ok; ++seq) {
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
             const ChunkTileItem& t = c.item[seq % S::kItems];
             if (t.tokens == 0) break;
-            if (lane == 0 && t.end > t.first) c.odd[items & 3] = 0;
+            const int first = t.first, end = t.end, item_lo = t.lo, item_hi = t.hi, all_lo = t.all_lo, all_hi = t.all_hi;
+            if (lane == 0 && end > first) c.odd[items & 3] = 0;
             __syncwarp();
-            for (int j = t.first; j < t.end; ++j, ++n) {
+            for (int j = first; j < end; ++j, ++n) {
                 const int stage = n % kStages, key0 = j * kKeys;
                 if (!(ok = warp_wait(&c.v_full[stage], (n / kStages) & 1, ctl, 247))) break;
-                const int dead0 = max(t.lo - key0, 0), dead1 = min(t.hi - key0, kKeys);  // rows before and from which on nobody may look
-                const bool cut = key0 < t.all_lo || key0 + kKeys > t.all_hi;
+                const int dead0 = max(item_lo - key0, 0), dead1 = min(item_hi - key0, kKeys);  // rows before and from which on nobody may look
+                const bool cut = key0 < all_lo || key0 + kKeys > all_hi;
                 if (dead0 > 0 || dead1 < kKeys || cut) {
                     uint8_t* base = v_ring + stage * S::kPlaneBytes;
                     bool odd = false;
@@ -350,14 +354,13 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c.v_clean[stage]);
             }
-            items += t.end > t.first;
+            items += end > first;
             if (!ok) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.item_empty[seq % S::kItems]);
         }
     } else if (warp == S::kSoftWarps + 3) {
         // ------------------------------------------------------------ planner
-        give();
         ChunkDesc tail = {0, 0, 0, 0};
         WaitCtl patient = ctl;  // for an item's time, not a tile's; the others' waits raise the flag that ends this one, too
         patient.limit_ns = 16 * ctl.limit_ns;
@@ -381,14 +384,24 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         if (lane == 0) p.desc[blockIdx.x] = tail;
     } else if (warp < S::kSoftWarps) {
         // ------------------------------------------------------------ softmax: thread = row = TMEM lane
-        take();
-        const int s = warp >> 2, r = tid & 127;
+        const int s = S::kHalves == 2 ? 0 : warp >> 2, half = S::kHalves == 2 ? warp >> 2 : 0, r = tid & 127, pair = s * 4 + (warp & 3);
         const uint32_t inv_heads = 65536u / p.part_heads + 1;
         const int tok = token_of(r, inv_heads), head = r - tok * p.part_heads;
         const uint32_t t_rows = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), t_o = t_rows + S::kOCol + s * (DB * 64);
         const float scale = PLAIN ? fmaxf(fabsf(p.scale_log2), 1.2e-38f) : 1.0f;  // zero would turn masked logits into NaN
         const float slack = 8.0f / scale;
         const uint64_t scale2 = pair32(scale, scale);
+        constexpr int kMine = S::kMine;
+        int turn = 0;  // of what the halves tell each other
+        auto tell = [&](float v) {  // the other half's number (whatever it is where the wait failed and ok is false)
+            c.told[pair][turn & 1][half][lane] = v;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.halves[pair]);
+            ok = warp_wait(&c.halves[pair], turn & 1, ctl, 251);
+            const float other = *reinterpret_cast<volatile float*>(&c.told[pair][turn & 1][half ^ 1][lane]);
+            ++turn;
+            return other;
+        };
         int n = 0, items = 0, all_items = 0, tiles = 0;  // tiles and items of this stream; items with tiles; copied tiles
         for (int seq = 0; ok; ++seq) {
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
@@ -397,18 +410,18 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             const int my_tok = s * per + tok, pos = t.pos + my_tok;
             const bool live = tok < per && my_tok < t.tokens && head < t.heads;
             const int from = t.from[s], to = t.to[s];
-            float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum
+            float m = -INFINITY, l = 0.0f;  // reference of the exponentials (in logits before scaling), sum over this half's keys
             int lo = 0, hi = 0x7FFFFFFF;    // rows that are nobody's look at everything: no tile is cut for them
             if (live) chunk_sees(p, t.r, pos, true, lo, hi);
             const int warp_lo = __reduce_max_sync(0xFFFFFFFFu, lo), warp_hi = __reduce_min_sync(0xFFFFFFFFu, hi);
             if (to > from) {
                 // queries: rows of 128 bytes to a 64-column block, 16-byte pieces exchanged by the row's low bits
-                constexpr int kPieces = DB * 8, kStep = 128 / kPieces;
+                constexpr int kPieces = DB * 8, kStep = S::kRowThreads / kPieces;
                 const int piece = r % kPieces;
                 const uint32_t dst = smem_u32(smem) + s * S::kQBytes + (piece >> 3) * (128 * 128);
                 const T* q0 = static_cast<const T*>(p.q) + static_cast<int64_t>(t.token + s * per) * p.q_stride[0] + static_cast<int64_t>(t.head0) * p.q_stride[1] + piece * 8;
 #pragma unroll 4
-                for (int row = r / kPieces; row < 128; row += kStep) {
+                for (int row = (half * 128 + r) / kPieces; row < 128; row += kStep) {
                     const int tk = token_of(row, inv_heads), hd = row - tk * p.part_heads;
                     const bool in = piece * 8 < p.dim && tk < per && s * per + tk < t.tokens && hd < t.heads;
                     cp_async16(dst + row * 128 + (((piece & 7) ^ (row & 7)) << 4), in ? q0 + tk * p.q_stride[0] + hd * p.q_stride[1] : static_cast<const T*>(p.q), in);
@@ -418,59 +431,64 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 fence_proxy_async_smem();
                 mbar_arrive(&c.q_full[s]);
             }
+            const unsigned hole0 = tiles - t.first;
             float slope = 0.0f;
             if (!PLAIN && p.slopes && live) slope = p.slopes[t.head0 + head] * 1.4426950408889634f;
 
             for (int j = from; j < to; ++j, ++n) {
-                const int key0 = j * kKeys;
-                const int buffer = kScores == 2 ? n & 1 : s;
+                const int key0 = j * kKeys + half * kMine;
+                const int buffer = s * 2 + (n & 1);
                 const uint32_t t_s = t_rows + buffer * kKeys;
-                if (!(ok = warp_wait(&c.s_full[buffer], kScores == 2 ? (n >> 1) & 1 : n & 1, ctl, 248))) break;
+                if (!(ok = warp_wait(&c.s_full[buffer], (n >> 1) & 1, ctl, 248))) break;
                 tc_fence_after_sync();
-                const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(tiles + j - t.first) % S::kHoles]);
-                uint32_t x[kKeys / 64][64];
-#pragma unroll
-                for (int q = 0; q < kKeys / 64; ++q) tmem_ld_32x32b_x64(t_s + q * 64, x[q]);
-#pragma unroll
-                for (int q = 0; q < kKeys / 64; ++q) tmem_wait_ld_regs(x[q]);
-                auto logit = [&](int i) -> uint32_t& { return x[i >> 6][i & 63]; };
+                uint32_t x[kMine];
+                if constexpr (kMine == 64) tmem_ld_32x32b_x64(t_s + half * kMine, x);
+                else tmem_ld_32x32b_x32(t_s + half * kMine, x);
+                const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(hole0 + j) % S::kHoles]) >> (half * (kMine / 16));
+                tmem_wait_ld_regs(x);
                 if (!PLAIN) {
 #pragma unroll
-                    for (int i = 0; i < kKeys; ++i) {
-                        float z = __uint_as_float(logit(i));
+                    for (int i = 0; i < kMine; ++i) {
+                        float z = __uint_as_float(x[i]);
                         z = p.cap_out == 0.0f ? z * fabsf(p.scale_log2) : fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(z * fabsf(p.cap_in))), p.cap_out);
                         if (p.slopes) z = fmaf(-slope, fabsf(static_cast<float>(pos - key0 - i)), z);
-                        logit(i) = __float_as_uint(z);
+                        x[i] = __float_as_uint(z);
                     }
                 }
-                if (key0 < warp_lo || key0 + kKeys > warp_hi || holes) {  // not all rows of the warp see all of it
+                if (key0 < warp_lo || key0 + kMine > warp_hi || holes) {  // not all rows of the warp see all of it
                     const int a = lo - key0, b = hi - key0;
 #pragma unroll
-                    for (int i = 0; i < kKeys; ++i)
-                        if (i < a || i >= b || (holes >> (i / 16) & 1)) logit(i) = 0xFF800000u;
+                    for (int i = 0; i < kMine; ++i)
+                        if (i < a || i >= b || (holes >> (i / 16) & 1)) x[i] = 0xFF800000u;
                 }
-                float top = -INFINITY;
+                float top;
                 {
                     float part[4];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) part[q] = fmaxf(__uint_as_float(logit(2 * q)), __uint_as_float(logit(2 * q + 1)));
+                    for (int q = 0; q < 4; ++q) part[q] = fmaxf(__uint_as_float(x[2 * q]), __uint_as_float(x[2 * q + 1]));
 #pragma unroll
-                    for (int i = 8; i < kKeys; i += 8)
+                    for (int i = 8; i < kMine; i += 8)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) part[q] = max3f(part[q], __uint_as_float(logit(i + 2 * q)), __uint_as_float(logit(i + 2 * q + 1)));
+                        for (int q = 0; q < 4; ++q) part[q] = max3f(part[q], __uint_as_float(x[i + 2 * q]), __uint_as_float(x[i + 2 * q + 1]));
                     top = fmaxf(max3f(part[0], part[1], part[2]), part[3]);
+                }
+                if (S::kHalves == 2) {
+                    tc_fence_before_sync();  // (the other half's P comes to lie over what this one has read)
+                    top = fmaxf(top, tell(top));
+                    if (!ok) break;
+                    tc_fence_after_sync();
                 }
                 const bool grow = top > m + slack || (m == -INFINITY && top > m);
                 if (__any_sync(0xFFFFFFFFu, grow)) {
-                    const float fix = grow && l > 0.0f ? exp2_fast((m - top) * scale) : 1.0f;
+                    // (the sums may be zero in one half alone: both rescale by the same number)
+                    const float fix = grow && m > -INFINITY ? exp2_fast((m - top) * scale) : 1.0f;
                     if (grow) m = top;
-                    if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (a sum that is not zero: j > from)
-                        if (kScores == 2) {  // (with one S its product follows the one before it)
-                            if (!(ok = warp_wait(&c.pv_done[s], (n - 1) & 1, ctl, 249))) break;
-                            tc_fence_after_sync();
-                        }
+                    if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (something was seen before: j > from)
+                        if (!(ok = warp_wait(&c.pv_done[s], (n - 1) & 1, ctl, 249))) break;
+                        tc_fence_after_sync();
                         l *= fix;
-                        for (int q = 0; q < p.dim >> 4; ++q) {  // 16 columns at a time: the logits stay in registers
+                        const int q1 = p.dim >> 4;  // the first half takes the first columns, 16 at a time: the logits stay in registers
+                        for (int q = half * ((q1 + 1) / 2); q < (S::kHalves == 2 && !half ? (q1 + 1) / 2 : q1); ++q) {
                             uint32_t o[16];
                             tmem_ld_32x32b_x16(t_o + q * 16, o);
 #pragma unroll
@@ -483,16 +501,16 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 const uint64_t off = pair32(-base, -base);
                 uint64_t sum[2] = {0, 0};  // of two 32-bit sums each
 #pragma unroll
-                for (int q = 0; q < kKeys / 32; ++q) {
+                for (int q = 0; q < kMine / 32; ++q) {
                     uint32_t out[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        const uint64_t z = fma2(pair32(__uint_as_float(logit(q * 32 + i)), __uint_as_float(logit(q * 32 + i + 1))), scale2, off);
+                        const uint64_t z = fma2(pair32(__uint_as_float(x[q * 32 + i]), __uint_as_float(x[q * 32 + i + 1])), scale2, off);
                         const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
                         sum[i / 2 & 1] = add2(sum[i / 2 & 1], pair32(a, b));
                         out[i / 2] = Pair16<T>::pack(a, b);
                     }
-                    tmem_st_32x32b_x16(t_s + q * 16, out);
+                    tmem_st_32x32b_x16(t_s + half * (kMine / 2) + q * 16, out);
                 }
                 const uint64_t both = add2(sum[0], sum[1]);
                 l += lo32(both) + hi32(both);
@@ -502,7 +520,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             }
             if (!ok) break;
             if (to > from) {
-                if (!(ok = warp_wait(&c.o_full[s], items & 1, ctl, 250))) break;
+                if (S::kHalves == 2) l += tell(l);
+                if (!ok || !(ok = warp_wait(&c.o_full[s], items & 1, ctl, 250))) break;
                 tc_fence_after_sync();
                 ++items;
             }
@@ -512,7 +531,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             const int row = my_tok * p.part_heads + head;
             float* slot = p.slots + static_cast<int64_t>(t.slot) * p.rows * (p.dim + 2);
             T* out = static_cast<T*>(p.out) + static_cast<int64_t>(t.token + my_tok) * p.out_stride[0] + static_cast<int64_t>(t.head0 + head) * p.out_stride[1];
-            for (int q = 0; q < (p.dim + 31) / 32; ++q) {
+            const int q1 = (p.dim + 31) / 32;
+            for (int q = half * ((q1 + 1) / 2); q < (S::kHalves == 2 && !half ? (q1 + 1) / 2 : q1); ++q) {
                 uint32_t o[32];
                 if (to > from) {
                     tmem_ld_32x32b_x32(t_o + q * 32, o);
@@ -541,7 +561,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 tc_fence_before_sync();
                 mbar_arrive(&c.o_free[s]);
             }
-            if (live) {
+            if (live && half == 0) {
                 const float best = m * scale;
                 if (whole) {
                     if (p.lse)
