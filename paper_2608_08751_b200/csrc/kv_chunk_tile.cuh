@@ -5,11 +5,10 @@
 //
 //   softmax warps   a thread per row: S out of TMEM, maximum and sum in registers, P over S in TMEM.  O is rescaled only when the maximum has
 //                   grown by more than 2^8 past the reference of the exponentials; the reference cancels in the final division
-//   issuer          one thread: S = Q K^T into TMEM, O += P V with P from TMEM.  While one stream's rows are in its softmax
-//                   warps the other stream's products run
+//   issuers         a thread to a stream: S = Q K^T into TMEM, O += P V with P from TMEM
 //   copier          the tiles' pages, looked up a tile ahead, by TMA
-//   planner         walks the CTA's span and leaves a record of each item for the other warps, whose loops need the registers
-//   cleaner         value rows that no row of the item may look at become zeros, and in tiles that not all rows see values that are not
+//   planner         walks the CTA's span and leaves a record of each item for the other warps, whose loops need the registers; and cleans: value
+//                   rows that no row of the item may look at become zeros, and in tiles that not all rows see values that are not
 //                   finite are taken out
 //
 // A tile is 64 keys.  A stream has two S, P lies over its S, and S(j + 1) is issued before P(j) V: the softmax warps find the next
@@ -62,7 +61,7 @@ struct ChunkTileControl {
     uint64_t item_full[S::kItems], item_empty[S::kItems];
     uint64_t k_full[S::kStages], v_full[S::kStages], k_empty[S::kStages], v_empty[S::kStages], v_clean[S::kStages];
     uint64_t q_full[S::kStreams], s_full[S::kStreams * 2], p_ready[S::kStreams * 2], pv_done[S::kStreams], o_full[S::kStreams], o_free[S::kStreams];
-    uint64_t halves[S::kStreams * 4], drain;
+    uint64_t halves[S::kStreams * 4], drain[S::kStreams];
     float told[S::kStreams * 4][2][2][32];  // by warp pair, turn and half: maxima of a tile, at last the sums
     ChunkPlan<S::kThreads> plan;
     uint32_t holes[S::kHoles];  // by tile: groups of 16 keys without a page
@@ -126,14 +125,15 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&c.k_full[i], 1);
             mbar_init(&c.v_full[i], 1);
-            mbar_init(&c.k_empty[i], 1);
-            mbar_init(&c.v_empty[i], 1);
+            mbar_init(&c.k_empty[i], kStreams);
+            mbar_init(&c.v_empty[i], kStreams);
             mbar_init(&c.v_clean[i], 1);
         }
         for (int i = 0; i < kStreams; ++i) {
             mbar_init(&c.q_full[i], S::kRowThreads);
             mbar_init(&c.pv_done[i], 1);
             mbar_init(&c.o_full[i], 1);
+            mbar_init(&c.drain[i], 1);
             mbar_init(&c.o_free[i], S::kRowThreads);
         }
         for (int i = 0; i < kStreams * 2; ++i) {
@@ -142,10 +142,9 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         }
         for (int i = 0; i < S::kItems; ++i) {
             mbar_init(&c.item_full[i], 1);
-            mbar_init(&c.item_empty[i], S::kWarps - 1);
+            mbar_init(&c.item_empty[i], S::kSoftWarps + kStreams + 1);
         }
         for (int i = 0; i < kStreams * 4; ++i) mbar_init(&c.halves[i], 2);
-        mbar_init(&c.drain, 1);
         c.abort_flag = 0;
         fence_mbar_init();
         tma_prefetch_desc(&map_k);
@@ -167,88 +166,80 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     ctl.limit_ns = p.limit_ns;
     const int per = p.tile_tokens / kStreams;  // tokens of a stream
     bool ok = true;
-    if (warp == S::kSoftWarps) {
-        // ------------------------------------------------------------ issuer
+    if (warp >= S::kSoftWarps && warp < S::kSoftWarps + kStreams) {
+        // ------------------------------------------------------------ issuers: one to a stream
         if (elect_one()) {
+            const int s = warp - S::kSoftWarps;
             const uint32_t negate = p.scale_log2 < 0.0f ? 1u << 13 : 0u;  // a negative scale is a positive one of negated queries
             const uint32_t idesc_s = tile_idesc<T>(kKeys, false) | negate, idesc_o = tile_idesc<T>(p.dim, true);
             const int ksteps = p.dim >> 4;
-            const uint32_t k0_lo = umma_desc_lo(smem_u32(k_ring)), q0_lo = umma_desc_lo(smem_u32(smem));
+            const uint32_t k0_lo = umma_desc_lo(smem_u32(k_ring)), q_lo = umma_desc_lo(smem_u32(smem)) + s * (S::kQBytes >> 4);
+            // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
             const uint32_t v0_lo = ((smem_u32(v_ring) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-            int tiles = 0;         // copied tiles before this item
-            int done[2] = {0, 0};  // tiles of a stream before this item
-            int items[2] = {0, 0}; // items with tiles of a stream so far
+            const uint32_t t_s = tmem + s * 2 * kKeys, t_o = tmem + S::kOCol + s * (DB * 64);
+            int tiles = 0;  // copied tiles before this item
+            int done = 0;   // tiles of the stream before it
+            int items = 0;  // items with tiles of the stream
             for (int seq = 0;; ++seq) {
                 if (!(ok = mbar_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
                 const ChunkTileItem& t = c.item[seq % S::kItems];
                 if (t.tokens == 0) break;
-                // (in registers, and counted from the part's first tile: read from shared memory at each use they cost the products more than
-                // the products cost)
-                const int count = t.end - t.first;
-                int from[kStreams], to[kStreams];
-#pragma unroll
-                for (int s = 0; s < kStreams; ++s) from[s] = t.from[s] - t.first, to[s] = t.to[s] - t.first;
-                auto scores = [&](int s, int i) {  // S of a stream and tile
-                    const int n = tiles + i, d = done[s] + i - from[s];
-                    if (!(ok = mbar_wait(&c.k_full[n % kStages], (n / kStages) & 1, ctl, 241))) return;
-                    if (i == from[s] && !(ok = mbar_wait(&c.q_full[s], items[s] & 1, ctl, 242))) return;
-                    tc_fence_after_sync();
-                    const uint32_t k_lo = k0_lo + (n % kStages) * (S::kPlaneBytes >> 4), q_lo = q0_lo + s * (S::kQBytes >> 4);
-                    const uint32_t at = tmem + (s * 2 + (d & 1)) * kKeys;
-#pragma unroll
-                    for (int k = 0; k < DB * 4; ++k)
-                        if (k < ksteps)
-                            umma_f16(at, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
-                                     umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc_s, k > 0);
-                    umma_commit(&c.s_full[s * 2 + (d & 1)]);
-                };
-                auto outputs = [&](int s, int i) {  // O of a stream, by a tile
-                    const int n = tiles + i, d = done[s] + i - from[s];
-                    if (!(ok = mbar_wait(&c.v_clean[n % kStages], (n / kStages) & 1, ctl, 243))) return;
-                    if (i == from[s] && items[s] > 0 && !(ok = mbar_wait(&c.o_free[s], (items[s] - 1) & 1, ctl, 244))) return;
-                    if (!(ok = mbar_wait(&c.p_ready[s * 2 + (d & 1)], (d >> 1) & 1, ctl, 245))) return;
-                    tc_fence_after_sync();
-                    // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
-                    const uint32_t v_lo = v0_lo + (n % kStages) * (S::kPlaneBytes >> 4);
-                    const uint32_t t_p = tmem + (s * 2 + (d & 1)) * kKeys, t_o = tmem + S::kOCol + s * (DB * 64);
-#pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        umma_f16_ts(t_o, t_p + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (i > from[s] || k > 0) ? 1u : 0u);
-                    umma_commit(&c.pv_done[s]);
-                    if (i == to[s] - 1) umma_commit(&c.o_full[s]);
-                };
-                // (S(i + 1) goes where P(i - 1) was, whose product was issued before it: a thread's products run in order)
+                // (in registers, and counted from the part's first tile: read from shared memory at each use they cost more than the products)
+                const int count = t.end - t.first, from = t.from[s] - t.first, to = t.to[s] - t.first;
+                // S(i + 1) goes where P(i - 1) was, whose product was issued before it: a thread's products run in order
                 for (int i = -1; ok && i < count; ++i) {
-                    if (i + 1 < count) {
+                    const int next = i + 1;
+                    if (next < count) {
+                        const int n = tiles + next, d = done + next - from;
+                        if (!(ok = mbar_wait(&c.k_full[n % kStages], (n / kStages) & 1, ctl, 241))) break;
+                        if (next >= from && next < to) {
+                            if (next == from && !(ok = mbar_wait(&c.q_full[s], items & 1, ctl, 242))) break;
+                            tc_fence_after_sync();
+                            const uint32_t k_lo = k0_lo + (n % kStages) * (S::kPlaneBytes >> 4);
 #pragma unroll
-                        for (int s = 0; s < kStreams; ++s)
-                            if (ok && i + 1 >= from[s] && i + 1 < to[s]) scores(s, i + 1);
-                        if (ok) umma_commit(&c.k_empty[(tiles + i + 1) % kStages]);
+                            for (int k = 0; k < DB * 4; ++k)
+                                if (k < ksteps)
+                                    umma_f16(t_s + (d & 1) * kKeys, umma_desc_join(q_lo + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, kDescHiSw128),
+                                             umma_desc_join(k_lo + (k >> 2) * (S::kBlockBytes >> 4) + (k & 3) * 2, kDescHiSw128), idesc_s, k > 0);
+                            umma_commit(&c.s_full[s * 2 + (d & 1)]);
+                            umma_commit(&c.k_empty[n % kStages]);
+                        } else {
+                            mbar_arrive(&c.k_empty[n % kStages]);
+                        }
                     }
                     if (i >= 0) {
+                        const int n = tiles + i, d = done + i - from;
+                        if (!(ok = mbar_wait(&c.v_clean[n % kStages], (n / kStages) & 1, ctl, 243))) break;
+                        if (i >= from && i < to) {
+                            if (i == from && items > 0 && !(ok = mbar_wait(&c.o_free[s], (items - 1) & 1, ctl, 244))) break;
+                            if (!(ok = mbar_wait(&c.p_ready[s * 2 + (d & 1)], (d >> 1) & 1, ctl, 245))) break;
+                            tc_fence_after_sync();
+                            const uint32_t v_lo = v0_lo + (n % kStages) * (S::kPlaneBytes >> 4);
 #pragma unroll
-                        for (int s = 0; s < kStreams; ++s)
-                            if (ok && i >= from[s] && i < to[s]) outputs(s, i);
-                        if (ok) umma_commit(&c.v_empty[(tiles + i) % kStages]);
+                            for (int k = 0; k < kKeys / 16; ++k)
+                                umma_f16_ts(t_o, t_s + (d & 1) * kKeys + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (i > from || k > 0) ? 1u : 0u);
+                            umma_commit(&c.pv_done[s]);
+                            umma_commit(&c.v_empty[n % kStages]);
+                            if (i == to - 1) umma_commit(&c.o_full[s]);
+                        } else {
+                            mbar_arrive(&c.v_empty[n % kStages]);
+                        }
                     }
                 }
                 if (!ok) break;
                 tiles += count;
-#pragma unroll
-                for (int s = 0; s < kStreams; ++s) {
-                    done[s] += to[s] - from[s];
-                    items[s] += to[s] > from[s];
-                }
+                done += to - from;
+                items += to > from;
                 mbar_arrive(&c.item_empty[seq % S::kItems]);
             }
             if (!ok) {  // gave up: products already issued end before the CTA and its TMEM go (bounded)
-                umma_commit(&c.drain);
+                umma_commit(&c.drain[s]);
                 const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
+                while (!mbar_try_wait(&c.drain[s], 0) && global_timer_ns() - t0 < 2000000000ull) {
                 }
             }
         }
-    } else if (warp == S::kSoftWarps + 1) {
+    } else if (warp == S::kSoftWarps + 2) {
         // ------------------------------------------------------------ copier
         const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
         const int boxes = kKeys >> box_shift;
@@ -319,17 +310,39 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     while (!mbar_try_wait(plane ? &c.v_full[i % kStages] : &c.k_full[i % kStages], (i / kStages) & 1) && global_timer_ns() - t0 < 100000000ull) {
                     }
         }
-    } else if (warp == S::kSoftWarps + 2) {
-        // ------------------------------------------------------------ cleaner
-        int n = 0, items = 0;
+    } else if (warp == S::kSoftWarps + 3) {
+        // ------------------------------------------------------------ planner and cleaner
+        ChunkDesc tail = {0, 0, 0, 0};
+        WaitCtl patient = ctl;  // for an item's time, not a tile's; the others' waits raise the flag that ends this one, too
+        patient.limit_ns = 16 * ctl.limit_ns;
+        int planned = 0, n = 0, items = 0;
+        bool end = false;
         for (int seq = 0; ok; ++seq) {
-            if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
-            const ChunkTileItem& t = c.item[seq % S::kItems];
-            if (t.tokens == 0) break;
-            const int first = t.first, end = t.end, item_lo = t.lo, item_hi = t.hi, all_lo = t.all_lo, all_hi = t.all_hi;
-            if (lane == 0 && end > first) c.odd[items & 3] = 0;
+            // two items ahead: their places are free when the item two before this one has ended
+            for (; !end && planned <= seq + 2; ++planned) {
+                ChunkTileItem& t = c.item[planned % S::kItems];
+                if (planned >= S::kItems && !(ok = warp_wait(&c.item_empty[planned % S::kItems], (planned / S::kItems - 1) & 1, patient, 239))) break;
+                end = at.left <= 0;
+                if (lane == 0) {
+                    if (end) {
+                        t.tokens = 0;
+                    } else {
+                        const ChunkItem it = chunk_item(p, at);
+                        chunk_record<kStreams, kKeys>(p, at, it, t);
+                        if (it.first && !it.last) tail = ChunkDesc{chunk_parts(c.plan.total, ctas, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
+                    }
+                    mbar_arrive(&c.item_full[planned % S::kItems]);
+                }
+                if (!end) chunk_next(p, at);
+            }
             __syncwarp();
-            for (int j = first; j < end; ++j, ++n) {
+            if (!ok) break;
+            const ChunkTileItem& t = c.item[seq % S::kItems];
+            if (*reinterpret_cast<const volatile int*>(&t.tokens) == 0) break;
+            const int first = t.first, last = t.end, item_lo = t.lo, item_hi = t.hi, all_lo = t.all_lo, all_hi = t.all_hi;
+            if (lane == 0 && last > first) c.odd[items & 3] = 0;
+            __syncwarp();
+            for (int j = first; j < last; ++j, ++n) {
                 const int stage = n % kStages, key0 = j * kKeys;
                 if (!(ok = warp_wait(&c.v_full[stage], (n / kStages) & 1, ctl, 247))) break;
                 const int dead0 = max(item_lo - key0, 0), dead1 = min(item_hi - key0, kKeys);  // rows before and from which on nobody may look
@@ -337,6 +350,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 if (dead0 > 0 || dead1 < kKeys || cut) {
                     uint8_t* base = v_ring + stage * S::kPlaneBytes;
                     bool odd = false;
+#pragma unroll 4
                     for (int x = lane; x < kKeys * 8 * DB; x += 32) {
                         const int row = (x >> 3) % kKeys;  // (16-byte pieces change places within a row only)
                         uint4* piece = reinterpret_cast<uint4*>(base + x * 16);
@@ -354,32 +368,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c.v_clean[stage]);
             }
-            items += end > first;
-            if (!ok) break;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.item_empty[seq % S::kItems]);
-        }
-    } else if (warp == S::kSoftWarps + 3) {
-        // ------------------------------------------------------------ planner
-        ChunkDesc tail = {0, 0, 0, 0};
-        WaitCtl patient = ctl;  // for an item's time, not a tile's; the others' waits raise the flag that ends this one, too
-        patient.limit_ns = 16 * ctl.limit_ns;
-        for (int seq = 0; ok; ++seq) {
-            ChunkTileItem& t = c.item[seq % S::kItems];
-            if (seq >= S::kItems && !(ok = warp_wait(&c.item_empty[seq % S::kItems], (seq / S::kItems - 1) & 1, patient, 239))) break;
-            const bool end = at.left <= 0;
-            if (lane == 0) {
-                if (end) {
-                    t.tokens = 0;
-                } else {
-                    const ChunkItem it = chunk_item(p, at);
-                    chunk_record<kStreams, kKeys>(p, at, it, t);
-                    if (it.first && !it.last) tail = ChunkDesc{chunk_parts(c.plan.total, ctas, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
-                }
-                mbar_arrive(&c.item_full[seq % S::kItems]);
-            }
-            if (end) break;
-            chunk_next(p, at);
+            items += last > first;
         }
         if (lane == 0) p.desc[blockIdx.x] = tail;
     } else if (warp < S::kSoftWarps) {
