@@ -35,7 +35,9 @@ struct ChunkTileShape {
     static constexpr int kRowThreads = 128 * kHalves;  // of a stream
     static constexpr int kWarps = kSoftWarps + 4;
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kOCol = 256, kCols = 512;
+    static constexpr int kOCol = 256, kCols = 512;   // of TMEM; S lies at 0
+    static constexpr int kPCol = DB == 4 ? 128 : -1; // -1: P lies over its S
+    static constexpr int kPStep = DB == 4 ? kKeys / 2 : kKeys;
     static constexpr int kHoles = 16;                // tiles whose missing pages are remembered
     static constexpr int kItems = 4;                 // items that are planned ahead
 };
@@ -107,6 +109,29 @@ __device__ __forceinline__ void chunk_record(const ChunkParams& p, const ChunkCu
     chunk_sees(p, it.r, it.pos + it.tokens - 1, true, t.all_lo, skip);
 }
 
+// 2^z for two z <= 127 on the multiply-add units: z = n + f with n whole and |f| <= 1/2, and a polynomial of degree 5 for 2^f (Remez
+// exchange on the relative error, 2.2e-7 in 32 bits: as near as the special function unit comes).  Below -126.5 it is 0, so -infinity, a masked
+// logit, gives exactly 0; NaN stays NaN.
+__device__ __forceinline__ uint64_t exp2_poly(uint64_t z) {
+    float a, b;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(lo32(z)), "f"(-127.0f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(hi32(z)), "f"(-127.0f));
+    const uint64_t x = pair32(a, b), big = pair32(12582912.0f, 12582912.0f);  // 1.5 * 2^23: the sum's last bits are round(x)
+    const uint64_t t = add2(x, big);
+    const uint64_t n = add2(t, pair32(-12582912.0f, -12582912.0f));
+    const uint64_t f = fma2(n, pair32(-1.0f, -1.0f), x);
+    uint64_t y = pair32(0.0013276472454890609f, 0.0013276472454890609f);
+    y = fma2(y, f, pair32(0.009675540961325169f, 0.009675540961325169f));
+    y = fma2(y, f, pair32(0.05550713092088699f, 0.05550713092088699f));
+    y = fma2(y, f, pair32(0.24022120237350464f, 0.24022120237350464f));
+    y = fma2(y, f, pair32(0.6931469440460205f, 0.6931469440460205f));
+    y = fma2(y, f, pair32(1.0000001192092896f, 1.0000001192092896f));
+    const uint32_t lo = (static_cast<uint32_t>(t) << 23) + 0x3F800000u, hi = (static_cast<uint32_t>(t >> 32) << 23) + 0x3F800000u;  // 2^n; 0 for n = -127
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(y), "l"(pair32(__uint_as_float(lo), __uint_as_float(hi))));
+    return r;
+}
+
 // PLAIN: neither a cap nor a bias.
 template <typename T, int DB, bool PLAIN>
 __global__ void __launch_bounds__(ChunkTileShape<DB>::kThreads, 1)
@@ -176,7 +201,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             const uint32_t k0_lo = umma_desc_lo(smem_u32(k_ring)), q_lo = umma_desc_lo(smem_u32(smem)) + s * (S::kQBytes >> 4);
             // values: N (the head's columns) contiguous; blocks of 64 columns kBlockBytes apart, 8 keys 1024 bytes
             const uint32_t v0_lo = ((smem_u32(v_ring) & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(S::kBlockBytes >> 4) << 16);
-            const uint32_t t_s = tmem + s * 2 * kKeys, t_o = tmem + S::kOCol + s * (DB * 64);
+            const uint32_t t_s = tmem + s * 2 * kKeys, t_p = S::kPCol >= 0 ? tmem + S::kPCol : t_s, t_o = tmem + S::kOCol + s * (DB * 64);
             int tiles = 0;  // copied tiles before this item
             int done = 0;   // tiles of the stream before it
             int items = 0;  // items with tiles of the stream
@@ -217,7 +242,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                             const uint32_t v_lo = v0_lo + (n % kStages) * (S::kPlaneBytes >> 4);
 #pragma unroll
                             for (int k = 0; k < kKeys / 16; ++k)
-                                umma_f16_ts(t_o, t_s + (d & 1) * kKeys + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (i > from || k > 0) ? 1u : 0u);
+                                umma_f16_ts(t_o, t_p + (d & 1) * S::kPStep + k * 8, umma_desc_join(v_lo + k * (2048 >> 4), kDescHiSw128), idesc_o, (i > from || k > 0) ? 1u : 0u);
                             umma_commit(&c.pv_done[s]);
                             umma_commit(&c.v_empty[n % kStages]);
                             if (i == to - 1) umma_commit(&c.o_full[s]);
@@ -243,6 +268,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         // ------------------------------------------------------------ copier
         const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
         const int boxes = kKeys >> box_shift;
+        const uint32_t k_at = smem_u32(k_ring), v_at = smem_u32(v_ring);
         int n = 0;  // tiles so far
         for (int seq = 0; ok; ++seq) {
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
@@ -273,33 +299,29 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 }
                 const int stage = n % kStages;
                 const unsigned none = __ballot_sync(0xFFFFFFFFu, page < 0) >> at_box;
-                for (int plane = 0; plane < 2; ++plane) {
-                    uint64_t* empty = plane ? &c.v_empty[stage] : &c.k_empty[stage];
-                    uint64_t* full = plane ? &c.v_full[stage] : &c.k_full[stage];
-                    if (n >= kStages && !(ok = warp_wait(empty, (n / kStages - 1) & 1, ctl, 246))) break;
-                    if (lane == 0) {
-                        if (plane == 0) {
-                            uint32_t holes = 0;
-                            for (int b = 0; b < boxes; ++b)
-                                if (none >> b & 1) holes |= ((1u << (box / 16)) - 1) << (b * (box / 16));
-                            *reinterpret_cast<volatile uint32_t*>(&c.holes[n % S::kHoles]) = holes;
-                        }
-                        mbar_arrive_expect_tx(full, S::kPlaneBytes);
-                    }
-                    const uint32_t to = smem_u32(plane ? v_ring : k_ring) + stage * S::kPlaneBytes;
-                    for (int b = 0; b < boxes; ++b) {
-                        const int pg = __shfl_sync(0xFFFFFFFFu, page, at_box + b);  // (page -1 lies outside the map: zeros)
-                        if (lane == 0) {
-                            const int row = (((first + i) * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
-#pragma unroll
-                            for (int d = 0; d < DB; ++d)
-                                tma_load_4d(to + b * box * 128 + d * S::kBlockBytes, plane ? &map_v : &map_k, full, d * 64, row, h, pg);
-                        }
-                    }
+                // a lane to each copy of 64 columns of a box: one after the other from one lane they took the warp 110 cycles each, and a tile of
+                // four pages of 16 tokens is 16 of them
+                const int b = lane / DB, d = lane % DB;
+                const int pg = __shfl_sync(0xFFFFFFFFu, page, at_box + b);  // (page -1 lies outside the map: zeros)
+                const int row = (((first + i) * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
+                const uint32_t place = stage * S::kPlaneBytes + b * box * 128 + d * S::kBlockBytes;
+                if (n >= kStages && !(ok = warp_wait(&c.k_empty[stage], (n / kStages - 1) & 1, ctl, 246))) break;
+                if (lane == 0) {
+                    uint32_t holes = 0;
+                    if (none & ((1u << boxes) - 1))
+                        for (int x = 0; x < boxes; ++x)
+                            if (none >> x & 1) holes |= ((1u << (box / 16)) - 1) << (x * (box / 16));
+                    *reinterpret_cast<volatile uint32_t*>(&c.holes[n % S::kHoles]) = holes;
+                    mbar_arrive_expect_tx(&c.k_full[stage], S::kPlaneBytes);
                 }
-                if (!ok) break;  // (the tile's values were not asked for; its keys are waited for below with those before)
+                __syncwarp();
+                if (b < boxes) tma_load_4d(k_at + place, &map_k, &c.k_full[stage], d * 64, row, h, pg);
+                if (n >= kStages && !(ok = warp_wait(&c.v_empty[stage], (n / kStages - 1) & 1, ctl, 246))) break;
+                if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], S::kPlaneBytes);
+                __syncwarp();
+                if (b < boxes) tma_load_4d(v_at + place, &map_v, &c.v_full[stage], d * 64, row, h, pg);
             }
-            if (!ok) break;
+            if (!ok) break;  // (a tile's values were not asked for; its keys are waited for below with those before)
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.item_empty[seq % S::kItems]);
         }
@@ -377,8 +399,10 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const uint32_t inv_heads = 65536u / p.part_heads + 1;
         const int tok = token_of(r, inv_heads), head = r - tok * p.part_heads;
         const uint32_t t_rows = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), t_o = t_rows + S::kOCol + s * (DB * 64);
+        const uint32_t t_p = S::kPCol >= 0 ? t_rows + S::kPCol : t_rows + s * 2 * kKeys;
         const float scale = PLAIN ? fmaxf(fabsf(p.scale_log2), 1.2e-38f) : 1.0f;  // zero would turn masked logits into NaN
-        const float slack = 8.0f / scale;
+        const float slack = fminf(8.0f / scale, 3e38f);  // (finite: added to a reference of -infinity it stays that)
+        const float factor = fabsf(p.cap_out == 0.0f ? p.scale_log2 : p.cap_in);  // of a product, where there is a cap or a bias
         const uint64_t scale2 = pair32(scale, scale);
         constexpr int kMine = S::kMine;
         int turn = 0;  // of what the halves tell each other
@@ -436,12 +460,18 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(hole0 + j) % S::kHoles]) >> (half * (kMine / 16));
                 tmem_wait_ld_regs(x);
                 if (!PLAIN) {
+                    if (p.cap_out == 0.0f) {
 #pragma unroll
-                    for (int i = 0; i < kMine; ++i) {
-                        float z = __uint_as_float(x[i]);
-                        z = p.cap_out == 0.0f ? z * fabsf(p.scale_log2) : fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(z * fabsf(p.cap_in))), p.cap_out);
-                        if (p.slopes) z = fmaf(-slope, fabsf(static_cast<float>(pos - key0 - i)), z);
-                        x[i] = __float_as_uint(z);
+                        for (int i = 0; i < kMine; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * factor);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kMine; ++i)
+                            x[i] = __float_as_uint(fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(__uint_as_float(x[i]) * factor)), p.cap_out));
+                    }
+                    if (p.slopes) {
+                        const float away = static_cast<float>(pos - key0);
+#pragma unroll
+                        for (int i = 0; i < kMine; ++i) x[i] = __float_as_uint(fmaf(-slope, fabsf(away - i), __uint_as_float(x[i])));
                     }
                 }
                 if (key0 < warp_lo || key0 + kMine > warp_hi || holes) {  // not all rows of the warp see all of it
@@ -450,26 +480,35 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     for (int i = 0; i < kMine; ++i)
                         if (i < a || i >= b || (holes >> (i / 16) & 1)) x[i] = 0xFF800000u;
                 }
-                float top;
-                {
-                    float part[4];
+                // The exponentials are taken against the reference as it is, the maximum beside them (the special function unit leaves room for
+                // it); where it turns out to be too far above, which is rare but for a row's first tile, they are taken again.
+                uint64_t sum[2];
+                while (true) {
+                    const float base = m == -INFINITY ? 0.0f : m * scale;
+                    const uint64_t off = pair32(-base, -base);
+                    float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    sum[0] = sum[1] = 0;  // of two 32-bit sums each
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) part[q] = fmaxf(__uint_as_float(x[2 * q]), __uint_as_float(x[2 * q + 1]));
+                    for (int q = 0; q < kMine / 32; ++q) {
+                        uint32_t out[16];
 #pragma unroll
-                    for (int i = 8; i < kMine; i += 8)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) part[q] = max3f(part[q], __uint_as_float(x[i + 2 * q]), __uint_as_float(x[i + 2 * q + 1]));
-                    top = fmaxf(max3f(part[0], part[1], part[2]), part[3]);
-                }
-                if (S::kHalves == 2) {
-                    tc_fence_before_sync();  // (the other half's P comes to lie over what this one has read)
-                    top = fmaxf(top, tell(top));
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                }
-                const bool grow = top > m + slack || (m == -INFINITY && top > m);
-                if (__any_sync(0xFFFFFFFFu, grow)) {
-                    // (the sums may be zero in one half alone: both rescale by the same number)
+                        for (int i = 0; i < 32; i += 2) {
+                            const float a = __uint_as_float(x[q * 32 + i]), b = __uint_as_float(x[q * 32 + i + 1]);
+                            part[i / 2 & 3] = max3f(part[i / 2 & 3], a, b);
+                            const uint64_t z = fma2(pair32(a, b), scale2, off);
+                            const uint64_t w = pair32(exp2_fast(lo32(z)), exp2_fast(hi32(z)));
+                            sum[i / 2 & 1] = add2(sum[i / 2 & 1], w);
+                            out[i / 2] = Pair16<T>::pack(lo32(w), hi32(w));
+                        }
+                        tmem_st_32x32b_x16(t_p + (n & 1) * S::kPStep + half * (kMine / 2) + q * 16, out);
+                    }
+                    float top = fmaxf(max3f(part[0], part[1], part[2]), part[3]);
+                    if (S::kHalves == 2) {
+                        top = fmaxf(top, tell(top));
+                        if (!ok) break;
+                    }
+                    const bool grow = top > m + slack;
+                    if (!__any_sync(0xFFFFFFFFu, grow)) break;
                     const float fix = grow && m > -INFINITY ? exp2_fast((m - top) * scale) : 1.0f;
                     if (grow) m = top;
                     if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (something was seen before: j > from)
@@ -486,21 +525,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                         }
                     }
                 }
-                const float base = m == -INFINITY ? 0.0f : m * scale;
-                const uint64_t off = pair32(-base, -base);
-                uint64_t sum[2] = {0, 0};  // of two 32-bit sums each
-#pragma unroll
-                for (int q = 0; q < kMine / 32; ++q) {
-                    uint32_t out[16];
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const uint64_t z = fma2(pair32(__uint_as_float(x[q * 32 + i]), __uint_as_float(x[q * 32 + i + 1])), scale2, off);
-                        const float a = exp2_fast(lo32(z)), b = exp2_fast(hi32(z));
-                        sum[i / 2 & 1] = add2(sum[i / 2 & 1], pair32(a, b));
-                        out[i / 2] = Pair16<T>::pack(a, b);
-                    }
-                    tmem_st_32x32b_x16(t_s + half * (kMine / 2) + q * 16, out);
-                }
+                if (!ok) break;
                 const uint64_t both = add2(sum[0], sum[1]);
                 l += lo32(both) + hi32(both);
                 tmem_wait_st();
