@@ -368,8 +368,10 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
         chunk_sees(p, it.r, it.pos + it.tokens - 1, true, all_lo, skip);
         const int piece0 = it.k0 >> 4, pieces = it.k1 > it.k0 ? ((it.k1 + 15) >> 4) - piece0 : 0;
         const int mine = pieces > warp ? (pieces - warp + kRowsWarps - 1) / kRowsWarps : 0;
-        auto page_of = [&](int j) {  // of this warp's piece j
-            const int block = ((piece0 + warp + j * kRowsWarps) << 4) >> p.page_shift;
+        // the warp's j-th piece, the last ones first: where a bias falls with the distance the maximum is found at once
+        auto key_of = [&](int j) { return (piece0 + warp + (mine - 1 - j) * kRowsWarps) << 4; };
+        auto page_of = [&](int j) {
+            const int block = key_of(j) >> p.page_shift;
             int page = -1;
             if (j < mine) page = pages[block];
             if (page >= p.num_pages) {
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
             const int64_t page = __shfl_sync(0xFFFFFFFFu, page_now, j & 31);
             there = page >= 0 ? there | 1u << stage : there & ~(1u << stage);
             if (page >= 0) {
-                const int key0 = (piece0 + warp + j * kRowsWarps) << 4;
+                const int key0 = key_of(j);
                 const int tok0 = key0 & ((1 << p.page_shift) - 1);
                 const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + S::kPlaneBytes;
                 const T* ks = static_cast<const T*>(p.kc.base) + page * p.kc.page_stride + h * p.kc.head_stride;
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
             const bool has = there >> stage & 1;
             if (++stage == S::kStages) stage = 0;
             if (!has) continue;
-            const int key0 = (piece0 + warp + j * kRowsWarps) << 4;
+            const int key0 = key_of(j);
             float sc[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) sc[0][i] = sc[1][i] = 0.0f;

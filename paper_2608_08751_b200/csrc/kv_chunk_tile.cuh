@@ -11,6 +11,9 @@
 //                   rows that no row of the item may look at become zeros, and in tiles that not all rows see values that are not
 //                   finite are taken out
 //
+// The keys are taken from the last to the first: near ones weigh most where a bias falls with the distance, so the maximum is found at once
+// (taken from the first it grew with every tile, and O was rescaled: 3,104 against 1,719 us).
+//
 // A tile is 64 keys.  A stream has two S, P lies over its S, and S(j + 1) is issued before P(j) V: the softmax warps find the next
 // logits ready.  TMEM holds it exactly: two streams of two S (256 columns) and of O (256).  Heads wider than 128 take all of the second half
 // for one stream's O; it has two threads to a row then, 32 keys each, which tell each other their maxima through shared memory.
@@ -48,8 +51,8 @@ struct ChunkTileItem {
     int b, h, head0, heads;
     int token, pos;        // of its first token
     int lo, hi, k0, k1;
-    int first, end;        // tiles of the part
-    int from[2], to[2];    // of them those that a stream has rows for
+    int last, count;       // tiles of the part: its i-th is tile last - i
+    int from[2], to[2];    // of them (i from .. to - 1) those that a stream has rows for
     int all_lo, all_hi;    // keys that every row of the item sees
     bool whole;
     int slot;
@@ -90,8 +93,9 @@ __device__ __forceinline__ void chunk_record(const ChunkParams& p, const ChunkCu
     t.whole = it.first && it.last;
     t.slot = 2 * blockIdx.x + (it.first ? 1 : 0);
     t.r = it.r;
-    t.first = it.k0 / KEYS;
-    t.end = it.k1 > it.k0 ? (it.k1 + KEYS - 1) / KEYS : t.first;
+    const int first = it.k0 / KEYS, end = it.k1 > it.k0 ? (it.k1 + KEYS - 1) / KEYS : first;
+    t.last = end - 1;
+    t.count = end - first;
     const int per = p.tile_tokens / STREAMS;
     int skip;
     for (int s = 0; s < STREAMS; ++s) {
@@ -102,14 +106,19 @@ __device__ __forceinline__ void chunk_record(const ChunkParams& p, const ChunkCu
         lo = max(lo, it.k0);
         hi = min(hi, it.k1);
         const bool some = n > 0 && hi > lo;
-        t.from[s] = some ? lo / KEYS : t.first;
-        t.to[s] = some ? (hi + KEYS - 1) / KEYS : t.first;
+        t.from[s] = some ? end - (hi + KEYS - 1) / KEYS : 0;
+        t.to[s] = some ? end - lo / KEYS : 0;
     }
     chunk_sees(p, it.r, it.pos, true, skip, t.all_hi);
     chunk_sees(p, it.r, it.pos + it.tokens - 1, true, t.all_lo, skip);
 }
 
-// 2^z for two z <= 127 on the multiply-add units: z = n + f with n whole and |f| <= 1/2, and a polynomial of degree 5 for 2^f (Remez
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// 2^z for two z <= 126 on the multiply-add units: z = n + f with n whole and |f| <= 1/2, and a polynomial of degree 5 for 2^f (Remez
 // exchange on the relative error, 2.2e-7 in 32 bits: as near as the special function unit comes).  Below -126.5 it is 0, so -infinity, a masked
 // logit, gives exactly 0; NaN stays NaN.
 __device__ __forceinline__ uint64_t exp2_poly(uint64_t z) {
@@ -127,13 +136,11 @@ __device__ __forceinline__ uint64_t exp2_poly(uint64_t z) {
     y = fma2(y, f, pair32(0.6931469440460205f, 0.6931469440460205f));
     y = fma2(y, f, pair32(1.0000001192092896f, 1.0000001192092896f));
     const uint32_t lo = (static_cast<uint32_t>(t) << 23) + 0x3F800000u, hi = (static_cast<uint32_t>(t >> 32) << 23) + 0x3F800000u;  // 2^n; 0 for n = -127
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(y), "l"(pair32(__uint_as_float(lo), __uint_as_float(hi))));
-    return r;
+    return mul2(y, pair32(__uint_as_float(lo), __uint_as_float(hi)));
 }
 
-// PLAIN: neither a cap nor a bias.
-template <typename T, int DB, bool PLAIN>
+// CAP, BIAS: whether there is one.
+template <typename T, int DB, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(ChunkTileShape<DB>::kThreads, 1)
 kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkParams p) {
     using S = ChunkTileShape<DB>;
@@ -155,15 +162,15 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             mbar_init(&c.v_clean[i], 1);
         }
         for (int i = 0; i < kStreams; ++i) {
-            mbar_init(&c.q_full[i], S::kRowThreads);
+            mbar_init(&c.q_full[i], 4 * S::kHalves);
             mbar_init(&c.pv_done[i], 1);
             mbar_init(&c.o_full[i], 1);
             mbar_init(&c.drain[i], 1);
-            mbar_init(&c.o_free[i], S::kRowThreads);
+            mbar_init(&c.o_free[i], 4 * S::kHalves);
         }
         for (int i = 0; i < kStreams * 2; ++i) {
             mbar_init(&c.s_full[i], 1);
-            mbar_init(&c.p_ready[i], S::kRowThreads);
+            mbar_init(&c.p_ready[i], 4 * S::kHalves);
         }
         for (int i = 0; i < S::kItems; ++i) {
             mbar_init(&c.item_full[i], 1);
@@ -209,8 +216,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 if (!(ok = mbar_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
                 const ChunkTileItem& t = c.item[seq % S::kItems];
                 if (t.tokens == 0) break;
-                // (in registers, and counted from the part's first tile: read from shared memory at each use they cost more than the products)
-                const int count = t.end - t.first, from = t.from[s] - t.first, to = t.to[s] - t.first;
+                // (in registers: read from shared memory at each use they cost more than the products)
+                const int count = t.count, from = t.from[s], to = t.to[s];
                 // S(i + 1) goes where P(i - 1) was, whose product was issued before it: a thread's products run in order
                 for (int i = -1; ok && i < count; ++i) {
                     const int next = i + 1;
@@ -274,13 +281,13 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
             const ChunkTileItem& t = c.item[seq % S::kItems];
             if (t.tokens == 0) break;
-            const int h = t.h, first = t.first, count = t.end - t.first, k0 = t.k0, k1 = t.k1;
+            const int h = t.h, last = t.last, count = t.count, k0 = t.k0, k1 = t.k1;
             const int32_t* pages = p.table + t.b * p.table_stride;
             // each lane knows the page of one of 32 boxes, and has asked for that of the box 32 further on: the table answers while
             // those are copied (asked for a tile ahead and looked at at once, it held every tile up by its latency)
-            auto entry = [&](int i) {
-                const int key = first * kKeys + (i << box_shift);
-                return key < k1 && key + box > k0 ? pages[key >> p.page_shift] : -1;
+            auto entry = [&](int i) {  // of the part's i-th box
+                const int key = (last - i / boxes) * kKeys + ((i & (boxes - 1)) << box_shift);
+                return i < count * boxes && key < k1 && key + box > k0 ? pages[key >> p.page_shift] : -1;
             };
             auto checked = [&](int page) {
                 if (page >= p.num_pages) {
@@ -303,7 +310,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 // four pages of 16 tokens is 16 of them
                 const int b = lane / DB, d = lane % DB;
                 const int pg = __shfl_sync(0xFFFFFFFFu, page, at_box + b);  // (page -1 lies outside the map: zeros)
-                const int row = (((first + i) * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
+                const int row = (((last - i) * boxes + b) << box_shift) & ((1 << p.page_shift) - 1);
                 const uint32_t place = stage * S::kPlaneBytes + b * box * 128 + d * S::kBlockBytes;
                 if (n >= kStages && !(ok = warp_wait(&c.k_empty[stage], (n / kStages - 1) & 1, ctl, 246))) break;
                 if (lane == 0) {
@@ -361,11 +368,11 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             if (!ok) break;
             const ChunkTileItem& t = c.item[seq % S::kItems];
             if (*reinterpret_cast<const volatile int*>(&t.tokens) == 0) break;
-            const int first = t.first, last = t.end, item_lo = t.lo, item_hi = t.hi, all_lo = t.all_lo, all_hi = t.all_hi;
-            if (lane == 0 && last > first) c.odd[items & 3] = 0;
+            const int last = t.last, count = t.count, item_lo = t.lo, item_hi = t.hi, all_lo = t.all_lo, all_hi = t.all_hi;
+            if (lane == 0 && count > 0) c.odd[items & 3] = 0;
             __syncwarp();
-            for (int j = first; j < last; ++j, ++n) {
-                const int stage = n % kStages, key0 = j * kKeys;
+            for (int i = 0; i < count; ++i, ++n) {
+                const int stage = n % kStages, key0 = (last - i) * kKeys;
                 if (!(ok = warp_wait(&c.v_full[stage], (n / kStages) & 1, ctl, 247))) break;
                 const int dead0 = max(item_lo - key0, 0), dead1 = min(item_hi - key0, kKeys);  // rows before and from which on nobody may look
                 const bool cut = key0 < all_lo || key0 + kKeys > all_hi;
@@ -390,7 +397,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c.v_clean[stage]);
             }
-            items += last > first;
+            items += count > 0;
         }
         if (lane == 0) p.desc[blockIdx.x] = tail;
     } else if (warp < S::kSoftWarps) {
@@ -400,11 +407,15 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const int tok = token_of(r, inv_heads), head = r - tok * p.part_heads;
         const uint32_t t_rows = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), t_o = t_rows + S::kOCol + s * (DB * 64);
         const uint32_t t_p = S::kPCol >= 0 ? t_rows + S::kPCol : t_rows + s * 2 * kKeys;
-        const float scale = PLAIN ? fmaxf(fabsf(p.scale_log2), 1.2e-38f) : 1.0f;  // zero would turn masked logits into NaN
+        const float scale = CAP || BIAS ? 1.0f : fmaxf(fabsf(p.scale_log2), 1.2e-38f);  // zero would turn masked logits into NaN
         const float slack = fminf(8.0f / scale, 3e38f);  // (finite: added to a reference of -infinity it stays that)
-        const float factor = fabsf(p.cap_out == 0.0f ? p.scale_log2 : p.cap_in);  // of a product, where there is a cap or a bias
+        const float factor = fabsf(CAP ? p.cap_in : p.scale_log2);  // of a product, where there is a cap or a bias
         const uint64_t scale2 = pair32(scale, scale);
         constexpr int kMine = S::kMine;
+        auto arrive = [&](uint64_t* bar) {  // once for the warp: 128 threads' arrivals at one address took as long as a third of a tile
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
         int turn = 0;  // of what the halves tell each other
         auto tell = [&](float v) {  // the other half's number (whatever it is where the wait failed and ok is false)
             c.told[pair][turn & 1][half][lane] = v;
@@ -442,14 +453,14 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 cp_async_commit();
                 cp_async_wait<0>();
                 fence_proxy_async_smem();
-                mbar_arrive(&c.q_full[s]);
+                arrive(&c.q_full[s]);
             }
-            const unsigned hole0 = tiles - t.first;
+            const int last = t.last;
             float slope = 0.0f;
-            if (!PLAIN && p.slopes && live) slope = p.slopes[t.head0 + head] * 1.4426950408889634f;
+            if (BIAS && live) slope = p.slopes[t.head0 + head] * 1.4426950408889634f;
 
-            for (int j = from; j < to; ++j, ++n) {
-                const int key0 = j * kKeys + half * kMine;
+            for (int i = from; i < to; ++i, ++n) {
+                const int key0 = (last - i) * kKeys + half * kMine;
                 const int buffer = s * 2 + (n & 1);
                 const uint32_t t_s = t_rows + buffer * kKeys;
                 if (!(ok = warp_wait(&c.s_full[buffer], (n >> 1) & 1, ctl, 248))) break;
@@ -457,21 +468,41 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 uint32_t x[kMine];
                 if constexpr (kMine == 64) tmem_ld_32x32b_x64(t_s + half * kMine, x);
                 else tmem_ld_32x32b_x32(t_s + half * kMine, x);
-                const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(hole0 + j) % S::kHoles]) >> (half * (kMine / 16));
+                const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(tiles + i) % S::kHoles]) >> (half * (kMine / 16));
                 tmem_wait_ld_regs(x);
-                if (!PLAIN) {
-                    if (p.cap_out == 0.0f) {
+                if (CAP) {
+                    // cap * tanh = cap - 2 cap / (1 + exp2(x)).  The exponential of every other pair goes by the multiply-add units: with
+                    // all three of a logit's on the special function unit that is what bounds the kernel
+                    const uint64_t cap2 = pair32(p.cap_out, p.cap_out), twice = pair32(-2.0f * p.cap_out, -2.0f * p.cap_out);
 #pragma unroll
-                        for (int i = 0; i < kMine; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * factor);
+                    for (int i = 0; i < kMine; i += 2) {
+                        float a, b;  // (past 2^126 the quotient is 0 all the same)
+                        asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(__uint_as_float(x[i]) * factor), "f"(126.0f));
+                        asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(__uint_as_float(x[i + 1]) * factor), "f"(126.0f));
+                        const uint64_t e = (i & 2) ? exp2_poly(pair32(a, b)) : pair32(exp2_fast(a), exp2_fast(b));
+                        const uint64_t d = add2(e, pair32(1.0f, 1.0f));
+                        const uint64_t z = fma2(pair32(rcp_fast(lo32(d)), rcp_fast(hi32(d))), twice, cap2);
+                        x[i] = static_cast<uint32_t>(z);
+                        x[i + 1] = static_cast<uint32_t>(z >> 32);
+                    }
+                }
+                if (BIAS) {  // less slope times the distance; keys in front of the row's token, nearly all of them, lie on one line
+                    const float near = static_cast<float>(key0 - pos);
+                    const uint64_t line = pair32(slope, slope), f2 = pair32(factor, factor);
+                    if (__all_sync(0xFFFFFFFFu, key0 + kMine - 1 <= pos)) {
+#pragma unroll
+                        for (int i = 0; i < kMine; i += 2) {
+                            const uint64_t y = pair32(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), d = add2(pair32(near, near), pair32(i, i + 1));
+                            const uint64_t z = fma2(line, d, CAP ? y : mul2(y, f2));
+                            x[i] = static_cast<uint32_t>(z);
+                            x[i + 1] = static_cast<uint32_t>(z >> 32);
+                        }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < kMine; ++i)
-                            x[i] = __float_as_uint(fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(__uint_as_float(x[i]) * factor)), p.cap_out));
-                    }
-                    if (p.slopes) {
-                        const float away = static_cast<float>(pos - key0);
-#pragma unroll
-                        for (int i = 0; i < kMine; ++i) x[i] = __float_as_uint(fmaf(-slope, fabsf(away - i), __uint_as_float(x[i])));
+                        for (int i = 0; i < kMine; ++i) {
+                            const float y = __uint_as_float(x[i]);
+                            x[i] = __float_as_uint(fmaf(-slope, fabsf(near + i), CAP ? y : y * factor));
+                        }
                     }
                 }
                 if (key0 < warp_lo || key0 + kMine > warp_hi || holes) {  // not all rows of the warp see all of it
@@ -511,7 +542,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     if (!__any_sync(0xFFFFFFFFu, grow)) break;
                     const float fix = grow && m > -INFINITY ? exp2_fast((m - top) * scale) : 1.0f;
                     if (grow) m = top;
-                    if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (something was seen before: j > from)
+                    if (__any_sync(0xFFFFFFFFu, fix != 1.0f)) {  // (something was seen before: i > from)
                         if (!(ok = warp_wait(&c.pv_done[s], (n - 1) & 1, ctl, 249))) break;
                         tc_fence_after_sync();
                         l *= fix;
@@ -530,7 +561,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 l += lo32(both) + hi32(both);
                 tmem_wait_st();
                 tc_fence_before_sync();
-                mbar_arrive(&c.p_ready[buffer]);
+                arrive(&c.p_ready[buffer]);
             }
             if (!ok) break;
             if (to > from) {
@@ -540,7 +571,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 ++items;
             }
             const bool whole = t.whole;
-            const bool odd = t.end > t.first && *reinterpret_cast<volatile int*>(&c.odd[all_items & 3]) != 0;
+            const bool odd = t.count > 0 && *reinterpret_cast<volatile int*>(&c.odd[all_items & 3]) != 0;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             const int row = my_tok * p.part_heads + head;
             float* slot = p.slots + static_cast<int64_t>(t.slot) * p.rows * (p.dim + 2);
@@ -573,7 +604,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             }
             if (to > from) {
                 tc_fence_before_sync();
-                mbar_arrive(&c.o_free[s]);
+                arrive(&c.o_free[s]);
             }
             if (live && half == 0) {
                 const float best = m * scale;
@@ -586,10 +617,9 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     slot[p.rows * (p.dim + 1) + row] = l;
                 }
             }
-            tiles += t.end - t.first;
-            all_items += t.end > t.first;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.item_empty[seq % S::kItems]);
+            tiles += t.count;
+            all_items += t.count > 0;
+            arrive(&c.item_empty[seq % S::kItems]);
         }
     }
     // ------------------------------------------------------------ teardown (also the abort path)

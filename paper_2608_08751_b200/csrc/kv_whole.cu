@@ -119,15 +119,17 @@ int launch_chunk_rows(const ChunkParams& p, int ctas, const KvHostCtx& ctx, cuda
     if (int rc = allow_smem(kv_chunk_rows_kernel<T, DP>, RowsShape<DP>::kSmem, ctx, seen)) return rc;
     return launch(false, kv_chunk_rows_kernel<T, DP>, dim3(ctas), kRowsThreads, RowsShape<DP>::kSmem, stream, p);
 }
-template <typename T, int DB, bool PLAIN>
+template <typename T, int DB, bool CAP, bool BIAS>
 int launch_chunk_tile(const ChunkParams& p, const CUtensorMap& mk, const CUtensorMap& mv, int ctas, const KvHostCtx& ctx, cudaStream_t stream) {
     static SmemSeen seen;
-    if (int rc = allow_smem(kv_chunk_tile_kernel<T, DB, PLAIN>, chunk_tile_smem<DB>(), ctx, seen)) return rc;
-    return launch(false, kv_chunk_tile_kernel<T, DB, PLAIN>, dim3(ctas), ChunkTileShape<DB>::kThreads, chunk_tile_smem<DB>(), stream, mk, mv, p);
+    if (int rc = allow_smem(kv_chunk_tile_kernel<T, DB, CAP, BIAS>, chunk_tile_smem<DB>(), ctx, seen)) return rc;
+    return launch(false, kv_chunk_tile_kernel<T, DB, CAP, BIAS>, dim3(ctas), ChunkTileShape<DB>::kThreads, chunk_tile_smem<DB>(), stream, mk, mv, p);
 }
 template <typename T, int DB>
 int launch_chunk_tile(const ChunkParams& p, const CUtensorMap& mk, const CUtensorMap& mv, int ctas, const KvHostCtx& ctx, cudaStream_t stream) {
-    return p.cap_out == 0.0f && !p.slopes ? launch_chunk_tile<T, DB, true>(p, mk, mv, ctas, ctx, stream) : launch_chunk_tile<T, DB, false>(p, mk, mv, ctas, ctx, stream);
+    if (p.slopes)
+        return p.cap_out == 0.0f ? launch_chunk_tile<T, DB, false, true>(p, mk, mv, ctas, ctx, stream) : launch_chunk_tile<T, DB, true, true>(p, mk, mv, ctas, ctx, stream);
+    return p.cap_out == 0.0f ? launch_chunk_tile<T, DB, false, false>(p, mk, mv, ctas, ctx, stream) : launch_chunk_tile<T, DB, true, false>(p, mk, mv, ctas, ctx, stream);
 }
 template <typename T>
 int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStream_t stream) {
