@@ -593,42 +593,62 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
     if (tid == 0) p.desc[blockIdx.x] = tail;
 }
 
-// Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.
+// Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.  A warp to a row: its lanes take the parts'
+// maxima and sums, then the columns.  (A thread to four columns that went over the parts twice by itself took 30 us for 37 parts, a third of the
+// attention; so it is a few waits.)
 constexpr int kJoinThreads = 128;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const ChunkParams p) {
     pdl_wait();
-    const int c = blockIdx.x;
+    const int c = blockIdx.x, lane = threadIdx.x & 31;
     const ChunkDesc d = p.desc[c];
-    if (d.parts == 0) return;
+    const int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5);
+    if (d.parts == 0 || r >= d.tokens * p.part_heads) return;
     const int h = d.hv / p.parts, g0 = d.hv % p.parts * p.part_heads;
-    const int heads = min(p.part_heads, p.group - g0), n_heads = p.group * p.n_kv_heads;
-    const int quads = p.dim / 4;
+    if (r % p.part_heads >= min(p.part_heads, p.group - g0)) return;
+    const int n_heads = p.group * p.n_kv_heads;
     const int64_t step = static_cast<int64_t>(p.rows) * (p.dim + 2);
     auto part = [&](int k) { return p.slots + (k == 0 ? 2 * c + 1 : 2 * (c + k)) * step; };
-    for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < d.tokens * p.part_heads * quads; i += gridDim.y * kJoinThreads) {
-        const int r = i / quads, col = i % quads;
-        if (r % p.part_heads >= heads) continue;
-        float best = -INFINITY, sum = 0.0f;
-#pragma unroll 4
-        for (int k = 0; k < d.parts; ++k) best = fmaxf(best, part(k)[p.rows * p.dim + r]);
-        const float base = best == -INFINITY ? 0.0f : best;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int k = 0; k < d.parts; ++k) {
-            const float* src = part(k);
-            const float4 v = *reinterpret_cast<const float4*>(src + r * p.dim + col * 4);
-            const float w = exp2_fast(src[p.rows * p.dim + r] - base);
-            sum += w * src[p.rows * (p.dim + 1) + r];
-            acc.x += w * v.x, acc.y += w * v.y, acc.z += w * v.z, acc.w += w * v.w;
+    float top = -INFINITY;
+    for (int k = lane; k < d.parts; k += 32) top = fmaxf(top, part(k)[p.rows * p.dim + r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float base = top == -INFINITY ? 0.0f : top;
+    const int quads = p.dim / 4;
+    float sum = 0.0f;
+    float4 acc[2] = {};
+    for (int k0 = 0; k0 < d.parts; k0 += 32) {
+        const int n = min(32, d.parts - k0);
+        float w = 0.0f;
+        if (lane < n) {
+            const float* src = part(k0 + lane) + p.rows * p.dim + r;
+            w = exp2_fast(src[0] - base);
+            sum += w * src[p.rows];
         }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int64_t t = d.token + r / p.part_heads;
-        const int head = h * p.group + g0 + r % p.part_heads;
-        const uint2 v = make_uint2(Pair16<T>::pack(acc.x * inv, acc.y * inv), Pair16<T>::pack(acc.z * inv, acc.w * inv));
-        *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + col * 4) = v;
-        if (col == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+#pragma unroll 8
+        for (int k = 0; k < n; ++k) {
+            const float* src = part(k0 + k) + static_cast<int64_t>(r) * p.dim;
+            const float f = __shfl_sync(0xFFFFFFFFu, w, k);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (lane + 32 * i >= quads) continue;
+                const float4 v = *reinterpret_cast<const float4*>(src + (lane + 32 * i) * 4);
+                acc[i].x += f * v.x, acc[i].y += f * v.y, acc[i].z += f * v.z, acc[i].w += f * v.w;
+            }
+        }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t t = d.token + r / p.part_heads;
+    const int head = h * p.group + g0 + r % p.part_heads;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (lane + 32 * i >= quads) continue;
+        const uint2 v = make_uint2(Pair16<T>::pack(acc[i].x * inv, acc[i].y * inv), Pair16<T>::pack(acc[i].z * inv, acc[i].w * inv));
+        *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + (lane + 32 * i) * 4) = v;
+    }
+    if (lane == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
 }
 
 }  // namespace ivf

@@ -155,7 +155,7 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
         rc = p.dim <= 64 ? launch_chunk_rows<T, 64>(p, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_rows<T, 128>(p, ctas, ctx, stream)
                                                                                          : launch_chunk_rows<T, 256>(p, ctas, ctx, stream);
     if (rc != IVF_OK) return rc;
-    return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (p.rows * p.dim / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, stream, p);
+    return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (p.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, stream, p);
 }
 
 // Whether rows of `a` (heads by tokens) may share memory with rows of `b`.
