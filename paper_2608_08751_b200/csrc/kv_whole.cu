@@ -95,7 +95,7 @@ ChunkShape chunk_shape(int group, int dim, bool tile) {
     s.parts = (group + rows - 1) / rows;
     s.tile_tokens = (group > rows ? 1 : rows / group) * std::max(s.streams, 1);
     s.rows = (s.tile_tokens * s.part_heads + 1) / 2 * 2;
-    s.ctas = (!tile && dim <= 128 ? 2 : 1) * kChunkMaxSms;
+    s.ctas = (tile || dim > 128 ? 1 : dim > 64 ? 2 : 3) * kChunkMaxSms;
     return s;
 }
 int64_t chunk_bytes(const ChunkShape& s, int dim) {
