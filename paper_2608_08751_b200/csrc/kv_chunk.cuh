@@ -118,18 +118,27 @@ struct ChunkCursor {
     int b, hv, tile;
     int64_t off;   // inside the item
     int64_t left;  // of the span
+    ChunkReq r;    // of request b
 };
 template <int THREADS>
 struct ChunkPlan {
     int64_t warp_sum[THREADS / 32];
-    int64_t total;
     ChunkCursor at;
 };
-__device__ __forceinline__ int64_t chunk_span(int64_t total, int ctas, int c) { return total / ctas * c + total % ctas * c / ctas; }
+// Where the spans begin: the line in `ctas` parts of `whole` and a share of what is left over.
+struct ChunkSpans {
+    int ctas, over;
+    int64_t whole;
+    __device__ __forceinline__ int64_t begin(int c) const { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(ctas); }
+};
+// (a 64-bit division takes a hundred instructions, and nearly every line is shorter)
+__device__ __forceinline__ int64_t chunk_div(int64_t a, int64_t b) {
+    return (a | b) >> 32 ? a / b : static_cast<int64_t>(static_cast<unsigned>(a) / static_cast<unsigned>(b));
+}
 
-// All threads: the CTA's cursor (left = 0: nothing to do) and the number of CTAs that take part.
+// All threads: the CTA's cursor (left = 0: nothing to do) and where the spans lie.
 template <int THREADS>
-__device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPlan<THREADS>& s, int& ctas) {
+__device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPlan<THREADS>& s, ChunkSpans& spans) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.n_req + THREADS - 1) / THREADS;
     const int b0 = min(tid * per, p.n_req), b1 = min(b0 + per, p.n_req);
@@ -155,10 +164,12 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
         if (w < warp) upto += s.warp_sum[w];
         total += s.warp_sum[w];
     }
-    ctas = static_cast<int>(max(min(total / p.least, static_cast<int64_t>(gridDim.x)), static_cast<int64_t>(1)));
+    spans.ctas = static_cast<int>(max(min(chunk_div(total, p.least), static_cast<int64_t>(gridDim.x)), static_cast<int64_t>(1)));
+    spans.whole = chunk_div(total, spans.ctas);
+    spans.over = static_cast<int>(total - spans.whole * spans.ctas);
     const int c = blockIdx.x;
-    if (c < ctas) {
-        const int64_t u0 = chunk_span(total, ctas, c), u1 = chunk_span(total, ctas, c + 1);
+    if (c < spans.ctas) {
+        const int64_t u0 = spans.begin(c), u1 = spans.begin(c + 1);
         if (u0 >= upto && u0 < upto + mine) {
             int64_t rest = u0 - upto;
             for (int b = b0; b < b1; ++b) {
@@ -169,7 +180,7 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
                     continue;
                 }
                 s.at.b = b;
-                s.at.hv = static_cast<int>(rest / one);
+                s.at.hv = static_cast<int>(chunk_div(rest, one));
                 rest -= s.at.hv * one;
                 int lo = 0, hi = r.tiles;  // before(lo) <= rest < before(hi)
                 while (hi - lo > 1) {
@@ -180,18 +191,17 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
                 s.at.tile = lo;
                 s.at.off = rest - chunk_before(p, r, lo);
                 s.at.left = u1 - u0;
+                s.at.r = r;
                 break;
             }
         }
     }
-    if (tid == 0) s.total = total;
     __syncthreads();
     return s.at;
 }
 
 // One item, or the part of it that a span has.
 struct ChunkItem {
-    ChunkReq r;
     int hv, token, tokens;  // first token of the tile, and how many
     int pos;                // position of the first
     int lo, hi;             // keys that some row sees
@@ -201,14 +211,14 @@ struct ChunkItem {
 };
 __device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const ChunkCursor& at) {
     ChunkItem it;
-    it.r = chunk_req(p, at.b, false);
-    const int64_t w = chunk_weight(p, it.r, at.tile), take = min(at.left, w - at.off);
+    const ChunkReq& r = at.r;
+    const int64_t w = chunk_weight(p, r, at.tile), take = min(at.left, w - at.off);
     it.hv = at.hv;
-    it.token = it.r.start + at.tile * p.tile_tokens;
-    it.tokens = min(p.tile_tokens, it.r.fresh - at.tile * p.tile_tokens);
-    it.pos = it.r.base + at.tile * p.tile_tokens;
-    it.lo = chunk_lo(p, it.r, at.tile);
-    it.hi = min(chunk_hi(p, it.r, at.tile), it.r.far);
+    it.token = r.start + at.tile * p.tile_tokens;
+    it.tokens = min(p.tile_tokens, r.fresh - at.tile * p.tile_tokens);
+    it.pos = r.base + at.tile * p.tile_tokens;
+    it.lo = chunk_lo(p, r, at.tile);
+    it.hi = min(chunk_hi(p, r, at.tile), r.far);
     it.lo = min(it.lo, it.hi);
     it.first = at.off == 0;
     it.last = at.off + take == w;
@@ -222,27 +232,22 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const Chun
     return it;
 }
 __device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkCursor& at) {
-    ChunkReq r = chunk_req(p, at.b, false);
-    const int64_t take = min(at.left, chunk_weight(p, r, at.tile) - at.off);
+    const int64_t take = min(at.left, chunk_weight(p, at.r, at.tile) - at.off);
     at.left -= take;
     at.off = 0;
-    if (++at.tile < r.tiles) return;
+    if (++at.tile < at.r.tiles) return;
     at.tile = 0;
     if (++at.hv < p.n_kv_heads * p.parts) return;
     at.hv = 0;
     if (at.left > 0)  // (weights left: there is a request with tokens)
-        do r = chunk_req(p, ++at.b, false);
-        while (r.tiles == 0 && at.b < p.n_req - 1);
+        do at.r = chunk_req(p, ++at.b, false);
+        while (at.r.tiles == 0 && at.b < p.n_req - 1);
 }
 // The CTAs that take part in an item whose rest lies behind this CTA's span.
-__device__ __forceinline__ int chunk_parts(int64_t total, int ctas, int c, int64_t rest) {
-    const int64_t end = chunk_span(total, ctas, c + 1) + rest;  // of the item
-    int last = c, past = ctas;  // span(last) < end <= span(past)
-    while (past - last > 1) {
-        const int mid = (last + past) >> 1;
-        if (chunk_span(total, ctas, mid) < end) last = mid;
-        else past = mid;
-    }
+__device__ __forceinline__ int chunk_parts(const ChunkSpans& spans, int c, int64_t rest) {
+    const int64_t end = spans.begin(c + 1) + rest;  // of the item
+    int past = min(c + 1 + static_cast<int>(chunk_div(rest, spans.whole + 1)), spans.ctas);  // no span is longer: none before it ends the item
+    while (past < spans.ctas && spans.begin(past) < end) ++past;
     return past - c;
 }
 
@@ -326,14 +331,15 @@ struct ChunkRowsControl {
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __grid_constant__ ChunkParams p) {
+__global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1) kv_chunk_rows_kernel(const __grid_constant__ ChunkParams p) {
     using S = RowsShape<DP>;
     extern __shared__ __align__(128) uint8_t rows_smem[];
     __shared__ ChunkRowsControl<DP> c;
     pdl_trigger();  // (the kernel that joins the parts waits for this one's end by itself)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int ctas;
-    ChunkCursor at = chunk_plan<kRowsThreads>(p, c.plan, ctas);
+    ChunkSpans spans;
+    chunk_plan<kRowsThreads>(p, c.plan, spans);
+    const ChunkCursor& at = c.plan.at;  // (in shared memory: the loop wants the registers)
     chunk_padding<T>(p, kRowsThreads);
     const uint32_t smem0 = smem_u32(rows_smem);
     const uint32_t s_q = smem0 + S::kSmem - S::kQBytes;
@@ -342,7 +348,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
     const int n_heads = p.group * p.n_kv_heads;
     ChunkDesc tail = {0, 0, 0, 0};
 
-    for (; at.left > 0; chunk_next(p, at)) {
+    while (at.left > 0) {
         const ChunkItem it = chunk_item(p, at);
         const int h = it.hv / p.parts, g0 = it.hv % p.parts * p.part_heads;
         const int heads = min(p.part_heads, p.group - g0);
@@ -351,29 +357,16 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
         auto row_token = [&](int r) { return r / p.part_heads; };
         auto row_live = [&](int r) { return row_token(r) < it.tokens && r % p.part_heads < heads; };
 
-        if (tid == 0) c.odd = 0;
-        for (int i = tid; i < 16 * (DP / 8); i += kRowsThreads) {
-            const int r = i / (DP / 8), col = i % (DP / 8);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (row_live(r) && col * 8 < p.dim)
-                v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + static_cast<int64_t>(it.token + row_token(r)) * p.q_stride[0] +
-                                                    static_cast<int64_t>(head0 + r % p.part_heads) * p.q_stride[1] + col * 8);
-            *reinterpret_cast<uint4*>(rows_smem + (rows_addr<DP>(s_q, r, col) - smem0)) = v;
-        }
-        __syncthreads();
-
         // keys that all rows see: those of the first and of the last token
         int all_lo, all_hi, skip;
-        chunk_sees(p, it.r, it.pos, true, skip, all_hi);
-        chunk_sees(p, it.r, it.pos + it.tokens - 1, true, all_lo, skip);
+        chunk_sees(p, at.r, it.pos, true, skip, all_hi);
+        chunk_sees(p, at.r, it.pos + it.tokens - 1, true, all_lo, skip);
         const int piece0 = it.k0 >> 4, pieces = it.k1 > it.k0 ? ((it.k1 + 15) >> 4) - piece0 : 0;
         const int mine = pieces > warp ? (pieces - warp + kRowsWarps - 1) / kRowsWarps : 0;
         // the warp's j-th piece, the last ones first: where a bias falls with the distance the maximum is found at once
         auto key_of = [&](int j) { return (piece0 + warp + (mine - 1 - j) * kRowsWarps) << 4; };
-        auto page_of = [&](int j) {
-            const int block = key_of(j) >> p.page_shift;
-            int page = -1;
-            if (j < mine) page = pages[block];
+        auto page_of = [&](int j) { return j < mine ? pages[key_of(j) >> p.page_shift] : -1; };
+        auto checked = [&](int page) {
             if (page >= p.num_pages) {
                 kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
                 page = -1;
@@ -382,10 +375,20 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
         };
         int page_now = page_of(lane), page_next = page_of(32 + lane);
         uint32_t there = 0;  // by stage: the piece has a page
+        // the queries, behind the table's entries that are asked for above and in front of the first keys: one wait for all three
+        if (tid == 0) c.odd = 0;
+        for (int i = tid; i < 16 * (DP / 8); i += kRowsThreads) {
+            const int r = i / (DP / 8), col = i % (DP / 8);
+            const bool ok = row_live(r) && col * 8 < p.dim;
+            cp_async16(rows_addr<DP>(s_q, r, col), ok ? static_cast<const T*>(p.q) + static_cast<int64_t>(it.token + row_token(r)) * p.q_stride[0] +
+                                                            static_cast<int64_t>(head0 + r % p.part_heads) * p.q_stride[1] + col * 8 : static_cast<const T*>(p.q), ok);
+        }
+        cp_async_commit();
+        page_now = checked(page_now);
 
         auto fetch = [&](int j, int stage) {
             if (j > 0 && (j & 31) == 0) {
-                page_now = page_next;
+                page_now = checked(page_next);
                 page_next = page_of(j + 32 + lane);
             }
             const int64_t page = __shfl_sync(0xFFFFFFFFu, page_now, j & 31);
@@ -414,6 +417,10 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
             cp_async_commit();
         };
 
+#pragma unroll
+        for (int s = 0; s < S::kStages - 1; ++s) fetch(s, s);
+        cp_async_wait<S::kStages - 1>();  // the queries
+        __syncthreads();
         uint32_t qf[DP / 16][4];
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) ldsm4(qf[k], rows_addr<DP>(s_q, lane & 15, 2 * k + (lane >> 4)));
@@ -427,12 +434,10 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
         for (int r = 0; r < 2; ++r) {
             const int row = (lane >> 2) + r * 8;
             pos[r] = it.pos + row_token(row);
-            chunk_sees(p, it.r, pos[r], row_live(row), lo[r], hi[r]);
+            chunk_sees(p, at.r, pos[r], row_live(row), lo[r], hi[r]);
             slope[r] = p.slopes && row_live(row) ? p.slopes[head0 + row % p.part_heads] * 1.4426950408889634f : 0.0f;
         }
 
-#pragma unroll
-        for (int s = 0; s < S::kStages - 1; ++s) fetch(s, s);
         int stage = 0;
         for (int j = 0; j < mine; ++j) {
             cp_async_wait<S::kStages - 2>();
@@ -565,7 +570,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
             }
             if (c.odd) {
                 int from, to;
-                chunk_sees(p, it.r, it.pos + row_token(r), true, from, to);
+                chunk_sees(p, at.r, it.pos + row_token(r), true, from, to);
                 add_odd<T>(p, at.b, h, from, to, it.k0, it.k1, (all_lo + 15) & ~15, all_hi & ~15, col * 8, acc);
             }
             if (whole) {
@@ -587,8 +592,10 @@ __global__ void __launch_bounds__(kRowsThreads) kv_chunk_rows_kernel(const __gri
             }
         }
         if (it.first && !it.last && tid == 0)
-            tail = ChunkDesc{chunk_parts(c.plan.total, ctas, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
+            tail = ChunkDesc{chunk_parts(spans, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
         __syncthreads();  // the next item's queries and ring lie over this one's
+        if (tid == 0) chunk_next(p, c.plan.at);
+        __syncthreads();
     }
     if (tid == 0) p.desc[blockIdx.x] = tail;
 }

@@ -92,7 +92,7 @@ __device__ __forceinline__ void chunk_record(const ChunkParams& p, const ChunkCu
     t.lo = it.lo, t.hi = it.hi, t.k0 = it.k0, t.k1 = it.k1;
     t.whole = it.first && it.last;
     t.slot = 2 * blockIdx.x + (it.first ? 1 : 0);
-    t.r = it.r;
+    t.r = at.r;
     const int first = it.k0 / KEYS, end = it.k1 > it.k0 ? (it.k1 + KEYS - 1) / KEYS : first;
     t.last = end - 1;
     t.count = end - first;
@@ -101,16 +101,16 @@ __device__ __forceinline__ void chunk_record(const ChunkParams& p, const ChunkCu
     for (int s = 0; s < STREAMS; ++s) {
         const int n = min(per, it.tokens - s * per);
         int lo, hi;
-        chunk_sees(p, it.r, it.pos + s * per, true, lo, skip);
-        chunk_sees(p, it.r, it.pos + s * per + n - 1, true, skip, hi);
+        chunk_sees(p, at.r, it.pos + s * per, true, lo, skip);
+        chunk_sees(p, at.r, it.pos + s * per + n - 1, true, skip, hi);
         lo = max(lo, it.k0);
         hi = min(hi, it.k1);
         const bool some = n > 0 && hi > lo;
         t.from[s] = some ? end - (hi + KEYS - 1) / KEYS : 0;
         t.to[s] = some ? end - lo / KEYS : 0;
     }
-    chunk_sees(p, it.r, it.pos, true, skip, t.all_hi);
-    chunk_sees(p, it.r, it.pos + it.tokens - 1, true, t.all_lo, skip);
+    chunk_sees(p, at.r, it.pos, true, skip, t.all_hi);
+    chunk_sees(p, at.r, it.pos + it.tokens - 1, true, t.all_lo, skip);
 }
 
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
@@ -187,8 +187,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         tmem_relinquish();
     }
     tc_fence_before_sync();
-    int ctas;
-    ChunkCursor at = chunk_plan<S::kThreads>(p, c.plan, ctas);  // (its barriers order the above, too)
+    ChunkSpans spans;
+    ChunkCursor at = chunk_plan<S::kThreads>(p, c.plan, spans);  // (its barriers order the above, too)
     tc_fence_after_sync();
     chunk_padding<T>(p, S::kThreads);
     const uint32_t tmem = c.tmem;
@@ -358,7 +358,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     } else {
                         const ChunkItem it = chunk_item(p, at);
                         chunk_record<kStreams, kKeys>(p, at, it, t);
-                        if (it.first && !it.last) tail = ChunkDesc{chunk_parts(c.plan.total, ctas, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
+                        if (it.first && !it.last) tail = ChunkDesc{chunk_parts(spans, blockIdx.x, it.rest), it.token, it.tokens, it.hv};
                     }
                     mbar_arrive(&c.item_full[planned % S::kItems]);
                 }

@@ -144,8 +144,8 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
     p.tile_tokens = s.tile_tokens, p.part_heads = s.part_heads, p.parts = s.parts, p.rows = s.rows;
     p.desc = static_cast<ChunkDesc*>(workspace);
     p.slots = reinterpret_cast<float*>(p.desc + s.ctas);
-    p.item_cost = tile ? 384 : 64;
-    p.least = tile ? 1024 : 256;
+    p.item_cost = tile ? 384 : 160;
+    p.least = tile ? 1024 : 160;
     p.grain = tile ? 128 : 64;
     int rc;
     if (tile)
