@@ -74,7 +74,7 @@ __device__ __forceinline__ int compact_blocks(const KvPagesParams& p, int b, boo
 __global__ void __launch_bounds__(kPageThreads) kv_pages_clear_kernel(const KvPagesParams p) {
     pdl_trigger();
     const int64_t step = static_cast<int64_t>(gridDim.x) * kPageThreads, me = static_cast<int64_t>(blockIdx.x) * kPageThreads + threadIdx.x;
-    for (int64_t w = me; w < p.words; w += step) p.bits[w] = 0;
+    for (int64_t w = me; w < (p.words + 3) / 4; w += step) reinterpret_cast<uint4*>(p.bits)[w] = make_uint4(0, 0, 0, 0);
     if (p.parent)
         for (int64_t i = me; i < p.n_new; i += step) {
             const ForkRow f = fork_row(p, static_cast<int>(i), true);
@@ -151,16 +151,26 @@ __device__ __forceinline__ int page_scan(int v, int* warp_sum, int& total) {
     total = warp_sum[31];
     return upto - v + (warp > 0 ? warp_sum[warp - 1] : 0);
 }
-// Sum of f over words [0, n), by the whole CTA.
-template <typename F>
-__device__ __forceinline__ int page_sum(int64_t n, int* warp_sum, F&& f) {
-    int v = 0;
-    for (int64_t w = threadIdx.x; w < n; w += kPageScan) v += f(w);
-    int total;
-    page_scan(v, warp_sum, total);
-    return total;
+// Held pages in words [0, w0) and in all words, by the whole CTA; words come by four (their number is rounded up to that, the last ones 0).
+__device__ __forceinline__ void page_sums(const KvPagesParams& p, int64_t w0, int* warp_sum, int& before, int& all) {
+    const uint4* bits = reinterpret_cast<const uint4*>(p.bits);
+    int mine = 0, front = 0;
+#pragma unroll 4
+    for (int64_t w = threadIdx.x; w < (p.words + 3) / 4; w += kPageScan) {
+        const uint4 v = bits[w];
+        const int n = __popc(v.x) + __popc(v.y) + __popc(v.z) + __popc(v.w);
+        mine += n;
+        front += w * 4 < w0 ? n : 0;
+    }
+    page_scan(mine, warp_sum, all);
+    page_scan(front, warp_sum, before);
 }
-
+// The words of a CTA: a multiple of four.
+__device__ __forceinline__ void page_share(const KvPagesParams& p, int64_t& w0, int64_t& w1) {
+    const int64_t per = ((p.words + gridDim.x - 1) / gridDim.x + 3) / 4 * 4;
+    w0 = min(per * blockIdx.x, p.words);
+    w1 = min(w0 + per, p.words);
+}
 // Bits of pages that exist in a word.
 __device__ __forceinline__ uint32_t word_mask(const KvPagesParams& p, int64_t w) {
     const int64_t left = p.num_pages - w * 32;
@@ -208,20 +218,27 @@ __device__ __forceinline__ void fork_copy(const KvPagesParams& p, int i, int pag
     }
 }
 // Free pages of words [w0, w1), `before` of them in earlier words: the first `copies` of all go to the rows that want copies, the others
-// into the list.  `bits_of(w)`: the held pages of a word; every thread of the CTA calls it.
+// into the list.  A warp takes 32 words, and then a word at a time with a lane to a page, so that the list is written in rows.
+// `bits_of(w)`: the held pages of a word; every thread of the CTA calls it.
 template <typename F>
 __device__ __forceinline__ void fork_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int copies, const int* row_of, int* warp_sum, F&& bits_of) {
+    const int lane = threadIdx.x & 31;
     for (int64_t base = w0; base < w1; base += kPageScan) {
         const int64_t w = base + threadIdx.x;
-        uint32_t free = w < w1 ? ~bits_of(w) & word_mask(p, w) : 0;
+        const uint32_t free = w < w1 ? ~bits_of(w) & word_mask(p, w) : 0;
         int total;
-        int rank = before + page_scan(__popc(free), warp_sum, total);
+        const int first = before + page_scan(__popc(free), warp_sum, total);
         before += total;
-        for (; free; free &= free - 1, ++rank) {
-            const int page = static_cast<int>(w * 32) + __ffs(free) - 1;
+        for (unsigned some = __ballot_sync(0xFFFFFFFFu, free != 0); some; some &= some - 1) {
+            const int x = __ffs(some) - 1;
+            const uint32_t word = __shfl_sync(0xFFFFFFFFu, free, x);
+            const int rank = __shfl_sync(0xFFFFFFFFu, first, x) + __popc(word & ((1u << lane) - 1));
+            if (!(word >> lane & 1)) continue;
+            const int page = static_cast<int>((w - lane + x) * 32) + lane;
             if (rank < copies) fork_copy(p, row_of[rank], page);
             else p.free_pages[rank - copies] = page;
         }
+        __syncwarp();
     }
 }
 
@@ -230,11 +247,12 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_place_kernel(const KvPagesP
     extern __shared__ int page_rows[];  // [n_new] rows that want copies, by rank
     __shared__ int warp_sum[32];
     pdl_wait();
-    const int64_t per = (p.words + gridDim.x - 1) / gridDim.x;
-    const int64_t w0 = min(per * blockIdx.x, p.words), w1 = min(w0 + per, p.words);
-    auto free_of = [&](int64_t w) { return __popc(~p.bits[w] & word_mask(p, w)); };
-    const int before = page_sum(w0, warp_sum, free_of);
-    const int all = before + page_sum(p.words - w0, warp_sum, [&](int64_t w) { return free_of(w0 + w); });
+    int64_t w0, w1;
+    int before, all;
+    page_share(p, w0, w1);
+    page_sums(p, w0, warp_sum, before, all);
+    before = static_cast<int>(min(w0 * 32, p.num_pages)) - before;  // free ones from here on
+    all = static_cast<int>(p.num_pages) - all;
     int copies = 0;
     for (int base = 0; base < p.n_new; base += kPageScan) {
         const int i = base + threadIdx.x;
@@ -255,61 +273,73 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_place_kernel(const KvPagesP
     }
 }
 
-// The whole of it in one CTA: small tables, where the launches would take longer than the work.
+// The whole of it in one CTA: small tables, where the launches would take longer than the work.  A row's thread keeps what it read of it.
 __global__ void __launch_bounds__(kPageScan) kv_fork_small_kernel(const KvPagesParams p) {
-    extern __shared__ int page_smem[];
-    uint32_t* bits = reinterpret_cast<uint32_t*>(page_smem);            // [words]
-    int* rows = page_smem + p.words;                                    // [n_new] rows that want copies, by rank
-    int* last = rows + p.n_new;                                         // [n_new] page of the partly filled block, or -1
+    extern __shared__ __align__(16) int page_smem[];
+    uint32_t* bits = reinterpret_cast<uint32_t*>(page_smem);  // [words]
+    int* rows = page_smem + p.words;                          // [n_new] rows that want copies, by rank
+    int* last = rows + p.n_new;                               // [n_new] page of the partly filled block, or -1
+    int* source = last + p.n_new;                             // [n_new] the old row
+    int* full = source + p.n_new;                             // [n_new] filled blocks
     __shared__ int warp_sum[32];
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x;
+    ForkRow mine = {-1, 0, 0, 0};  // of row `tid` (there are at most as many rows as threads)
+    if (tid < p.n_new) {
+        mine = fork_row(p, tid, true);
+        source[tid] = mine.keep > 0 ? mine.parent : 0;
+        full[tid] = mine.full;
+        p.out_lens[tid] = mine.keep;
+    }
     for (int w = tid; w < p.words; w += kPageScan) bits[w] = 0;
-    for (int i = tid; i < p.n_new; i += kPageScan) {
-        const ForkRow f = fork_row(p, i, true);
-        last[i] = f.rest ? held_page(p, p.table[f.parent * p.table_stride + f.full], KV_SITE_FORK) : -1;
-        p.out_lens[i] = f.keep;
-    }
     __syncthreads();
-    for (int i = tid >> 5; i < p.n_new; i += kPageScan / 32) {
-        const ForkRow f = fork_row(p, i, false);
-        const int32_t* src = p.table + (f.keep > 0 ? f.parent : 0) * p.table_stride;
-#pragma unroll 4
-        for (int j = lane; j < p.max_blocks; j += 32) {
-            const int page = j < f.full ? held_page(p, src[j], KV_SITE_FORK) : -1;
-            if (page >= 0) atomicOr(&bits[page >> 5], 1u << (page & 31));
-            p.out[i * p.out_stride + j] = page;
+    // (asked for before the rows are read, looked at behind them)
+    const int partly = mine.rest ? p.table[mine.parent * p.table_stride + mine.full] : -1;
+    // a thread to entries kPageScan apart of all rows together, four at a time
+    const int entries = p.n_new * p.max_blocks;  // (32,768 at most)
+    for (int e0 = tid; e0 < entries; e0 += 4 * kPageScan) {
+        int row[4], j[4], page[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = e0 + k * kPageScan;
+            row[k] = e / p.max_blocks;
+            j[k] = e - row[k] * p.max_blocks;
+            page[k] = e < entries && j[k] < full[row[k]] ? p.table[source[row[k]] * p.table_stride + j[k]] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (e0 + k * kPageScan >= entries) continue;
+            page[k] = held_page(p, page[k], KV_SITE_FORK);
+            if (page[k] >= 0) atomicOr(&bits[page[k] >> 5], 1u << (page[k] & 31));
+            p.out[row[k] * p.out_stride + j[k]] = page[k];
         }
     }
+    const int page = mine.rest ? held_page(p, partly, KV_SITE_FORK) : -1;
+    if (tid < p.n_new) last[tid] = page;
     __syncthreads();
-    int copies = 0;
-    for (int base = 0; base < p.n_new; base += kPageScan) {  // (once: rows are at most the CTA's threads)
-        const int i = base + tid;
-        bool own = false, wants = false;
-        ForkRow f = {};
-        if (i < p.n_new) f = fork_row(p, i, false);
-        if (i < p.n_new && last[i] >= 0) {
-            own = !(bits[last[i] >> 5] >> (last[i] & 31) & 1);
-            for (int j = 0; own && j < i; ++j) own = last[j] != last[i];
-            wants = !own;
-        }
-        __syncthreads();
-        if (own) {
-            atomicOr(&bits[last[i] >> 5], 1u << (last[i] & 31));
-            p.out[i * p.out_stride + f.full] = last[i];
-        }
-        if (i < p.n_new) {
-            p.copy_from[i] = wants ? last[i] : -1;
-            p.copy_to[i] = -1;
-            p.copy_fill[i] = wants ? f.rest : 0;
-        }
-        int total;
-        const int rank = copies + page_scan(wants, warp_sum, total);
-        if (wants) rows[rank] = i;
-        copies += total;
+    bool own = false;
+    if (page >= 0) {
+        own = !(bits[page >> 5] >> (page & 31) & 1);
+        for (int j = 0; own && j < tid; ++j) own = last[j] != page;
     }
+    const bool wants = page >= 0 && !own;
     __syncthreads();
-    int all = 0;
-    all = page_sum(p.words, warp_sum, [&](int64_t w) { return __popc(~bits[w] & word_mask(p, w)); });
+    if (own) {
+        atomicOr(&bits[page >> 5], 1u << (page & 31));
+        p.out[tid * p.out_stride + mine.full] = page;
+    }
+    if (tid < p.n_new) {
+        p.copy_from[tid] = wants ? page : -1;
+        p.copy_to[tid] = -1;
+        p.copy_fill[tid] = wants ? mine.rest : 0;
+    }
+    int copies;
+    const int rank = page_scan(wants, warp_sum, copies);
+    if (wants) rows[rank] = tid;
+    __syncthreads();  // (the bits, too)
+    int held = 0, all;
+    for (int w = tid; w < p.words; w += kPageScan) held += __popc(bits[w]);
+    page_scan(held, warp_sum, all);
+    all = static_cast<int>(p.num_pages) - all;
     fork_list(p, 0, p.words, 0, copies, rows, warp_sum, [&](int64_t w) { return bits[w]; });
     const int left = max(all - copies, 0);
     for (int64_t k = left + tid; k < p.num_pages; k += kPageScan) p.free_pages[k] = -1;
@@ -321,33 +351,45 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_small_kernel(const KvPagesP
 // Moves of a run of words: `before` held pages lie in earlier ones.  held: of all; moves: how many are made.
 template <typename F>
 __device__ __forceinline__ void compact_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int held, int64_t moves, int* warp_sum, int32_t* before_of, F&& bits_of) {
+    const int lane = threadIdx.x & 31;
     for (int64_t base = w0; base < w1; base += kPageScan) {
         const int64_t w = base + threadIdx.x;
         const uint32_t bits = w < w1 ? bits_of(w) : 0;
         int total;
         const int upto = before + page_scan(__popc(bits), warp_sum, total);  // held pages before the word
         before += total;
-        if (w >= w1) continue;
-        before_of[w] = upto;
-        const int64_t first = w * 32;
-        // holes below `held`, from the lowest; pages from `held` on, from the highest
-        for (uint32_t hole = first < held ? ~bits & word_mask(p, w) : 0; hole; hole &= hole - 1) {
-            const int x = __ffs(hole) - 1;
-            const int64_t rank = first + x - (upto + __popc(bits & ((1u << x) - 1)));
-            if (first + x < held && rank < moves) p.copy_to[rank] = static_cast<int>(first + x);
+        if (w < w1) before_of[w] = upto;
+        // a lane to a page: holes below `held`, from the lowest; pages from `held` on, from the highest
+        const int64_t first0 = (w - lane) * 32;
+        const unsigned some = __ballot_sync(0xFFFFFFFFu, w < w1 && (w * 32 < held ? bits != 0xFFFFFFFFu || w * 32 + 32 > held : bits != 0));
+        for (unsigned rest = some; rest; rest &= rest - 1) {
+            const int x = __ffs(rest) - 1;
+            const uint32_t word = __shfl_sync(0xFFFFFFFFu, bits, x);
+            const int below = __shfl_sync(0xFFFFFFFFu, upto, x) + __popc(word & ((1u << lane) - 1));
+            const int64_t page = first0 + x * 32 + lane;
+            const bool is = word >> lane & 1;
+            if (page < held ? is : !is) continue;
+            const int64_t rank = page < held ? page - below : static_cast<int64_t>(held) - 1 - below;
+            if (rank < moves) (page < held ? p.copy_to : p.copy_from)[rank] = static_cast<int>(page);
         }
-        for (uint32_t page = first + 31 >= held ? bits : 0; page; page &= page - 1) {
-            const int x = __ffs(page) - 1;
-            const int64_t rank = static_cast<int64_t>(held) - 1 - (upto + __popc(bits & ((1u << x) - 1)));
-            if (first + x >= held && rank < moves) p.copy_from[rank] = static_cast<int>(first + x);
-        }
+        __syncwarp();
     }
 }
-// Held pages among the first n pages.
-template <typename F>
-__device__ __forceinline__ int held_below(const KvPagesParams& p, int n, int* warp_sum, F&& bits_of) {
-    const int64_t words = (static_cast<int64_t>(n) + 31) / 32;
-    return page_sum(words, warp_sum, [&](int64_t w) { return __popc(bits_of(w) & (w * 32 + 32 <= n ? 0xFFFFFFFFu : (1u << (n & 31)) - 1)); });
+// Held pages among the first n pages, of bits in global memory (four words at a time) or in shared memory.
+__device__ __forceinline__ int held_below(const uint32_t* bits, int n, int* warp_sum) {
+    int v = 0;
+    const int words = n / 32;
+#pragma unroll 4
+    for (int w = threadIdx.x; w < words / 4; w += kPageScan) {
+        const uint4 u = reinterpret_cast<const uint4*>(bits)[w];
+        v += __popc(u.x) + __popc(u.y) + __popc(u.z) + __popc(u.w);
+    }
+    const int w = words / 4 * 4 + threadIdx.x;  // up to three words, and a part of one
+    if (w < words) v += __popc(bits[w]);
+    else if (w == words && n % 32) v += __popc(bits[w] & ((1u << n % 32) - 1));
+    int total;
+    page_scan(v, warp_sum, total);
+    return total;
 }
 // The number that a held page has afterwards.
 template <typename F>
@@ -362,12 +404,12 @@ __global__ void __launch_bounds__(kPageScan) kv_compact_place_kernel(const KvPag
     __shared__ int warp_sum[32];
     pdl_wait();
     pdl_trigger();
-    const int64_t per = (p.words + gridDim.x - 1) / gridDim.x;
-    const int64_t w0 = min(per * blockIdx.x, p.words), w1 = min(w0 + per, p.words);
+    int64_t w0, w1;
+    int before, held;
+    page_share(p, w0, w1);
+    page_sums(p, w0, warp_sum, before, held);
     auto bits_of = [&](int64_t w) { return p.bits[w]; };
-    const int before = page_sum(w0, warp_sum, [&](int64_t w) { return __popc(p.bits[w]); });
-    const int held = before + page_sum(p.words - w0, warp_sum, [&](int64_t w) { return __popc(p.bits[w0 + w]); });
-    const int64_t moves = min(static_cast<int64_t>(held - held_below(p, held, warp_sum, bits_of)), p.max_moves);
+    const int64_t moves = min(static_cast<int64_t>(held - held_below(p.bits, held, warp_sum)), p.max_moves);
     compact_list(p, w0, w1, before, held, moves, warp_sum, p.before, bits_of);
     for (int64_t k = moves + static_cast<int64_t>(blockIdx.x) * kPageScan + threadIdx.x; k < p.max_moves; k += static_cast<int64_t>(gridDim.x) * kPageScan)
         p.copy_from[k] = p.copy_to[k] = -1;
@@ -403,9 +445,9 @@ __global__ void __launch_bounds__(kPageThreads) kv_compact_rename_kernel(const K
 }
 
 __global__ void __launch_bounds__(kPageScan) kv_compact_small_kernel(const KvPagesParams p) {
-    extern __shared__ int page_smem[];
+    extern __shared__ __align__(16) int page_smem[];
     uint32_t* bits = reinterpret_cast<uint32_t*>(page_smem);  // [words]
-    int32_t* before_of = page_smem + p.words;                 // [words]
+    int32_t* before_of = page_smem + p.words;                 // [words] (the bits by four: at a multiple of 16 bytes)
     __shared__ int warp_sum[32];
     const int tid = threadIdx.x, lane = tid & 31;
     for (int w = tid; w < p.words; w += kPageScan) bits[w] = 0;
@@ -420,8 +462,10 @@ __global__ void __launch_bounds__(kPageScan) kv_compact_small_kernel(const KvPag
     }
     __syncthreads();
     auto bits_of = [&](int64_t w) { return bits[w]; };
-    const int held = page_sum(p.words, warp_sum, [&](int64_t w) { return __popc(bits[w]); });
-    const int64_t moves = min(static_cast<int64_t>(held - held_below(p, held, warp_sum, bits_of)), p.max_moves);
+    int held = 0;
+    for (int w = tid; w < p.words; w += kPageScan) held += __popc(bits[w]);
+    page_scan(held, warp_sum, held);
+    const int64_t moves = min(static_cast<int64_t>(held - held_below(bits, held, warp_sum)), p.max_moves);
     compact_list(p, 0, p.words, 0, held, moves, warp_sum, before_of, bits_of);
     for (int64_t k = moves + tid; k < p.max_moves; k += kPageScan) p.copy_from[k] = p.copy_to[k] = -1;
     if (tid == 0) *p.count = held;

@@ -101,11 +101,14 @@ ChunkShape chunk_shape(int group, int dim, bool tile) {
 int64_t chunk_bytes(const ChunkShape& s, int dim) {
     return s.ctas * (static_cast<int64_t>(sizeof(ChunkDesc)) + 2ll * s.rows * (dim + 2) * sizeof(float));
 }
-// Large tiles read the keys once for up to 256 rows, small ones once for 16.
+// Small tiles read the keys once for 16 rows, large ones for up to 256, at some cost of starting.  By rows (new tokens by the heads of a
+// group) to a request, small / large tiles in us: one request of 65,536 tokens by 8 heads of 128 in groups of 4: 16 rows 63 / 69, 32 rows 94 / 69, 128
+// rows 282 / 79; 64 requests of 8,192: 16 rows 223 / 248, 32 rows 422 / 253.  Heads of 64: 16 rows 129 / 230, 32 rows 235 / 241.  Heads
+// wider than 128 leave the small tiles one CTA on an SM: 64 requests of 8,192 by 4 heads of 256, 2 rows 384 / 232.
 bool chunk_tiles_pay(int64_t n_tokens, int n_req, int group, int dim) {
     const int kernel = g_kv_chunk.load();
     if (kernel == 1 || dim < 64) return false;
-    return kernel == 2 || n_tokens * group > 32ll * std::max(n_req, 1);
+    return kernel == 2 || dim > 128 || n_tokens * group > (dim > 64 ? 16ll : 32ll) * std::max(n_req, 1);
 }
 int64_t chunk_workspace(int64_t n_tokens, int n_req, int group, int dim) {
     int64_t bytes = chunk_bytes(chunk_shape(group, dim, false), dim);
@@ -183,7 +186,7 @@ PagesPlace pages_place(int n_new, int64_t num_pages) {
 bool pages_small(int n_new, int max_blocks, int64_t num_pages) {
     return n_new <= kPageScan && num_pages <= 32768 && static_cast<int64_t>(n_new) * max_blocks <= 32768;
 }
-constexpr int kSmallSmem = (2 * 32768 / 32 + 2 * kPageScan) * 4;
+constexpr int kSmallSmem = (2 * 32768 / 32 + 4 * kPageScan) * 4;
 
 int check_pages(const char* op, const int32_t* table, int64_t table_stride, const int32_t* lens, int n_old, int n_new, int max_blocks, int64_t num_pages,
                 int page_size, const int32_t* out, int64_t out_stride) {
@@ -315,7 +318,7 @@ int ivf_kv_fork(const int32_t* table, int64_t table_stride, const int32_t* kv_le
     if (small) {
         static SmemSeen seen;
         if ((rc = allow_smem(kv_fork_small_kernel, kSmallSmem, ctx, seen)) != IVF_OK) return rc;
-        return launch(false, kv_fork_small_kernel, dim3(1), kPageScan, static_cast<int>((w.words + 2 * n_new) * 4), stream, p);
+        return launch(false, kv_fork_small_kernel, dim3(1), kPageScan, static_cast<int>((w.words + 4 * n_new) * 4), stream, p);
     }
     char* ws = static_cast<char*>(workspace);
     p.bits = reinterpret_cast<uint32_t*>(ws), p.claim = reinterpret_cast<int32_t*>(ws + w.claim), p.wish = reinterpret_cast<int32_t*>(ws + w.wish);
@@ -323,7 +326,7 @@ int ivf_kv_fork(const int32_t* table, int64_t table_stride, const int32_t* kv_le
     if ((rc = allow_smem(kv_fork_place_kernel, kPageMaxRows * 4, ctx, seen)) != IVF_OK) return rc;
     auto ctas = [&](int64_t items, int per, int most) { return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((items + per - 1) / per, most)))); };
     const int64_t pieces = (max_blocks + 32ll * kMarkBatch - 1) / (32 * kMarkBatch);
-    if ((rc = launch(false, kv_pages_clear_kernel, ctas(w.words + n_new, kPageThreads, 4 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
+    if ((rc = launch(false, kv_pages_clear_kernel, ctas(w.words / 4 + n_new, kPageThreads, 2 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_pages_mark_kernel, ctas(n_new * pieces, kPageThreads / 32, 8 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_fork_own_kernel, ctas(n_new, kPageThreads, kMaxCount), kPageThreads, 0, stream, p)) != IVF_OK)
         return rc;
@@ -363,7 +366,7 @@ int ivf_kv_compact(const int32_t* table, int64_t table_stride, const int32_t* kv
     p.bits = reinterpret_cast<uint32_t*>(ws), p.before = reinterpret_cast<int32_t*>(ws + w.before);
     auto ctas = [&](int64_t items, int per, int most) { return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((items + per - 1) / per, most)))); };
     const int64_t pieces = (max_blocks + 32ll * kMarkBatch - 1) / (32 * kMarkBatch);
-    if ((rc = launch(false, kv_pages_clear_kernel, ctas(w.words, kPageThreads, 4 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
+    if ((rc = launch(false, kv_pages_clear_kernel, ctas(w.words / 4, kPageThreads, 2 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_pages_mark_kernel, ctas(n_req * pieces, kPageThreads / 32, 8 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_compact_place_kernel, ctas(w.words, kPageScan / 8, ctx.num_sms), kPageScan, 0, stream, p)) != IVF_OK)
         return rc;

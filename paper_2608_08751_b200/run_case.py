@@ -353,9 +353,83 @@ def kv_case(args):
                       "keys_read_share": seen / args.context}))
 
 
+def kv_whole_case(args):
+    """A layer that attends to its whole cache, as a server runs it: prompts in chunks; every request branches into some samples that
+    share its filled pages; single tokens; half of the rows end and the cache is compacted; single tokens again.  Prints
+    the times of the steps and how many pages are held."""
+    dev, kind, page, heads, kv_heads, d = "cuda", torch.bfloat16, 64, 32, 8, 128
+    n, total = args.requests, args.context + args.decode_steps
+    columns = -(-total // page)
+    rows = n * args.samples
+    pages = n * columns + rows * (-(-args.decode_steps // page) + 2)
+    g = torch.Generator(device=dev)
+    g.manual_seed(0)
+    k_cache, v_cache = (torch.empty(pages, kv_heads, page, d, dtype=kind, device=dev) for _ in range(2))
+    angle = torch.arange(total, device=dev)[:, None] * torch.exp(torch.arange(0, d, 2, device=dev) * (-math.log(10000.0) / d))[None]
+    rotary = torch.cat([angle.cos(), angle.sin()], 1).float().contiguous()
+    state = {"table": torch.full((n, columns), -1, dtype=torch.int32, device=dev), "lens": torch.zeros(n, dtype=torch.int32, device=dev),
+             "free": torch.randperm(pages, device=dev, generator=g).to(torch.int32)}
+
+    def timed(f):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        got = f()
+        e1.record()
+        B.ivf_check()
+        return 1e3 * e0.elapsed_time(e1), got
+
+    def step(fresh, tokens):
+        q, k, v = (torch.randn(tokens, h, d, device=dev, generator=g).to(kind) for h in (heads, kv_heads, kv_heads))
+
+        def calls():
+            plan = B.ivf_kv_tables(state["lens"], fresh, state["free"], state["table"], page, tokens)
+            turned = B.ivf_kv_append(q, k, v, k_cache, v_cache, plan.token_pos, plan.token_slot, rotary=rotary)
+            return plan, B.ivf_kv_attend_chunk(turned, k_cache, v_cache, state["table"], plan.token_start, plan.kv_lens, d ** -0.5)[0]
+        us, (plan, out) = timed(calls)
+        state["lens"] = plan.kv_lens.clone()
+        state["free"] = state["free"][int(plan.used):]
+        assert torch.isfinite(out.float()).all()
+        return us
+
+    def fork(parent):
+        def calls():
+            f = B.ivf_kv_fork(state["table"], state["lens"], parent, None, pages, page)
+            B.ivf_kv_copy(k_cache, v_cache, f.copy_from, f.copy_to, f.copy_fill)
+            return f
+        us, f = timed(calls)
+        state.update(table=f.table, lens=f.kv_lens, free=f.free_pages[: int(f.n_free)])
+        return us, pages - int(f.n_free)
+
+    def middle(values):
+        return sorted(values)[len(values) // 2]
+    prompt = []
+    for at in range(0, args.context, args.chunk):
+        size = min(args.chunk, args.context - at)
+        for r in range(n):
+            fresh = torch.zeros(n, dtype=torch.int32, device=dev)
+            fresh[r] = size
+            prompt.append(step(fresh, size))
+    fork_us, held = fork(torch.arange(rows, dtype=torch.int32, device=dev) // args.samples)
+    first = [step(torch.ones(rows, dtype=torch.int32, device=dev), rows) for _ in range(args.decode_steps // 2)]
+    _, _ = fork(torch.arange(0, rows, 2, dtype=torch.int32, device=dev))  # every other row has ended
+
+    def compact():
+        moves = B.ivf_kv_compact(state["table"], state["lens"], pages, page)
+        B.ivf_kv_copy(k_cache, v_cache, moves.copy_from, moves.copy_to)
+        return moves
+    compact_us, moves = timed(compact)
+    kept = int(moves.n_held)
+    state["free"] = torch.arange(kept, pages, dtype=torch.int32, device=dev)
+    left = state["lens"].numel()
+    second = [step(torch.ones(left, dtype=torch.int32, device=dev), left) for _ in range(args.decode_steps - args.decode_steps // 2)]
+    print(json.dumps({"op": "kv-whole", "requests": n, "samples": args.samples, "context": args.context, "heads": heads, "kv_heads": kv_heads, "d": d, "page": page,
+                      "prompt_chunk_us": middle(prompt), "fork_us": fork_us, "pages_after_fork": held, "pages_without_sharing": rows * -(-args.context // page),
+                      "decode_step_us": middle(first), "compact_us": compact_us, "pages_after_compact": kept, "decode_step_after_us": middle(second)}))
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--op", default="assign", choices=["assign", "route", "update", "stream", "serve", "pq", "candidates", "build", "kv"])
+    ap.add_argument("--op", default="assign", choices=["assign", "route", "update", "stream", "serve", "pq", "candidates", "build", "kv", "kv-whole"])
     ap.add_argument("--train-rows", type=int, default=1 << 20, dest="train_rows", help="sample size of --op build")
     ap.add_argument("--pq-m", type=int, default=32, dest="pq_m")
     ap.add_argument("--n-rerank", type=int, default=512, dest="n_rerank")
@@ -368,10 +442,11 @@ def main():
     ap.add_argument("--d", type=int, default=128)
     ap.add_argument("--k", type=int, default=64)
     ap.add_argument("--dtype", default="u8", choices=["u8", "f32", "i8"])
-    ap.add_argument("--requests", type=int, default=8, help="--op kv: requests served")
-    ap.add_argument("--context", type=int, default=32768, help="--op kv: prompt tokens of a request, fed in chunks")
-    ap.add_argument("--chunk", type=int, default=2048, help="--op kv: tokens of a prompt chunk")
-    ap.add_argument("--decode-steps", type=int, default=32, dest="decode_steps", help="--op kv: single-token steps after the prompts")
+    ap.add_argument("--requests", type=int, default=8, help="--op kv, kv-whole: requests served")
+    ap.add_argument("--context", type=int, default=32768, help="--op kv, kv-whole: prompt tokens of a request, fed in chunks")
+    ap.add_argument("--chunk", type=int, default=2048, help="--op kv, kv-whole: tokens of a prompt chunk")
+    ap.add_argument("--decode-steps", type=int, default=32, dest="decode_steps", help="--op kv, kv-whole: single-token steps after the prompts")
+    ap.add_argument("--samples", type=int, default=4, help="--op kv-whole: rows that each request branches into after its prompt")
     ap.add_argument("--reps", type=int, default=3)
     ap.add_argument("--dependent-launch", type=int, default=-1, help="kernel-family mask of dependent launches (0 = none)")
     ap.add_argument("--crossing-cost", type=int, default=-1, help="span-partition crossing cost in units (0 = equal counts)")
@@ -398,6 +473,8 @@ def main():
         return build_case(args)
     if args.op == "kv":
         return kv_case(args)
+    if args.op == "kv-whole":
+        return kv_whole_case(args)
     if args.dtype == "i8":
         x, c = synth.spacev_like(args.n, args.nlist, seed=0, d=args.d)
     elif args.dtype == "u8":

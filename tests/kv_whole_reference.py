@@ -47,54 +47,55 @@ def attend_chunk(q, k_cache, v_cache, table, start, lens, scale, cap=0.0, slopes
 def fork(table, lens, parent, keep, num_pages, page):
     """Row by row; shortages and bad values included."""
     n, columns = len(parent), table.shape[1]
+    table = np.where((table >= 0) & (table < num_pages), table, -1)
     new = np.full((n, columns), -1, np.int64)
     kept = np.zeros(n, np.int64)
     for i, p in enumerate(parent):
         if 0 <= p < len(lens):
             want = lens[p] if keep is None else keep[i]
             kept[i] = want if 0 <= want <= lens[p] and want <= columns * page else 0
-
-    def entry(i, j):
-        p = int(table[parent[i], j])
-        return p if 0 <= p < num_pages else -1
-    shared = set()
-    for i in range(n):
-        for j in range(kept[i] // page):
-            new[i, j] = entry(i, j)
-            shared.add(new[i, j])
-    owned, source, to, fill = set(), np.full(n, -1, np.int64), np.full(n, -1, np.int64), np.zeros(n, np.int64)
+        if kept[i]:
+            new[i, : kept[i] // page] = table[p, : kept[i] // page]
+    held = np.zeros(num_pages, bool)
+    held[new[new >= 0]] = True
+    shared = held.copy()
+    source, to, fill = np.full(n, -1, np.int64), np.full(n, -1, np.int64), np.zeros(n, np.int64)
+    owned = set()
     for i in range(n):
         j = kept[i] // page
-        if kept[i] % page and entry(i, j) >= 0:
-            p = entry(i, j)
-            if p in shared or p in owned:
+        if kept[i] % page and table[parent[i], j] >= 0:
+            p = int(table[parent[i], j])
+            if shared[p] or p in owned:
                 source[i], fill[i] = p, kept[i] % page
             else:
                 owned.add(p)
+                held[p] = True
                 new[i, j] = p
-    free = [p for p in range(num_pages) if p not in shared and p not in owned]
+    free = np.flatnonzero(~held)
+    taken = 0
     for i in range(n):
         if source[i] >= 0:
-            if free:
-                to[i] = new[i, kept[i] // page] = free.pop(0)
+            if taken < len(free):
+                to[i] = new[i, kept[i] // page] = free[taken]
+                taken += 1
             else:
                 source[i], fill[i] = -1, 0
+    left = free[taken:]
     return {"table": new, "kv_lens": kept, "copy_from": source, "copy_to": to, "copy_fill": fill,
-            "free_pages": np.array(free + [-1] * (num_pages - len(free)), np.int64), "n_free": np.array([len(free)])}
+            "free_pages": np.concatenate([left, np.full(num_pages - len(left), -1)]), "n_free": np.array([len(left)])}
 
 
 def compact(table, lens, num_pages, page, max_moves):
     n, columns = table.shape
+    table = np.where((table >= 0) & (table < num_pages), table, -1)
     out = np.full((n, columns), -1, np.int64)
     for b in range(n):
         blocks = min(-(-max(0, int(lens[b])) // page), columns)
-        out[b, :blocks] = [p if 0 <= p < num_pages else -1 for p in table[b, :blocks]]
-    held = sorted(set(out[out >= 0].tolist()))
-    high = [p for p in held if p >= len(held)][::-1]
-    low = [p for p in range(len(held)) if p not in set(held)]
-    moves = list(zip(high, low))[:max_moves]
-    where = dict(moves)
-    out = np.array([[where.get(p, p) for p in row] for row in out.tolist()], np.int64).reshape(n, columns)
-    pad = [-1] * (max_moves - len(moves))
-    return {"table": out, "copy_from": np.array([m[0] for m in moves] + pad, np.int64), "copy_to": np.array([m[1] for m in moves] + pad, np.int64),
-            "n_held": np.array([len(held)])}
+        out[b, :blocks] = table[b, :blocks]
+    held = np.unique(out[out >= 0])
+    high = held[held >= len(held)][::-1][:max_moves]
+    low = np.setdiff1d(np.arange(len(held)), held)[:max_moves]
+    where = np.concatenate([np.arange(num_pages), [-1]])  # (-1 stays -1)
+    where[high] = low
+    pad = np.full(max_moves - len(high), -1)
+    return {"table": where[out], "copy_from": np.concatenate([high, pad]), "copy_to": np.concatenate([low, pad]), "n_held": np.array([len(held)])}
