@@ -547,7 +547,7 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
  * Columns of out_table behind a row's blocks get -1.  Where pages do not suffice the rows of the surplus copies get -1 in their last block
  * (and no copy) and the status word IVF_ERR_NO_PAGES.  A parent past the table, a length or a keep that is negative, past the parent's or past the
  * columns gives an empty row, a page past num_pages counts as missing (-1); both set IVF_ERR_BAD_ID.  The outputs must not lie over the
- * inputs (refused).  n_old, n_new <= 16384.
+ * inputs or each other (refused).  n_old, n_new <= 16384.
  *
  * ivf_kv_compact: with n_held pages held, the held pages from number n_held on move into the holes below it, the highest into the lowest
  * hole, max_moves of them at most (the highest first); afterwards, if all are made, pages n_held and up are free.

@@ -161,11 +161,15 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
     return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (p.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, stream, p);
 }
 
-// Whether rows of `a` (heads by tokens) may share memory with rows of `b`.
-bool rows_meet(const void* a, const int64_t* as, const void* b, const int64_t* bs, int64_t n, int64_t heads, int dim) {
-    auto span = [&](const int64_t* s) { return ((n - 1) * s[0] + (heads - 1) * s[1] + dim) * 2; };
-    const char *a0 = static_cast<const char*>(a), *b0 = static_cast<const char*>(b);
-    return a0 < b0 + span(bs) && b0 < a0 + span(as);
+// Whether `out` has an element of `q`'s memory.  Rows of one buffer in turn (the same token stride) are told apart, other tensors
+// by their ranges.
+bool out_over_q(const void* q, const int64_t* q_stride, const void* out, const int64_t* out_stride, int64_t n, int64_t heads, int dim) {
+    const int64_t q_row = (heads - 1) * q_stride[1] + dim, o_row = (heads - 1) * out_stride[1] + dim, step = q_stride[0];
+    const int64_t q0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(q)) / 2, o0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(out)) / 2;
+    if (q0 + (n - 1) * step + q_row <= o0 || o0 + (n - 1) * out_stride[0] + o_row <= q0) return false;
+    if (step == 0 || step != out_stride[0]) return true;
+    const int64_t after = ((o0 - q0) % step + step) % step;  // of an output row behind the start of a query row
+    return after < q_row || after + o_row > step;
 }
 
 // ------------------------------------------------------------------ pages
@@ -249,7 +253,7 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
     if ((rc = kv_check_rows("q", q, q_stride, 2)) != IVF_OK || (rc = kv_check_rows("out", out, out_stride, 2)) != IVF_OK ||
         (rc = kv_check_apart("out", out_stride, {n_tokens, n_heads}, cache->head_dim)) != IVF_OK)
         return rc;
-    if (rows_meet(q, q_stride, out, out_stride, n_tokens, n_heads, cache->head_dim))
+    if (out_over_q(q, q_stride, out, out_stride, n_tokens, n_heads, cache->head_dim))
         return fail(IVF_ERR_INVALID_ARG, "out must not share memory with q: rows are read again by other blocks of threads");
     const int64_t need = chunk_workspace(n_tokens, n_req, n_heads / cache->n_kv_heads, cache->head_dim);
     if (!workspace || workspace_bytes < need || kv_misaligned(workspace, 16))
@@ -303,6 +307,9 @@ int ivf_kv_fork(const int32_t* table, int64_t table_stride, const int32_t* kv_le
     for (const Span& i : in)
         for (const Span& o : outs)
             if (spans_meet(i, o)) return fail(IVF_ERR_INVALID_ARG, "the outputs must not lie over the table, kv_lens, parent or keep");
+    for (const Span& a : outs)
+        for (const Span& b : outs)
+            if (&a != &b && spans_meet(a, b)) return fail(IVF_ERR_INVALID_ARG, "the outputs must not lie over each other");
     const bool small = pages_small(n_new, max_blocks, num_pages);
     const PagesPlace w = pages_place(n_new, num_pages);
     if (!small && (!workspace || workspace_bytes < w.bytes || kv_misaligned(workspace, 16)))
@@ -344,7 +351,10 @@ int ivf_kv_compact(const int32_t* table, int64_t table_stride, const int32_t* kv
     const Span t = {table, row, n_req > 1 ? 4 * table_stride : row, n_req}, o = {out_table, row, n_req > 1 ? 4 * out_stride : row, n_req}, l = {kv_lens, 4ll * n_req, 0, 1};
     const Span lists[] = {{copy_from, 4 * max_moves, 0, 1}, {copy_to, 4 * max_moves, 0, 1}, {n_held, 4, 0, 1}};
     bool over = spans_meet(l, o) || (spans_meet(t, o) && (table != out_table || (n_req > 1 && table_stride != out_stride)));
-    for (const Span& s : lists) over |= spans_meet(s, t) || spans_meet(s, l) || spans_meet(s, o);
+    for (const Span& s : lists) {
+        over |= spans_meet(s, t) || spans_meet(s, l) || spans_meet(s, o);
+        for (const Span& x : lists) over |= &s != &x && spans_meet(s, x);
+    }
     if (over) return fail(IVF_ERR_INVALID_ARG, "the outputs must not lie over the table (unless out is the table itself), kv_lens or each other");
     const bool small = pages_small(n_req, max_blocks, num_pages);
     const PagesPlace w = pages_place(n_req, num_pages);

@@ -78,6 +78,9 @@ def test_fork():
     for out in ("out", "out_lens", "from", "to", "fill", "free", "count"):
         for src in ("table", "lens", "parent", "keep"):
             assert _fork(**{out: PLACES[src]}) == INV and b"must not lie over" in _error(), (out, src)
+    for a in ("out", "out_lens", "from", "to", "fill", "free", "count"):
+        for b in ("out", "out_lens", "from", "to", "fill", "free", "count"):
+            assert a == b or (_fork(**{a: PLACES[b]}) == INV and b"each other" in _error()), (a, b)
     assert _fork(table=PLACES["out"] + 96) == INV and b"must not lie over" in _error()
     assert _fork(pages=1 << 20, free=P + 30000) == INV and b"workspace" in _error()
 
@@ -90,6 +93,7 @@ def test_compact():
     for out in ("from", "to", "count"):
         for src in ("table", "lens", "out"):
             assert _compact(**{out: PLACES[src]}) == INV and b"must not lie over" in _error(), (out, src)
+    assert _compact(to=PLACES["from"]) == INV and _compact(count=PLACES["to"] + 8) == INV and _compact(count=PLACES["from"]) == INV
     assert _compact(out=PLACES["lens"]) == INV and _compact(out=PLACES["table"] + 4) == INV and _compact(out=PLACES["table"], out_stride=9) == INV
     assert _compact(pages=1 << 20) == INV and b"workspace" in _error()
     got = ctypes.c_int64(-1)
@@ -119,6 +123,10 @@ def test_neighbours_are_not_refused():
         return rc == INV
     assert not refused(_fork()) and not refused(_fork(keep=None)) and not refused(_fork(n_old=0, table=None, lens=None)) and not refused(_fork(pages=0, free=None))
     assert not refused(_fork(n_new=1, out_stride=0)) and not refused(_fork(table=PLACES["out"] + 32, stride=16, out_stride=16))
+    def attend(q, out, n=4):
+        return B.lib().ivf_kv_attend_chunk(q, _s(1024, 64), n, 4, _cache(), P, 8, 2, 8, P, P, 1.0, 0.0, None, 0, None, out, _s(1024, 64), None, P, 1 << 40, None)
+    # an output that shares rows of one buffer with the queries, but no element
+    assert not refused(attend(P, P + 512)) and not refused(attend(P + 1024, P)) and refused(attend(P, P + 256)) and refused(attend(P + 256, P))
     assert not refused(_compact()) and not refused(_compact(out=PLACES["table"])) and not refused(_compact(moves=0, **{"from": None, "to": None}))
 
 
