@@ -41,7 +41,7 @@ struct ChunkParams {
     const int32_t *token_start, *kv_lens, *prefix;  // prefix may be null
     int window;            // 0: none
     float scale_log2;      // scale * log2(e)
-    float cap_in, cap_out; // with a cap: z in base 2 = cap_out * tanh(x), 2 x log2(e) = cap_in * (q . k); cap_out 0: none
+    float cap_in, cap_out; // with a cap: z in base 2 = cap_out * tanh(cap_in * (q . k)); cap_out 0: none
     const float* slopes;   // [n_heads] or null
     void* out;
     int64_t out_stride[2];
@@ -281,10 +281,26 @@ __device__ __forceinline__ float rcp_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// A product as a logit in base 2, before the bias.  tanh(x) = 1 - 2 / (1 + exp(2 x)): off by a few 2^-24 of the cap.
+// tanh(x) for |x| <= 1 is x P(x^2), P of degree 6 (Remez exchange on the relative error; 1.6e-7 in 32 bits).  As 1 - 2 / (1 + exp(2 x)), which
+// is what is left for larger ones, a small logit would keep no more digits than the cap has.
+__host__ __device__ constexpr float tanh_term(int k) {
+    constexpr float term[7] = {0.9999999403953552f, -0.33332839608192444f, 0.13325203955173492f, -0.05345702916383743f, 0.020289979875087738f,
+                               -0.006203379016369581f, 0.0010410225950181484f};
+    return term[k];
+}
+__device__ __forceinline__ float tanh_far(float x) {
+    return copysignf(fmaf(-2.0f, rcp_fast(1.0f + exp2_fast(2.885390043258667f * fabsf(x))), 1.0f), x);
+}
+// A product as a logit in base 2, before the bias.
 __device__ __forceinline__ float chunk_logit(const ChunkParams& p, float s) {
     if (p.cap_out == 0.0f) return s * p.scale_log2;
-    return fmaf(-2.0f * p.cap_out, rcp_fast(1.0f + exp2_fast(s * p.cap_in)), p.cap_out);
+    const float x = s * p.cap_in, u = x * x;
+    float y = tanh_term(6);
+#pragma unroll
+    for (int i = 5; i >= 0; --i) y = fmaf(y, u, tanh_term(i));
+    float t = x * y;
+    if (fabsf(x) > 1.0f) t = tanh_far(x);
+    return p.cap_out * t;
 }
 
 // The numbers of `v` (two 16-bit ones to a word) that are not finite; `clean` gets zeros in their places.

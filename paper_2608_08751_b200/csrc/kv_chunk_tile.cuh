@@ -118,27 +118,6 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// 2^z for two z <= 126 on the multiply-add units: z = n + f with n whole and |f| <= 1/2, and a polynomial of degree 5 for 2^f (Remez
-// exchange on the relative error, 2.2e-7 in 32 bits: as near as the special function unit comes).  Below -126.5 it is 0, so -infinity, a masked
-// logit, gives exactly 0; NaN stays NaN.
-__device__ __forceinline__ uint64_t exp2_poly(uint64_t z) {
-    float a, b;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(lo32(z)), "f"(-127.0f));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(hi32(z)), "f"(-127.0f));
-    const uint64_t x = pair32(a, b), big = pair32(12582912.0f, 12582912.0f);  // 1.5 * 2^23: the sum's last bits are round(x)
-    const uint64_t t = add2(x, big);
-    const uint64_t n = add2(t, pair32(-12582912.0f, -12582912.0f));
-    const uint64_t f = fma2(n, pair32(-1.0f, -1.0f), x);
-    uint64_t y = pair32(0.0013276472454890609f, 0.0013276472454890609f);
-    y = fma2(y, f, pair32(0.009675540961325169f, 0.009675540961325169f));
-    y = fma2(y, f, pair32(0.05550713092088699f, 0.05550713092088699f));
-    y = fma2(y, f, pair32(0.24022120237350464f, 0.24022120237350464f));
-    y = fma2(y, f, pair32(0.6931469440460205f, 0.6931469440460205f));
-    y = fma2(y, f, pair32(1.0000001192092896f, 1.0000001192092896f));
-    const uint32_t lo = (static_cast<uint32_t>(t) << 23) + 0x3F800000u, hi = (static_cast<uint32_t>(t >> 32) << 23) + 0x3F800000u;  // 2^n; 0 for n = -127
-    return mul2(y, pair32(__uint_as_float(lo), __uint_as_float(hi)));
-}
-
 // CAP, BIAS: whether there is one.
 template <typename T, int DB, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(ChunkTileShape<DB>::kThreads, 1)
@@ -471,19 +450,38 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&c.holes[(tiles + i) % S::kHoles]) >> (half * (kMine / 16));
                 tmem_wait_ld_regs(x);
                 if (CAP) {
-                    // cap * tanh = cap - 2 cap / (1 + exp2(x)).  The exponential of every other pair goes by the multiply-add units: with
-                    // all three of a logit's on the special function unit that is what bounds the kernel
-                    const uint64_t cap2 = pair32(p.cap_out, p.cap_out), twice = pair32(-2.0f * p.cap_out, -2.0f * p.cap_out);
+                    float most = 0.0f;
+                    const uint64_t f2 = pair32(factor, factor);
 #pragma unroll
                     for (int i = 0; i < kMine; i += 2) {
-                        float a, b;  // (past 2^126 the quotient is 0 all the same)
-                        asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(__uint_as_float(x[i]) * factor), "f"(126.0f));
-                        asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(__uint_as_float(x[i + 1]) * factor), "f"(126.0f));
-                        const uint64_t e = (i & 2) ? exp2_poly(pair32(a, b)) : pair32(exp2_fast(a), exp2_fast(b));
-                        const uint64_t d = add2(e, pair32(1.0f, 1.0f));
-                        const uint64_t z = fma2(pair32(rcp_fast(lo32(d)), rcp_fast(hi32(d))), twice, cap2);
-                        x[i] = static_cast<uint32_t>(z);
-                        x[i + 1] = static_cast<uint32_t>(z >> 32);
+                        const uint64_t y = mul2(pair32(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), f2);
+                        x[i] = static_cast<uint32_t>(y);
+                        x[i + 1] = static_cast<uint32_t>(y >> 32);
+                        most = max3f(most, fabsf(lo32(y)), fabsf(hi32(y)));
+                    }
+                    const uint64_t cap2 = pair32(p.cap_out, p.cap_out);
+                    auto near = [&](uint64_t y) {  // cap * tanh of a pair within [-1, 1]
+                        const uint64_t u = mul2(y, y);
+                        uint64_t t = pair32(tanh_term(6), tanh_term(6));
+#pragma unroll
+                        for (int k = 5; k >= 0; --k) t = fma2(t, u, pair32(tanh_term(k), tanh_term(k)));
+                        return mul2(t, mul2(y, cap2));
+                    };
+                    if (!__any_sync(0xFFFFFFFFu, most > 1.0f)) {  // as a rule, for caps that keep logits within reason
+#pragma unroll
+                        for (int i = 0; i < kMine; i += 2) {
+                            const uint64_t t = near(pair32(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+                            x[i] = static_cast<uint32_t>(t);
+                            x[i + 1] = static_cast<uint32_t>(t >> 32);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kMine; i += 2) {
+                            const float a = __uint_as_float(x[i]), b = __uint_as_float(x[i + 1]);
+                            const uint64_t t = near(pair32(a, b)), far = mul2(pair32(tanh_far(a), tanh_far(b)), cap2);
+                            x[i] = fabsf(a) > 1.0f ? static_cast<uint32_t>(far) : static_cast<uint32_t>(t);
+                            x[i + 1] = fabsf(b) > 1.0f ? static_cast<uint32_t>(far >> 32) : static_cast<uint32_t>(t >> 32);
+                        }
                     }
                 }
                 if (BIAS) {  // less slope times the distance; keys in front of the row's token, nearly all of them, lie on one line

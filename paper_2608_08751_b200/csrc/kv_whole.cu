@@ -270,7 +270,7 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
     p.table = table, p.table_stride = table_stride, p.n_req = n_req, p.max_blocks = max_blocks, p.page_shift = kv_shift(cache->page_size);
     p.token_start = token_start, p.kv_lens = kv_lens, p.prefix = prefix, p.window = window;
     p.scale_log2 = scale * log2e;
-    p.cap_in = cap > 0.0f ? 2.0f * log2e * scale / cap : 0.0f;
+    p.cap_in = cap > 0.0f ? scale / cap : 0.0f;
     p.cap_out = cap * log2e;
     p.slopes = slopes, p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = ctx.status;
     p.limit_ns = ctx.limit_ns;

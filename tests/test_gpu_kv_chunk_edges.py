@@ -70,6 +70,18 @@ def test_a_saturated_cap(kernel):  # noqa: F811
     _check(c, out, lse, cap=2.0)
 
 
+def test_small_capped_logits_keep_their_digits(kernel):  # noqa: F811
+    """One key to a token and one number to a query, so that the product is exact and lse is the logit: tanh, the cap, and the way to base 2 and
+    back are a dozen roundings of 2^-24 of the logit, 2^-20 at most; nothing of the cap's own size."""
+    c = _case([(90, 40)], 1, 4, 64, 32, "fp16", seed=11)
+    c["q"][:, :, 1:] = 0
+    for cap in (50.0, 1000.0):
+        out, lse = _run(c, cap=cap, window=1)
+        B.ivf_check()
+        want = W.attend_chunk(_np(c["q"]), _finite(_np(c["kc"])), _finite(_np(c["vc"])), c["table"], c["start"], c["lens"], c["scale"], cap, window=1)[1]
+        assert (np.abs(_np(lse) - want) <= 2.0 ** -20 * np.abs(want) + 1e-30).all()
+
+
 def test_prefixes_in_front_of_inside_and_behind_the_new_tokens(kernel):  # noqa: F811
     c = _case([(100, 60)] * 6, 1, 4, 64, 32, "bf16", seed=6)
     prefix = np.array([50, 100, 101, 130, 160, 10 ** 6])
