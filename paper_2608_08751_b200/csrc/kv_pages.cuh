@@ -30,7 +30,7 @@ struct KvPagesParams {
     uint32_t* bits;   // [words]: pages held as filled blocks; compaction: all held ones
     int32_t* claim;   // [num_pages]: lowest row that holds the page as a partly filled block; only claimed pages' are set
     int32_t* before;  // [words + 1] compaction: held pages before the word
-    int32_t* wish;    // [n_new] page that a row wants a copy of, or -1
+    int32_t* wish;    // [2 * n_new] page that a row wants a copy of, or -1; then the row's filled blocks
     int64_t words;
     int* status;
 };
@@ -201,15 +201,16 @@ __global__ void __launch_bounds__(kPageThreads) kv_fork_own_kernel(const KvPages
         p.out[i * p.out_stride + f.full] = entry;
     }
     p.wish[i] = from;
+    p.wish[p.n_new + i] = f.full;
     p.copy_from[i] = from;
     p.copy_to[i] = -1;
     p.copy_fill[i] = from >= 0 ? f.rest : 0;
 }
 
-// The page that a row's copy goes to; page < 0: there is none left.
-__device__ __forceinline__ void fork_copy(const KvPagesParams& p, int i, int page) {
+// The page that a row's copy goes to, its block `full`; page < 0: there is none left.
+__device__ __forceinline__ void fork_copy(const KvPagesParams& p, int i, int full, int page) {
     if (page >= 0) {
-        p.out[i * p.out_stride + fork_row(p, i, false).full] = page;
+        p.out[i * p.out_stride + full] = page;
         p.copy_to[i] = page;
     } else {
         p.copy_from[i] = -1;
@@ -217,35 +218,50 @@ __device__ __forceinline__ void fork_copy(const KvPagesParams& p, int i, int pag
         kv_report(p.status, kKvStatusNoPages, KV_SITE_FORK);
     }
 }
-// Free pages of words [w0, w1), `before` of them in earlier words: the first `copies` of all go to the rows that want copies, the others
-// into the list.  A warp takes 32 words, and then a word at a time with a lane to a page, so that the list is written in rows.
-// `bits_of(w)`: the held pages of a word; every thread of the CTA calls it.
-template <typename F>
-__device__ __forceinline__ void fork_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int copies, const int* row_of, int* warp_sum, F&& bits_of) {
-    const int lane = threadIdx.x & 31;
+// Words of bits by the whole CTA: f(word's number, its bits, pages counted before it) is called by every warp for words of its own, a lane to a
+// page.  `count` says which pages of a word count, `some` whether f wants the word at all; both are called once for a word.
+struct PageWords {
+    uint32_t bits[kPageScan];
+    int before[kPageScan];
+    int warp_sum[32];
+};
+template <typename B, typename C, typename S, typename F>
+__device__ __forceinline__ void each_word(int64_t w0, int64_t w1, int before, PageWords& s, B&& bits_of, C&& count, S&& some, F&& f) {
     for (int64_t base = w0; base < w1; base += kPageScan) {
         const int64_t w = base + threadIdx.x;
-        const uint32_t free = w < w1 ? ~bits_of(w) & word_mask(p, w) : 0;
+        const uint32_t bits = w < w1 ? bits_of(w) : 0;
         int total;
-        const int first = before + page_scan(__popc(free), warp_sum, total);
+        const int first = before + page_scan(w < w1 ? __popc(count(w, bits)) : 0, s.warp_sum, total);  // (its barriers part the rounds)
         before += total;
-        for (unsigned some = __ballot_sync(0xFFFFFFFFu, free != 0); some; some &= some - 1) {
-            const int x = __ffs(some) - 1;
-            const uint32_t word = __shfl_sync(0xFFFFFFFFu, free, x);
-            const int rank = __shfl_sync(0xFFFFFFFFu, first, x) + __popc(word & ((1u << lane) - 1));
-            if (!(word >> lane & 1)) continue;
-            const int page = static_cast<int>((w - lane + x) * 32) + lane;
-            if (rank < copies) fork_copy(p, row_of[rank], page);
-            else p.free_pages[rank - copies] = page;
-        }
-        __syncwarp();
+        s.bits[threadIdx.x] = bits;
+        s.before[threadIdx.x] = first;
+        __syncthreads();
+        const int n = static_cast<int>(min(w1 - base, static_cast<int64_t>(kPageScan)));
+        for (int x = threadIdx.x >> 5; x < n; x += kPageScan / 32)
+            if (some(base + x, s.bits[x])) f(base + x, s.bits[x], s.before[x]);
     }
+}
+// Free pages of words [w0, w1), `before` of them in earlier words: the first `copies` of all go to the rows that want copies (by rank, with their
+// filled blocks), the others into the list.  Every thread of the CTA calls it.
+template <typename F>
+__device__ __forceinline__ void fork_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int copies, const int* row_of, const int* full_of, PageWords& s, F&& bits_of) {
+    const int lane = threadIdx.x & 31;
+    auto free_of = [&](int64_t w, uint32_t bits) { return ~bits & word_mask(p, w); };
+    each_word(w0, w1, before, s, bits_of, free_of, [&](int64_t w, uint32_t bits) { return free_of(w, bits) != 0; }, [&](int64_t w, uint32_t bits, int first) {
+        const uint32_t free = free_of(w, bits);
+        if (!(free >> lane & 1)) return;
+        const int rank = first + __popc(free & ((1u << lane) - 1)), page = static_cast<int>(w * 32) + lane;
+        if (rank < copies) fork_copy(p, row_of[rank], full_of[rank], page);
+        else p.free_pages[rank - copies] = page;
+    });
 }
 
 // Ranks of the rows that want copies and of the free pages.  A CTA takes a run of words.
 __global__ void __launch_bounds__(kPageScan) kv_fork_place_kernel(const KvPagesParams p) {
-    extern __shared__ int page_rows[];  // [n_new] rows that want copies, by rank
-    __shared__ int warp_sum[32];
+    extern __shared__ int page_rows[];  // [2 * n_new] rows that want copies, by rank, and their filled blocks
+    int* page_full = page_rows + p.n_new;
+    __shared__ PageWords words;
+    int* warp_sum = words.warp_sum;
     pdl_wait();
     int64_t w0, w1;
     int before, all;
@@ -259,16 +275,16 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_place_kernel(const KvPagesP
         const bool wants = i < p.n_new && p.wish[i] >= 0;
         int total;
         const int rank = copies + page_scan(wants, warp_sum, total);
-        if (wants) page_rows[rank] = i;
+        if (wants) page_rows[rank] = i, page_full[rank] = p.wish[p.n_new + i];
         copies += total;
     }
     __syncthreads();
-    fork_list(p, w0, w1, before, copies, page_rows, warp_sum, [&](int64_t w) { return p.bits[w]; });
+    fork_list(p, w0, w1, before, copies, page_rows, page_full, words, [&](int64_t w) { return p.bits[w]; });
     const int left = max(all - copies, 0);
     for (int64_t k = left + static_cast<int64_t>(blockIdx.x) * kPageScan + threadIdx.x; k < p.num_pages; k += static_cast<int64_t>(gridDim.x) * kPageScan)
         p.free_pages[k] = -1;
     if (blockIdx.x == 0) {
-        for (int k = all + threadIdx.x; k < copies; k += kPageScan) fork_copy(p, page_rows[k], -1);
+        for (int k = all + threadIdx.x; k < copies; k += kPageScan) fork_copy(p, page_rows[k], page_full[k], -1);
         if (threadIdx.x == 0) *p.count = left;
     }
 }
@@ -281,7 +297,9 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_small_kernel(const KvPagesP
     int* last = rows + p.n_new;                               // [n_new] page of the partly filled block, or -1
     int* source = last + p.n_new;                             // [n_new] the old row
     int* full = source + p.n_new;                             // [n_new] filled blocks
-    __shared__ int warp_sum[32];
+    int* wants_full = full + p.n_new;                         // [n_new] those of `rows`
+    __shared__ PageWords words;
+    int* warp_sum = words.warp_sum;
     const int tid = threadIdx.x;
     ForkRow mine = {-1, 0, 0, 0};  // of row `tid` (there are at most as many rows as threads)
     if (tid < p.n_new) {
@@ -334,46 +352,36 @@ __global__ void __launch_bounds__(kPageScan) kv_fork_small_kernel(const KvPagesP
     }
     int copies;
     const int rank = page_scan(wants, warp_sum, copies);
-    if (wants) rows[rank] = tid;
+    if (wants) rows[rank] = tid, wants_full[rank] = mine.full;
     __syncthreads();  // (the bits, too)
     int held = 0, all;
     for (int w = tid; w < p.words; w += kPageScan) held += __popc(bits[w]);
     page_scan(held, warp_sum, all);
     all = static_cast<int>(p.num_pages) - all;
-    fork_list(p, 0, p.words, 0, copies, rows, warp_sum, [&](int64_t w) { return bits[w]; });
+    fork_list(p, 0, p.words, 0, copies, rows, wants_full, words, [&](int64_t w) { return bits[w]; });
     const int left = max(all - copies, 0);
     for (int64_t k = left + tid; k < p.num_pages; k += kPageScan) p.free_pages[k] = -1;
-    for (int k = all + tid; k < copies; k += kPageScan) fork_copy(p, rows[k], -1);
+    for (int k = all + tid; k < copies; k += kPageScan) fork_copy(p, rows[k], wants_full[k], -1);
     if (tid == 0) *p.count = left;
 }
 
 // ---------------------------------------------------------------------------------------------- compaction
 // Moves of a run of words: `before` held pages lie in earlier ones.  held: of all; moves: how many are made.
 template <typename F>
-__device__ __forceinline__ void compact_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int held, int64_t moves, int* warp_sum, int32_t* before_of, F&& bits_of) {
+__device__ __forceinline__ void compact_list(const KvPagesParams& p, int64_t w0, int64_t w1, int before, int held, int64_t moves, PageWords& s, int32_t* before_of, F&& bits_of) {
     const int lane = threadIdx.x & 31;
-    for (int64_t base = w0; base < w1; base += kPageScan) {
-        const int64_t w = base + threadIdx.x;
-        const uint32_t bits = w < w1 ? bits_of(w) : 0;
-        int total;
-        const int upto = before + page_scan(__popc(bits), warp_sum, total);  // held pages before the word
-        before += total;
-        if (w < w1) before_of[w] = upto;
-        // a lane to a page: holes below `held`, from the lowest; pages from `held` on, from the highest
-        const int64_t first0 = (w - lane) * 32;
-        const unsigned some = __ballot_sync(0xFFFFFFFFu, w < w1 && (w * 32 < held ? bits != 0xFFFFFFFFu || w * 32 + 32 > held : bits != 0));
-        for (unsigned rest = some; rest; rest &= rest - 1) {
-            const int x = __ffs(rest) - 1;
-            const uint32_t word = __shfl_sync(0xFFFFFFFFu, bits, x);
-            const int below = __shfl_sync(0xFFFFFFFFu, upto, x) + __popc(word & ((1u << lane) - 1));
-            const int64_t page = first0 + x * 32 + lane;
-            const bool is = word >> lane & 1;
-            if (page < held ? is : !is) continue;
-            const int64_t rank = page < held ? page - below : static_cast<int64_t>(held) - 1 - below;
-            if (rank < moves) (page < held ? p.copy_to : p.copy_from)[rank] = static_cast<int>(page);
-        }
-        __syncwarp();
-    }
+    each_word(w0, w1, before, s, bits_of, [](int64_t, uint32_t bits) { return bits; },
+              [&](int64_t, uint32_t) { return true; },
+              [&](int64_t w, uint32_t bits, int upto) {
+        if (lane == 0) before_of[w] = upto;
+        // holes below `held`, from the lowest; pages from `held` on, from the highest
+        const int below = upto + __popc(bits & ((1u << lane) - 1));
+        const int64_t page = w * 32 + lane;
+        const bool is = bits >> lane & 1;
+        if (page < held ? is : !is) return;
+        const int64_t rank = page < held ? page - below : static_cast<int64_t>(held) - 1 - below;
+        if (rank < moves) (page < held ? p.copy_to : p.copy_from)[rank] = static_cast<int>(page);
+    });
 }
 // Held pages among the first n pages, of bits in global memory (four words at a time) or in shared memory.
 __device__ __forceinline__ int held_below(const uint32_t* bits, int n, int* warp_sum) {
@@ -401,7 +409,8 @@ __device__ __forceinline__ int renamed(const KvPagesParams& p, int page, int hel
 }
 
 __global__ void __launch_bounds__(kPageScan) kv_compact_place_kernel(const KvPagesParams p) {
-    __shared__ int warp_sum[32];
+    __shared__ PageWords words;
+    int* warp_sum = words.warp_sum;
     pdl_wait();
     pdl_trigger();
     int64_t w0, w1;
@@ -410,7 +419,7 @@ __global__ void __launch_bounds__(kPageScan) kv_compact_place_kernel(const KvPag
     page_sums(p, w0, warp_sum, before, held);
     auto bits_of = [&](int64_t w) { return p.bits[w]; };
     const int64_t moves = min(static_cast<int64_t>(held - held_below(p.bits, held, warp_sum)), p.max_moves);
-    compact_list(p, w0, w1, before, held, moves, warp_sum, p.before, bits_of);
+    compact_list(p, w0, w1, before, held, moves, words, p.before, bits_of);
     for (int64_t k = moves + static_cast<int64_t>(blockIdx.x) * kPageScan + threadIdx.x; k < p.max_moves; k += static_cast<int64_t>(gridDim.x) * kPageScan)
         p.copy_from[k] = p.copy_to[k] = -1;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -448,7 +457,8 @@ __global__ void __launch_bounds__(kPageScan) kv_compact_small_kernel(const KvPag
     extern __shared__ __align__(16) int page_smem[];
     uint32_t* bits = reinterpret_cast<uint32_t*>(page_smem);  // [words]
     int32_t* before_of = page_smem + p.words;                 // [words] (the bits by four: at a multiple of 16 bytes)
-    __shared__ int warp_sum[32];
+    __shared__ PageWords words;
+    int* warp_sum = words.warp_sum;
     const int tid = threadIdx.x, lane = tid & 31;
     for (int w = tid; w < p.words; w += kPageScan) bits[w] = 0;
     __syncthreads();
@@ -466,7 +476,7 @@ __global__ void __launch_bounds__(kPageScan) kv_compact_small_kernel(const KvPag
     for (int w = tid; w < p.words; w += kPageScan) held += __popc(bits[w]);
     page_scan(held, warp_sum, held);
     const int64_t moves = min(static_cast<int64_t>(held - held_below(bits, held, warp_sum)), p.max_moves);
-    compact_list(p, 0, p.words, 0, held, moves, warp_sum, before_of, bits_of);
+    compact_list(p, 0, p.words, 0, held, moves, words, before_of, bits_of);
     for (int64_t k = moves + tid; k < p.max_moves; k += kPageScan) p.copy_from[k] = p.copy_to[k] = -1;
     if (tid == 0) *p.count = held;
     __syncthreads();  // the list of places, and the words' sums

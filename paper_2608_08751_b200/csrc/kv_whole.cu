@@ -183,14 +183,14 @@ PagesPlace pages_place(int n_new, int64_t num_pages) {
     w.before = up(w.words * 4);
     w.claim = w.before + up((w.words + 1) * 4);
     w.wish = w.claim + up(num_pages * 4);
-    w.bytes = w.wish + up(4ll * n_new);
+    w.bytes = w.wish + up(8ll * n_new);
     return w;
 }
 // One CTA does it all where its launch costs less than the three or four of the other way.
 bool pages_small(int n_new, int max_blocks, int64_t num_pages) {
     return n_new <= kPageScan && num_pages <= 32768 && static_cast<int64_t>(n_new) * max_blocks <= 32768;
 }
-constexpr int kSmallSmem = (2 * 32768 / 32 + 4 * kPageScan) * 4;
+constexpr int kSmallSmem = (2 * 32768 / 32 + 5 * kPageScan) * 4;
 
 int check_pages(const char* op, const int32_t* table, int64_t table_stride, const int32_t* lens, int n_old, int n_new, int max_blocks, int64_t num_pages,
                 int page_size, const int32_t* out, int64_t out_stride) {
@@ -325,19 +325,19 @@ int ivf_kv_fork(const int32_t* table, int64_t table_stride, const int32_t* kv_le
     if (small) {
         static SmemSeen seen;
         if ((rc = allow_smem(kv_fork_small_kernel, kSmallSmem, ctx, seen)) != IVF_OK) return rc;
-        return launch(false, kv_fork_small_kernel, dim3(1), kPageScan, static_cast<int>((w.words + 4 * n_new) * 4), stream, p);
+        return launch(false, kv_fork_small_kernel, dim3(1), kPageScan, static_cast<int>((w.words + 5 * n_new) * 4), stream, p);
     }
     char* ws = static_cast<char*>(workspace);
     p.bits = reinterpret_cast<uint32_t*>(ws), p.claim = reinterpret_cast<int32_t*>(ws + w.claim), p.wish = reinterpret_cast<int32_t*>(ws + w.wish);
     static SmemSeen seen;
-    if ((rc = allow_smem(kv_fork_place_kernel, kPageMaxRows * 4, ctx, seen)) != IVF_OK) return rc;
+    if ((rc = allow_smem(kv_fork_place_kernel, 2 * kPageMaxRows * 4, ctx, seen)) != IVF_OK) return rc;
     auto ctas = [&](int64_t items, int per, int most) { return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((items + per - 1) / per, most)))); };
     const int64_t pieces = (max_blocks + 32ll * kMarkBatch - 1) / (32 * kMarkBatch);
     if ((rc = launch(false, kv_pages_clear_kernel, ctas(w.words / 4 + n_new, kPageThreads, 2 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_pages_mark_kernel, ctas(n_new * pieces, kPageThreads / 32, 8 * ctx.num_sms), kPageThreads, 0, stream, p)) != IVF_OK ||
         (rc = launch(true, kv_fork_own_kernel, ctas(n_new, kPageThreads, kMaxCount), kPageThreads, 0, stream, p)) != IVF_OK)
         return rc;
-    return launch(true, kv_fork_place_kernel, ctas(w.words, kPageScan / 8, ctx.num_sms), kPageScan, 4 * n_new, stream, p);
+    return launch(true, kv_fork_place_kernel, ctas(w.words, kPageScan / 8, ctx.num_sms), kPageScan, 8 * n_new, stream, p);
 }
 
 int ivf_kv_compact(const int32_t* table, int64_t table_stride, const int32_t* kv_lens, int n_req, int max_blocks, int64_t num_pages,
