@@ -339,7 +339,10 @@ __device__ __noinline__ void add_odd(const ChunkParams& p, int b, int h, int lo,
 
 // ---------------------------------------------------------------------------------------------- rows
 // Tiles of 16 rows: single and drafted tokens.  As in ivf_kv_attend's kernel of that name each of four warps takes pieces of 16 keys
-// through a ring of its own and the warps meet at an item's end.
+// through a ring of its own and the warps meet at an item's end.  Bound by the keys' bytes: one token over 131,072 by 8 heads of 128 takes 98 us
+// (537 MB, 5.5 TB/s with the joining of 37 parts to an item), 64 requests of 4,000 tokens 114 us (5.9 TB/s, 0.90 of a copy's rate), drafted tokens by 16 heads
+// of 64 184 us (5.6 TB/s; three CTAs on an SM, with two 232).  A small call is a chain of waits: lengths, place, table, keys, warps,
+// join: 10 us.
 template <int DP>
 struct ChunkRowsControl {
     ChunkPlan<kRowsThreads> plan;

@@ -17,6 +17,12 @@
 // A tile is 64 keys.  A stream has two S, P lies over its S, and S(j + 1) is issued before P(j) V: the softmax warps find the next
 // logits ready.  TMEM holds it exactly: two streams of two S (256 columns) and of O (256).  Heads wider than 128 take all of the second half
 // for one stream's O; it has two threads to a row then, 32 keys each, which tell each other their maxima through shared memory.
+//
+// 4,096 tokens of two requests of 32,768 by 4 heads of a group of 8, d = 128 (1.67 TFLOP of useful products): 1.45 ms in short runs, 1.67 ms under the
+// power limit, 1,150 and 1,000 TFLOP/s.  A tile of the two streams takes 1,850 cycles: its products alone 1,500 (with 64 keys to an
+// instruction S waits for the queries' tile in shared memory, 48 cycles for 32), its softmax alone 1,650 (1,024 of them the special function unit's
+// 16 exponentials a cycle), its copies alone 950.  What was tried: 128 keys to a tile with one S (1.74 ms), two threads to a row here
+// too (1.97), a quarter or an eighth of the exponentials by polynomial (1.62, 1.45), taking turns at the exponentials (1.73).
 #pragma once
 #include "kv_chunk.cuh"
 #include "kv_attend_tile.cuh"
@@ -325,11 +331,27 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         patient.limit_ns = 16 * ctl.limit_ns;
         int planned = 0, n = 0, items = 0;
         bool end = false;
+        // A span that begins inside an item takes the end of that one last: then all CTAs of a head begin at the same keys and go over them
+        // together, and the keys come from L2 more often (4,096 tokens on caches larger than L2: 1,714 against 1,669 us).
+        ChunkCursor kept = at;
+        bool keeps = false;
+        if (at.left > 0) {
+            const int64_t w = chunk_weight(p, at.r, at.tile) - at.off;
+            if (at.off > 0 && at.left > w) {
+                keeps = true;
+                kept.left = w;
+                chunk_next(p, at);
+            }
+        }
         for (int seq = 0; ok; ++seq) {
             // two items ahead: their places are free when the item two before this one has ended
             for (; !end && planned <= seq + 2; ++planned) {
                 ChunkTileItem& t = c.item[planned % S::kItems];
                 if (planned >= S::kItems && !(ok = warp_wait(&c.item_empty[planned % S::kItems], (planned / S::kItems - 1) & 1, patient, 239))) break;
+                if (at.left <= 0 && keeps) {
+                    at = kept;
+                    keeps = false;
+                }
                 end = at.left <= 0;
                 if (lane == 0) {
                     if (end) {
