@@ -339,8 +339,8 @@ __device__ __noinline__ void add_odd(const ChunkParams& p, int b, int h, int lo,
 
 // ---------------------------------------------------------------------------------------------- rows
 // Tiles of 16 rows: single and drafted tokens.  As in ivf_kv_attend's kernel of that name each of four warps takes pieces of 16 keys
-// through a ring of its own and the warps meet at an item's end.  Bound by the keys' bytes: one token over 131,072 by 8 heads of 128 takes 98 us
-// (537 MB, 5.5 TB/s with the joining of 37 parts to an item), 64 requests of 4,000 tokens 114 us (5.9 TB/s, 0.90 of a copy's rate), drafted tokens by 16 heads
+// through a ring of its own and the warps meet at an item's end.  Bound by the keys' bytes: one token over 131,072 by 8 heads of 128 takes 93 us
+// (537 MB, 5.8 TB/s with the joining of 37 parts to an item), 64 requests of 4,000 tokens 113 us (5.9 TB/s, 0.90 of a copy's rate), drafted tokens by 16 heads
 // of 64 184 us (5.6 TB/s; three CTAs on an SM, with two 232).  A small call is a chain of waits: lengths, place, table, keys, warps,
 // join: 10 us.
 template <int DP>
@@ -619,52 +619,85 @@ __global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1
     if (tid == 0) p.desc[blockIdx.x] = tail;
 }
 
-// Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.  A warp to a row: its lanes take the parts'
-// maxima and sums, then the columns.  (A thread to four columns that went over the parts twice by itself took 30 us for 37 parts, a third of the
-// attention; so it is a few waits.)
+// Joins the parts of the items that spans have cut: blockIdx.x is the CTA that the item began in.  WARPS warps to a row, each with its
+// share of the parts, eight at a time: sums, maxima and totals of those are asked for together.  (A thread to four columns that went over the parts twice by
+// itself took 30 us for 37 parts, a third of the attention; one warp to a row 10 us, four 4 us.)
 constexpr int kJoinThreads = 128;
-template <typename T>
+template <typename T, int WARPS>
 __global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const ChunkParams p) {
+    constexpr int kRows = kJoinThreads / 32 / WARPS, kAtOnce = 8;
+    __shared__ float4 s_acc[WARPS > 1 ? WARPS : 1][64];
+    __shared__ float2 s_ml[WARPS];
     pdl_wait();
-    const int c = blockIdx.x, lane = threadIdx.x & 31;
+    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp % WARPS;
     const ChunkDesc d = p.desc[c];
-    const int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5);
-    if (d.parts == 0 || r >= d.tokens * p.part_heads) return;
+    const int r = blockIdx.y * kRows + warp / WARPS;
+    if (d.parts == 0 || r >= d.tokens * p.part_heads) return;  // (with several warps to a row the whole CTA)
     const int h = d.hv / p.parts, g0 = d.hv % p.parts * p.part_heads;
     if (r % p.part_heads >= min(p.part_heads, p.group - g0)) return;
-    const int n_heads = p.group * p.n_kv_heads;
+    const int n_heads = p.group * p.n_kv_heads, quads = p.dim / 4;
     const int64_t step = static_cast<int64_t>(p.rows) * (p.dim + 2);
     auto part = [&](int k) { return p.slots + (k == 0 ? 2 * c + 1 : 2 * (c + k)) * step; };
-    float top = -INFINITY;
-    for (int k = lane; k < d.parts; k += 32) top = fmaxf(top, part(k)[p.rows * p.dim + r]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float base = top == -INFINITY ? 0.0f : top;
-    const int quads = p.dim / 4;
-    float sum = 0.0f;
+    float m = -INFINITY, sum = 0.0f;
     float4 acc[2] = {};
-    for (int k0 = 0; k0 < d.parts; k0 += 32) {
-        const int n = min(32, d.parts - k0);
-        float w = 0.0f;
-        if (lane < n) {
-            const float* src = part(k0 + lane) + p.rows * p.dim + r;
-            w = exp2_fast(src[0] - base);
-            sum += w * src[p.rows];
-        }
-#pragma unroll 8
-        for (int k = 0; k < n; ++k) {
-            const float* src = part(k0 + k) + static_cast<int64_t>(r) * p.dim;
-            const float f = __shfl_sync(0xFFFFFFFFu, w, k);
+    for (int k0 = share; k0 < d.parts; k0 += WARPS * kAtOnce) {
+        float4 v[kAtOnce][2];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if (lane + 32 * i >= quads) continue;
-                const float4 v = *reinterpret_cast<const float4*>(src + (lane + 32 * i) * 4);
-                acc[i].x += f * v.x, acc[i].y += f * v.y, acc[i].z += f * v.z, acc[i].w += f * v.w;
+                const int at = k0 + k * WARPS;
+                v[k][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (at < d.parts && lane + 32 * i < quads) v[k][i] = *reinterpret_cast<const float4*>(part(at) + static_cast<int64_t>(r) * p.dim + (lane + 32 * i) * 4);
             }
+        float mine = -INFINITY, total = 0.0f;  // of part k0 + lane * WARPS
+        if (lane < kAtOnce && k0 + lane * WARPS < d.parts) {
+            const float* src = part(k0 + lane * WARPS) + p.rows * p.dim + r;
+            mine = src[0];
+            total = src[p.rows];
+        }
+        float top = mine;
+#pragma unroll
+        for (int o = kAtOnce / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        top = fmaxf(m, __shfl_sync(0xFFFFFFFFu, top, 0));
+        const float base = top == -INFINITY ? 0.0f : top, fix = exp2_fast(m - base), w = exp2_fast(mine - base);
+        m = top;
+        sum = sum * fix + w * total;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i].x *= fix, acc[i].y *= fix, acc[i].z *= fix, acc[i].w *= fix;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float f = __shfl_sync(0xFFFFFFFFu, w, k);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                acc[i].x += f * v[k][i].x, acc[i].y += f * v[k][i].y, acc[i].z += f * v[k][i].z, acc[i].w += f * v[k][i].w;
         }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (WARPS > 1) {
+        if (lane == 0) s_ml[share] = make_float2(m, sum);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s_acc[share][lane + 32 * i] = acc[i];
+        __syncthreads();
+        if (share > 0) return;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) top = fmaxf(top, s_ml[w].x);
+        m = top;
+        sum = 0.0f;
+        acc[0] = acc[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = exp2_fast(s_ml[w].x - (top == -INFINITY ? 0.0f : top));
+            sum += f * s_ml[w].y;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float4 v = s_acc[w][lane + 32 * i];
+                acc[i].x += f * v.x, acc[i].y += f * v.y, acc[i].z += f * v.z, acc[i].w += f * v.w;
+            }
+        }
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t t = d.token + r / p.part_heads;
     const int head = h * p.group + g0 + r % p.part_heads;
@@ -674,7 +707,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv_chunk_join_kernel(const Chunk
         const uint2 v = make_uint2(Pair16<T>::pack(acc[i].x * inv, acc[i].y * inv), Pair16<T>::pack(acc[i].z * inv, acc[i].w * inv));
         *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + t * p.out_stride[0] + head * p.out_stride[1] + (lane + 32 * i) * 4) = v;
     }
-    if (lane == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+    if (lane == 0 && p.lse) p.lse[t * n_heads + head] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
 }
 
 }  // namespace ivf

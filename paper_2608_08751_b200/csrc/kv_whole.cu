@@ -158,7 +158,11 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
         rc = p.dim <= 64 ? launch_chunk_rows<T, 64>(p, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_rows<T, 128>(p, ctas, ctx, stream)
                                                                                          : launch_chunk_rows<T, 256>(p, ctas, ctx, stream);
     if (rc != IVF_OK) return rc;
-    return launch(true, kv_chunk_join_kernel<T>, dim3(ctas, (p.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, stream, p);
+    // Several warps to a row where items have many parts: one token over 131,072 (37 parts) 93 us, with one warp 99; 37 requests in
+    // windows (2 parts) 29, with one warp 27: the more blocks of threads there are to start.
+    const bool many = !tile && ctas >= 8ll * std::max(p.n_req, 1) * p.n_kv_heads * p.parts;
+    const dim3 grid(ctas, many ? p.rows : (p.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+    return launch(true, many ? kv_chunk_join_kernel<T, kJoinThreads / 32> : kv_chunk_join_kernel<T, 1>, grid, kJoinThreads, 0, stream, p);
 }
 
 // Whether `out` has an element of `q`'s memory.  Rows of one buffer in turn (the same token stride) are told apart, other tensors
