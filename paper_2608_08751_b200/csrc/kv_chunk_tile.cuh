@@ -249,11 +249,11 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 items += to > from;
                 mbar_arrive(&c.item_empty[seq % S::kItems]);
             }
-            if (!ok) {  // gave up: products already issued end before the CTA and its TMEM go (bounded)
-                umma_commit(&c.drain[s]);
-                const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain[s], 0) && global_timer_ns() - t0 < 2000000000ull) {
-                }
+            // Products already issued end before the CTA and its TMEM go (bounded), whoever gave up: this thread may have issued its
+            // last ones and left its loop in good order before another warp's wait ran out.
+            umma_commit(&c.drain[s]);
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(&c.drain[s], 0) && global_timer_ns() - t0 < 2000000000ull) {
             }
         }
     } else if (warp == S::kSoftWarps + 2) {
@@ -261,7 +261,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const int box_shift = min(p.page_shift, 6), box = 1 << box_shift;  // a page of 128 tokens is two boxes of 64
         const int boxes = kKeys >> box_shift;
         const uint32_t k_at = smem_u32(k_ring), v_at = smem_u32(v_ring);
-        int n = 0;  // tiles so far
+        int n = 0, n_v = 0;  // tiles whose keys, whose values have been asked for
         for (int seq = 0; ok; ++seq) {
             if (!(ok = warp_wait(&c.item_full[seq % S::kItems], (seq / S::kItems) & 1, ctl, 240))) break;
             const ChunkTileItem& t = c.item[seq % S::kItems];
@@ -283,7 +283,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             };
             int page = checked(entry(lane)), ahead = entry(32 + lane);
             int at_box = 0;  // the tile's first box, among the 32
-            for (int i = 0; i < count; ++i, ++n, at_box += boxes) {
+            for (int i = 0; i < count; ++i, at_box += boxes) {
                 if (at_box == 32) {
                     page = checked(ahead);
                     ahead = entry(i * boxes + 32 + lane);
@@ -308,22 +308,26 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 }
                 __syncwarp();
                 if (b < boxes) tma_load_4d(k_at + place, &map_k, &c.k_full[stage], d * 64, row, h, pg);
-                if (n >= kStages && !(ok = warp_wait(&c.v_empty[stage], (n / kStages - 1) & 1, ctl, 246))) break;
+                ++n;
+                if (n_v >= kStages && !(ok = warp_wait(&c.v_empty[stage], (n_v / kStages - 1) & 1, ctl, 246))) break;
                 if (lane == 0) mbar_arrive_expect_tx(&c.v_full[stage], S::kPlaneBytes);
                 __syncwarp();
                 if (b < boxes) tma_load_4d(v_at + place, &map_v, &c.v_full[stage], d * 64, row, h, pg);
+                ++n_v;
             }
-            if (!ok) break;  // (a tile's values were not asked for; its keys are waited for below with those before)
+            if (!ok) break;  // (a tile's values were not asked for, its keys may have been)
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.item_empty[seq % S::kItems]);
         }
-        if (!ok) {  // gave up: copies in flight land before the CTA goes (bounded)
-            const uint64_t t0 = global_timer_ns();
-            for (int i = max(0, n - kStages); i <= n; ++i)
-                for (int plane = 0; plane < 2; ++plane)
-                    while (!mbar_try_wait(plane ? &c.v_full[i % kStages] : &c.k_full[i % kStages], (i / kStages) & 1) && global_timer_ns() - t0 < 100000000ull) {
-                    }
-        }
+        // Copies in flight land before the CTA goes (bounded), whoever gave up; those of a place before its last ones have (the place was
+        // free again).
+        const uint64_t t0 = global_timer_ns();
+        for (int i = max(0, n - kStages); i < n; ++i)
+            while (!mbar_try_wait(&c.k_full[i % kStages], (i / kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
+            }
+        for (int i = max(0, n_v - kStages); i < n_v; ++i)
+            while (!mbar_try_wait(&c.v_full[i % kStages], (i / kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
+            }
     } else if (warp == S::kSoftWarps + 3) {
         // ------------------------------------------------------------ planner and cleaner
         ChunkDesc tail = {0, 0, 0, 0};
@@ -641,6 +645,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             all_items += t.count > 0;
             arrive(&c.item_empty[seq % S::kItems]);
         }
+        __syncwarp();
+        tmem_wait_st();  // (a wait that ran out may have left stores behind it)
     }
     // ------------------------------------------------------------ teardown (also the abort path)
     tc_fence_before_sync();
