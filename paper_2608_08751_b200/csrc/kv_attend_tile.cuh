@@ -435,7 +435,6 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             int sj = 0, pj = 0;  // next S and P V
             uint64_t since = 0;
             uint32_t idle = 0;
-            bool ok = true;
             while (pj < tiles) {
                 bool moved = false;
                 if (sj < k && mbar_test_wait(&c.k_full[sj % S::kStages], (sj / S::kStages) & 1) &&
@@ -487,24 +486,21 @@ kv_attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     const uint64_t t = global_timer_ns();
                     if (idle == 256u) since = t;
                     if (t - since > ctl.limit_ns) report_timeout(ctl, 202);
-                    if (*ctl.abort_flag) {
-                        ok = false;
-                        break;
-                    }
+                    if (*ctl.abort_flag) break;
                 }
             }
-            if (!ok) {  // gave up: copies and products already issued end before the CTA and its TMEM go (bounded)
-                umma_commit(&c.drain);
-                const uint64_t t0 = global_timer_ns();
-                while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
-                }
-                for (int i = max(0, k - S::kStages); i < k; ++i)
-                    while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
-                    }
-                for (int i = max(0, v - S::kStages); i < v; ++i)
-                    while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
-                    }
+            // Copies and products already issued end before the CTA and its TMEM go (bounded), whoever gave up: this thread may have issued
+            // its last ones and left its loop in good order before a softmax warp's wait ran out.
+            umma_commit(&c.drain);
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(&c.drain, 0) && global_timer_ns() - t0 < 2000000000ull) {
             }
+            for (int i = max(0, k - S::kStages); i < k; ++i)
+                while (!mbar_try_wait(&c.k_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
+                }
+            for (int i = max(0, v - S::kStages); i < v; ++i)
+                while (!mbar_try_wait(&c.v_full[i % S::kStages], (i / S::kStages) & 1) && global_timer_ns() - t0 < 2000000000ull) {
+                }
         }
     } else {
         // ------------------------------------------------------------ softmax: thread = row = TMEM lane

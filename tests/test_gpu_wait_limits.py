@@ -36,7 +36,7 @@ def _sweep(call, right):
         assert right(call())
         B.ivf_check()
     print("ran out:", "".join("x" if e else "." for e in ends))
-    assert any(ends[:8])  # (no wait for memory is as short as that)
+    assert any(ends[:8])  # (no wait for memory is over within a few looks)
 
 
 @pytest.mark.parametrize("dim,more", [(64, {}), (128, {}), (256, {}), (128, {"cap": 5.0}), (96, {"window": 100})], ids=str)
