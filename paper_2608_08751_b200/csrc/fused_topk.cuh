@@ -804,8 +804,9 @@ fused_topk_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_const
             ++seg;
             u = r * NT + t1;
         }
-        if (lane == 0 && !ok) {
-            // gave up: let the copies already issued land before the CTA goes away (bounded)
+        if (lane == 0) {
+            // the copies already issued land before the CTA goes away (bounded), whoever gave up: this thread may have
+            // issued its last ones and left its loop in good order before another warp's wait ran out
             const uint64_t t_start = global_timer_ns();
             const int first = it > p.nstage ? it - p.nstage : 0;
             for (int i = first; i < it; ++i) {
@@ -905,12 +906,10 @@ fused_topk_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_const
                 ++seg;
                 u = r * NT + t1;
             }
-            if (!ok && it > 0) {
-                // gave up: wait (bounded) until the MMAs already issued have retired before TMEM is freed
-                umma_commit(drain);
-                const uint64_t t_start = global_timer_ns();
-                while (!mbar_try_wait(drain, 0) && global_timer_ns() - t_start < 2000000000ull) {
-                }
+            // the MMAs already issued retire before TMEM is freed (bounded), whoever gave up
+            umma_commit(drain);
+            const uint64_t t_start = global_timer_ns();
+            while (!mbar_try_wait(drain, 0) && global_timer_ns() - t_start < 2000000000ull) {
             }
         }
     } else {
