@@ -578,6 +578,14 @@ int ivf_kv_copy(const ivf_kv_cache* cache, const int32_t* copy_from, const int32
  * 2 = the one that takes windows of tokens wherever it can run. */
 int ivf_debug_set_kv_attend(int kernel);
 int ivf_debug_set_kv_select(int kernel);  /* the same for ivf_kv_select */
+/* Test hook (host only): how ivf_kv_attend_chunk shares its work out on a device with `num_sms` SMs, by tiles of 16 rows (tiles = 0) or by large ones.
+ * token_start, kv_lens and prefix (or NULL) lie in host memory.  A row of items [max_items][11] for each item or part of one, in the order in which
+ * its block of threads takes them: block, request, kv head * parts + part of the group, first token, tokens, position of the first,
+ * first key, one past the last key, begins the item, ends the item, and where it begins but does not end one, the blocks that have a part of it.
+ * info: rows there are, blocks with work, tokens of a tile, length of the line. */
+int ivf_debug_kv_chunk_spans(int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, int n_req, int max_blocks, const int32_t* token_start,
+                             const int32_t* kv_lens, int window, const int32_t* prefix, int tiles, int num_sms, int64_t* items, int64_t max_items,
+                             int64_t info[4]);
 int ivf_debug_set_kv_chunk(int kernel);   /* the same for ivf_kv_attend_chunk: 1 = tiles of 16 rows, 2 = tiles of 128 or 256 wherever they can run */
 
 #ifdef __cplusplus

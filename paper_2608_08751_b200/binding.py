@@ -30,7 +30,7 @@ EXPORTS = (
     "ivf_pq_encode", "ivf_pq_search", "ivf_pq_residuals", "ivf_assign_candidates", "ivf_merge_shards",
     "ivf_kv_tables", "ivf_kv_append", "ivf_kv_summarize", "ivf_kv_select", "ivf_kv_attend",
     "ivf_kv_attend_chunk", "ivf_kv_attend_chunk_workspace", "ivf_kv_fork", "ivf_kv_compact", "ivf_kv_pages_workspace", "ivf_kv_copy",
-    "ivf_debug_set_kv_attend", "ivf_debug_set_kv_select", "ivf_debug_set_kv_chunk",
+    "ivf_debug_set_kv_attend", "ivf_debug_set_kv_select", "ivf_debug_set_kv_chunk", "ivf_debug_kv_chunk_spans",
     "ivf_set_deferred_host_outputs", "ivf_wait_host_outputs",
     "ivf_check", "ivf_last_error", "ivf_release_workspace", "ivf_launch_count",
     "ivf_debug_plan", "ivf_debug_span", "ivf_debug_rotation", "ivf_debug_set_rotation", "ivf_debug_set_threshold_pass", "ivf_debug_fail_next_alloc", "ivf_debug_bounds_checked", "ivf_debug_bounds_probe", "ivf_debug_set_wait_limit_ns",
@@ -112,6 +112,7 @@ def lib() -> ctypes.CDLL:
     L.ivf_kv_attend.argtypes = [vp, vp, i64, i32, cache, vp, i64, i32, i32, vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp]
     L.ivf_kv_attend_chunk_workspace.argtypes = [i64, i32, cache, i32, ctypes.POINTER(i64)]
     L.ivf_kv_attend_chunk.argtypes = [vp, vp, i64, i32, cache, vp, i64, i32, i32, vp, vp, ctypes.c_float, ctypes.c_float, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+    L.ivf_debug_kv_chunk_spans.argtypes = [i64, i32, cache, i32, i32, vp, vp, i32, vp, i32, i32, vp, i64, vp]
     L.ivf_kv_pages_workspace.argtypes = [i32, i32, i64, ctypes.POINTER(i64)]
     L.ivf_kv_fork.argtypes = [vp, i64, vp, i32, i32, vp, vp, i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     L.ivf_kv_compact.argtypes = [vp, i64, vp, i32, i32, i64, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp]

@@ -59,6 +59,7 @@ struct ChunkParams {
 };
 
 // ------------------------------------------------------------------ the line of items
+// (also compiled for the host, where ivf_debug_kv_chunk_span walks it)
 struct ChunkReq {
     int start, fresh;  // its first token, its tokens in this call
     int base;          // position of the first
@@ -68,14 +69,16 @@ struct ChunkReq {
     int64_t j_hi, j_lo;  // tiles before these end at the prefix, begin at key 0
 };
 
-__device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, bool report) {
+__host__ __device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, bool report) {
     ChunkReq r;
     const int s0 = p.token_start[b], s1 = p.token_start[b + 1], len = p.kv_lens[b];
     const bool none = s0 < 0 || s1 < s0;
     const int given = none ? 0 : s1 - s0;
     r.blind = len < given || len < 0;
     const int64_t room = static_cast<int64_t>(p.max_blocks) << p.page_shift;
+#ifdef __CUDA_ARCH__
     if (report && (none || r.blind || len > room)) kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
+#endif
     r.start = s0;
     r.fresh = static_cast<int>(max(min(static_cast<int64_t>(s0) + given, p.n_tokens) - s0, static_cast<int64_t>(0)));
     r.len = r.blind ? 0 : len;
@@ -90,18 +93,18 @@ __device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, bool 
     r.j_lo = p.window <= 0 ? r.tiles : c < 0 ? 0 : static_cast<unsigned>(c) / T + 1;
     return r;
 }
-__device__ __forceinline__ int chunk_hi(const ChunkParams& p, const ChunkReq& r, int j) {  // one past the last key that the tile sees
+__host__ __device__ __forceinline__ int chunk_hi(const ChunkParams& p, const ChunkReq& r, int j) {  // one past the last key that the tile sees
     const int last = min((j + 1) * p.tile_tokens, r.fresh);
     return r.blind ? 0 : max(r.base + last, r.prefix);
 }
-__device__ __forceinline__ int chunk_lo(const ChunkParams& p, const ChunkReq& r, int j) {
+__host__ __device__ __forceinline__ int chunk_lo(const ChunkParams& p, const ChunkReq& r, int j) {
     return r.blind || p.window <= 0 ? 0 : max(r.base + j * p.tile_tokens - p.window + 1, 0);
 }
-__device__ __forceinline__ int64_t chunk_weight(const ChunkParams& p, const ChunkReq& r, int j) {
+__host__ __device__ __forceinline__ int64_t chunk_weight(const ChunkParams& p, const ChunkReq& r, int j) {
     return static_cast<int64_t>(chunk_hi(p, r, j)) - chunk_lo(p, r, j) + p.item_cost;
 }
 // Weights of the tiles before tile i of one head.
-__device__ __forceinline__ int64_t chunk_before(const ChunkParams& p, const ChunkReq& r, int64_t i) {
+__host__ __device__ __forceinline__ int64_t chunk_before(const ChunkParams& p, const ChunkReq& r, int64_t i) {
     const int64_t cost = i * p.item_cost;
     if (r.blind || i == 0) return cost;
     const int64_t n = i == r.tiles ? i - 1 : i, T = p.tile_tokens;  // the last tile may be short
@@ -129,11 +132,45 @@ struct ChunkPlan {
 struct ChunkSpans {
     int ctas, over;
     int64_t whole;
-    __device__ __forceinline__ int64_t begin(int c) const { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(ctas); }
+    __host__ __device__ __forceinline__ int64_t begin(int c) const { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(ctas); }
 };
 // (a 64-bit division takes a hundred instructions, and nearly every line is shorter)
-__device__ __forceinline__ int64_t chunk_div(int64_t a, int64_t b) {
+__host__ __device__ __forceinline__ int64_t chunk_div(int64_t a, int64_t b) {
     return (a | b) >> 32 ? a / b : static_cast<int64_t>(static_cast<unsigned>(a) / static_cast<unsigned>(b));
+}
+
+// Where a weight `rest` behind the start of request b0 lies, before request b1.
+__host__ __device__ __forceinline__ void chunk_locate(const ChunkParams& p, int b0, int b1, int64_t rest, ChunkCursor& at) {
+    const int hvs = p.n_kv_heads * p.parts;
+    for (int b = b0; b < b1; ++b) {
+        const ChunkReq r = chunk_req(p, b, false);
+        const int64_t one = chunk_before(p, r, r.tiles);
+        if (rest >= one * hvs) {
+            rest -= one * hvs;
+            continue;
+        }
+        at.b = b;
+        at.hv = static_cast<int>(chunk_div(rest, one));
+        rest -= at.hv * one;
+        int lo = 0, hi = r.tiles;  // before(lo) <= rest < before(hi)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (chunk_before(p, r, mid) <= rest) lo = mid;
+            else hi = mid;
+        }
+        at.tile = lo;
+        at.off = rest - chunk_before(p, r, lo);
+        at.r = r;
+        return;
+    }
+}
+// The line in spans of at least p.least keys, as many as `most` at the most.
+__host__ __device__ __forceinline__ ChunkSpans chunk_spans(const ChunkParams& p, int64_t total, int most) {
+    ChunkSpans spans;
+    spans.ctas = static_cast<int>(max(min(chunk_div(total, p.least), static_cast<int64_t>(most)), static_cast<int64_t>(1)));
+    spans.whole = chunk_div(total, spans.ctas);
+    spans.over = static_cast<int>(total - spans.whole * spans.ctas);
+    return spans;
 }
 
 // All threads: the CTA's cursor (left = 0: nothing to do) and where the spans lie.
@@ -164,36 +201,13 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
         if (w < warp) upto += s.warp_sum[w];
         total += s.warp_sum[w];
     }
-    spans.ctas = static_cast<int>(max(min(chunk_div(total, p.least), static_cast<int64_t>(gridDim.x)), static_cast<int64_t>(1)));
-    spans.whole = chunk_div(total, spans.ctas);
-    spans.over = static_cast<int>(total - spans.whole * spans.ctas);
+    spans = chunk_spans(p, total, gridDim.x);
     const int c = blockIdx.x;
     if (c < spans.ctas) {
         const int64_t u0 = spans.begin(c), u1 = spans.begin(c + 1);
         if (u0 >= upto && u0 < upto + mine) {
-            int64_t rest = u0 - upto;
-            for (int b = b0; b < b1; ++b) {
-                const ChunkReq r = chunk_req(p, b, false);
-                const int64_t one = chunk_before(p, r, r.tiles);
-                if (rest >= one * hvs) {
-                    rest -= one * hvs;
-                    continue;
-                }
-                s.at.b = b;
-                s.at.hv = static_cast<int>(chunk_div(rest, one));
-                rest -= s.at.hv * one;
-                int lo = 0, hi = r.tiles;  // before(lo) <= rest < before(hi)
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (chunk_before(p, r, mid) <= rest) lo = mid;
-                    else hi = mid;
-                }
-                s.at.tile = lo;
-                s.at.off = rest - chunk_before(p, r, lo);
-                s.at.left = u1 - u0;
-                s.at.r = r;
-                break;
-            }
+            chunk_locate(p, b0, b1, u0 - upto, s.at);
+            s.at.left = u1 - u0;
         }
     }
     __syncthreads();
@@ -209,7 +223,7 @@ struct ChunkItem {
     bool first, last;       // the part begins, ends the item
     int64_t rest;           // of the item behind the part
 };
-__device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const ChunkCursor& at) {
+__host__ __device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const ChunkCursor& at) {
     ChunkItem it;
     const ChunkReq& r = at.r;
     const int64_t w = chunk_weight(p, r, at.tile), take = min(at.left, w - at.off);
@@ -231,7 +245,7 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkParams& p, const Chun
     it.k1 = it.last ? it.hi : cut(at.off + take);
     return it;
 }
-__device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkCursor& at) {
+__host__ __device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkCursor& at) {
     const int64_t take = min(at.left, chunk_weight(p, at.r, at.tile) - at.off);
     at.left -= take;
     at.off = 0;
@@ -243,8 +257,18 @@ __device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkCursor& at
         do at.r = chunk_req(p, ++at.b, false);
         while (at.r.tiles == 0 && at.b < p.n_req - 1);
 }
+// A span that begins inside an item and goes on behind it: `at` moves on to the next item, `kept` is the end of the first one, to be taken last.
+__host__ __device__ __forceinline__ bool chunk_keep(const ChunkParams& p, ChunkCursor& at, ChunkCursor& kept) {
+    if (at.left <= 0 || at.off == 0) return false;
+    const int64_t w = chunk_weight(p, at.r, at.tile) - at.off;
+    if (at.left <= w) return false;
+    kept = at;
+    kept.left = w;
+    chunk_next(p, at);
+    return true;
+}
 // The CTAs that take part in an item whose rest lies behind this CTA's span.
-__device__ __forceinline__ int chunk_parts(const ChunkSpans& spans, int c, int64_t rest) {
+__host__ __device__ __forceinline__ int chunk_parts(const ChunkSpans& spans, int c, int64_t rest) {
     const int64_t end = spans.begin(c + 1) + rest;  // of the item
     int past = min(c + 1 + static_cast<int>(chunk_div(rest, spans.whole + 1)), spans.ctas);  // no span is longer: none before it ends the item
     while (past < spans.ctas && spans.begin(past) < end) ++past;
@@ -252,7 +276,7 @@ __device__ __forceinline__ int chunk_parts(const ChunkSpans& spans, int c, int64
 }
 
 // Keys that a token at position pos sees.
-__device__ __forceinline__ void chunk_sees(const ChunkParams& p, const ChunkReq& r, int pos, bool live, int& lo, int& hi) {
+__host__ __device__ __forceinline__ void chunk_sees(const ChunkParams& p, const ChunkReq& r, int pos, bool live, int& lo, int& hi) {
     live = live && !r.blind;
     lo = live && p.window > 0 ? max(pos - p.window + 1, 0) : 0;
     hi = live ? min(max(pos + 1, r.prefix), r.far) : 0;

@@ -337,16 +337,8 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         bool end = false;
         // A span that begins inside an item takes the end of that one last: then all CTAs of a head begin at the same keys and go over them
         // together, and the keys come from L2 more often (4,096 tokens on caches larger than L2: 1,714 against 1,669 us).
-        ChunkCursor kept = at;
-        bool keeps = false;
-        if (at.left > 0) {
-            const int64_t w = chunk_weight(p, at.r, at.tile) - at.off;
-            if (at.off > 0 && at.left > w) {
-                keeps = true;
-                kept.left = w;
-                chunk_next(p, at);
-            }
-        }
+        ChunkCursor kept;
+        bool keeps = chunk_keep(p, at, kept);
         for (int seq = 0; ok; ++seq) {
             // two items ahead: their places are free when the item two before this one has ended
             for (; !end && planned <= seq + 2; ++planned) {

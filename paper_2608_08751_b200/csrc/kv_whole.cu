@@ -98,6 +98,13 @@ ChunkShape chunk_shape(int group, int dim, bool tile) {
     s.ctas = (tile || dim > 128 ? 1 : dim > 64 ? 2 : 3) * kChunkMaxSms;
     return s;
 }
+void chunk_settings(ChunkParams& p, const ChunkShape& s) {
+    p.tile_tokens = s.tile_tokens, p.part_heads = s.part_heads, p.parts = s.parts, p.rows = s.rows;
+    p.item_cost = s.streams ? 384 : 160;
+    p.least = s.streams ? 1024 : 160;
+    p.grain = s.streams ? 128 : 64;
+}
+int chunk_ctas(const ChunkShape& s, int num_sms) { return s.ctas / kChunkMaxSms * std::min(num_sms, kChunkMaxSms); }
 int64_t chunk_bytes(const ChunkShape& s, int dim) {
     return s.ctas * (static_cast<int64_t>(sizeof(ChunkDesc)) + 2ll * s.rows * (dim + 2) * sizeof(float));
 }
@@ -143,13 +150,10 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
     const bool tile = chunk_tiles_pay(p.n_tokens, p.n_req, p.group, p.dim) && p.num_pages > 0 &&
                       kv_host_map(&mk, p.kc, p.dim, page, p.n_kv_heads, p.num_pages, bf16) && kv_host_map(&mv, p.vc, p.dim, page, p.n_kv_heads, p.num_pages, bf16);
     const ChunkShape s = chunk_shape(p.group, p.dim, tile);
-    const int ctas = s.ctas / kChunkMaxSms * std::min(ctx.num_sms, kChunkMaxSms);
-    p.tile_tokens = s.tile_tokens, p.part_heads = s.part_heads, p.parts = s.parts, p.rows = s.rows;
+    const int ctas = chunk_ctas(s, ctx.num_sms);
+    chunk_settings(p, s);
     p.desc = static_cast<ChunkDesc*>(workspace);
     p.slots = reinterpret_cast<float*>(p.desc + s.ctas);
-    p.item_cost = tile ? 384 : 160;
-    p.least = tile ? 1024 : 160;
-    p.grain = tile ? 128 : 64;
     int rc;
     if (tile)
         rc = p.dim <= 64 ? launch_chunk_tile<T, 1>(p, mk, mv, ctas, ctx, stream) : p.dim <= 128 ? launch_chunk_tile<T, 2>(p, mk, mv, ctas, ctx, stream)
@@ -285,6 +289,52 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
 int ivf_debug_set_kv_chunk(int kernel) {
     if (kernel < 0 || kernel > 2) return fail(IVF_ERR_INVALID_ARG, "kernel = %d", kernel);
     g_kv_chunk = kernel;
+    return IVF_OK;
+}
+
+int ivf_debug_kv_chunk_spans(int64_t n_tokens, int n_heads, const ivf_kv_cache* cache, int n_req, int max_blocks, const int32_t* token_start,
+                             const int32_t* kv_lens, int window, const int32_t* prefix, int tiles, int num_sms, int64_t* items, int64_t max_items,
+                             int64_t info[4]) {
+    if (!cache || !token_start || !kv_lens || !info || (max_items > 0 && !items)) return fail(IVF_ERR_INVALID_ARG, "null pointer argument");
+    int rc = kv_check_page(cache->page_size);
+    if (rc == IVF_OK) rc = kv_check_dim(cache->head_dim);
+    if (rc == IVF_OK) rc = kv_check_heads(n_heads, cache->n_kv_heads);
+    if (rc != IVF_OK) return rc;
+    if (n_tokens < 0 || n_req < 0 || max_blocks < 1 || window < 0 || num_sms < 1 || max_items < 0) return fail(IVF_ERR_INVALID_ARG, "negative size");
+    const ChunkShape s = chunk_shape(n_heads / cache->n_kv_heads, cache->head_dim, tiles != 0);
+    ChunkParams p = {};
+    p.n_tokens = n_tokens, p.group = n_heads / cache->n_kv_heads, p.n_kv_heads = cache->n_kv_heads, p.dim = cache->head_dim;
+    p.n_req = n_req, p.max_blocks = max_blocks, p.page_shift = kv_shift(cache->page_size);
+    p.token_start = token_start, p.kv_lens = kv_lens, p.prefix = prefix, p.window = window;
+    chunk_settings(p, s);
+    int64_t total = 0, n = 0;
+    for (int b = 0; b < n_req; ++b) {
+        const ChunkReq r = chunk_req(p, b, false);
+        total += p.n_kv_heads * p.parts * chunk_before(p, r, r.tiles);
+    }
+    const ChunkSpans spans = chunk_spans(p, total, chunk_ctas(s, num_sms));
+    for (int c = 0; c < spans.ctas; ++c) {
+        ChunkCursor at = {}, kept = {};
+        at.left = spans.begin(c + 1) - spans.begin(c);
+        if (at.left > 0) chunk_locate(p, 0, n_req, spans.begin(c), at);
+        bool keeps = tiles && chunk_keep(p, at, kept);
+        while (true) {
+            if (at.left <= 0 && keeps) {
+                at = kept;
+                keeps = false;
+            }
+            if (at.left <= 0) break;
+            const ChunkItem it = chunk_item(p, at);
+            if (n < max_items) {
+                const int64_t row[11] = {c, at.b, it.hv, it.token, it.tokens, it.pos, it.k0, it.k1, it.first, it.last,
+                                         it.first && !it.last ? chunk_parts(spans, c, it.rest) : 0};
+                std::copy(row, row + 11, items + 11 * n);
+            }
+            ++n;
+            chunk_next(p, at);
+        }
+    }
+    info[0] = n, info[1] = spans.ctas, info[2] = s.tile_tokens, info[3] = total;
     return IVF_OK;
 }
 
