@@ -519,8 +519,9 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
  *   out             must not share memory with q (refused), the caches or the workspace
  *   workspace       what ivf_kv_attend_chunk_workspace says for the same sizes, 16-byte aligned.  It is written and read by this call alone;
  *                   two calls that may run at the same time need one each
- * The tokens of a request with fewer tokens in the cache than new ones see nothing (zeros; -infinity); one whose rows of token_start
- * descend has none.  Both set IVF_ERR_BAD_ID, as a page past the cache and a length past the table's columns do; a page that is missing (-1), and what lies past the
+ * The tokens of a request with fewer tokens in the cache than new ones see nothing (zeros; -infinity).  Where token_start descends or is negative its running
+ * maximum from 0 counts: a row belongs to the first request that reaches it, at the position that it has there.
+ * Both set IVF_ERR_BAD_ID, as a page past the cache and a length past the table's columns do; a page that is missing (-1), and what lies past the
  * columns, is not seen.  What pages hold past a request's last token, or before every window, is never used; a value that is not
  * finite reaches only the tokens that see it.  The weights are rounded as in ivf_kv_attend.  The result is the same on every call.
  */

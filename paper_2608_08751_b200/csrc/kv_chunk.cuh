@@ -61,7 +61,7 @@ struct ChunkParams {
 // ------------------------------------------------------------------ the line of items
 // (also compiled for the host, where ivf_debug_kv_chunk_span walks it)
 struct ChunkReq {
-    int start, fresh;  // its first token, its tokens in this call
+    int start, fresh;  // its first row, its rows in this call
     int base;          // position of the first
     int len, far;      // tokens in the cache; keys that the table has columns for
     int prefix, tiles;
@@ -69,20 +69,21 @@ struct ChunkReq {
     int64_t j_hi, j_lo;  // tiles before these end at the prefix, begin at key 0
 };
 
-__host__ __device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, bool report) {
+// `taken`: rows before it are an earlier request's, or nobody's.  That is the start of the request before (where token_start descends, which is an
+// error, the largest so far), so every row has one request.
+__host__ __device__ __forceinline__ ChunkReq chunk_req(const ChunkParams& p, int b, int taken, bool report) {
     ChunkReq r;
     const int s0 = p.token_start[b], s1 = p.token_start[b + 1], len = p.kv_lens[b];
-    const bool none = s0 < 0 || s1 < s0;
-    const int given = none ? 0 : s1 - s0;
-    r.blind = len < given || len < 0;
+    const int64_t given = max(static_cast<int64_t>(s1) - s0, static_cast<int64_t>(0));
+    r.blind = len < given;
+    r.start = max(s0, taken);
     const int64_t room = static_cast<int64_t>(p.max_blocks) << p.page_shift;
 #ifdef __CUDA_ARCH__
-    if (report && (none || r.blind || len > room)) kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
+    if (report && (s0 < 0 || s1 < s0 || r.blind || len > room)) kv_report(p.status, kKvStatusBadId, KV_SITE_CHUNK);
 #endif
-    r.start = s0;
-    r.fresh = static_cast<int>(max(min(static_cast<int64_t>(s0) + given, p.n_tokens) - s0, static_cast<int64_t>(0)));
+    r.fresh = static_cast<int>(max(min(static_cast<int64_t>(s1), p.n_tokens) - r.start, static_cast<int64_t>(0)));
     r.len = r.blind ? 0 : len;
-    r.base = r.blind ? 0 : len - given;
+    r.base = r.blind ? 0 : static_cast<int>(len - given + min(static_cast<int64_t>(r.start) - s0, given));
     r.far = static_cast<int>(min(static_cast<int64_t>(r.len), room));
     r.prefix = p.prefix ? max(0, min(p.prefix[b], r.len)) : 0;
     r.tiles = (r.fresh + p.tile_tokens - 1) / p.tile_tokens;
@@ -132,6 +133,7 @@ struct ChunkPlan {
 struct ChunkSpans {
     int ctas, over;
     int64_t whole;
+    int end;  // rows from here on are no request's
     __host__ __device__ __forceinline__ int64_t begin(int c) const { return whole * c + static_cast<unsigned>(over * c) / static_cast<unsigned>(ctas); }
 };
 // (a 64-bit division takes a hundred instructions, and nearly every line is shorter)
@@ -140,10 +142,11 @@ __host__ __device__ __forceinline__ int64_t chunk_div(int64_t a, int64_t b) {
 }
 
 // Where a weight `rest` behind the start of request b0 lies, before request b1.
-__host__ __device__ __forceinline__ void chunk_locate(const ChunkParams& p, int b0, int b1, int64_t rest, ChunkCursor& at) {
+__host__ __device__ __forceinline__ void chunk_locate(const ChunkParams& p, int b0, int b1, int taken, int64_t rest, ChunkCursor& at) {
     const int hvs = p.n_kv_heads * p.parts;
     for (int b = b0; b < b1; ++b) {
-        const ChunkReq r = chunk_req(p, b, false);
+        const ChunkReq r = chunk_req(p, b, taken, false);
+        taken = r.start;
         const int64_t one = chunk_before(p, r, r.tiles);
         if (rest >= one * hvs) {
             rest -= one * hvs;
@@ -165,12 +168,10 @@ __host__ __device__ __forceinline__ void chunk_locate(const ChunkParams& p, int 
     }
 }
 // The line in spans of at least p.least keys, as many as `most` at the most.
-__host__ __device__ __forceinline__ ChunkSpans chunk_spans(const ChunkParams& p, int64_t total, int most) {
-    ChunkSpans spans;
+__host__ __device__ __forceinline__ void chunk_spans(const ChunkParams& p, int64_t total, int most, ChunkSpans& spans) {
     spans.ctas = static_cast<int>(max(min(chunk_div(total, p.least), static_cast<int64_t>(most)), static_cast<int64_t>(1)));
     spans.whole = chunk_div(total, spans.ctas);
     spans.over = static_cast<int>(total - spans.whole * spans.ctas);
-    return spans;
 }
 
 // All threads: the CTA's cursor (left = 0: nothing to do) and where the spans lie.
@@ -180,20 +181,36 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
     const int per = (p.n_req + THREADS - 1) / THREADS;
     const int b0 = min(tid * per, p.n_req), b1 = min(b0 + per, p.n_req);
     const int hvs = p.n_kv_heads * p.parts;
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) {
-        const ChunkReq r = chunk_req(p, b, blockIdx.x == 0);
-        mine += hvs * chunk_before(p, r, r.tiles);
-    }
-    int64_t upto = mine;
+    int64_t mine, upto;
+    int taken = 0;
+    auto add_up = [&](bool report) {  // whether token_start descends among the thread's requests
+        bool down = false;
+        mine = 0;
+        int t = taken;
+        for (int b = b0; b < b1; ++b) {
+            const ChunkReq r = chunk_req(p, b, t, report);
+            t = r.start;
+            down |= p.token_start[b + 1] < t;
+            mine += hvs * chunk_before(p, r, r.tiles);
+        }
+        upto = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 31) s.warp_sum[warp] = upto;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) s.warp_sum[warp] = upto;
+        return down;
+    };
+    const bool down = add_up(blockIdx.x == 0);
     if (tid == 0) s.at.left = 0;
-    __syncthreads();
+    spans.end = p.token_start[p.n_req];
+    if (__syncthreads_or(down)) {  // an error: once more, with what all requests before the thread's have taken
+        for (int b = 0; b < b0; ++b) taken = max(taken, p.token_start[b]);
+        for (int b = 0; b < p.n_req; ++b) spans.end = max(spans.end, p.token_start[b]);
+        add_up(false);
+        __syncthreads();
+    }
     int64_t total = 0;
     upto -= mine;
 #pragma unroll
@@ -201,12 +218,12 @@ __device__ __forceinline__ ChunkCursor chunk_plan(const ChunkParams& p, ChunkPla
         if (w < warp) upto += s.warp_sum[w];
         total += s.warp_sum[w];
     }
-    spans = chunk_spans(p, total, gridDim.x);
+    chunk_spans(p, total, gridDim.x, spans);
     const int c = blockIdx.x;
     if (c < spans.ctas) {
         const int64_t u0 = spans.begin(c), u1 = spans.begin(c + 1);
         if (u0 >= upto && u0 < upto + mine) {
-            chunk_locate(p, b0, b1, u0 - upto, s.at);
+            chunk_locate(p, b0, b1, taken, u0 - upto, s.at);
             s.at.left = u1 - u0;
         }
     }
@@ -254,7 +271,7 @@ __host__ __device__ __forceinline__ void chunk_next(const ChunkParams& p, ChunkC
     if (++at.hv < p.n_kv_heads * p.parts) return;
     at.hv = 0;
     if (at.left > 0)  // (weights left: there is a request with tokens)
-        do at.r = chunk_req(p, ++at.b, false);
+        do at.r = chunk_req(p, ++at.b, at.r.start, false);
         while (at.r.tiles == 0 && at.b < p.n_req - 1);
 }
 // A span that begins inside an item and goes on behind it: `at` moves on to the next item, `kept` is the end of the first one, to be taken last.
@@ -284,10 +301,10 @@ __host__ __device__ __forceinline__ void chunk_sees(const ChunkParams& p, const 
 
 // Tokens that belong to no request: zeros.
 template <typename T>
-__device__ __forceinline__ void chunk_padding(const ChunkParams& p, int threads) {
+__device__ __forceinline__ void chunk_padding(const ChunkParams& p, const ChunkSpans& spans, int threads) {
     const int n_heads = p.group * p.n_kv_heads;
     const int64_t before = max(static_cast<int64_t>(0), min(static_cast<int64_t>(p.token_start[0]), p.n_tokens));
-    const int64_t from = max(before, min(static_cast<int64_t>(p.token_start[p.n_req]), p.n_tokens));
+    const int64_t from = max(before, min(static_cast<int64_t>(spans.end), p.n_tokens));
     const int64_t pad = before + p.n_tokens - from;
     if (pad == 0) return;
     const int pieces = p.dim / 8;
@@ -383,7 +400,7 @@ __global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1
     ChunkSpans spans;
     chunk_plan<kRowsThreads>(p, c.plan, spans);
     const ChunkCursor& at = c.plan.at;  // (in shared memory: the loop wants the registers)
-    chunk_padding<T>(p, kRowsThreads);
+    chunk_padding<T>(p, spans, kRowsThreads);
     const uint32_t smem0 = smem_u32(rows_smem);
     const uint32_t s_q = smem0 + S::kSmem - S::kQBytes;
     const uint32_t ring = smem0 + warp * (S::kStages * S::kStageBytes);

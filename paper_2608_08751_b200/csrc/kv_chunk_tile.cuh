@@ -175,7 +175,7 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     ChunkSpans spans;
     ChunkCursor at = chunk_plan<S::kThreads>(p, c.plan, spans);  // (its barriers order the above, too)
     tc_fence_after_sync();
-    chunk_padding<T>(p, S::kThreads);
+    chunk_padding<T>(p, spans, S::kThreads);
     const uint32_t tmem = c.tmem;
     WaitCtl ctl;
     ctl.abort_flag = &c.abort_flag;

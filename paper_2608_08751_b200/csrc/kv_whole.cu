@@ -308,15 +308,17 @@ int ivf_debug_kv_chunk_spans(int64_t n_tokens, int n_heads, const ivf_kv_cache* 
     p.token_start = token_start, p.kv_lens = kv_lens, p.prefix = prefix, p.window = window;
     chunk_settings(p, s);
     int64_t total = 0, n = 0;
-    for (int b = 0; b < n_req; ++b) {
-        const ChunkReq r = chunk_req(p, b, false);
+    for (int b = 0, taken = 0; b < n_req; ++b) {
+        const ChunkReq r = chunk_req(p, b, taken, false);
+        taken = r.start;
         total += p.n_kv_heads * p.parts * chunk_before(p, r, r.tiles);
     }
-    const ChunkSpans spans = chunk_spans(p, total, chunk_ctas(s, num_sms));
+    ChunkSpans spans;
+    chunk_spans(p, total, chunk_ctas(s, num_sms), spans);
     for (int c = 0; c < spans.ctas; ++c) {
         ChunkCursor at = {}, kept = {};
         at.left = spans.begin(c + 1) - spans.begin(c);
-        if (at.left > 0) chunk_locate(p, 0, n_req, spans.begin(c), at);
+        if (at.left > 0) chunk_locate(p, 0, n_req, 0, spans.begin(c), at);
         bool keeps = tiles && chunk_keep(p, at, kept);
         while (true) {
             if (at.left <= 0 && keeps) {

@@ -1,0 +1,40 @@
+"""Further calls of ivf_kv_attend_chunk: batches that are not in order, short tensors, and the bits that single tokens keep.  Tolerances as in the tests of
+the formula."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_08751_b200 import binding as B
+from test_gpu_kv_chunk import _case, _check, _run, kernel  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("start", [[0, 10, 8, 19], [0, 5, 3, 8], [5, 3, 9, 12], [0, 30, 0, 30], [-3, 4, 9, 11], [0, 0, 7, 2]], ids=str)
+@pytest.mark.parametrize("padding", [0, 6])
+def test_a_descending_token_start_counts_as_its_running_maximum(kernel, start, padding):  # noqa: F811
+    c = _case([(100, 10), (200, 6), (60, 3)], 2, 2, 64, 32, "fp16", seed=7)
+    n = max(start) + padding
+    c["q"] = torch.randn(n, 4, 64, device="cuda").half()
+    out, lse = _run(dict(c, start=np.array(start)), out=torch.full_like(c["q"], 7.0))
+    with pytest.raises(B.IvfError) as e:
+        B.ivf_check()
+    assert e.value.code == B.IVF_ERR_BAD_ID and "ivf_kv_attend_chunk" in str(e.value)
+    _check(dict(c, start=np.maximum(np.maximum.accumulate(start), 0)), out, lse)
+
+
+def test_a_descending_token_start_of_many_requests(kernel):  # noqa: F811
+    rng = np.random.default_rng(1)
+    c = _case([(int(rng.integers(0, 60)), int(rng.integers(0, 4))) for _ in range(700)], 1, 4, 64, 16, "bf16", seed=1)
+    start = c["start"].copy()
+    for b in (3, 150, 400, 401, 699):
+        start[b] = max(0, start[b] - 5)
+    start[300] += 40
+    lens = c["lens"]
+    lens = np.maximum(lens, np.diff(start).clip(0))  # (no request with fewer tokens in the cache than new ones)
+    c["table"] = np.where(c["table"] < 0, 0, c["table"])
+    c["kc"], c["vc"] = torch.nan_to_num(c["kc"]), torch.nan_to_num(c["vc"])
+    out, lse = _run(dict(c, start=start, lens=lens))
+    with pytest.raises(B.IvfError):
+        B.ivf_check()
+    _check(dict(c, start=np.maximum.accumulate(start), lens=lens), out, lse)

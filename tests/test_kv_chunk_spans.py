@@ -130,6 +130,30 @@ def test_as_many_requests_as_there_may_be(tiles):
     assert info["ctas"] == 1 and info["line"] == 0
 
 
+@pytest.mark.parametrize("tiles", [0, 1], ids=["rows", "tiles"])
+@pytest.mark.parametrize("start", [[0, 10, 8, 19], [0, 5, 3], [5, 3, 9], [4, 4, 2, 2, 9, 1, 30], [-3, 4, 9], [0, 40, 0, 40, 0, 40, 12, 90], [7, -2 ** 31, 5]], ids=str)
+def test_a_row_belongs_to_one_request_where_token_start_descends(tiles, start):
+    """The first request whose rows reach a row has it, at the position that it has there."""
+    n = len(start) - 1
+    lens = np.array([60 + 7 * b for b in range(n)])
+    n_tokens = max(start) + 3
+    got, info = _spans(start, lens, n_tokens, heads=6, kv=2, tiles=tiles)
+    owner, pos = {}, {}
+    for b in range(n):
+        for t in range(max(start[b], 0), start[b + 1]):
+            if t >= start[0] and t not in owner:
+                owner[t], pos[t] = b, lens[b] - (start[b + 1] - start[b]) + t - start[b]
+    for hv in range(2):
+        seen = {}
+        for i in np.flatnonzero((got["hv"] == hv) & (got["first"] == 1)):
+            for t in range(got["tokens"][i]):
+                row = int(got["token"][i]) + t
+                assert row not in seen, (row, "has two requests")
+                seen[row] = int(got["b"][i])
+                assert seen[row] == owner[row] and got["pos"][i] + t == pos[row]
+        assert seen.keys() == owner.keys()
+
+
 def test_refusals():
     cache = ctypes.byref(B._KvCache(None, None, (ctypes.c_int64 * 3)(), (ctypes.c_int64 * 3)(), 1, 16, 1, 64, B.IVF_BF16))
     a = np.zeros(8, np.int64)
