@@ -4,7 +4,8 @@
 //   z_k = scale * q . k,  with a cap  z_k = cap * tanh(scale * q . k / cap),  with a bias  z_k - slope_head * |p - k|
 //   seen: k < the request's length, k <= p or k < its prefix, and p - k < the window.  Always an interval [lo, hi).
 // One pass over the keys with a running maximum and sum, both in 32 bits; the exponentials take the cache's 16-bit type as
-// operands of the second product (off by up to 2^-8 or 2^-11 of themselves), the sum that divides them is of the unrounded ones.
+// operands of the second product (off by up to 2^-8 or 2^-11 of themselves; in two parts, 2^-16 or 2^-22, where a tile of 16 rows has 8 of them at
+// most), the sum that divides them is of the unrounded ones.
 //
 // How the work is shared out.  An item is a tile of new tokens of one request and one kv head: the tile's tokens by the
 // head's group of query heads are the rows of one matrix product.  Only the device knows the lengths, and they are ragged,
@@ -414,6 +415,9 @@ __global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1
         const int heads = min(p.part_heads, p.group - g0);
         const int head0 = h * p.group + g0;
         const int32_t* pages = p.table + at.b * p.table_stride;
+        // At most 8 rows: as in ivf_kv_attend's kernel the product's other rows take the second parts of the weights, what their rounding to 16
+        // bits leaves over (2^-16 or 2^-22 of themselves then)
+        const bool split = it.tokens * p.part_heads <= 8;
         auto row_token = [&](int r) { return r / p.part_heads; };
         auto row_live = [&](int r) { return row_token(r) < it.tokens && r % p.part_heads < heads; };
 
@@ -562,12 +566,17 @@ __global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
+                for (int r = 1; r >= 0; --r) {
                     const float w0 = exp2_fast(sc[n][2 * r] - base[r]), w1 = exp2_fast(sc[n][2 * r + 1] - base[r]);
                     add[r] += w0 + w1;
                     pf[2 * n + r] = Pair16<T>::pack(w0, w1);
+                    if (r == 0 && split) {
+                        const float2 first = Pair16<T>::unpack(pf[2 * n]);
+                        pf[2 * n + 1] = Pair16<T>::pack(w0 - first.x, w1 - first.y);
+                    }
                 }
             }
+            if (split) fix[1] = fix[0];
 #pragma unroll
             for (int r = 0; r < 2; ++r) l[r] = l[r] * fix[r] + add[r];
             if (__any_sync(0xFFFFFFFFu, fix[0] != 1.0f || fix[1] != 1.0f)) {
@@ -587,6 +596,13 @@ __global__ void __launch_bounds__(kRowsThreads, DP == 64 ? 3 : DP == 128 ? 2 : 1
                     mma16816<T>(o[2 * n], pf, b[0], b[1]);
                     mma16816<T>(o[2 * n + 1], pf, b[2], b[3]);
                 }
+            }
+        }
+        if (split) {
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) {  // an infinite value is infinite with the first parts; with the second ones it may be 0 * inf
+                o[i][0] += is_finite(o[i][0]) ? o[i][2] : 0.0f;
+                o[i][1] += is_finite(o[i][1]) ? o[i][3] : 0.0f;
             }
         }
         cp_async_wait<0>();

@@ -4,8 +4,11 @@ import numpy as np
 import pytest
 import torch
 
+import kv_reference as R
+import kv_whole_reference as W
 from paper_2608_08751_b200 import binding as B
-from test_gpu_kv_chunk import _case, _check, _run, kernel  # noqa: F401
+from test_gpu_kv import _np
+from test_gpu_kv_chunk import _case, _check, _finite, _run, kernel  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +41,23 @@ def test_a_descending_token_start_of_many_requests(kernel):  # noqa: F811
     with pytest.raises(B.IvfError):
         B.ivf_check()
     _check(dict(c, start=np.maximum.accumulate(start), lens=lens), out, lse)
+
+
+@pytest.mark.parametrize("requests,group,dim,kind", [
+    ([(700, 1), (90, 1), (0, 1)], 4, 128, "bf16"), ([(700, 1), (31, 1)], 7, 96, "fp16"), ([(3000, 1)], 8, 64, "bf16"), ([(400, 1)] * 5, 1, 112, "fp16"),
+    ([(500, 2), (60, 2)], 4, 64, "bf16"), ([(300, 5)], 1, 64, "fp16"), ([(20000, 1)], 2, 128, "bf16"), ([(900, 3), (40, 1)], 2, 16, "bf16"),
+], ids=str)
+def test_weights_of_few_rows_keep_their_bits(requests, group, dim, kind):
+    """Up to 8 rows of a request and kv head: the weights come in two parts, so beside the output's own rounding, u of the value, and the logits'
+    own error an output is off by u^2 of the weighted mean of |v|, not u; and by half a step of the type's least number for each key, against a largest
+    weight of one."""
+    c = _case(requests, 2, group, dim, 32, kind, seed=dim + group)
+    out, lse = _run(c)
+    B.ivf_check()
+    want, _, size, unit = W.attend_chunk(_np(c["q"]), _finite(_np(c["kc"])), _finite(_np(c["vc"])), c["table"], c["start"], c["lens"], c["scale"])
+    u = R.UNIT[kind]
+    move = (dim + 16) * 2.0 ** -24 * unit + 2.0 ** -20
+    least = {"bf16": 2.0 ** -134, "fp16": 2.0 ** -25}[kind] * max(c["lens"]) * np.abs(_finite(_np(c["vc"]))).max()
+    tol = u * np.abs(want) + (u * u + 2 * move[..., None]) * size + least + R.TINY[kind]
+    off = np.abs(_np(out) - want)
+    assert (off <= tol).all(), (off / tol).max()
