@@ -515,6 +515,7 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
  *   token_start     [n_req + 1] as ivf_kv_tables gives it: request b has rows token_start[b] .. token_start[b + 1] - 1 of q and out.
  *                   Rows from n_tokens on do not exist; rows that belong to no request get zeros and an out_lse of -infinity
  *   kv_lens         [n_req] tokens in the cache, the new ones among them: they are the last ones.  n_req <= 16384
+ *   scale, cap      finite, and so are scale * log2(e), cap * log2(e) and scale / cap; that one is not below the normal numbers (refused)
  *   slopes          [n_heads] float32, or NULL: no bias.  prefix [n_req], or NULL: none (a negative one counts as 0)
  *   out             must not share memory with q (refused), the caches or the workspace
  *   workspace       what ivf_kv_attend_chunk_workspace says for the same sizes, 16-byte aligned.  It is written and read by this call alone;

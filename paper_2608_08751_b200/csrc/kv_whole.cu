@@ -7,9 +7,11 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <initializer_list>
+#include <limits>
 #include <type_traits>
 #include <utility>
 
@@ -253,6 +255,10 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
     if (rc != IVF_OK) return rc;
     if (!(scale - scale == 0.0f)) return fail(IVF_ERR_INVALID_ARG, "scale must be finite");
     if (!(cap >= 0.0f && cap - cap == 0.0f)) return fail(IVF_ERR_INVALID_ARG, "cap must be finite and not negative (0: none)");
+    const float log2e = 1.4426950408889634f, scale_log2 = scale * log2e, cap_in = cap > 0.0f ? scale / cap : 0.0f, cap_out = cap * log2e;
+    if (!(scale_log2 - scale_log2 == 0.0f && cap_in - cap_in == 0.0f && cap_out - cap_out == 0.0f) ||
+        (cap > 0.0f && scale != 0.0f && std::fabs(cap_in) < std::numeric_limits<float>::min()))
+        return fail(IVF_ERR_INVALID_ARG, "scale = %g, cap = %g: scale * log2(e), cap * log2(e) and scale / cap must be finite, and scale / cap not below the normal numbers", scale, cap);
     if (window < 0) return fail(IVF_ERR_INVALID_ARG, "window = %d: must not be negative (0: none)", window);
     if (n_tokens == 0) return IVF_OK;
     if (max_blocks < 1 || (n_req > 1 && table_stride < max_blocks))
@@ -268,7 +274,6 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
         return fail(IVF_ERR_INVALID_ARG, "workspace: %lld bytes, 16-byte aligned, are needed (ivf_kv_attend_chunk_workspace)", (long long)need);
     KvHostCtx ctx;
     if ((rc = kv_host_ctx(&ctx)) != IVF_OK) return rc;
-    const float log2e = 1.4426950408889634f;
     ChunkParams p;
     p.q = q, p.q_stride[0] = q_stride[0], p.q_stride[1] = q_stride[1], p.n_tokens = n_tokens;
     p.group = n_heads / cache->n_kv_heads, p.n_kv_heads = cache->n_kv_heads, p.dim = cache->head_dim;
@@ -277,9 +282,7 @@ int ivf_kv_attend_chunk(const void* q, const int64_t q_stride[2], int64_t n_toke
     p.num_pages = cache->num_pages;
     p.table = table, p.table_stride = table_stride, p.n_req = n_req, p.max_blocks = max_blocks, p.page_shift = kv_shift(cache->page_size);
     p.token_start = token_start, p.kv_lens = kv_lens, p.prefix = prefix, p.window = window;
-    p.scale_log2 = scale * log2e;
-    p.cap_in = cap > 0.0f ? scale / cap : 0.0f;
-    p.cap_out = cap * log2e;
+    p.scale_log2 = scale_log2, p.cap_in = cap_in, p.cap_out = cap_out;
     p.slopes = slopes, p.out = out, p.out_stride[0] = out_stride[0], p.out_stride[1] = out_stride[1], p.lse = out_lse, p.status = ctx.status;
     p.limit_ns = ctx.limit_ns;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);

@@ -145,3 +145,14 @@ def test_tensors_are_refused_in_python():
         B.ivf_kv_fork([[0]], i32, i32, None, 10, 16)
     with pytest.raises(TypeError):
         B.ivf_kv_attend_chunk(q, half, half, table, i32)
+
+
+def test_scales_and_caps_that_base_2_cannot_hold():
+    """The kernels take scale * log2(e), cap * log2(e) and scale / cap: out of the range of a float they gave NaN without a word, and scale / cap below the
+    normal numbers a logit with few digits."""
+    def call(scale, cap):
+        return B.lib().ivf_kv_attend_chunk(None, _s(256, 64), 0, 4, _cache(), None, 8, 2, 8, None, None, scale, cap, None, 0, None, None, _s(256, 64), None, None, 0, None)
+    for scale, cap in ((3e38, 0.0), (-3e38, 0.0), (1.0, 3.4e38), (1.0, 1e-39), (0.1, 1e38), (-0.1, 1e38), (1e-30, 1e20), (3e38, 3e38)):
+        assert call(scale, cap) == INV and b"scale" in _error() and b"cap" in _error(), (scale, cap)
+    for scale, cap in ((2e38, 0.0), (-0.125, 50.0), (0.0, 2e38), (1.0, 1e37), (1e-40, 0.0), (0.0, 0.0), (1e30, 1e-5)):
+        assert call(scale, cap) == OK, (scale, cap)
