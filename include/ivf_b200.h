@@ -517,7 +517,8 @@ int ivf_kv_attend(const void* q, const int64_t q_stride[2], int64_t n_tokens, in
  *   kv_lens         [n_req] tokens in the cache, the new ones among them: they are the last ones.  n_req <= 16384
  *   scale, cap      finite, and so are scale * log2(e), cap * log2(e) and scale / cap; that one is not below the normal numbers (refused)
  *   slopes          [n_heads] float32, or NULL: no bias.  prefix [n_req], or NULL: none (a negative one counts as 0)
- *   out             must not share memory with q (refused), the caches or the workspace
+ *   out             must not share memory with q (refused; so are a q and an out whose ranges meet and whose strides differ, unless they are rows of one
+ *                   buffer in turn), the caches or the workspace
  *   workspace       what ivf_kv_attend_chunk_workspace says for the same sizes, 16-byte aligned.  It is written and read by this call alone;
  *                   two calls that may run at the same time need one each
  * The tokens of a request with fewer tokens in the cache than new ones see nothing (zeros; -infinity).  Where token_start descends or is negative its running

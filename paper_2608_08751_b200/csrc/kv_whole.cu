@@ -10,6 +10,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <initializer_list>
 #include <limits>
 #include <type_traits>
@@ -171,12 +172,22 @@ int launch_chunk(ChunkParams& p, void* workspace, const KvHostCtx& ctx, cudaStre
     return launch(true, many ? kv_chunk_join_kernel<T, kJoinThreads / 32> : kv_chunk_join_kernel<T, 1>, grid, kJoinThreads, 0, stream, p);
 }
 
-// Whether `out` has an element of `q`'s memory.  Rows of one buffer in turn (the same token stride) are told apart, other tensors
-// by their ranges.
+// Whether `out` has an element of `q`'s memory.  Views with the same strides (two parts of one buffer, its axes in any order) are told apart by
+// the distance of their starts, rows of one buffer in turn (the same token stride) by their place in the turn, other tensors by their ranges.
 bool out_over_q(const void* q, const int64_t* q_stride, const void* out, const int64_t* out_stride, int64_t n, int64_t heads, int dim) {
     const int64_t q_row = (heads - 1) * q_stride[1] + dim, o_row = (heads - 1) * out_stride[1] + dim, step = q_stride[0];
     const int64_t q0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(q)) / 2, o0 = static_cast<int64_t>(reinterpret_cast<uintptr_t>(out)) / 2;
     if (q0 + (n - 1) * step + q_row <= o0 || o0 + (n - 1) * out_stride[0] + o_row <= q0) return false;
+    if ((n == 1 || step == out_stride[0]) && (heads == 1 || q_stride[1] == out_stride[1])) {
+        // output (t', h') and query (t, h) lie o0 - q0 + (t' - t) step + (h' - h) q_stride[1] apart
+        for (int64_t h = 1 - heads; h < heads; ++h) {
+            const int64_t apart = o0 - q0 + h * q_stride[1];
+            const int64_t t = n == 1 ? 0 : -apart / step;  // the nearest (a written tensor's stride is not 0), or one from it
+            for (int64_t i = t - 1; i <= t + 1; ++i)
+                if (i > -n && i < n && std::abs(apart + i * step) < dim) return true;
+        }
+        return false;
+    }
     if (step == 0 || step != out_stride[0]) return true;
     const int64_t after = ((o0 - q0) % step + step) % step;  // of an output row behind the start of a query row
     return after < q_row || after + o_row > step;

@@ -61,3 +61,25 @@ def test_weights_of_few_rows_keep_their_bits(requests, group, dim, kind):
     tol = u * np.abs(want) + (u * u + 2 * move[..., None]) * size + least + R.TINY[kind]
     off = np.abs(_np(out) - want)
     assert (off <= tol).all(), (off / tol).max()
+
+
+def test_queries_and_outputs_of_a_head_in_turn(kernel):  # noqa: F811
+    c = _case([(50, 20), (7, 9)], 2, 2, 64, 16, "bf16", seed=7)
+    both = torch.zeros(4, 2, 29, 64, dtype=torch.bfloat16, device="cuda")
+    both[:, 0] = c["q"].transpose(0, 1)
+    q, out = both[:, 0].transpose(0, 1), both[:, 1].transpose(0, 1)
+    _, lse = _run(dict(c, q=q), out=out)
+    B.ivf_check()
+    _check(c, out, lse)
+    assert torch.equal(q, c["q"])
+    with pytest.raises(B.IvfError, match="share memory"):
+        _run(dict(c, q=q), out=both[:, 0].transpose(0, 1))
+
+
+def test_fewer_rows_than_token_start_speaks_of(kernel):  # noqa: F811
+    c = _case([(70, 5), (0, 12), (9, 3)], 2, 4, 64, 32, "bf16")
+    for n in (1, 5, 14, 19):
+        short = dict(c, q=c["q"][:n].contiguous())
+        out, lse = _run(short)
+        B.ivf_check()
+        _check(short, out, lse)

@@ -156,3 +156,41 @@ def test_scales_and_caps_that_base_2_cannot_hold():
         assert call(scale, cap) == INV and b"scale" in _error() and b"cap" in _error(), (scale, cap)
     for scale, cap in ((2e38, 0.0), (-0.125, 50.0), (0.0, 2e38), (1.0, 1e37), (1e-40, 0.0), (0.0, 0.0), (1e30, 1e-5)):
         assert call(scale, cap) == OK, (scale, cap)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="these are host addresses: what is not refused here would run")
+def test_outputs_in_the_gaps_of_the_queries_are_not_refused():
+    """Views of one buffer with the same strides, in any order of its axes, are told apart exactly."""
+    def refused(gap, q_stride, n, heads, out_stride=None):
+        out_stride = out_stride or q_stride
+        kv = 2 if heads % 2 == 0 else 1
+        rc = B.lib().ivf_kv_attend_chunk(P, _s(*q_stride), n, heads, _cache(kv=kv), P, 8, 2, 8, P, P, 1.0, 0.0, None, 0, None, P + 2 * gap, _s(*out_stride), None, P,
+                                         1 << 40, None)
+        return rc == INV and b"must not share" in _error()
+    n, heads = 7, 4
+    # heads first, [heads, 2, n, 64]: queries and outputs of a head in turn
+    assert not refused(n * 64, (64, 2 * n * 64), n, heads) and refused((n - 1) * 64, (64, 2 * n * 64), n, heads) and refused(0, (64, 2 * n * 64), n, heads)
+    # [heads, n, 2, 64] and [n, heads, 2, 64]: rows in turn
+    for strides in ((128, n * 128), (heads * 128, 128)):
+        assert not refused(64, strides, n, heads) and refused(56, strides, n, heads) and refused(128, strides, n, heads) and refused(72, strides, n, heads)
+    # [n, 2, heads, 64]: tokens in turn
+    assert not refused(heads * 64, (2 * heads * 64, 64), n, heads) and refused(heads * 64 - 8, (2 * heads * 64, 64), n, heads)
+    # behind the last row of one order and among the rows of the next
+    assert not refused(n * 64, (64, 2 * n * 64), n, 1) and refused(8, (64, 64), 1, 1) and not refused(64, (0, 0), 1, 1)
+    # strides that differ, ranges that meet: refused, whatever the elements
+    assert refused(64, (256, 1024), n, heads, (512, 4096))
+    # brute force
+    rng = torch.Generator().manual_seed(0)
+    pick = lambda *v: v[int(torch.randint(0, len(v), (1,), generator=rng))]  # noqa: E731
+    seen = set()
+    for _ in range(400):
+        n, heads = pick(1, 2, 3, 5), pick(1, 2, 4)
+        st, sh = pick(64, 128, 192, 320, 448, 1024), pick(64, 128, 256, 640, 1088)
+        if (n > 1 and heads > 1 and (max(st, sh) < 64 + ((n - 1) * st if st < sh else (heads - 1) * sh))) or (n > 1 and heads > 1 and st == sh):
+            continue  # (an output with two elements in one place is another refusal)
+        gap = pick(0, 8, 56, 64, 72, 128, 192, 256, 320, 640, 1024)
+        rows = {t * st + h * sh + x for t in range(n) for h in range(heads) for x in range(64)}
+        share = any(r + gap in rows for r in rows)
+        assert refused(gap, (st, sh), n, heads) == share, (gap, st, sh, n, heads)
+        seen.add(share)
+    assert seen == {False, True}
