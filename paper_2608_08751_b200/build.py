@@ -45,6 +45,21 @@ def _stale(path: str = LIB_PATH) -> bool:
     return any(_newer(_deps(unit), path) for unit in _UNITS)
 
 
+def _remove(path: str) -> None:
+    if os.path.exists(path):
+        os.remove(path)
+
+
+def _write(out: str, cmd) -> None:
+    """Runs cmd(file), whose output takes the place of `out` if it comes through."""
+    tmp = out + f".{os.getpid()}.tmp"
+    try:
+        subprocess.check_call(cmd(tmp))
+        os.replace(tmp, out)
+    finally:
+        _remove(tmp)
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Compiles the units side by side (those whose objects are older than their sources) and links them."""
     out = CHECKED_LIB_PATH if checked else LIB_PATH
@@ -56,25 +71,29 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
            "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include")]
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    objects, running = [], []
-    for unit in _UNITS:
-        other = checked and unit in _CHECKED
-        obj = os.path.join(folder, unit.removesuffix(".cu") + ("_checked.o" if other else ".o"))
-        objects.append(obj)
-        if force or _newer(_deps(unit), obj):
-            tmp = obj + f".{os.getpid()}.tmp.o"
-            running.append((subprocess.Popen(cmd + (["-DIVF_CHECK_BOUNDS"] if other else []) + ["-c", os.path.join(_CSRC, unit), "-o", tmp]), tmp, obj))
-    failed = None
-    for process, tmp, obj in running:
-        if process.wait() == 0:
-            os.replace(tmp, obj)
-        else:
-            failed = process.args
+    objects, running, failed = [], [], None
+    try:
+        for unit in _UNITS:
+            other = checked and unit in _CHECKED
+            obj = os.path.join(folder, unit.removesuffix(".cu") + ("_checked.o" if other else ".o"))
+            objects.append(obj)
+            if force or _newer(_deps(unit), obj):
+                tmp = obj + f".{os.getpid()}.tmp.o"
+                running.append((subprocess.Popen(cmd + (["-DIVF_CHECK_BOUNDS"] if other else []) + ["-c", os.path.join(_CSRC, unit), "-o", tmp]), tmp, obj))
+        for process, tmp, obj in running:
+            if process.wait() == 0:
+                os.replace(tmp, obj)
+            else:
+                failed = process.args
+    finally:  # (one that fails or is broken off leaves nothing behind)
+        for process, tmp, _ in running:
+            if process.poll() is None:
+                process.kill()
+                process.wait()
+            _remove(tmp)
     if failed:
         raise subprocess.CalledProcessError(1, failed)
-    tmp = out + f".{os.getpid()}.tmp"
-    subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", *objects, "-o", tmp])
-    os.replace(tmp, out)
+    _write(out, lambda tmp: [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", *objects, "-o", tmp])
     return out
 
 
@@ -86,14 +105,12 @@ def build_bind(force: bool = False) -> str:
     import torch
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
-    tmp = BIND_PATH + f".{os.getpid()}.tmp"
     libs = os.path.join(base, "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+    cmd = lambda tmp: ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
            "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), src, "-o", tmp,
            "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
-    subprocess.check_call(cmd)
-    os.replace(tmp, BIND_PATH)
+    _write(BIND_PATH, cmd)
     return BIND_PATH
 
 
