@@ -22,7 +22,7 @@
 
 namespace ivf {
 
-constexpr int kChunkMaxSms = 148;  // CTAs that a call may use: two on each of so many SMs, one of the kernel of large tiles
+constexpr int kChunkMaxSms = 148;  // CTAs that a call may use: on each of so many SMs three, two or one of small tiles (heads of up to 64, 128, 256), one of large ones
 
 struct ChunkDesc {  // of the item that a CTA's span ends in
     int parts;      // CTAs that have a part of it; 0: the span ends with an item
@@ -383,7 +383,7 @@ __device__ __noinline__ void add_odd(const ChunkParams& p, int b, int h, int lo,
 // Tiles of 16 rows: single and drafted tokens.  As in ivf_kv_attend's kernel of that name each of four warps takes pieces of 16 keys
 // through a ring of its own and the warps meet at an item's end.  Bound by the keys' bytes: one token over 131,072 by 8 heads of 128 takes 93 us
 // (537 MB, 5.8 TB/s with the joining of 37 parts to an item), 64 requests of 4,000 tokens 113 us (5.9 TB/s, 0.90 of a copy's rate), drafted tokens by 16 heads
-// of 64 184 us (5.6 TB/s; three CTAs on an SM, with two 232).  A small call is a chain of waits: lengths, place, table, keys, warps,
+// of 64 184 to 205 us (5.1 to 5.6 TB/s; three CTAs on an SM, with two 232).  A small call is a chain of waits: lengths, place, table, keys, warps,
 // join: 10 us.
 template <int DP>
 struct ChunkRowsControl {

@@ -18,11 +18,11 @@
 // logits ready.  TMEM holds it exactly: two streams of two S (256 columns) and of O (256).  Heads wider than 128 take all of the second half
 // for one stream's O; it has two threads to a row then, 32 keys each, which tell each other their maxima through shared memory.
 //
-// 4,096 tokens of two requests of 32,768 by 4 heads of a group of 8, d = 128 (1.67 TFLOP of useful products): 1.45 ms in short runs, 1.67 ms under the
-// power limit, 1,150 and 1,000 TFLOP/s.  A tile of the two streams takes 1,850 cycles: its products alone 1,500 (with 64 keys to an
+// 4,096 tokens of two requests of 32,768 by 4 heads of a group of 8, d = 128 (1.67 TFLOP of useful products): 1.45 ms in short runs, 1.68 to 1.73 ms under the
+// power limit, 1,150 and 980 TFLOP/s.  A tile of the two streams takes 1,850 cycles: its products alone 1,500 (with 64 keys to an
 // instruction S waits for the queries' tile in shared memory, 48 cycles for 32), its softmax alone 1,650 (1,024 of them the special function unit's
-// 16 exponentials a cycle), its copies alone 950.  What was tried: 128 keys to a tile with one S (1.74 ms), two threads to a row here
-// too (1.97), a quarter or an eighth of the exponentials by polynomial (1.62, 1.45), taking turns at the exponentials (1.73).
+// 16 exponentials a cycle), its copies alone 950.  What was tried: 128 keys to a tile with one S (1.74 ms where 64
+// keys with two took 2.00; not again since then), two threads to a row here too (1.97), a quarter or an eighth of the exponentials by polynomial (1.62, 1.45), taking turns at the exponentials (1.73).
 #pragma once
 #include "kv_chunk.cuh"
 #include "kv_attend_tile.cuh"
@@ -336,7 +336,9 @@ kv_chunk_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         int planned = 0, n = 0, items = 0;
         bool end = false;
         // A span that begins inside an item takes the end of that one last: then all CTAs of a head begin at the same keys and go over them
-        // together, and the keys come from L2 more often (4,096 tokens on caches larger than L2: 1,714 against 1,669 us).
+        // together, and the keys come from L2 more often.  Groups of 4 or 2, heads of 128, with it / without: 8 requests of 65,536 by 512 tokens
+        // 4,107 / 4,271 us, 4 of 32,768 by 1,024 2,073 / 2,150, 16 of 8,192 by 1,024 2,158 / 2,170; no difference for 4,096 tokens of two requests of
+        // 32,768 by 4 heads; 512 tokens of two requests of 131,072 by heads of 256 4,768 / 4,679.
         ChunkCursor kept;
         bool keeps = chunk_keep(p, at, kept);
         for (int seq = 0; ok; ++seq) {

@@ -114,7 +114,10 @@ int64_t chunk_bytes(const ChunkShape& s, int dim) {
 // Small tiles read the keys once for 16 rows, large ones for up to 256, at some cost of starting.  By rows (new tokens by the heads of a
 // group) to a request, small / large tiles in us: one request of 65,536 tokens by 8 heads of 128 in groups of 4: 16 rows 63 / 69, 32 rows 94 / 69, 128
 // rows 282 / 79; 64 requests of 8,192: 16 rows 223 / 248, 32 rows 422 / 253.  Heads of 64: 16 rows 129 / 230, 32 rows 235 / 241.  Heads
-// wider than 128 leave the small tiles one CTA on an SM: 64 requests of 8,192 by 4 heads of 256, 2 rows 384 / 232.
+// wider than 128 leave the small tiles one CTA on an SM: 64 requests of 8,192 by 4 heads of 256, 2 rows 384 / 232.  Those are of requests alike.  The host
+// knows no request's tokens, only their sum and the table's rows, so rows without new tokens, or with one, count against a prompt beside
+// them: 2,048 tokens of one request of 32,768, 8 heads of 128 in groups of 4, in a table of 1 or 64 rows 950 us by large tiles, of 512 rows 7,830 by
+// small ones (955 by large); 512 tokens of 8,192 beside 255 single ones of 4,000 1,069 / 1,068.
 bool chunk_tiles_pay(int64_t n_tokens, int n_req, int group, int dim) {
     const int kernel = g_kv_chunk.load();
     if (kernel == 1 || dim < 64) return false;
